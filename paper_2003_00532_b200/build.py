@@ -6,18 +6,19 @@ import os
 import shlex
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdgemm.so")
-SOURCES = [os.path.join(CSRC, "dgemm_api.cu"), os.path.join(CSRC, "sgemm_api.cu")]
+SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "layernorm.cu")]
 # every source, header and public header: an edit to any of them makes the built library stale
 DEPS = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh")) +
               glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-cudart", "static",
+    "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-cudart", "static",
 ]
 
 
@@ -81,14 +82,32 @@ def build(force: bool = False, verbose: bool = False, check: bool = False) -> st
     if force or is_stale():
         tmp = LIB + ".tmp.%d" % os.getpid()
         extra = shlex.split(os.environ.get("DGEMM_NVCC_FLAGS", ""))  # e.g. -D switches for experiments
-        cmd = [nvcc_path(), *NVCC_FLAGS, *extra, *(["-Xptxas", "-v"] if (verbose or check) else []), "-o", tmp, *SOURCES]
-        res = subprocess.run(cmd, cwd=CSRC, capture_output=True, text=True)
-        if verbose or res.returncode != 0:
-            sys.stderr.write(res.stdout + res.stderr)
-        if res.returncode != 0:
+        flags = [*NVCC_FLAGS, *extra, *(["-Xptxas", "-v"] if (verbose or check) else [])]
+        with tempfile.TemporaryDirectory() as objs:
+            # one compiler process per source, side by side
+            jobs = []
+            for src in SOURCES:
+                obj = os.path.join(objs, os.path.basename(src) + ".o")
+                log = open(obj + ".log", "w+")
+                jobs.append((obj, log, subprocess.Popen([nvcc_path(), *flags, "-c", "-o", obj, src], cwd=CSRC, stdout=log,
+                                                        stderr=subprocess.STDOUT, text=True)))
+            failed, text = False, ""
+            for obj, log, proc in jobs:
+                failed = proc.wait() != 0 or failed
+                log.seek(0)
+                text += log.read()
+                log.close()
+            if not failed:
+                res = subprocess.run([nvcc_path(), *flags, "-shared", "-o", tmp, *(j[0] for j in jobs)], cwd=CSRC,
+                                     capture_output=True, text=True)
+                failed = res.returncode != 0
+                text += res.stdout + res.stderr
+        if verbose or failed:
+            sys.stderr.write(text)
+        if failed:
             raise RuntimeError("nvcc failed building libdgemm.so")
         if check and not extra:
-            check_ptxas(res.stdout + res.stderr)
+            check_ptxas(text)
         os.replace(tmp, LIB)
     return LIB
 

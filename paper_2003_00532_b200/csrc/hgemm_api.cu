@@ -1,0 +1,874 @@
+// C ABI of the 16-bit products (include/hgemm.h): validation, packing of operands TMA cannot
+// address, choice of tile and work decomposition, tensor maps, launches.
+#include <atomic>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "../../include/hgemm.h"
+#include "hgemm_aux.cuh"
+#include "hgemm_tc.cuh"
+#include "lm_state.h"
+
+namespace {
+
+using namespace hgemm;
+
+constexpr int kMaxDevices = 64;
+constexpr unsigned long long kWaitLimitNs = 4000000000ull;  // bounded device-side waits give up after 4 s
+constexpr int64_t kMaxDim = (int64_t)INT32_MAX - 1024;
+
+__device__ int g_hgemm_status_word;
+__device__ int g_hgemm_counters[scratch::kMaxLeases * lm::kCounters];
+
+lm::DeviceState g_dev[kMaxDevices];
+std::mutex g_mutex;
+lm::EncodeTiledFn g_encode = nullptr;
+std::atomic<int> g_drop_limit_us{0};
+
+// ---- kernels by configuration -----------------------------------------------------------------------
+
+struct Config {
+  int cg, bm;
+};
+constexpr Config kConfigs[] = {{1, 16}, {1, 32}, {1, 64}, {1, 128}, {2, 128}, {2, 256}};
+constexpr int kNumConfigs = sizeof(kConfigs) / sizeof(kConfigs[0]);
+
+template <typename T, int CG, int BM, bool GATED>
+bool launch_one(int clusters, cudaStream_t stream, const Params& p) {
+  return lm::launch(hgemm_tc_kernel<T, CG, BM, GATED>, dim3(clusters * CG), dim3(THREADS), (size_t)Cfg<CG, BM, GATED>::SMEM_BYTES, CG,
+                    stream, p);
+}
+template <typename T, bool GATED>
+bool launch_config(int c, int clusters, cudaStream_t stream, const Params& p) {
+  switch (c) {
+    case 0: return launch_one<T, 1, 16, GATED>(clusters, stream, p);
+    case 1: return launch_one<T, 1, 32, GATED>(clusters, stream, p);
+    case 2: return launch_one<T, 1, 64, GATED>(clusters, stream, p);
+    case 3: return launch_one<T, 1, 128, GATED>(clusters, stream, p);
+    case 4: return launch_one<T, 2, 128, GATED>(clusters, stream, p);
+    default: return launch_one<T, 2, 256, GATED>(clusters, stream, p);
+  }
+}
+bool launch_tc(int type, bool gated, int c, int clusters, cudaStream_t stream, const Params& p) {
+  if (type == HGEMM_TYPE_BF16)
+    return gated ? launch_config<__nv_bfloat16, true>(c, clusters, stream, p) : launch_config<__nv_bfloat16, false>(c, clusters, stream, p);
+  return gated ? launch_config<__half, true>(c, clusters, stream, p) : launch_config<__half, false>(c, clusters, stream, p);
+}
+
+template <typename T, int CG, int BM, bool GATED>
+bool configure_one() {
+  return cudaFuncSetAttribute(hgemm_tc_kernel<T, CG, BM, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Cfg<CG, BM, GATED>::SMEM_BYTES) == cudaSuccess;
+}
+template <typename T, bool GATED>
+bool configure_all() {
+  return configure_one<T, 1, 16, GATED>() && configure_one<T, 1, 32, GATED>() && configure_one<T, 1, 64, GATED>() &&
+         configure_one<T, 1, 128, GATED>() && configure_one<T, 2, 128, GATED>() && configure_one<T, 2, 256, GATED>();
+}
+
+// ---- work decomposition -------------------------------------------------------------------------------
+
+// Sizes of one product: output columns N (lanes) and rows M, k-blocks.
+struct Size {
+  int64_t N, M;
+  int kblocks;
+};
+
+struct Plan {
+  int config = 0;
+  int clusters = 0;
+  int units = 0;
+  int nt = 0;
+  struct Part {
+    int tiles_n, tiles_m, dp_tiles, split, kb_per_split, units, slot0, counter0;
+  } part[MAX_PROBLEMS];
+  int slots = 0;  // workspace slots of bm * 128 * cg binary32 values
+};
+
+// Estimated clocks of one launch, from the sizes that bound each part (per CTA): the MMAs of a k-block
+// (8192 flop per clock), its operand bytes from L2 (64 per clock), an epilogue, and for cut tiles the
+// partial sums' way through L2.
+double step_clocks(const Config& c) {
+  const double mma = 2.0 * c.bm, bytes = (16384.0 + 128.0 * (c.bm / c.cg < 64 ? 64 : c.bm / c.cg)) / 64.0;
+  return mma > bytes ? mma : bytes;
+}
+
+// Decomposes the problems (longest contraction first) into units for one configuration: whole waves of
+// tiles run whole; the tiles of the last partial wave are cut into parts of at most `len` k-blocks.
+double decompose(const Size* sz, int n, bool gated, int sms, int config, int len, Plan* out) {
+  const Config& c = kConfigs[config];
+  const int clusters = sms / c.cg;
+  const int nt = (gated ? 64 : 128) * c.cg;
+  Plan pl;
+  pl.config = config;
+  pl.nt = nt;
+  int64_t tiles[MAX_PROBLEMS], total = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t tn = (sz[i].N + nt - 1) / nt, tm = (sz[i].M + c.bm - 1) / c.bm;
+    tiles[i] = tn * tm;
+    if (tiles[i] > INT32_MAX / 64) return -1.0;
+    pl.part[i].tiles_n = (int)tn;
+    pl.part[i].tiles_m = (int)tm;
+    total += tiles[i];
+  }
+  if (total > INT32_MAX / 64) return -1.0;
+  int64_t tail = total % clusters;
+  // whole waves: each as long as its longest tile
+  const double step = step_clocks(c);
+  double clocks = 0.0;
+  {
+    int i = 0;
+    int64_t left = total - tail, in_problem = tiles[0];
+    while (left > 0) {
+      while (in_problem == 0) in_problem = tiles[++i];
+      // waves that start inside problem i
+      const int64_t waves = (in_problem < left ? in_problem : left) + clusters - 1;
+      int64_t w = waves / clusters;
+      if (w * clusters > left) w = left / clusters;
+      clocks += (double)w * sz[i].kblocks * step;
+      int64_t used = w * clusters;
+      left -= used;
+      while (used > 0) {
+        const int64_t d = used < in_problem ? used : in_problem;
+        in_problem -= d;
+        used -= d;
+        if (in_problem == 0 && i + 1 < n) in_problem = tiles[++i];
+        else if (in_problem == 0) break;
+      }
+    }
+  }
+  int64_t units = 0, slots = 0, tail_units = 0;
+  int counters = 0, longest = 0, max_split = 1;
+  for (int i = n - 1; i >= 0; --i) {
+    const int64_t t = tail < tiles[i] ? tail : tiles[i];
+    tail -= t;
+    Plan::Part& q = pl.part[i];
+    int kps = sz[i].kblocks < len ? sz[i].kblocks : len;
+    int split = (sz[i].kblocks + kps - 1) / kps;
+    kps = (sz[i].kblocks + split - 1) / split;
+    split = (sz[i].kblocks + kps - 1) / kps;
+    if (split == 1 || t == 0) {
+      q.dp_tiles = (int)tiles[i];
+      q.split = 1;
+      q.kb_per_split = sz[i].kblocks;
+      if (t > 0 && sz[i].kblocks > longest) longest = sz[i].kblocks;
+      tail_units += t;
+    } else {
+      q.dp_tiles = (int)(tiles[i] - t);
+      q.split = split;
+      q.kb_per_split = kps;
+      if (kps > longest) longest = kps;
+      if (split > max_split) max_split = split;
+      tail_units += t * split;
+      q.slot0 = (int)slots;
+      q.counter0 = counters;
+      slots += t * split;
+      counters += (int)t;
+    }
+    q.units = (int)(q.dp_tiles + (tiles[i] - q.dp_tiles) * q.split);
+    units += q.units;
+    if (q.split == 1) q.slot0 = q.counter0 = 0;
+  }
+  if (counters * c.cg > lm::kCounters) return -1.0;
+  const int64_t tail_rounds = (tail_units + clusters - 1) / clusters;
+  clocks += (double)tail_rounds * longest * step;
+  if (max_split > 1) clocks += (double)tail_rounds * 10.0 * c.bm + 8.0 * c.bm * max_split + 2500.0;
+  clocks += 12.0 * c.bm + 2000.0;
+  pl.units = (int)units;
+  pl.slots = (int)slots;
+  pl.clusters = units < clusters ? (int)units : clusters;
+  *out = pl;
+  return clocks;
+}
+
+// The configuration and cut with the smallest estimate.
+bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
+  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
+  double best_clocks = -1.0;
+  int64_t max_m = 0;
+  int kmax = 1;
+  for (int i = 0; i < n; ++i) {
+    if (sz[i].M > max_m) max_m = sz[i].M;
+    if (sz[i].kblocks > kmax) kmax = sz[i].kblocks;
+  }
+  for (int c = 0; c < kNumConfigs; ++c) {
+    if (c > 0 && kConfigs[c - 1].cg == 1 && kConfigs[c - 1].bm >= max_m && kConfigs[c].bm > 16) continue;  // only more padding
+    for (int cut : kCuts) {
+      if (cut > kmax) break;
+      Plan pl;
+      const double t = decompose(sz, n, gated, sms, c, (kmax + cut - 1) / cut, &pl);
+      if (t >= 0.0 && (best_clocks < 0.0 || t < best_clocks)) {
+        best_clocks = t;
+        *best = pl;
+      }
+    }
+  }
+  return best_clocks >= 0.0;
+}
+
+// ---- operands -----------------------------------------------------------------------------------------
+
+// A matrix as it is stored: rows x cols values, row-major.
+struct Matrix {
+  const void* ptr;
+  int64_t rows, cols, ld;
+};
+
+// TMA takes 16-byte aligned rows. A single row has no stride that matters.
+bool addressable(const Matrix& m) { return ((uintptr_t)m.ptr & 15) == 0 && (m.ld % 8 == 0 || m.rows == 1); }
+
+bool make_map(CUtensorMap* map, int type, const Matrix& m, int box_rows) {
+  const int64_t ld = m.rows == 1 ? (m.cols + 7) / 8 * 8 : m.ld;
+  const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {(cuuint32_t)TK, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return g_encode(map, type == HGEMM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                  const_cast<void*>(m.ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int64_t padded(int64_t cols) { return (cols + 63) / 64 * 64; }
+inline unsigned capped(int64_t n) { return (unsigned)(n < 65535 ? n : 65535); }
+
+// Operands that need rewriting, collected so that one launch and one buffer serve them all.
+class Packer {
+ public:
+  explicit Packer(size_t first_free = 0) : bytes_(first_free) {}
+  void add(Matrix* m) {
+    if (addressable(*m)) return;
+    for (int i = 0; i < n_; ++i)
+      if (src_[i].ptr == m->ptr && src_[i].ld == m->ld && src_[i].rows == m->rows && src_[i].cols == m->cols) {
+        users_[nu_] = m;
+        of_[nu_++] = i;
+        return;
+      }
+    src_[n_] = *m;
+    at_[n_] = bytes_;
+    bytes_ += (size_t)m->rows * padded(m->cols) * 2;
+    users_[nu_] = m;
+    of_[nu_++] = n_++;
+  }
+  size_t bytes() const { return bytes_; }
+  bool launch(char* buf, cudaStream_t stream) {
+    if (n_ == 0) return true;
+    PackOps ops;
+    memset(&ops, 0, sizeof(ops));
+    int64_t gx = 0, gy = 0;
+    for (int i = 0; i < n_; ++i) {
+      const Matrix& m = src_[i];
+      ops.op[i] = PackOp{static_cast<const uint16_t*>(m.ptr), m.ld, (int)m.rows, (int)m.cols,
+                         reinterpret_cast<uint16_t*>(buf + at_[i]), padded(m.cols)};
+      if ((m.cols + 255) / 256 > gx) gx = (m.cols + 255) / 256;
+      if (m.rows > gy) gy = m.rows;
+    }
+    if (!lm::launch(hgemm_pack_kernel, dim3((unsigned)gx, capped(gy), (unsigned)n_), dim3(256), 0, 1, stream, ops)) return false;
+    for (int i = 0; i < nu_; ++i) *users_[i] = Matrix{buf + at_[of_[i]], users_[i]->rows, users_[i]->cols, padded(users_[i]->cols)};
+    return true;
+  }
+
+ private:
+  size_t bytes_;
+  int n_ = 0, nu_ = 0;
+  Matrix src_[3];
+  size_t at_[3];
+  Matrix* users_[6];
+  int of_[6];
+};
+
+// One product for the tensor-core kernel: out (M x N, rows m, columns n) from lane operand P and column
+// operand Q, over one or two contraction segments.
+struct Product {
+  int64_t N, M;
+  int nseg;
+  int64_t K[2];
+  Matrix p[2], q[2];
+  bool p_mn, q_mn;
+  int act = HGEMM_ACT_NONE;
+  const void* bias = nullptr;
+  const void* R = nullptr;
+  int64_t ldr = 0;
+  void* D = nullptr;
+  int64_t ldd = 0;
+  void* Z = nullptr;
+  int64_t ldz = 0;
+  void* U = nullptr;
+  int64_t ldu = 0;
+  Size size() const {
+    int64_t kb = 0;
+    for (int i = 0; i < nseg; ++i) kb += (K[i] + TK - 1) / TK;
+    return Size{N, M, (int)kb};
+  }
+};
+
+size_t workspace_bytes(const Plan& pl) {
+  const Config& c = kConfigs[pl.config];
+  return (size_t)pl.slots * c.cg * c.bm * 128 * sizeof(float);
+}
+
+// Longest contraction first (the schedule assumes it), stable.
+void order(Product** pr, int n) {
+  for (int i = 1; i < n; ++i)
+    for (int j = i; j > 0 && pr[j]->size().kblocks > pr[j - 1]->size().kblocks; --j) {
+      Product* t = pr[j];
+      pr[j] = pr[j - 1];
+      pr[j - 1] = t;
+    }
+}
+
+bool plan_products(Product** pr, int n, bool gated, int sms, Plan* pl) {
+  Size sz[MAX_PROBLEMS];
+  for (int i = 0; i < n; ++i) sz[i] = pr[i]->size();
+  return make_plan(sz, n, gated, sms, pl);
+}
+
+int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::DeviceState* st, float* ws, int* counters,
+                 cudaStream_t stream) {
+  const Config& c = kConfigs[pl.config];
+  Params p;
+  memset(&p, 0, sizeof(p));
+  const int qrows = c.bm / c.cg;
+  for (int i = 0; i < n; ++i) {
+    const Product& s = *pr[i];
+    Problem& d = p.prob[i];
+    const Plan::Part& q = pl.part[i];
+    const int np = gated ? 2 : s.nseg, nq = s.nseg;
+    for (int j = 0; j < np; ++j)
+      if (!make_map(&d.p[j], type, s.p[j], 64)) return DGEMM_ERR_CUDA;
+    for (int j = 0; j < nq; ++j)
+      if (!make_map(&d.q[j], type, s.q[j], s.q_mn || qrows >= 64 ? 64 : qrows)) return DGEMM_ERR_CUDA;
+    d.N = (int)s.N;
+    d.M = (int)s.M;
+    d.tiles_n = q.tiles_n;
+    d.tiles_m = q.tiles_m;
+    d.kblocks = s.size().kblocks;
+    d.kb_seg0 = (int)((s.K[0] + TK - 1) / TK);
+    d.p_mn = s.p_mn;
+    d.q_mn = s.q_mn;
+    d.dp_tiles = q.dp_tiles;
+    d.split = q.split;
+    d.kb_per_split = q.kb_per_split;
+    d.units = q.units;
+    d.slot0 = q.slot0;
+    d.counter0 = q.counter0;
+    d.act = s.act;
+    d.bias = s.bias;
+    d.R = s.R;
+    d.D = s.D;
+    d.Z = s.Z;
+    d.U = s.U;
+    d.ldr = s.ldr;
+    d.ldd = s.ldd;
+    d.ldz = s.ldz;
+    d.ldu = s.ldu;
+  }
+  p.nprob = n;
+  p.units = pl.units;
+  p.ws = ws;
+  p.counters = counters;
+  const int drop = g_drop_limit_us.load();
+  p.wait_limit_ns = drop > 0 ? (unsigned long long)drop * 1000ull : kWaitLimitNs;
+  p.drop = drop > 0;
+  p.status = st->status;
+  return launch_tc(type, gated, pl.config, pl.clusters, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
+}
+
+// ---- validation -----------------------------------------------------------------------------------------
+
+bool bad_type(int type) { return type != HGEMM_TYPE_F16 && type != HGEMM_TYPE_BF16; }
+bool bad_op(int op) { return op != DGEMM_OP_N && op != DGEMM_OP_T; }
+bool bad_act(int act) { return act < 0 || act >= HGEMM_ACT_COUNT; }
+
+int64_t span(int64_t rows, int64_t cols, int64_t ld) { return rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * 2 : 0; }
+
+// A matrix argument: NULL only where it is empty or optional, element-aligned, ld >= max(1, cols).
+int check(const void* ptr, int64_t rows, int64_t cols, int64_t ld, bool optional = false) {
+  if (optional && !ptr) return DGEMM_OK;
+  if (ld < (cols > 0 ? cols : 1)) return DGEMM_ERR_BAD_LD;
+  if (rows == 0 || cols == 0) return DGEMM_OK;
+  if (!ptr) return DGEMM_ERR_NULL;
+  if ((uintptr_t)ptr & 1) return DGEMM_ERR_ALIGN;
+  if (ld > (int64_t)1 << 38) return DGEMM_ERR_BAD_LD;
+  return DGEMM_OK;
+}
+
+struct Range {
+  const void* ptr;
+  int64_t bytes;
+};
+// Outputs must not overlap inputs or one another; the first `nout` ranges are the outputs.
+bool aliased(const Range* r, int nout, int n) {
+  for (int i = 0; i < nout; ++i)
+    for (int j = i + 1; j < n; ++j)
+      if (r[i].ptr && r[j].ptr && r[i].bytes > 0 && r[j].bytes > 0 && lm::ranges_overlap(r[i].ptr, r[i].bytes, r[j].ptr, r[j].bytes))
+        return true;
+  return false;
+}
+
+#define HGEMM_TRY(expr)             \
+  do {                              \
+    const int rc_ = (expr);         \
+    if (rc_ != DGEMM_OK) return rc_; \
+  } while (0)
+
+template <typename T>
+bool launch_empty(int64_t M, int64_t N, const void* bias, int act, const void* R, int64_t ldr, void* D, int64_t ldd, void* Z, int64_t ldz,
+                  cudaStream_t stream) {
+  return lm::launch(hgemm_empty_kernel<T>, dim3((unsigned)((N + 255) / 256), capped(M)), dim3(256), 0, 1, stream, (int)M, (int)N,
+                    static_cast<const T*>(bias), act, static_cast<const T*>(R), (long long)ldr, static_cast<T*>(D), (long long)ldd,
+                    static_cast<T*>(Z), (long long)ldz);
+}
+int run_empty(int type, int64_t M, int64_t N, const void* bias, int act, const void* R, int64_t ldr, void* D, int64_t ldd, void* Z,
+              int64_t ldz, cudaStream_t stream) {
+  const bool ok = type == HGEMM_TYPE_BF16 ? launch_empty<__nv_bfloat16>(M, N, bias, act, R, ldr, D, ldd, Z, ldz, stream)
+                                          : launch_empty<__half>(M, N, bias, act, R, ldr, D, ldd, Z, ldz, stream);
+  return ok ? DGEMM_OK : DGEMM_ERR_CUDA;
+}
+
+// Packs what needs it and runs the products: the whole of a forward call.
+int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
+  lm::DeviceState* st = nullptr;
+  HGEMM_TRY(lm::device_state(&st));
+  Plan pl;
+  if (!plan_products(&prod, 1, gated, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
+  scratch::Hold hold(st->scratch, stream);
+  Packer pack;
+  pack.add(&prod->p[0]);
+  if (gated) pack.add(&prod->p[1]);
+  pack.add(&prod->q[0]);
+  if (pack.bytes() > 0) {
+    char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes()));
+    if (!buf || !pack.launch(buf, stream)) return DGEMM_ERR_CUDA;
+  }
+  float* ws = nullptr;
+  if (pl.slots > 0) {
+    ws = static_cast<float*>(hold.workspace(workspace_bytes(pl)));
+    if (!ws) return DGEMM_ERR_CUDA;
+  }
+  return run_products(type, gated, &prod, 1, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, stream);
+}
+
+}  // namespace
+
+namespace lm {
+
+EncodeTiledFn encode_tiled() { return g_encode; }
+
+int device_state(DeviceState** out) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
+    (void)cudaGetLastError();
+    return DGEMM_ERR_DEVICE;
+  }
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceState& st = g_dev[dev];
+  if (!st.ready) {
+    int major = 0, sms = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return DGEMM_ERR_DEVICE;
+    }
+    if (major != 10) return DGEMM_ERR_DEVICE;
+    if (cudaGetSymbolAddress(reinterpret_cast<void**>(&st.status), g_hgemm_status_word) != cudaSuccess ||
+        cudaGetSymbolAddress(reinterpret_cast<void**>(&st.counters), g_hgemm_counters) != cudaSuccess)
+      return DGEMM_ERR_CUDA;
+    if (!configure_all<__half, false>() || !configure_all<__half, true>() || !configure_all<__nv_bfloat16, false>() ||
+        !configure_all<__nv_bfloat16, true>())
+      return DGEMM_ERR_CUDA;
+    if (!g_encode) {
+      void* fn = nullptr;
+      cudaDriverEntryPointQueryResult qres;
+      if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn ||
+          qres != cudaDriverEntryPointSuccess)
+        return DGEMM_ERR_CUDA;
+      g_encode = reinterpret_cast<EncodeTiledFn>(fn);
+    }
+    st.sm_count = sms;
+    st.ready = true;
+  }
+  *out = &st;
+  return DGEMM_OK;
+}
+
+}  // namespace lm
+
+extern "C" {
+
+int hgemm_epilogue(int type, int transa, int transb, int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* B,
+                   int64_t ldb, const void* bias, int act, const void* R, int64_t ldr, void* D, int64_t ldd, void* Z, int64_t ldz,
+                   void* stream) {
+  if (bad_type(type) || bad_act(act)) return DGEMM_ERR_VARIANT;
+  if (bad_op(transa) || bad_op(transb)) return DGEMM_ERR_BAD_DIM;
+  if (M < 0 || N < 0 || K < 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  if (M == 0 || N == 0) return DGEMM_OK;
+  const int64_t ar = transa ? K : M, ac = transa ? M : K, br = transb ? N : K, bc = transb ? K : N;
+  HGEMM_TRY(check(A, ar, ac, lda));
+  HGEMM_TRY(check(B, br, bc, ldb));
+  HGEMM_TRY(check(R, M, N, ldr, true));
+  HGEMM_TRY(check(D, M, N, ldd));
+  HGEMM_TRY(check(Z, M, N, ldz, true));
+  if ((uintptr_t)bias & 1) return DGEMM_ERR_ALIGN;
+  const bool in_place = R == D && ldr == ldd;
+  const Range rg[6] = {{D, span(M, N, ldd)},   {Z, span(M, N, ldz)}, {A, span(ar, ac, lda)},
+                       {B, span(br, bc, ldb)}, {bias, N * 2},        {R, span(M, N, ldr)}};
+  if (aliased(rg, 2, in_place ? 5 : 6)) return DGEMM_ERR_ALIAS;
+  if (in_place && Z && lm::ranges_overlap(Z, span(M, N, ldz), R, span(M, N, ldr))) return DGEMM_ERR_ALIAS;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (K == 0) {
+    lm::DeviceState* st = nullptr;
+    HGEMM_TRY(lm::device_state(&st));
+    return run_empty(type, M, N, bias, act, R, ldr, D, ldd, Z, ldz, s);
+  }
+  Product pr;
+  pr.N = N;
+  pr.M = M;
+  pr.nseg = 1;
+  pr.K[0] = K;
+  pr.p[0] = Matrix{B, br, bc, ldb};
+  pr.p_mn = !transb;
+  pr.q[0] = Matrix{A, ar, ac, lda};
+  pr.q_mn = transa != 0;
+  pr.act = act;
+  pr.bias = bias;
+  pr.R = R;
+  pr.ldr = ldr;
+  pr.D = D;
+  pr.ldd = ldd;
+  pr.Z = Z;
+  pr.ldz = ldz;
+  return forward(type, false, &pr, s);
+}
+
+int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* B,
+                       int64_t ldb, int act, const void* Z, int64_t ldz, const void* dD, int64_t lddd, void* dA, int64_t ldda, void* dB,
+                       int64_t lddb, float* dbias, void* stream) {
+  if (bad_type(type) || bad_act(act)) return DGEMM_ERR_VARIANT;
+  if (bad_op(transa) || bad_op(transb)) return DGEMM_ERR_BAD_DIM;
+  if (M < 0 || N < 0 || K < 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  const int64_t ar = transa ? K : M, ac = transa ? M : K, br = transb ? N : K, bc = transb ? K : N;
+  if (dB) HGEMM_TRY(check(A, ar, ac, lda));
+  if (dA) HGEMM_TRY(check(B, br, bc, ldb));
+  if (act != HGEMM_ACT_NONE) HGEMM_TRY(check(Z, M, N, ldz));
+  HGEMM_TRY(check(dD, M, N, lddd));
+  HGEMM_TRY(check(dA, ar, ac, ldda, true));
+  HGEMM_TRY(check(dB, br, bc, lddb, true));
+  if ((uintptr_t)dbias & 3) return DGEMM_ERR_ALIGN;
+  const Range rg[7] = {{dA, span(ar, ac, ldda)}, {dB, span(br, bc, lddb)}, {dbias, N * 4},
+                       {dB ? A : nullptr, span(ar, ac, lda)}, {dA ? B : nullptr, span(br, bc, ldb)},
+                       {act != HGEMM_ACT_NONE ? Z : nullptr, span(M, N, ldz)}, {dD, span(M, N, lddd)}};
+  if (aliased(rg, 3, 7)) return DGEMM_ERR_ALIAS;
+  lm::DeviceState* st = nullptr;
+  HGEMM_TRY(lm::device_state(&st));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // empty sums
+  if (dA && N == 0 && M > 0 && K > 0) HGEMM_TRY(run_empty(type, ar, ac, nullptr, HGEMM_ACT_NONE, nullptr, 0, dA, ldda, nullptr, 0, s));
+  if (dB && M == 0 && N > 0 && K > 0) HGEMM_TRY(run_empty(type, br, bc, nullptr, HGEMM_ACT_NONE, nullptr, 0, dB, lddb, nullptr, 0, s));
+  if (dbias && M == 0 && N > 0 && cudaMemsetAsync(dbias, 0, (size_t)N * 4, s) != cudaSuccess) return DGEMM_ERR_CUDA;
+  if (M == 0 || N == 0) return DGEMM_OK;
+  const bool want_a = dA && K > 0, want_b = dB && K > 0;
+  if (!want_a && !want_b && !dbias) return DGEMM_OK;
+
+  Product pa, pb;
+  Product* list[2];
+  int n = 0;
+  Matrix dz{dD, M, N, lddd};
+  const bool want_dz = (want_a || want_b) && (act != HGEMM_ACT_NONE || !addressable(dz));
+  const Matrix a{A, ar, ac, lda}, b{B, br, bc, ldb};
+  if (want_a) {
+    pa.N = ac;
+    pa.M = ar;
+    pa.nseg = 1;
+    pa.K[0] = N;
+    pa.D = dA;
+    pa.ldd = ldda;
+    pa.p[0] = transa ? dz : b;
+    pa.q[0] = transa ? b : dz;
+    (transa ? pa.p_mn : pa.q_mn) = false;          // dZ: contraction over its columns
+    (transa ? pa.q_mn : pa.p_mn) = transb != 0;    // B stored N x K: contraction over its rows
+    list[n++] = &pa;
+  }
+  if (want_b) {
+    pb.N = bc;
+    pb.M = br;
+    pb.nseg = 1;
+    pb.K[0] = M;
+    pb.D = dB;
+    pb.ldd = lddb;
+    pb.p[0] = transb ? a : dz;
+    pb.q[0] = transb ? dz : a;
+    (transb ? pb.q_mn : pb.p_mn) = true;           // dZ: contraction over its rows
+    (transb ? pb.p_mn : pb.q_mn) = transa == 0;    // A stored M x K: contraction over its rows
+    list[n++] = &pb;
+  }
+  Plan pl;
+  order(list, n);
+  if (n > 0 && !plan_products(list, n, false, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
+
+  scratch::Hold hold(st->scratch, s);
+  const int64_t lddz = padded(N);
+  Packer pack(want_dz ? (size_t)M * lddz * 2 : 0);
+  if (want_a) pack.add(transa ? &pa.q[0] : &pa.p[0]);
+  if (want_b) pack.add(transb ? &pb.p[0] : &pb.q[0]);
+  char* buf = nullptr;
+  if (pack.bytes() > 0 && !(buf = static_cast<char*>(hold.pack_buffer(pack.bytes())))) return DGEMM_ERR_CUDA;
+
+  // dZ and dbias
+  const bool want_act = want_dz || dbias;
+  ActBwdParams ap;
+  memset(&ap, 0, sizeof(ap));
+  int vec = 1;
+  int64_t strips = 0, chunks = 1;
+  if (want_act) {
+    const Matrix z{act != HGEMM_ACT_NONE ? Z : dD, M, N, act != HGEMM_ACT_NONE ? ldz : lddd};
+    vec = addressable(dz) && addressable(z) ? 8 : 1;
+    strips = (N + 32 * vec - 1) / (32 * vec);
+    // enough blocks for the machine, at least 32 rows each (8 warps x 4 rows)
+    chunks = ((int64_t)st->sm_count * 8 + strips - 1) / strips;
+    if (chunks > (M + 31) / 32) chunks = (M + 31) / 32;
+    if (chunks > 1 && strips > lm::kCounters) chunks = 1;
+    if (chunks > 256) chunks = 256;
+    if (!dbias) {
+      chunks = (M + 31) / 32;
+      if (chunks > 65535) chunks = 65535;
+    }
+    ap.rows_per_chunk = (int)((M + chunks - 1) / chunks);
+    chunks = (M + ap.rows_per_chunk - 1) / ap.rows_per_chunk;
+    ap.M = (int)M;
+    ap.N = (int)N;
+    ap.Z = act != HGEMM_ACT_NONE ? Z : nullptr;
+    ap.dD = dD;
+    ap.dZ = want_dz ? buf : nullptr;
+    ap.dbias = dbias;
+    ap.ldz = ldz;
+    ap.lddd = lddd;
+    ap.lddz = lddz;
+    ap.act = act;
+  }
+  size_t ws_bytes = n > 0 ? workspace_bytes(pl) : 0;
+  if (dbias && chunks > 1 && (size_t)chunks * N * 4 > ws_bytes) ws_bytes = (size_t)chunks * N * 4;
+  float* ws = nullptr;
+  if (ws_bytes > 0 && !(ws = static_cast<float*>(hold.workspace(ws_bytes)))) return DGEMM_ERR_CUDA;
+  int* counters = st->counters + hold.lease_index() * lm::kCounters;
+  if (want_act) {
+    ap.partial = ws;
+    ap.counters = counters;
+    const dim3 grid((unsigned)strips, (unsigned)chunks);
+    bool ok;
+    if (type == HGEMM_TYPE_BF16)
+      ok = vec == 8 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, 1, s, ap)
+                    : lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, 1, s, ap);
+    else
+      ok = vec == 8 ? lm::launch(hgemm_act_bwd_kernel<__half, 8>, grid, dim3(256), 0, 1, s, ap)
+                    : lm::launch(hgemm_act_bwd_kernel<__half, 1>, grid, dim3(256), 0, 1, s, ap);
+    if (!ok) return DGEMM_ERR_CUDA;
+  }
+  if (n == 0) return DGEMM_OK;
+  if (want_dz) {
+    const Matrix packed{buf, M, N, lddz};
+    if (want_a) (transa ? pa.p[0] : pa.q[0]) = packed;
+    if (want_b) (transb ? pb.q[0] : pb.p[0]) = packed;
+  }
+  if (!pack.launch(buf, s)) return DGEMM_ERR_CUDA;
+  return run_products(type, false, list, n, pl, st, ws, counters, s);
+}
+
+int hgemm_gated(int type, int transw, int64_t M, int64_t F, int64_t K, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
+                const void* Wu, int64_t ldwu, int act, void* H, int64_t ldh, void* G, int64_t ldg, void* U, int64_t ldu, void* stream) {
+  if (bad_type(type) || bad_act(act)) return DGEMM_ERR_VARIANT;
+  if (bad_op(transw)) return DGEMM_ERR_BAD_DIM;
+  if (M < 0 || F < 0 || K < 0 || M > kMaxDim || F > kMaxDim || K > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  if (M == 0 || F == 0) return DGEMM_OK;
+  const int64_t wr = transw ? F : K, wc = transw ? K : F;
+  HGEMM_TRY(check(X, M, K, ldx));
+  HGEMM_TRY(check(Wg, wr, wc, ldwg));
+  HGEMM_TRY(check(Wu, wr, wc, ldwu));
+  HGEMM_TRY(check(H, M, F, ldh));
+  HGEMM_TRY(check(G, M, F, ldg, true));
+  HGEMM_TRY(check(U, M, F, ldu, true));
+  if ((G == nullptr) != (U == nullptr)) return DGEMM_ERR_NULL;
+  const Range rg[6] = {{H, span(M, F, ldh)}, {G, span(M, F, ldg)},    {U, span(M, F, ldu)},
+                       {X, span(M, K, ldx)}, {Wg, span(wr, wc, ldwg)}, {Wu, span(wr, wc, ldwu)}};
+  if (aliased(rg, 3, 6)) return DGEMM_ERR_ALIAS;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (K == 0) {  // G = U = 0, H = act(0) 0
+    lm::DeviceState* st = nullptr;
+    HGEMM_TRY(lm::device_state(&st));
+    HGEMM_TRY(run_empty(type, M, F, nullptr, HGEMM_ACT_NONE, nullptr, 0, H, ldh, G, ldg, s));
+    return U ? run_empty(type, M, F, nullptr, HGEMM_ACT_NONE, nullptr, 0, U, ldu, nullptr, 0, s) : (int)DGEMM_OK;
+  }
+  Product pr;
+  pr.N = F;
+  pr.M = M;
+  pr.nseg = 1;
+  pr.K[0] = K;
+  pr.p[0] = Matrix{Wg, wr, wc, ldwg};
+  pr.p[1] = Matrix{Wu, wr, wc, ldwu};
+  pr.p_mn = !transw;
+  pr.q[0] = Matrix{X, M, K, ldx};
+  pr.q_mn = false;
+  pr.act = act;
+  pr.D = H;
+  pr.ldd = ldh;
+  pr.Z = G;
+  pr.ldz = ldg;
+  pr.U = U;
+  pr.ldu = ldu;
+  return forward(type, true, &pr, s);
+}
+
+int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
+                    const void* Wu, int64_t ldwu, int act, const void* G, int64_t ldg, const void* U, int64_t ldu, const void* dH,
+                    int64_t lddh, void* dX, int64_t lddx, void* dWg, int64_t lddwg, void* dWu, int64_t lddwu, void* stream) {
+  if (bad_type(type) || bad_act(act)) return DGEMM_ERR_VARIANT;
+  if (bad_op(transw)) return DGEMM_ERR_BAD_DIM;
+  if (M < 0 || F < 0 || K < 0 || M > kMaxDim || F > kMaxDim || K > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  const int64_t wr = transw ? F : K, wc = transw ? K : F;
+  const bool need_x = dWg || dWu;
+  if (need_x) HGEMM_TRY(check(X, M, K, ldx));
+  if (dX) {
+    HGEMM_TRY(check(Wg, wr, wc, ldwg));
+    HGEMM_TRY(check(Wu, wr, wc, ldwu));
+  }
+  HGEMM_TRY(check(G, M, F, ldg));
+  HGEMM_TRY(check(U, M, F, ldu));
+  HGEMM_TRY(check(dH, M, F, lddh));
+  HGEMM_TRY(check(dX, M, K, lddx, true));
+  HGEMM_TRY(check(dWg, wr, wc, lddwg, true));
+  HGEMM_TRY(check(dWu, wr, wc, lddwu, true));
+  const Range rg[9] = {{dX, span(M, K, lddx)}, {dWg, span(wr, wc, lddwg)}, {dWu, span(wr, wc, lddwu)},
+                       {need_x ? X : nullptr, span(M, K, ldx)}, {dX ? Wg : nullptr, span(wr, wc, ldwg)},
+                       {dX ? Wu : nullptr, span(wr, wc, ldwu)}, {G, span(M, F, ldg)}, {U, span(M, F, ldu)}, {dH, span(M, F, lddh)}};
+  if (aliased(rg, 3, 9)) return DGEMM_ERR_ALIAS;
+  lm::DeviceState* st = nullptr;
+  HGEMM_TRY(lm::device_state(&st));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (K == 0) return DGEMM_OK;  // every output is empty
+  if (dX && F == 0 && M > 0) HGEMM_TRY(run_empty(type, M, K, nullptr, HGEMM_ACT_NONE, nullptr, 0, dX, lddx, nullptr, 0, s));
+  for (int i = 0; i < 2; ++i) {
+    void* w = i ? dWu : dWg;
+    if (w && M == 0 && F > 0)
+      HGEMM_TRY(run_empty(type, wr, wc, nullptr, HGEMM_ACT_NONE, nullptr, 0, w, i ? lddwu : lddwg, nullptr, 0, s));
+  }
+  if (M == 0 || F == 0 || (!dX && !dWg && !dWu)) return DGEMM_OK;
+
+  // dG and dU, rounded, in scratch rows of a multiple of 128 bytes
+  const int64_t ldo = padded(F);
+  const size_t half_bytes = (size_t)M * ldo * 2;
+  Product px, pw[2];
+  Product* list[3];
+  int n = 0;
+  Matrix dgu[2] = {Matrix{nullptr, M, F, ldo}, Matrix{nullptr, M, F, ldo}};
+  Matrix x{X, M, K, ldx}, w[2] = {Matrix{Wg, wr, wc, ldwg}, Matrix{Wu, wr, wc, ldwu}};
+  if (dX) {
+    px.N = K;
+    px.M = M;
+    px.nseg = 2;
+    px.K[0] = px.K[1] = F;
+    px.p_mn = transw != 0;
+    px.q_mn = false;
+    px.D = dX;
+    px.ldd = lddx;
+    list[n++] = &px;
+  }
+  for (int i = 0; i < 2; ++i) {
+    void* out = i ? dWu : dWg;
+    if (!out) continue;
+    pw[i].N = wc;
+    pw[i].M = wr;
+    pw[i].nseg = 1;
+    pw[i].K[0] = M;
+    pw[i].p_mn = pw[i].q_mn = true;
+    pw[i].D = out;
+    pw[i].ldd = i ? lddwu : lddwg;
+    list[n++] = &pw[i];
+  }
+  Plan pl;
+  order(list, n);
+  if (!plan_products(list, n, false, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
+
+  scratch::Hold hold(st->scratch, s);
+  Packer pack(2 * half_bytes);
+  if (need_x) pack.add(&x);
+  if (dX) {
+    pack.add(&w[0]);
+    pack.add(&w[1]);
+  }
+  char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes()));
+  if (!buf) return DGEMM_ERR_CUDA;
+  float* ws = nullptr;
+  if (pl.slots > 0 && !(ws = static_cast<float*>(hold.workspace(workspace_bytes(pl))))) return DGEMM_ERR_CUDA;
+  GatedBwdParams gp;
+  memset(&gp, 0, sizeof(gp));
+  gp.M = (int)M;
+  gp.F = (int)F;
+  gp.G = G;
+  gp.U = U;
+  gp.dH = dH;
+  gp.dG = buf;
+  gp.dU = buf + half_bytes;
+  gp.ldg = ldg;
+  gp.ldu = ldu;
+  gp.lddh = lddh;
+  gp.ldo = ldo;
+  gp.act = act;
+  dgu[0].ptr = gp.dG;
+  dgu[1].ptr = gp.dU;
+  const int vec = addressable(Matrix{G, M, F, ldg}) && addressable(Matrix{U, M, F, ldu}) && addressable(Matrix{dH, M, F, lddh}) ? 8 : 1;
+  int64_t blocks = ((F + vec - 1) / vec * M + 255) / 256;
+  if (blocks > (int64_t)st->sm_count * 16) blocks = (int64_t)st->sm_count * 16;
+  const dim3 grid((unsigned)blocks);
+  bool ok;
+  if (type == HGEMM_TYPE_BF16)
+    ok = vec == 8 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, 1, s, gp)
+                  : lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, 1, s, gp);
+  else
+    ok = vec == 8 ? lm::launch(hgemm_gated_bwd_kernel<__half, 8>, grid, dim3(256), 0, 1, s, gp)
+                  : lm::launch(hgemm_gated_bwd_kernel<__half, 1>, grid, dim3(256), 0, 1, s, gp);
+  if (!ok || !pack.launch(buf, s)) return DGEMM_ERR_CUDA;
+  for (int i = 0; i < 2; ++i) {
+    px.p[i] = w[i];
+    px.q[i] = dgu[i];
+    pw[i].p[0] = transw ? x : dgu[i];
+    pw[i].q[0] = transw ? dgu[i] : x;
+  }
+  return run_products(type, false, list, n, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, s);
+}
+
+int hgemm_last_device_status(void* stream) {
+  lm::DeviceState* st = nullptr;
+  HGEMM_TRY(lm::device_state(&st));
+  if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return DGEMM_ERR_CUDA;
+  }
+  int v = 0;
+  if (cudaMemcpy(&v, st->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return DGEMM_ERR_CUDA;
+  if (v != 0 && cudaMemset(st->status, 0, sizeof(int)) != cudaSuccess) return DGEMM_ERR_CUDA;
+  return v;
+}
+
+int hgemm_plan(int64_t M, int64_t N, int64_t K, int gated, int sm_count, int* out) {
+  if (!out) return DGEMM_ERR_NULL;
+  if (M <= 0 || N <= 0 || K <= 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim || sm_count < 0 || sm_count == 1) return DGEMM_ERR_BAD_DIM;
+  const Size sz{N, M, (int)((K + TK - 1) / TK)};
+  Plan pl;
+  if (!make_plan(&sz, 1, gated != 0, sm_count ? sm_count : 148, &pl)) return DGEMM_ERR_BAD_DIM;
+  const Config& c = kConfigs[pl.config];
+  const Plan::Part& q = pl.part[0];
+  const int v[8] = {c.cg, c.bm, pl.nt, pl.clusters, sz.kblocks, q.dp_tiles, q.split, q.kb_per_split};
+  memcpy(out, v, sizeof(v));
+  return DGEMM_OK;
+}
+
+int hgemm_set_test_drop_loads(int limit_us) {
+  if (limit_us < 0 || limit_us > 4000000) return DGEMM_ERR_VARIANT;
+  g_drop_limit_us.store(limit_us);
+  return DGEMM_OK;
+}
+
+}  // extern "C"

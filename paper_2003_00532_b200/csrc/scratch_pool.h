@@ -84,6 +84,10 @@ class Hold {
   // use under stream capture). The contents are whatever the previous user left.
   void* workspace(size_t bytes) { return get(kWorkspace, bytes, 0); }
 
+  // Which of the pool's leases this call holds (after a request above or below has succeeded): an
+  // index for state kept beside the buffers.
+  int lease_index() const { return lease_ ? (int)(lease_ - pool_.lease) : 0; }
+
   // At least `bytes` for packed operands; grown with `bytes / 4` of head room against regrowing on
   // slightly larger problems.
   void* pack_buffer(size_t bytes) { return get(kPack, bytes, bytes / 4); }
