@@ -338,9 +338,9 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     const Plan::Part& q = pl.part[i];
     const int np = gated ? 2 : s.nseg, nq = s.nseg;
     for (int j = 0; j < np; ++j)
-      if (!make_map(&d.p[j], type, s.p[j], 64)) return DGEMM_ERR_CUDA;
+      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated ? 64 : 128)) return DGEMM_ERR_CUDA;
     for (int j = 0; j < nq; ++j)
-      if (!make_map(&d.q[j], type, s.q[j], s.q_mn || qrows >= 64 ? 64 : qrows)) return DGEMM_ERR_CUDA;
+      if (!make_map(&d.q[j], type, s.q[j], s.q_mn ? 64 : qrows)) return DGEMM_ERR_CUDA;
     d.N = (int)s.N;
     d.M = (int)s.M;
     d.tiles_n = q.tiles_n;

@@ -20,8 +20,9 @@
 // a workspace; the CTA that finishes the last part of a tile (a counter per tile) adds all parts in
 // order and runs the epilogue: one launch, no CTA waits for another, same bits every time.
 //
-// Roles (384 threads): warp 0 stages, warp 1 issues the MMAs, warp 2 owns the TMEM allocation, warps
-// 4-11 run the epilogue of one accumulator while the MMAs fill the other. In a pair the MMAs of
+// Roles (384 threads): warps 0 and 3 stage P and Q (one thread that issued all copies was the limit:
+// 479 ns per 64-wide k-block with four copies, against 366 ns for its MMAs; two threads with one or
+// two copies each are not), warp 1 issues the MMAs, warp 2 owns the TMEM allocation, warps 4-11 run the epilogue of one accumulator while the MMAs fill the other. In a pair the MMAs of
 // both CTAs are issued by the leader; each CTA stages its own 128 lanes and its half of Q.
 #pragma once
 
@@ -155,82 +156,83 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// Rows m0 .. m0 + CH - 1 (those below M) of column n: v[j] is the sum of row m0 + j.
-template <typename T, int CH, int ACT>
+// Rows m0 .. m0 + CH - 1 of column n: v[j] is the sum of row m0 + j. WHOLE: all of them are inside the
+// matrix; otherwise those below M. All loads are issued before the first store (R may be D).
+template <typename T, int CH, int ACT, bool WHOLE>
 __device__ __forceinline__ void emit_plain(const Problem& pr, const float* v, float bias, int m0, int n) {
-  const int rows = min(CH, pr.M - m0);
-  float r[CH];
+  const int rows = pr.M - m0;
+  T r[CH];
   if (pr.R) {
-    // all loads before the first store: R may be D
     const T* src = static_cast<const T*>(pr.R) + (long long)m0 * pr.ldr + n;
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-      r[j] = j < rows ? to_f32(*src) : 0.f;
-      src += pr.ldr;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < CH; ++j) r[j] = 0.f;
+    for (int j = 0; j < CH; ++j) r[j] = src[(WHOLE || j < rows ? j : 0) * pr.ldr];
   }
   if (pr.Z) {
     T* dst = static_cast<T*>(pr.Z) + (long long)m0 * pr.ldz + n;
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-      if (j < rows) *dst = from_f32<T>(v[j] + bias);
-      dst += pr.ldz;
-    }
+    for (int j = 0; j < CH; ++j)
+      if (WHOLE || j < rows) dst[j * pr.ldz] = from_f32<T>(v[j] + bias);
   }
   T* dst = static_cast<T*>(pr.D) + (long long)m0 * pr.ldd + n;
+  if (pr.R) {
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    if (j < rows) *dst = from_f32<T>(act_fwd<ACT>(v[j] + bias) + r[j]);
-    dst += pr.ldd;
+    for (int j = 0; j < CH; ++j)
+      if (WHOLE || j < rows) dst[j * pr.ldd] = from_f32<T>(act_fwd<ACT>(v[j] + bias) + to_f32(r[j]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+      if (WHOLE || j < rows) dst[j * pr.ldd] = from_f32<T>(act_fwd<ACT>(v[j] + bias));
   }
 }
 
-template <typename T, int CH, int ACT>
+template <typename T, int CH, int ACT, bool WHOLE>
 __device__ __forceinline__ void emit_gated(const Problem& pr, const float* g, const float* u, int m0, int n) {
-  const int rows = min(CH, pr.M - m0);
+  const int rows = pr.M - m0;
   if (pr.Z) {
     T* zg = static_cast<T*>(pr.Z) + (long long)m0 * pr.ldz + n;
     T* zu = static_cast<T*>(pr.U) + (long long)m0 * pr.ldu + n;
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-      if (j < rows) {
-        *zg = from_f32<T>(g[j]);
-        *zu = from_f32<T>(u[j]);
+    for (int j = 0; j < CH; ++j)
+      if (WHOLE || j < rows) {
+        zg[j * pr.ldz] = from_f32<T>(g[j]);
+        zu[j * pr.ldu] = from_f32<T>(u[j]);
       }
-      zg += pr.ldz;
-      zu += pr.ldu;
-    }
   }
   T* dst = static_cast<T*>(pr.D) + (long long)m0 * pr.ldd + n;
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    if (j < rows) *dst = from_f32<T>(act_fwd<ACT>(g[j]) * u[j]);
-    dst += pr.ldd;
-  }
+  for (int j = 0; j < CH; ++j)
+    if (WHOLE || j < rows) dst[j * pr.ldd] = from_f32<T>(act_fwd<ACT>(g[j]) * u[j]);
 }
 
+template <typename T, int CH, bool WHOLE>
+__device__ __forceinline__ void emit_plain_act(const Problem& pr, const float* v, float bias, int m0, int n) {
+  switch (pr.act) {
+    case HGEMM_ACT_NONE: emit_plain<T, CH, HGEMM_ACT_NONE, WHOLE>(pr, v, bias, m0, n); break;
+    case HGEMM_ACT_RELU: emit_plain<T, CH, HGEMM_ACT_RELU, WHOLE>(pr, v, bias, m0, n); break;
+    case HGEMM_ACT_GELU: emit_plain<T, CH, HGEMM_ACT_GELU, WHOLE>(pr, v, bias, m0, n); break;
+    case HGEMM_ACT_GELU_TANH: emit_plain<T, CH, HGEMM_ACT_GELU_TANH, WHOLE>(pr, v, bias, m0, n); break;
+    default: emit_plain<T, CH, HGEMM_ACT_SILU, WHOLE>(pr, v, bias, m0, n); break;
+  }
+}
 template <typename T, int CH>
 __device__ __forceinline__ void emit_plain_any(const Problem& pr, const float* v, float bias, int m0, int n) {
+  if (m0 + CH <= pr.M) emit_plain_act<T, CH, true>(pr, v, bias, m0, n);
+  else emit_plain_act<T, CH, false>(pr, v, bias, m0, n);
+}
+template <typename T, int CH, bool WHOLE>
+__device__ __forceinline__ void emit_gated_act(const Problem& pr, const float* g, const float* u, int m0, int n) {
   switch (pr.act) {
-    case HGEMM_ACT_NONE: emit_plain<T, CH, HGEMM_ACT_NONE>(pr, v, bias, m0, n); break;
-    case HGEMM_ACT_RELU: emit_plain<T, CH, HGEMM_ACT_RELU>(pr, v, bias, m0, n); break;
-    case HGEMM_ACT_GELU: emit_plain<T, CH, HGEMM_ACT_GELU>(pr, v, bias, m0, n); break;
-    case HGEMM_ACT_GELU_TANH: emit_plain<T, CH, HGEMM_ACT_GELU_TANH>(pr, v, bias, m0, n); break;
-    default: emit_plain<T, CH, HGEMM_ACT_SILU>(pr, v, bias, m0, n); break;
+    case HGEMM_ACT_NONE: emit_gated<T, CH, HGEMM_ACT_NONE, WHOLE>(pr, g, u, m0, n); break;
+    case HGEMM_ACT_RELU: emit_gated<T, CH, HGEMM_ACT_RELU, WHOLE>(pr, g, u, m0, n); break;
+    case HGEMM_ACT_GELU: emit_gated<T, CH, HGEMM_ACT_GELU, WHOLE>(pr, g, u, m0, n); break;
+    case HGEMM_ACT_GELU_TANH: emit_gated<T, CH, HGEMM_ACT_GELU_TANH, WHOLE>(pr, g, u, m0, n); break;
+    default: emit_gated<T, CH, HGEMM_ACT_SILU, WHOLE>(pr, g, u, m0, n); break;
   }
 }
 template <typename T, int CH>
 __device__ __forceinline__ void emit_gated_any(const Problem& pr, const float* g, const float* u, int m0, int n) {
-  switch (pr.act) {
-    case HGEMM_ACT_NONE: emit_gated<T, CH, HGEMM_ACT_NONE>(pr, g, u, m0, n); break;
-    case HGEMM_ACT_RELU: emit_gated<T, CH, HGEMM_ACT_RELU>(pr, g, u, m0, n); break;
-    case HGEMM_ACT_GELU: emit_gated<T, CH, HGEMM_ACT_GELU>(pr, g, u, m0, n); break;
-    case HGEMM_ACT_GELU_TANH: emit_gated<T, CH, HGEMM_ACT_GELU_TANH>(pr, g, u, m0, n); break;
-    default: emit_gated<T, CH, HGEMM_ACT_SILU>(pr, g, u, m0, n); break;
-  }
+  if (m0 + CH <= pr.M) emit_gated_act<T, CH, true>(pr, g, u, m0, n);
+  else emit_gated_act<T, CH, false>(pr, g, u, m0, n);
 }
 
 template <int CH>
@@ -298,8 +300,9 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
   ptx5::launch_dependents();
   grid_dependency_wait();
 
-  if (warp == 0 && lane == 0) {
-    // ---- stages: P boxes, then Q boxes; zero fill outside the matrices ----
+  if ((warp == 0 || warp == 3) && lane == 0) {
+    // ---- stages: warp 0 copies the P boxes, warp 3 the Q boxes; zero fill outside the matrices ----
+    const bool is_p = warp == 0;
     uint32_t it = 0;
     bool ok = !p.drop;
     for (int u = cluster; u < p.units && ok; u += clusters) {
@@ -307,10 +310,13 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       const Problem& pr = p.prob[w.prob];
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
-      const int n0 = tn * C::NT + rank * (GATED ? 64 : 128);
-      const int m0 = tm * BM + rank * C::QROWS;
-      const uint32_t q_box = pr.q_mn || C::QROWS >= 64 ? BOX_BYTES : C::QROWS * 128;
-      const uint32_t bytes = CG * (C::P_BYTES + C::QBOXES * q_box);
+      const bool mn = is_p ? pr.p_mn : pr.q_mn;
+      // first outer index of this CTA's rows of the operand
+      const int o0 = is_p ? tn * C::NT + rank * (GATED ? 64 : 128) : tm * BM + rank * C::QROWS;
+      const int boxes = is_p ? (GATED || mn ? 2 : 1) : (mn ? C::QBOXES : 1);
+      const int o_step = is_p && GATED ? 0 : 64;
+      const CUtensorMap* maps = is_p ? pr.p : pr.q;
+      const uint32_t bytes = CG * (C::P_BYTES + (pr.q_mn ? C::QBOXES * BOX_BYTES : C::QROWS * 128));
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
         const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u;
         if (!wait_bounded(empty_bar + 8 * s, ph ^ 1u, abort_flag, p)) {
@@ -318,27 +324,20 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
           break;
         }
         const uint32_t fb = CG == 1 ? full_bar + 8 * s : map_to_cta(full_bar + 8 * s, 0);
-        if (rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, bytes);
+        if (is_p && rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, bytes);
         const int seg = kb >= pr.kb_seg0 ? 1 : 0;
         const int k0 = (kb - (seg ? pr.kb_seg0 : 0)) * TK;
-        const uint32_t dst = base + s * C::STAGE_BYTES;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const CUtensorMap* map = &pr.p[GATED ? i : seg];
-          const int n = GATED ? n0 : n0 + 64 * i;
-          if (pr.p_mn) ptx5::tma_load_2d<CG>(dst + i * BOX_BYTES, map, n, k0, fb);
-          else ptx5::tma_load_2d<CG>(dst + i * BOX_BYTES, map, k0, n, fb);
-        }
-#pragma unroll
-        for (int i = 0; i < C::QBOXES; ++i) {
-          if (pr.q_mn) ptx5::tma_load_2d<CG>(dst + C::P_BYTES + i * BOX_BYTES, &pr.q[GATED ? 0 : seg], m0 + 64 * i, k0, fb);
-          else ptx5::tma_load_2d<CG>(dst + C::P_BYTES + i * BOX_BYTES, &pr.q[GATED ? 0 : seg], k0, m0 + 64 * i, fb);
+        const uint32_t dst = base + s * C::STAGE_BYTES + (is_p ? 0 : C::P_BYTES);
+        for (int i = 0; i < boxes; ++i) {
+          const CUtensorMap* map = maps + (GATED ? (is_p ? i : 0) : seg);
+          const int o = o0 + i * o_step;
+          ptx5::tma_load_2d<CG>(dst + i * BOX_BYTES, map, mn ? o : k0, mn ? k0 : o, fb);
         }
       }
     }
     // After a normal run every copy has been consumed. After an abort let the copies in flight land
     // (bounded); the leader's barriers count the bytes of both CTAs of a pair.
-    if (!ok && !p.drop && rank == 0) {
+    if (!ok && !p.drop && is_p && rank == 0) {
       const uint32_t n_inflight = it < (uint32_t)STAGES ? it : (uint32_t)STAGES;
       for (uint32_t j = it - n_inflight; j < it; ++j) {
         const unsigned long long t0 = globaltimer_ns();
