@@ -356,6 +356,8 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.slot0 = q.slot0;
     d.counter0 = q.counter0;
     d.act = s.act;
+    d.vec = (addressable(Matrix{s.D, s.M, s.N, s.ldd}) ? VEC_D : 0) | (addressable(Matrix{s.Z, s.M, s.N, s.ldz}) ? VEC_Z : 0) |
+            (addressable(Matrix{s.U, s.M, s.N, s.ldu}) ? VEC_U : 0) | (addressable(Matrix{s.R, s.M, s.N, s.ldr}) ? VEC_R : 0);
     d.bias = s.bias;
     d.R = s.R;
     d.D = s.D;

@@ -61,21 +61,25 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
                  : "memory");
 }
 
-// ---- TMEM loads: one warp reads 32 lanes (its own quarter) x 16 columns ------------------------------
-
-__device__ __forceinline__ void tmem_ld_x8(uint32_t addr, float* v) {
+// ---- TMEM loads ------------------------------------------------------------------------------------
+// One warp reads 16 lanes (the first or second half of its own quarter) x 8 X columns. Thread t gets, for
+// each block b of 8 columns, v[4 b + r]: lane t / 4 + 8 (r / 2), column 8 b + 2 (t % 4) + r % 2 -- the layout of
+// the 8 x 8 matrices that stmatrix and ldmatrix move.
+template <int X>
+__device__ __forceinline__ void tmem_ld_16x256b(uint32_t addr, float* v);
+template <>
+__device__ __forceinline__ void tmem_ld_16x256b<1>(uint32_t addr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr));
 }
-__device__ __forceinline__ void tmem_ld_x16(uint32_t addr, float* v) {
+template <>
+__device__ __forceinline__ void tmem_ld_16x256b<2>(uint32_t addr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr));
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
 }
 // Waits for this warp's TMEM loads. The loaded registers are operands, so no use of them can move
 // ahead of the wait.
@@ -97,6 +101,33 @@ __device__ __forceinline__ void tmem_ld_wait<16>(float* v) {
                :
                : "memory");
 }
+
+// ---- 8 x 8 matrices of 16-bit values between registers and shared memory, transposed ---------------------
+// Lane l gives the address of row l % 8 (16 bytes) of matrix l / 8; register i of thread t holds row values
+// t / 4 of rows 2 (t % 4) and 2 (t % 4) + 1 of matrix i.
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t* v) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint16_t lds16(uint32_t addr) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t addr, uint16_t v) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory"); }
 
 // ---- barriers and tile loads of a CTA pair -------------------------------------------------------------
 

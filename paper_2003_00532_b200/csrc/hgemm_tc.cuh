@@ -3,12 +3,15 @@
 //
 // Orientation. The tile's 128 TMEM lanes (256 over a CTA pair) run along the output's columns n and
 // its BM TMEM columns along the output's rows m: D^T = P Q^T with P = op(B)^T ("lane operand", the
-// weights) and Q = op(A) ("column operand", the tokens). Then
-//   - a warp of the epilogue holds 32 consecutive n of one row m in its 32 lanes, so that every load
-//     and store of D, Z, R is one contiguous 64-byte piece of a row, whatever the alignment or leading
-//     dimension: no staging through shared memory and no aligned / unaligned variants;
-//   - a bias is one register per thread;
-//   - few rows (single tokens) need a small BM, not a 128-row tile: BM = 16 .. 256.
+// weights) and Q = op(A) ("column operand", the tokens). Few rows (single tokens) then need a small
+// BM, not a 128-row tile: BM = 16 .. 256.
+//
+// Epilogue. A warp takes 32 lanes x CH columns at a time, in the register layout of 8 x 8 matrices. Results
+// are packed in pairs and turned into row pieces of 32 values by transposing matrix stores into a small
+// buffer of the warp's own, from which they leave as 16-byte vectors (rows that are 16-byte aligned)
+// or value by value (any other alignment, ragged last columns); a residual comes in the same way
+// backwards. Storing each lane's column directly, 2 bytes per lane, made the store instructions the
+// limit: 4096 x 9472 x 1024 took 94 us (125 with bias and GELU) where the MMAs take 54.
 //
 // Operands. Either may be stored with its contraction index contiguous ("K-major") or with its
 // outer index contiguous ("MN-major"): both are staged by TMA in boxes of 64 x 64 values (rows of 128
@@ -57,10 +60,11 @@ struct Cfg {
   static constexpr int STAGE_BYTES = P_BYTES + QBOXES * BOX_BYTES;
   static constexpr int CH = GATED ? (BM < 32 ? 8 : 16) : 16;  // TMEM columns one warp takes at a time
   static constexpr int XCHG_BYTES = GATED ? EPI_WARPS * CH * 128 : 0;  // g / u exchange between warps
+  static constexpr int PATCH_BYTES = EPI_WARPS * CH * 80;              // the epilogue warps' patch buffers
   static constexpr int CTRL_BYTES = 512;
-  static constexpr int FIT = (MAX_SMEM - 1024 - XCHG_BYTES - CTRL_BYTES) / STAGE_BYTES;
+  static constexpr int FIT = (MAX_SMEM - 1024 - XCHG_BYTES - PATCH_BYTES - CTRL_BYTES) / STAGE_BYTES;
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + XCHG_BYTES + CTRL_BYTES + 1024;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + XCHG_BYTES + PATCH_BYTES + CTRL_BYTES + 1024;
   static constexpr int TMEM_COLS = 2 * BM < 32 ? 32 : 2 * BM;  // two accumulators (a power of two)
   static constexpr int NT = (GATED ? 64 : 128) * CG;           // output columns per tile
 };
@@ -76,6 +80,7 @@ struct alignas(64) Problem {
   int units;               // dp_tiles + (tiles - dp_tiles) * split
   int slot0, counter0;     // first workspace slot and tile counter of the cut tiles
   int act;
+  int vec;                 // which of D, Z, U, R have 16-byte aligned rows (VEC_*)
   const void* bias;
   const void* R;
   void* D;
@@ -156,89 +161,204 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// Rows m0 .. m0 + CH - 1 of column n: v[j] is the sum of row m0 + j. WHOLE: all of them are inside the
-// matrix; otherwise those below M. All loads are issued before the first store (R may be D).
-template <typename T, int CH, int ACT, bool WHOLE>
-__device__ __forceinline__ void emit_plain(const Problem& pr, const float* v, float bias, int m0, int n) {
-  const int rows = pr.M - m0;
-  T r[CH];
-  if (pr.R) {
-    const T* src = static_cast<const T*>(pr.R) + (long long)m0 * pr.ldr + n;
-#pragma unroll
-    for (int j = 0; j < CH; ++j) r[j] = src[(WHOLE || j < rows ? j : 0) * pr.ldr];
-  }
-  if (pr.Z) {
-    T* dst = static_cast<T*>(pr.Z) + (long long)m0 * pr.ldz + n;
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (WHOLE || j < rows) dst[j * pr.ldz] = from_f32<T>(v[j] + bias);
-  }
-  T* dst = static_cast<T*>(pr.D) + (long long)m0 * pr.ldd + n;
-  if (pr.R) {
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (WHOLE || j < rows) dst[j * pr.ldd] = from_f32<T>(act_fwd<ACT>(v[j] + bias) + to_f32(r[j]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (WHOLE || j < rows) dst[j * pr.ldd] = from_f32<T>(act_fwd<ACT>(v[j] + bias));
-  }
+// Two values rounded to T, `lo` in the lower half.
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v);
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v) {
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
 }
 
-template <typename T, int CH, int ACT, bool WHOLE>
-__device__ __forceinline__ void emit_gated(const Problem& pr, const float* g, const float* u, int m0, int n) {
-  const int rows = pr.M - m0;
-  if (pr.Z) {
-    T* zg = static_cast<T*>(pr.Z) + (long long)m0 * pr.ldz + n;
-    T* zu = static_cast<T*>(pr.U) + (long long)m0 * pr.ldu + n;
+// A warp's patch of the output: CH rows from m0, 32 columns from n0. A thread's CH values of it, v[i]:
+// i = 4 (h MB + b) + r (h: half of the 32 lanes, b: block of 8 rows, MB = CH / 8) is column
+// 16 h + 8 (r / 2) + lane / 4 and row 8 b + 2 (lane % 4) + r % 2 of the patch; the pair (v[i], v[i + 1]), i even, is
+// one register of an 8 x 8 matrix.
+constexpr int PITCH = 80;  // bytes per patch row in shared memory: 64 + 16, no two of 8 rows on the same banks
+template <int CH>
+struct Patch {
+  static constexpr int MB = CH / 8;
+  int m0, n0, M, N, lane;
+  uint32_t buf;  // this warp's CH * PITCH bytes
+
+  // Row address for the matrix instructions: lane l -> row l % 8 of block b, columns 8 (l / 8).
+  __device__ __forceinline__ uint32_t matrix_addr(int b) const { return buf + (b * 8 + (lane & 7)) * PITCH + (lane >> 3) * 16; }
+
+  // Stores the patch given as packed pairs: q[i / 2].
+  __device__ __forceinline__ void store(void* out, long long ld, bool vec, const uint32_t* q) const {
 #pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (WHOLE || j < rows) {
-        zg[j * pr.ldz] = from_f32<T>(g[j]);
-        zu[j * pr.ldu] = from_f32<T>(u[j]);
+    for (int b = 0; b < MB; ++b)
+      ptx5::stmatrix_x4_trans(matrix_addr(b), q[2 * b], q[2 * b + 1], q[2 * (MB + b)], q[2 * (MB + b) + 1]);
+    __syncwarp();
+    uint16_t* o = static_cast<uint16_t*>(out) + (long long)m0 * ld + n0;
+    if (vec && n0 + 32 <= N) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const int row = 8 * i + (lane >> 2);
+        const uint4 x = ptx5::lds128(buf + row * PITCH + (lane & 3) * 16);
+        if (m0 + row < M) *reinterpret_cast<uint4*>(o + row * ld + (lane & 3) * 8) = x;
       }
-  }
-  T* dst = static_cast<T*>(pr.D) + (long long)m0 * pr.ldd + n;
+    } else {
 #pragma unroll
-  for (int j = 0; j < CH; ++j)
-    if (WHOLE || j < rows) dst[j * pr.ldd] = from_f32<T>(act_fwd<ACT>(g[j]) * u[j]);
+      for (int row = 0; row < CH; ++row) {
+        const uint16_t x = ptx5::lds16(buf + row * PITCH + lane * 2);
+        if (m0 + row < M && n0 + lane < N) o[row * ld + lane] = x;
+      }
+    }
+    __syncwarp();
+  }
+
+  // The patch of a 16-bit matrix on its way into registers: fetch() issues the global loads, take() turns
+  // them into packed pairs.
+  struct Raw {
+    uint32_t w[CH / 2];
+  };
+  __device__ __forceinline__ void fetch(Raw& raw, const void* src, long long ld, bool vec, int at_m0) const {
+    const uint16_t* s = static_cast<const uint16_t*>(src) + (long long)at_m0 * ld + n0;
+    if (vec && n0 + 32 <= N) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const int row = 8 * i + (lane >> 2);
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (at_m0 + row < M) x = *reinterpret_cast<const uint4*>(s + row * ld + (lane & 3) * 8);
+        raw.w[4 * i] = x.x;
+        raw.w[4 * i + 1] = x.y;
+        raw.w[4 * i + 2] = x.z;
+        raw.w[4 * i + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int row = 0; row < CH; row += 2) {
+        uint32_t lo = 0, hi = 0;
+        if (at_m0 + row < M && n0 + lane < N) lo = s[row * ld + lane];
+        if (at_m0 + row + 1 < M && n0 + lane < N) hi = s[(row + 1) * ld + lane];
+        raw.w[row / 2] = lo | hi << 16;
+      }
+    }
+  }
+  __device__ __forceinline__ void take(const Raw& raw, bool vec, uint32_t* q) const {
+    if (vec && n0 + 32 <= N) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+        ptx5::sts128(buf + (8 * i + (lane >> 2)) * PITCH + (lane & 3) * 16,
+                     make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]));
+    } else {
+#pragma unroll
+      for (int row = 0; row < CH; row += 2) {
+        ptx5::sts16(buf + row * PITCH + lane * 2, (uint16_t)raw.w[row / 2]);
+        ptx5::sts16(buf + (row + 1) * PITCH + lane * 2, (uint16_t)(raw.w[row / 2] >> 16));
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      uint32_t r[4];
+      ptx5::ldmatrix_x4_trans(matrix_addr(b), r);
+      q[2 * b] = r[0];
+      q[2 * b + 1] = r[1];
+      q[2 * (MB + b)] = r[2];
+      q[2 * (MB + b) + 1] = r[3];
+    }
+    __syncwarp();
+  }
+};
+
+// `vec` bits of a problem: 16-byte rows of D, Z, U, R.
+constexpr int VEC_D = 1, VEC_Z = 2, VEC_U = 4, VEC_R = 8;
+
+// bias[j]: of column 8 j + lane / 4 of the patch.
+template <typename T, int CH, int ACT>
+__device__ __forceinline__ void emit_plain(const Problem& pr, const Patch<CH>& pt, const float* v, const float* bias, const typename Patch<CH>::Raw& raw) {
+  constexpr int MB = CH / 8;
+  uint32_t q[CH / 2], r[CH / 2];
+  if (pr.R) pt.take(raw, pr.vec & VEC_R, r);
+  if (pr.Z) {
+#pragma unroll
+    for (int i = 0; i < CH; i += 2) {
+      const float b = bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+      q[i / 2] = pack2<T>(v[i] + b, v[i + 1] + b);
+    }
+    pt.store(pr.Z, pr.ldz, pr.vec & VEC_Z, q);
+  }
+#pragma unroll
+  for (int i = 0; i < CH; i += 2) {
+    const float b = bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+    float x = act_fwd<ACT>(v[i] + b), y = act_fwd<ACT>(v[i + 1] + b);
+    if (pr.R) {
+      const float2 a = unpack2<T>(r[i / 2]);
+      x += a.x;
+      y += a.y;
+    }
+    q[i / 2] = pack2<T>(x, y);
+  }
+  pt.store(pr.D, pr.ldd, pr.vec & VEC_D, q);
 }
 
-template <typename T, int CH, bool WHOLE>
-__device__ __forceinline__ void emit_plain_act(const Problem& pr, const float* v, float bias, int m0, int n) {
+template <typename T, int CH, int ACT>
+__device__ __forceinline__ void emit_gated(const Problem& pr, const Patch<CH>& pt, const float* g, const float* u) {
+  uint32_t q[CH / 2];
+  if (pr.Z) {
+#pragma unroll
+    for (int i = 0; i < CH; i += 2) q[i / 2] = pack2<T>(g[i], g[i + 1]);
+    pt.store(pr.Z, pr.ldz, pr.vec & VEC_Z, q);
+#pragma unroll
+    for (int i = 0; i < CH; i += 2) q[i / 2] = pack2<T>(u[i], u[i + 1]);
+    pt.store(pr.U, pr.ldu, pr.vec & VEC_U, q);
+  }
+#pragma unroll
+  for (int i = 0; i < CH; i += 2) q[i / 2] = pack2<T>(act_fwd<ACT>(g[i]) * u[i], act_fwd<ACT>(g[i + 1]) * u[i + 1]);
+  pt.store(pr.D, pr.ldd, pr.vec & VEC_D, q);
+}
+
+template <typename T, int CH>
+__device__ __forceinline__ void emit_plain_any(const Problem& pr, const Patch<CH>& pt, const float* v, const float* bias, const typename Patch<CH>::Raw& raw) {
   switch (pr.act) {
-    case HGEMM_ACT_NONE: emit_plain<T, CH, HGEMM_ACT_NONE, WHOLE>(pr, v, bias, m0, n); break;
-    case HGEMM_ACT_RELU: emit_plain<T, CH, HGEMM_ACT_RELU, WHOLE>(pr, v, bias, m0, n); break;
-    case HGEMM_ACT_GELU: emit_plain<T, CH, HGEMM_ACT_GELU, WHOLE>(pr, v, bias, m0, n); break;
-    case HGEMM_ACT_GELU_TANH: emit_plain<T, CH, HGEMM_ACT_GELU_TANH, WHOLE>(pr, v, bias, m0, n); break;
-    default: emit_plain<T, CH, HGEMM_ACT_SILU, WHOLE>(pr, v, bias, m0, n); break;
+    case HGEMM_ACT_NONE: emit_plain<T, CH, HGEMM_ACT_NONE>(pr, pt, v, bias, raw); break;
+    case HGEMM_ACT_RELU: emit_plain<T, CH, HGEMM_ACT_RELU>(pr, pt, v, bias, raw); break;
+    case HGEMM_ACT_GELU: emit_plain<T, CH, HGEMM_ACT_GELU>(pr, pt, v, bias, raw); break;
+    case HGEMM_ACT_GELU_TANH: emit_plain<T, CH, HGEMM_ACT_GELU_TANH>(pr, pt, v, bias, raw); break;
+    default: emit_plain<T, CH, HGEMM_ACT_SILU>(pr, pt, v, bias, raw); break;
   }
 }
 template <typename T, int CH>
-__device__ __forceinline__ void emit_plain_any(const Problem& pr, const float* v, float bias, int m0, int n) {
-  if (m0 + CH <= pr.M) emit_plain_act<T, CH, true>(pr, v, bias, m0, n);
-  else emit_plain_act<T, CH, false>(pr, v, bias, m0, n);
-}
-template <typename T, int CH, bool WHOLE>
-__device__ __forceinline__ void emit_gated_act(const Problem& pr, const float* g, const float* u, int m0, int n) {
+__device__ __forceinline__ void emit_gated_any(const Problem& pr, const Patch<CH>& pt, const float* g, const float* u) {
   switch (pr.act) {
-    case HGEMM_ACT_NONE: emit_gated<T, CH, HGEMM_ACT_NONE, WHOLE>(pr, g, u, m0, n); break;
-    case HGEMM_ACT_RELU: emit_gated<T, CH, HGEMM_ACT_RELU, WHOLE>(pr, g, u, m0, n); break;
-    case HGEMM_ACT_GELU: emit_gated<T, CH, HGEMM_ACT_GELU, WHOLE>(pr, g, u, m0, n); break;
-    case HGEMM_ACT_GELU_TANH: emit_gated<T, CH, HGEMM_ACT_GELU_TANH, WHOLE>(pr, g, u, m0, n); break;
-    default: emit_gated<T, CH, HGEMM_ACT_SILU, WHOLE>(pr, g, u, m0, n); break;
+    case HGEMM_ACT_NONE: emit_gated<T, CH, HGEMM_ACT_NONE>(pr, pt, g, u); break;
+    case HGEMM_ACT_RELU: emit_gated<T, CH, HGEMM_ACT_RELU>(pr, pt, g, u); break;
+    case HGEMM_ACT_GELU: emit_gated<T, CH, HGEMM_ACT_GELU>(pr, pt, g, u); break;
+    case HGEMM_ACT_GELU_TANH: emit_gated<T, CH, HGEMM_ACT_GELU_TANH>(pr, pt, g, u); break;
+    default: emit_gated<T, CH, HGEMM_ACT_SILU>(pr, pt, g, u); break;
   }
 }
-template <typename T, int CH>
-__device__ __forceinline__ void emit_gated_any(const Problem& pr, const float* g, const float* u, int m0, int n) {
-  if (m0 + CH <= pr.M) emit_gated_act<T, CH, true>(pr, g, u, m0, n);
-  else emit_gated_act<T, CH, false>(pr, g, u, m0, n);
-}
 
+// CH columns of a warp's 32 lanes, in the patch's order, from the lane and column in `addr`.
 template <int CH>
 __device__ __forceinline__ void tmem_load(uint32_t addr, float* v) {
-  if (CH == 8) ptx5::tmem_ld_x8(addr, v);
-  else ptx5::tmem_ld_x16(addr, v);
+  ptx5::tmem_ld_16x256b<CH / 8>(addr, v);
+  ptx5::tmem_ld_16x256b<CH / 8>(addr + (16u << 16), v + CH / 2);
+}
+
+// The sum of a cut tile's parts, in order, for one thread's CH values.
+template <int CH>
+__device__ __forceinline__ void add_parts(const float4* ws, int split, long long stride, float* v) {
+#pragma unroll
+  for (int j = 0; j < CH; ++j) v[j] = 0.f;
+  for (int s = 0; s < split; ++s)
+#pragma unroll
+    for (int j = 0; j < CH / 4; ++j) {
+      const float4 x = __ldcg(ws + s * stride + j * 32);
+      v[4 * j] += x.x;
+      v[4 * j + 1] += x.y;
+      v[4 * j + 2] += x.z;
+      v[4 * j + 3] += x.w;
+    }
 }
 
 // Shared-memory descriptor of an operand tile made of 64 x 64 boxes with 128-byte swizzle. K-major:
@@ -260,9 +380,10 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
   const uint32_t pad = (1024 - (raw & 1023)) & 1023;
   const uint32_t base = raw + pad;  // the same offset in both CTAs of a pair (same kernel, same launch)
   uint8_t* gen = smem_raw + pad;
-  float* xchg = reinterpret_cast<float*>(gen + STAGES * C::STAGE_BYTES);
-  uint8_t* ctrl = gen + STAGES * C::STAGE_BYTES + C::XCHG_BYTES;
-  const uint32_t bars = base + STAGES * C::STAGE_BYTES + C::XCHG_BYTES;
+  const uint32_t xchg = base + STAGES * C::STAGE_BYTES;
+  const uint32_t patches = xchg + C::XCHG_BYTES;
+  uint8_t* ctrl = gen + STAGES * C::STAGE_BYTES + C::XCHG_BYTES + C::PATCH_BYTES;
+  const uint32_t bars = patches + C::PATCH_BYTES;
   const uint32_t full_bar = bars, empty_bar = bars + 8 * STAGES;        // stage s at + 8 s
   const uint32_t acc_full = bars + 16 * STAGES, acc_empty = acc_full + 16;  // accumulator a at + 8 a
   const uint32_t drain_bar = acc_empty + 16;
@@ -388,7 +509,6 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     // ---- epilogue ----
     const int e = warp - 4, quad = warp & 3, half = e >> 2;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
-    const int l = quad * 32 + lane;  // this thread's TMEM lane
     uint32_t acc_it = 0;
     // After a wait has given up, the warps still walk through the rest of the units together (without
     // waiting again), so that every named barrier below is met by all of its warps.
@@ -399,13 +519,30 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
       const int m_base = tm * BM;
-      const int n = GATED ? tn * C::NT + rank * 64 + (l & 63) : tn * C::NT + rank * 128 + l;
-      const bool n_in = n < pr.N;
+      const int n0 = GATED ? tn * C::NT + rank * 64 + (quad & 1) * 32 : tn * C::NT + rank * 128 + quad * 32;
+      const bool n_in = n0 < pr.N;  // (the whole warp: a patch beyond the last column has nothing to do)
+      Patch<CH> pt{m_base, n0, pr.M, pr.N, lane, patches + e * (CH * PITCH)};
       const uint32_t a = acc_it & 1u;
-      const float bias = !GATED && pr.bias && n_in ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
+      float bias[4] = {0.f, 0.f, 0.f, 0.f};
+      if (!GATED && pr.bias) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int n = n0 + 8 * j + (lane >> 2);
+          if (n < pr.N) bias[j] = to_f32(static_cast<const T*>(pr.bias)[n]);
+        }
+      }
+      typename Patch<CH>::Raw raw;
+      const bool use_r = !GATED && pr.R && n_in;
+      if (use_r && w.part < 0 && m_base + half * CH < pr.M) pt.fetch(raw, pr.R, pr.ldr, pr.vec & VEC_R, m_base + half * CH);
       if (!dead) dead = !wait_bounded(acc_full + 8 * a, (acc_it >> 1) & 1u, abort_flag, p);
+      __syncwarp();
       ptx5::fence_after_sync();
       const uint32_t t_acc = tmem + a * BM + lane_addr;
+      // a cut tile's sums in the workspace: [part][CTA][quad][chunk][CH / 4][lane] of float4
+      const int rel = w.part < 0 ? 0 : w.tile - pr.dp_tiles;
+      constexpr long long WS_TILE = (long long)CG * BM * 32;  // float4 per part
+      constexpr int WS_CHUNK = CH / 4 * 32;                   // float4 per quad and chunk
+      float4* ws_tile = reinterpret_cast<float4*>(p.ws) + ((long long)(pr.slot0 + rel * pr.split) * CG + rank) * (BM * 32);
       if (w.part < 0) {
         if (!GATED) {
           for (int c = half; c < BM / CH; c += 2) {
@@ -413,14 +550,19 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
             float v[CH];
             tmem_load<CH>(t_acc + c * CH, v);
             ptx5::tmem_ld_wait<CH>(v);
-            if (n_in) emit_plain_any<T, CH>(pr, v, bias, m_base + c * CH, n);
+            pt.m0 = m_base + c * CH;
+            if (n_in) {
+              typename Patch<CH>::Raw now = raw;
+              // the next chunk's residual is on its way while this one is computed
+              if (use_r && c + 2 < BM / CH && pt.m0 + 2 * CH < pr.M) pt.fetch(raw, pr.R, pr.ldr, pr.vec & VEC_R, pt.m0 + 2 * CH);
+              emit_plain_any<T, CH>(pr, pt, v, bias, now);
+            }
           }
         } else {
           // Lanes 0-63 hold g, lanes 64-127 hold u of the same 64 columns. Two chunks at a time: the
           // g warp takes u of the first from its partner, the u warp takes g of the second.
           const bool is_g = quad < 2;
-          float* mine = xchg + e * (CH * 32);
-          const float* theirs = xchg + (e ^ 2) * (CH * 32);
+          const uint32_t mine = xchg + e * (CH * 128) + lane * 16, theirs = xchg + (e ^ 2) * (CH * 128) + lane * 16;
           for (int c = 2 * half; c < BM / CH; c += 4) {
             if (m_base + c * CH >= pr.M) break;
             float v[CH], o[CH];
@@ -429,26 +571,27 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
             ptx5::tmem_ld_wait<CH>(o);
             ptx5::tmem_ld_wait<CH>(v);
 #pragma unroll
-            for (int j = 0; j < CH; ++j) mine[j * 32 + lane] = o[j];
+            for (int j = 0; j < CH / 4; ++j) ptx5::sts128(mine + j * 512, *reinterpret_cast<const uint4*>(o + 4 * j));
             named_barrier_sync(1 + half * 2 + (quad & 1), 64);
 #pragma unroll
-            for (int j = 0; j < CH; ++j) o[j] = theirs[j * 32 + lane];
+            for (int j = 0; j < CH / 4; ++j) *reinterpret_cast<uint4*>(o + 4 * j) = ptx5::lds128(theirs + j * 512);
             named_barrier_sync(1 + half * 2 + (quad & 1), 64);
-            const int m0 = m_base + (is_g ? c : c + 1) * CH;
-            if (n_in && m0 < pr.M) emit_gated_any<T, CH>(pr, is_g ? v : o, is_g ? o : v, m0, n);
+            pt.m0 = m_base + (is_g ? c : c + 1) * CH;
+            if (n_in && pt.m0 < pr.M) {
+              if (is_g) emit_gated_any<T, CH>(pr, pt, v, o);
+              else emit_gated_any<T, CH>(pr, pt, o, v);
+            }
           }
         }
       } else {
-        // a part of a tile: its sums go to the workspace as [m][128 lanes]
-        const int rel = w.tile - pr.dp_tiles;
-        float* ws = p.ws + ((long long)(pr.slot0 + rel * pr.split + w.part) * CG + rank) * (BM * 128) + l;
+        float4* ws = ws_tile + w.part * WS_TILE + (quad * (BM / CH)) * WS_CHUNK + lane;
         for (int c = half; c < BM / CH; c += 2) {
           if (m_base + c * CH >= pr.M) break;
           float v[CH];
           tmem_load<CH>(t_acc + c * CH, v);
           ptx5::tmem_ld_wait<CH>(v);
 #pragma unroll
-          for (int j = 0; j < CH; ++j) __stcg(ws + (c * CH + j) * 128, v[j]);
+          for (int j = 0; j < CH / 4; ++j) __stcg(ws + c * WS_CHUNK + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
         }
       }
       // the accumulator may be overwritten
@@ -459,7 +602,6 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         else ptx5::mbar_arrive_cluster(map_to_cta(acc_empty + 8 * a, 0));
       }
       if (w.part >= 0) {
-        const int rel = w.tile - pr.dp_tiles;
         int* counter = p.counters + (pr.counter0 + rel) * CG + rank;
         __threadfence();
         named_barrier_sync(8, EPI_WARPS * 32);
@@ -471,32 +613,25 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         named_barrier_sync(8, EPI_WARPS * 32);
         if (*last_flag) {
           __threadfence();
-          const float* ws = p.ws + ((long long)(pr.slot0 + rel * pr.split) * CG + rank) * (BM * 128);
-          const long long stride = (long long)CG * BM * 128;
           if (!GATED) {
+            const float4* ws = ws_tile + (quad * (BM / CH)) * WS_CHUNK + lane;
             for (int c = half; c < BM / CH; c += 2) {
               if (m_base + c * CH >= pr.M) break;
+              pt.m0 = m_base + c * CH;
+              if (use_r) pt.fetch(raw, pr.R, pr.ldr, pr.vec & VEC_R, pt.m0);
               float v[CH];
-#pragma unroll
-              for (int j = 0; j < CH; ++j) v[j] = 0.f;
-              for (int s = 0; s < pr.split; ++s)
-#pragma unroll
-                for (int j = 0; j < CH; ++j) v[j] += __ldcg(ws + s * stride + (c * CH + j) * 128 + l);
-              if (n_in) emit_plain_any<T, CH>(pr, v, bias, m_base + c * CH, n);
+              add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, v);
+              if (n_in) emit_plain_any<T, CH>(pr, pt, v, bias, raw);
             }
           } else {
+            const float4* ws = ws_tile + ((quad & 1) * (BM / CH)) * WS_CHUNK + lane;
             for (int c = 2 * half + (quad >> 1); c < BM / CH; c += 4) {
               if (m_base + c * CH >= pr.M) break;
+              pt.m0 = m_base + c * CH;
               float g[CH], uu[CH];
-#pragma unroll
-              for (int j = 0; j < CH; ++j) g[j] = uu[j] = 0.f;
-              for (int s = 0; s < pr.split; ++s)
-#pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                  g[j] += __ldcg(ws + s * stride + (c * CH + j) * 128 + (l & 63));
-                  uu[j] += __ldcg(ws + s * stride + (c * CH + j) * 128 + 64 + (l & 63));
-                }
-              if (n_in) emit_gated_any<T, CH>(pr, g, uu, m_base + c * CH, n);
+              add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, g);
+              add_parts<CH>(ws + (2 * (BM / CH) + c) * WS_CHUNK, pr.split, WS_TILE, uu);
+              if (n_in) emit_gated_any<T, CH>(pr, pt, g, uu);
             }
           }
         }
