@@ -11,11 +11,17 @@ constexpr float SQRT_HALF = 0.70710678118654752f;
 constexpr float INV_SQRT_2PI = 0.39894228040143268f;
 constexpr float TANH_C = 0.79788456080286536f;   // sqrt(2 / pi)
 constexpr float TANH_A = 0.044715f;
+constexpr float LOG2E = 1.4426950408889634f;
 
-// 1 / (1 + exp(-x)). The fast exponential and division are off by a few units of 2^-22 here, far below
-// the rounding of a 16-bit result; 1 + inf divides to 0.
-__device__ __forceinline__ float sigmoid_fast(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
-// The same to binary32 accuracy, for values that are summed in binary32.
+// 1 / (1 + 2^x). The approximate exponential and reciprocal are off by a few units of 2^-22, far below
+// the rounding of a 16-bit result; 1 + inf gives 0.
+__device__ __forceinline__ float inv_1p_exp2(float x) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+// 1 / (1 + exp(-x)) to binary32 accuracy, for values that are summed in binary32.
 __device__ __forceinline__ float sigmoid_full(float x) { return 1.f / (1.f + expf(-x)); }
 
 // act(z) for a result that is rounded to 16 bits.
@@ -23,9 +29,9 @@ template <int ACT>
 __device__ __forceinline__ float act_fwd(float z) {
   if (ACT == HGEMM_ACT_RELU) return z <= 0.f ? 0.f : z;  // NaN stays NaN
   if (ACT == HGEMM_ACT_GELU) return 0.5f * z * (1.f + erff(z * SQRT_HALF));
-  // (1 + tanh(p)) / 2 = sigmoid(2 p)
-  if (ACT == HGEMM_ACT_GELU_TANH) return z * sigmoid_fast(2.f * TANH_C * (z + TANH_A * z * z * z));
-  if (ACT == HGEMM_ACT_SILU) return z * sigmoid_fast(z);
+  // (1 + tanh(p)) / 2 = 1 / (1 + exp(-2 p))
+  if (ACT == HGEMM_ACT_GELU_TANH) return z * inv_1p_exp2(z * (-2.f * LOG2E * TANH_C - 2.f * LOG2E * TANH_C * TANH_A * z * z));
+  if (ACT == HGEMM_ACT_SILU) return z * inv_1p_exp2(-LOG2E * z);
   return z;
 }
 

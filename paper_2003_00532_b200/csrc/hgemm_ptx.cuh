@@ -131,9 +131,12 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint16_t v) { asm volatile(
 
 // ---- barriers and tile loads of a CTA pair -------------------------------------------------------------
 
-// Arrival on a barrier in the shared memory of any CTA of the cluster (`addr` from map_to_cta).
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+// Arrival on a barrier in the shared memory of any CTA of the cluster (`addr` from map_to_cta). Relaxed: it
+// publishes no memory, only that this warp's TMEM loads are done (they have been waited for, and
+// tcgen05.fence::before_thread_sync orders them). A release at cluster scope would wait for all of the
+// warp's stores to global memory: measured, 4 us per tile.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 
 // Tile load into the issuing CTA's shared memory. For a pair, `bar` may be the leader's barrier

@@ -25,8 +25,8 @@
 //
 // Roles (384 threads): warps 0 and 3 stage P and Q (one thread that issued all copies was the limit:
 // 479 ns per 64-wide k-block with four copies, against 366 ns for its MMAs; two threads with one or
-// two copies each are not), warp 1 issues the MMAs, warp 2 owns the TMEM allocation, warps 4-11 run the epilogue of one accumulator while the MMAs fill the other. In a pair the MMAs of
-// both CTAs are issued by the leader; each CTA stages its own 128 lanes and its half of Q.
+// two copies each are not), warp 1 issues the MMAs, warp 2 owns the TMEM allocation, warps 4-11 run
+// the epilogue of one accumulator while the MMAs fill the other. In a pair the MMAs of both CTAs are issued by the leader; each CTA stages its own 128 lanes and its half of Q.
 #pragma once
 
 #include <cstdint>
@@ -44,8 +44,9 @@ namespace hgemm {
 
 constexpr int TK = 64;           // k-block: 64 values of 16 bits = one 128-byte swizzled row
 constexpr int BOX_BYTES = 8192;  // 64 x 64 values
-constexpr int THREADS = 384;
 constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 128 + 32 * EPI_WARPS;
+constexpr int PITCH = 80;  // bytes per patch row in shared memory: 64 + 16, no two of 8 rows on the same banks
 constexpr int MAX_SMEM = 232448;  // 227 KB
 constexpr int MAX_PROBLEMS = 3;
 
@@ -59,12 +60,13 @@ struct Cfg {
   static constexpr int P_BYTES = 2 * BOX_BYTES;
   static constexpr int STAGE_BYTES = P_BYTES + QBOXES * BOX_BYTES;
   static constexpr int CH = GATED ? (BM < 32 ? 8 : 16) : 16;  // TMEM columns one warp takes at a time
-  static constexpr int XCHG_BYTES = GATED ? EPI_WARPS * CH * 128 : 0;  // g / u exchange between warps
-  static constexpr int PATCH_BYTES = EPI_WARPS * CH * 80;              // the epilogue warps' patch buffers
+  // Each epilogue warp's buffer: a patch of the output or, before that, the values it hands to its partner.
+  static constexpr int BUF_BYTES = GATED ? CH * 128 : CH * PITCH;
+  static constexpr int BUFS_BYTES = EPI_WARPS * BUF_BYTES;
   static constexpr int CTRL_BYTES = 512;
-  static constexpr int FIT = (MAX_SMEM - 1024 - XCHG_BYTES - PATCH_BYTES - CTRL_BYTES) / STAGE_BYTES;
+  static constexpr int FIT = (MAX_SMEM - 1024 - BUFS_BYTES - CTRL_BYTES) / STAGE_BYTES;
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + XCHG_BYTES + PATCH_BYTES + CTRL_BYTES + 1024;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + BUFS_BYTES + CTRL_BYTES + 1024;
   static constexpr int TMEM_COLS = 2 * BM < 32 ? 32 : 2 * BM;  // two accumulators (a power of two)
   static constexpr int NT = (GATED ? 64 : 128) * CG;           // output columns per tile
 };
@@ -181,35 +183,54 @@ template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v)
 // i = 4 (h MB + b) + r (h: half of the 32 lanes, b: block of 8 rows, MB = CH / 8) is column
 // 16 h + 8 (r / 2) + lane / 4 and row 8 b + 2 (lane % 4) + r % 2 of the patch; the pair (v[i], v[i + 1]), i even, is
 // one register of an 8 x 8 matrix.
-constexpr int PITCH = 80;  // bytes per patch row in shared memory: 64 + 16, no two of 8 rows on the same banks
 template <int CH>
 struct Patch {
   static constexpr int MB = CH / 8;
-  int m0, n0, M, N, lane;
-  uint32_t buf;  // this warp's CH * PITCH bytes
 
-  // Row address for the matrix instructions: lane l -> row l % 8 of block b, columns 8 (l / 8).
-  __device__ __forceinline__ uint32_t matrix_addr(int b) const { return buf + (b * 8 + (lane & 7)) * PITCH + (lane >> 3) * 16; }
+  // A matrix as one lane sees it: the address of its piece of the tile's first row(s), and whether the warp moves
+  // 16-byte vectors (lane -> row lane / 4, columns 8 (lane % 4)) or single values (lane -> column).
+  struct View {
+    char* p;
+    long long ld;  // bytes
+    bool vec;
+  };
 
-  // Stores the patch given as packed pairs: q[i / 2].
-  __device__ __forceinline__ void store(void* out, long long ld, bool vec, const uint32_t* q) const {
+  int rows;  // rows of the matrix from the tile's first one
+  int cols;  // columns of the matrix from the patch's first one
+  int lane;
+  uint32_t buf;     // this warp's buffer
+  uint32_t matrix;  // this lane's row address for the matrix instructions: row lane % 8, columns 8 (lane / 8)
+
+  __device__ __forceinline__ View view(const void* ptr, long long ld, bool aligned, int m_base, int n0) const {
+    View w;
+    w.ld = ld * 2;
+    w.vec = aligned && cols >= 32;
+    w.p = static_cast<char*>(const_cast<void*>(ptr)) + m_base * w.ld + n0 * 2ll + (w.vec ? (lane >> 2) * w.ld + (lane & 3) * 16 : lane * 2);
+    return w;
+  }
+
+  // Stores the patch that begins at row m of the tile, given as packed pairs: q[i / 2].
+  __device__ __forceinline__ void store(const View& out, int m, const uint32_t* q) const {
 #pragma unroll
     for (int b = 0; b < MB; ++b)
-      ptx5::stmatrix_x4_trans(matrix_addr(b), q[2 * b], q[2 * b + 1], q[2 * (MB + b)], q[2 * (MB + b) + 1]);
+      ptx5::stmatrix_x4_trans(matrix + b * 8 * PITCH, q[2 * b], q[2 * b + 1], q[2 * (MB + b)], q[2 * (MB + b) + 1]);
     __syncwarp();
-    uint16_t* o = static_cast<uint16_t*>(out) + (long long)m0 * ld + n0;
-    if (vec && n0 + 32 <= N) {
+    char* o = out.p + m * out.ld;
+    if (out.vec) {
+      uint4 x[MB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) x[i] = ptx5::lds128(buf + (8 * i + (lane >> 2)) * PITCH + (lane & 3) * 16);
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
-        const int row = 8 * i + (lane >> 2);
-        const uint4 x = ptx5::lds128(buf + row * PITCH + (lane & 3) * 16);
-        if (m0 + row < M) *reinterpret_cast<uint4*>(o + row * ld + (lane & 3) * 8) = x;
+        if (m + 8 * i + (lane >> 2) < rows) *reinterpret_cast<uint4*>(o) = x[i];
+        o += 8 * out.ld;
       }
-    } else {
+    } else if (lane < cols) {
 #pragma unroll
-      for (int row = 0; row < CH; ++row) {
-        const uint16_t x = ptx5::lds16(buf + row * PITCH + lane * 2);
-        if (m0 + row < M && n0 + lane < N) o[row * ld + lane] = x;
+      for (int r = 0; r < CH; ++r) {
+        const uint16_t x = ptx5::lds16(buf + r * PITCH + lane * 2);
+        if (m + r < rows) *reinterpret_cast<uint16_t*>(o) = x;
+        o += out.ld;
       }
     }
     __syncwarp();
@@ -220,14 +241,14 @@ struct Patch {
   struct Raw {
     uint32_t w[CH / 2];
   };
-  __device__ __forceinline__ void fetch(Raw& raw, const void* src, long long ld, bool vec, int at_m0) const {
-    const uint16_t* s = static_cast<const uint16_t*>(src) + (long long)at_m0 * ld + n0;
-    if (vec && n0 + 32 <= N) {
+  __device__ __forceinline__ void fetch(Raw& raw, const View& in, int m) const {
+    const char* s = in.p + m * in.ld;
+    if (in.vec) {
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
-        const int row = 8 * i + (lane >> 2);
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (at_m0 + row < M) x = *reinterpret_cast<const uint4*>(s + row * ld + (lane & 3) * 8);
+        if (m + 8 * i + (lane >> 2) < rows) x = *reinterpret_cast<const uint4*>(s);
+        s += 8 * in.ld;
         raw.w[4 * i] = x.x;
         raw.w[4 * i + 1] = x.y;
         raw.w[4 * i + 2] = x.z;
@@ -235,32 +256,34 @@ struct Patch {
       }
     } else {
 #pragma unroll
-      for (int row = 0; row < CH; row += 2) {
+      for (int r = 0; r < CH; r += 2) {
         uint32_t lo = 0, hi = 0;
-        if (at_m0 + row < M && n0 + lane < N) lo = s[row * ld + lane];
-        if (at_m0 + row + 1 < M && n0 + lane < N) hi = s[(row + 1) * ld + lane];
-        raw.w[row / 2] = lo | hi << 16;
+        if (m + r < rows && lane < cols) lo = *reinterpret_cast<const uint16_t*>(s);
+        s += in.ld;
+        if (m + r + 1 < rows && lane < cols) hi = *reinterpret_cast<const uint16_t*>(s);
+        s += in.ld;
+        raw.w[r / 2] = lo | hi << 16;
       }
     }
   }
   __device__ __forceinline__ void take(const Raw& raw, bool vec, uint32_t* q) const {
-    if (vec && n0 + 32 <= N) {
+    if (vec) {
 #pragma unroll
       for (int i = 0; i < MB; ++i)
         ptx5::sts128(buf + (8 * i + (lane >> 2)) * PITCH + (lane & 3) * 16,
                      make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]));
     } else {
 #pragma unroll
-      for (int row = 0; row < CH; row += 2) {
-        ptx5::sts16(buf + row * PITCH + lane * 2, (uint16_t)raw.w[row / 2]);
-        ptx5::sts16(buf + (row + 1) * PITCH + lane * 2, (uint16_t)(raw.w[row / 2] >> 16));
+      for (int r = 0; r < CH; r += 2) {
+        ptx5::sts16(buf + r * PITCH + lane * 2, (uint16_t)raw.w[r / 2]);
+        ptx5::sts16(buf + (r + 1) * PITCH + lane * 2, (uint16_t)(raw.w[r / 2] >> 16));
       }
     }
     __syncwarp();
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
       uint32_t r[4];
-      ptx5::ldmatrix_x4_trans(matrix_addr(b), r);
+      ptx5::ldmatrix_x4_trans(matrix + b * 8 * PITCH, r);
       q[2 * b] = r[0];
       q[2 * b + 1] = r[1];
       q[2 * (MB + b)] = r[2];
@@ -273,69 +296,57 @@ struct Patch {
 // `vec` bits of a problem: 16-byte rows of D, Z, U, R.
 constexpr int VEC_D = 1, VEC_Z = 2, VEC_U = 4, VEC_R = 8;
 
-// bias[j]: of column 8 j + lane / 4 of the patch.
+// What a warp needs of a problem for one tile.
+template <int CH>
+struct Epilogue {
+  Patch<CH> pt;
+  typename Patch<CH>::View d, z, u, r;
+  bool has_z, has_r;
+  int act;
+  float bias[4];  // bias[j]: of column 8 j + lane / 4 of the patch
+};
+
 template <typename T, int CH, int ACT>
-__device__ __forceinline__ void emit_plain(const Problem& pr, const Patch<CH>& pt, const float* v, const float* bias, const typename Patch<CH>::Raw& raw) {
+__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, const float* v, const typename Patch<CH>::Raw& raw) {
   constexpr int MB = CH / 8;
   uint32_t q[CH / 2], r[CH / 2];
-  if (pr.R) pt.take(raw, pr.vec & VEC_R, r);
-  if (pr.Z) {
+  if (ep.has_r) ep.pt.take(raw, ep.r.vec, r);
+  if (ep.has_z) {
 #pragma unroll
     for (int i = 0; i < CH; i += 2) {
-      const float b = bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+      const float b = ep.bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
       q[i / 2] = pack2<T>(v[i] + b, v[i + 1] + b);
     }
-    pt.store(pr.Z, pr.ldz, pr.vec & VEC_Z, q);
+    ep.pt.store(ep.z, m, q);
   }
 #pragma unroll
   for (int i = 0; i < CH; i += 2) {
-    const float b = bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+    const float b = ep.bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
     float x = act_fwd<ACT>(v[i] + b), y = act_fwd<ACT>(v[i + 1] + b);
-    if (pr.R) {
+    if (ep.has_r) {
       const float2 a = unpack2<T>(r[i / 2]);
       x += a.x;
       y += a.y;
     }
     q[i / 2] = pack2<T>(x, y);
   }
-  pt.store(pr.D, pr.ldd, pr.vec & VEC_D, q);
+  ep.pt.store(ep.d, m, q);
 }
 
 template <typename T, int CH, int ACT>
-__device__ __forceinline__ void emit_gated(const Problem& pr, const Patch<CH>& pt, const float* g, const float* u) {
+__device__ __forceinline__ void emit_gated(const Epilogue<CH>& ep, int m, const float* g, const float* u) {
   uint32_t q[CH / 2];
-  if (pr.Z) {
+  if (ep.has_z) {
 #pragma unroll
     for (int i = 0; i < CH; i += 2) q[i / 2] = pack2<T>(g[i], g[i + 1]);
-    pt.store(pr.Z, pr.ldz, pr.vec & VEC_Z, q);
+    ep.pt.store(ep.z, m, q);
 #pragma unroll
     for (int i = 0; i < CH; i += 2) q[i / 2] = pack2<T>(u[i], u[i + 1]);
-    pt.store(pr.U, pr.ldu, pr.vec & VEC_U, q);
+    ep.pt.store(ep.u, m, q);
   }
 #pragma unroll
   for (int i = 0; i < CH; i += 2) q[i / 2] = pack2<T>(act_fwd<ACT>(g[i]) * u[i], act_fwd<ACT>(g[i + 1]) * u[i + 1]);
-  pt.store(pr.D, pr.ldd, pr.vec & VEC_D, q);
-}
-
-template <typename T, int CH>
-__device__ __forceinline__ void emit_plain_any(const Problem& pr, const Patch<CH>& pt, const float* v, const float* bias, const typename Patch<CH>::Raw& raw) {
-  switch (pr.act) {
-    case HGEMM_ACT_NONE: emit_plain<T, CH, HGEMM_ACT_NONE>(pr, pt, v, bias, raw); break;
-    case HGEMM_ACT_RELU: emit_plain<T, CH, HGEMM_ACT_RELU>(pr, pt, v, bias, raw); break;
-    case HGEMM_ACT_GELU: emit_plain<T, CH, HGEMM_ACT_GELU>(pr, pt, v, bias, raw); break;
-    case HGEMM_ACT_GELU_TANH: emit_plain<T, CH, HGEMM_ACT_GELU_TANH>(pr, pt, v, bias, raw); break;
-    default: emit_plain<T, CH, HGEMM_ACT_SILU>(pr, pt, v, bias, raw); break;
-  }
-}
-template <typename T, int CH>
-__device__ __forceinline__ void emit_gated_any(const Problem& pr, const Patch<CH>& pt, const float* g, const float* u) {
-  switch (pr.act) {
-    case HGEMM_ACT_NONE: emit_gated<T, CH, HGEMM_ACT_NONE>(pr, pt, g, u); break;
-    case HGEMM_ACT_RELU: emit_gated<T, CH, HGEMM_ACT_RELU>(pr, pt, g, u); break;
-    case HGEMM_ACT_GELU: emit_gated<T, CH, HGEMM_ACT_GELU>(pr, pt, g, u); break;
-    case HGEMM_ACT_GELU_TANH: emit_gated<T, CH, HGEMM_ACT_GELU_TANH>(pr, pt, g, u); break;
-    default: emit_gated<T, CH, HGEMM_ACT_SILU>(pr, pt, g, u); break;
-  }
+  ep.pt.store(ep.d, m, q);
 }
 
 // CH columns of a warp's 32 lanes, in the patch's order, from the lane and column in `addr`.
@@ -361,6 +372,127 @@ __device__ __forceinline__ void add_parts(const float4* ws, int split, long long
     }
 }
 
+// One epilogue warp: its accumulator quarter, buffers and place.
+struct EpiWarp {
+  uint32_t acc, bufs, last_flag, acc_empty;
+  int e, quad, group, lane, rank;
+};
+
+__device__ __forceinline__ void sts32(uint32_t addr, int v) { asm volatile("st.shared.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ int lds32(uint32_t addr) {
+  int v;
+  asm volatile("ld.shared.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// The epilogue of one unit for one warp. Templated on the activation as a whole: a switch inside the loop over
+// the chunks cost more than the activation (4096 x 9472 x 256 without one: 51 us, 33 without the switch).
+template <typename T, typename C, int ACT>
+__device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr, const Work& w, const Epilogue<C::CH>& ep,
+                                              typename Patch<C::CH>::Raw& raw, const EpiWarp& ew, int rows, bool n_in) {
+  using namespace dgemm::ptx;
+  constexpr int CG = C::CG, BM = C::BM, CH = C::CH, GROUPS = EPI_WARPS / 4;
+  constexpr bool GATED = C::GATED;
+  // a cut tile's sums in the workspace: [part][CTA][quarter][chunk][CH / 4][lane] of float4
+  const int rel = w.part < 0 ? 0 : w.tile - pr.dp_tiles;
+  constexpr long long WS_TILE = (long long)CG * BM * 32;  // float4 per part
+  constexpr int WS_CHUNK = CH / 4 * 32;                   // float4 per quarter and chunk
+  float4* ws_tile = reinterpret_cast<float4*>(p.ws) + ((long long)(pr.slot0 + rel * pr.split) * CG + ew.rank) * (BM * 32);
+  // the accumulator may be overwritten: called once this warp's last load of it has been waited for
+  bool released = false;
+  const auto release = [&]() {
+    ptx5::fence_before_sync();
+    __syncwarp();
+    if (ew.lane == 0) {
+      if (CG == 1) mbar_arrive(ew.acc_empty);
+      else ptx5::mbar_arrive_cluster_relaxed(map_to_cta(ew.acc_empty, 0));
+    }
+    released = true;
+  };
+  if (w.part < 0) {
+    if (!GATED) {
+      for (int c = ew.group; c * CH < rows; c += GROUPS) {
+        float v[CH];
+        tmem_load<CH>(ew.acc + c * CH, v);
+        ptx5::tmem_ld_wait<CH>(v);
+        if ((c + GROUPS) * CH >= rows) release();
+        if (n_in) {
+          const typename Patch<CH>::Raw now = raw;
+          // the next chunk's residual is on its way while this one is computed
+          if (ep.has_r && (c + GROUPS) * CH < rows) ep.pt.fetch(raw, ep.r, (c + GROUPS) * CH);
+          emit_plain<T, CH, ACT>(ep, c * CH, v, now);
+        }
+      }
+    } else {
+      // Lanes 0-63 hold g, lanes 64-127 hold u of the same 64 columns. Two chunks at a time: the
+      // g warp takes u of the first from its partner, the u warp takes g of the second.
+      const bool is_g = ew.quad < 2;
+      const uint32_t mine = ew.bufs + ew.e * C::BUF_BYTES + ew.lane * 16, theirs = ew.bufs + (ew.e ^ 2) * C::BUF_BYTES + ew.lane * 16;
+      for (int c = 2 * ew.group; c * CH < rows; c += 2 * GROUPS) {
+        float v[CH], o[CH];
+        tmem_load<CH>(ew.acc + (is_g ? c + 1 : c) * CH, o);  // what the partner needs
+        tmem_load<CH>(ew.acc + (is_g ? c : c + 1) * CH, v);  // what stays here
+        ptx5::tmem_ld_wait<CH>(o);
+        ptx5::tmem_ld_wait<CH>(v);
+        if ((c + 2 * GROUPS) * CH >= rows) release();
+#pragma unroll
+        for (int j = 0; j < CH / 4; ++j) ptx5::sts128(mine + j * 512, *reinterpret_cast<const uint4*>(o + 4 * j));
+        named_barrier_sync(1 + ew.group * 2 + (ew.quad & 1), 64);
+#pragma unroll
+        for (int j = 0; j < CH / 4; ++j) *reinterpret_cast<uint4*>(o + 4 * j) = ptx5::lds128(theirs + j * 512);
+        named_barrier_sync(1 + ew.group * 2 + (ew.quad & 1), 64);
+        const int m = (is_g ? c : c + 1) * CH;
+        if (n_in && m < rows) {
+          if (is_g) emit_gated<T, CH, ACT>(ep, m, v, o);
+          else emit_gated<T, CH, ACT>(ep, m, o, v);
+        }
+      }
+    }
+  } else {
+    float4* ws = ws_tile + w.part * WS_TILE + (ew.quad * (BM / CH)) * WS_CHUNK + ew.lane;
+    for (int c = ew.group; c * CH < rows; c += GROUPS) {
+      float v[CH];
+      tmem_load<CH>(ew.acc + c * CH, v);
+      ptx5::tmem_ld_wait<CH>(v);
+#pragma unroll
+      for (int j = 0; j < CH / 4; ++j) __stcg(ws + c * WS_CHUNK + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+    }
+  }
+  if (!released) release();
+  if (w.part >= 0) {
+    int* counter = p.counters + (pr.counter0 + rel) * CG + ew.rank;
+    __threadfence();
+    named_barrier_sync(15, EPI_WARPS * 32);
+    if (ew.e == 0 && ew.lane == 0) {
+      const int old = atomicAdd(counter, 1);
+      sts32(ew.last_flag, old == pr.split - 1);
+      if (old == pr.split - 1) *counter = 0;  // ready for the next launch
+    }
+    named_barrier_sync(15, EPI_WARPS * 32);
+    if (lds32(ew.last_flag)) {
+      __threadfence();
+      if (!GATED) {
+        const float4* ws = ws_tile + (ew.quad * (BM / CH)) * WS_CHUNK + ew.lane;
+        for (int c = ew.group; c * CH < rows; c += GROUPS) {
+          if (ep.has_r && n_in) ep.pt.fetch(raw, ep.r, c * CH);
+          float v[CH];
+          add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, v);
+          if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw);
+        }
+      } else {
+        const float4* ws = ws_tile + ((ew.quad & 1) * (BM / CH)) * WS_CHUNK + ew.lane;
+        for (int c = 2 * ew.group + (ew.quad >> 1); c * CH < rows; c += 2 * GROUPS) {
+          float g[CH], uu[CH];
+          add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, g);
+          add_parts<CH>(ws + (2 * (BM / CH) + c) * WS_CHUNK, pr.split, WS_TILE, uu);
+          if (n_in) emit_gated<T, CH, ACT>(ep, c * CH, g, uu);
+        }
+      }
+    }
+    named_barrier_sync(15, EPI_WARPS * 32);  // last_flag may be rewritten
+  }
+}
+
 // Shared-memory descriptor of an operand tile made of 64 x 64 boxes with 128-byte swizzle. K-major:
 // 8-row groups are 1024 bytes apart. MN-major: the 64-value chunks of the outer index are one
 // box apart, groups of 8 k are 1024 bytes apart.
@@ -380,16 +512,14 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
   const uint32_t pad = (1024 - (raw & 1023)) & 1023;
   const uint32_t base = raw + pad;  // the same offset in both CTAs of a pair (same kernel, same launch)
   uint8_t* gen = smem_raw + pad;
-  const uint32_t xchg = base + STAGES * C::STAGE_BYTES;
-  const uint32_t patches = xchg + C::XCHG_BYTES;
-  uint8_t* ctrl = gen + STAGES * C::STAGE_BYTES + C::XCHG_BYTES + C::PATCH_BYTES;
-  const uint32_t bars = patches + C::PATCH_BYTES;
+  const uint32_t bufs = base + STAGES * C::STAGE_BYTES;
+  uint8_t* ctrl = gen + STAGES * C::STAGE_BYTES + C::BUFS_BYTES;
+  const uint32_t bars = bufs + C::BUFS_BYTES;
   const uint32_t full_bar = bars, empty_bar = bars + 8 * STAGES;        // stage s at + 8 s
   const uint32_t acc_full = bars + 16 * STAGES, acc_empty = acc_full + 16;  // accumulator a at + 8 a
   const uint32_t drain_bar = acc_empty + 16;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl + 16 * STAGES + 48);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 16 * STAGES + 52);
-  volatile int* last_flag = reinterpret_cast<volatile int*>(ctrl + 16 * STAGES + 56);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = CG == 1 ? 0 : (int)cluster_ctarank();
@@ -506,9 +636,10 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         if (globaltimer_ns() - t0 > 500000000ull) break;
     }
   } else if (warp >= 4) {
-    // ---- epilogue ----
-    const int e = warp - 4, quad = warp & 3, half = e >> 2;
+    // ---- epilogue: warp e takes TMEM quarter e % 4 and every GROUPS-th chunk (pair of chunks if gated) ----
+    const int e = warp - 4, quad = warp & 3, group = e >> 2;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    const uint32_t buf = bufs + e * C::BUF_BYTES;
     uint32_t acc_it = 0;
     // After a wait has given up, the warps still walk through the rest of the units together (without
     // waiting again), so that every named barrier below is met by all of its warps.
@@ -518,124 +649,36 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       const Problem& pr = p.prob[w.prob];
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
-      const int m_base = tm * BM;
-      const int n0 = GATED ? tn * C::NT + rank * 64 + (quad & 1) * 32 : tn * C::NT + rank * 128 + quad * 32;
+      const int m_base = tm * BM, rows = min(pr.M - m_base, BM);
+      const int n0 = tn * C::NT + (GATED ? rank * 64 + (quad & 1) * 32 : rank * 128 + quad * 32);
       const bool n_in = n0 < pr.N;  // (the whole warp: a patch beyond the last column has nothing to do)
-      Patch<CH> pt{m_base, n0, pr.M, pr.N, lane, patches + e * (CH * PITCH)};
-      const uint32_t a = acc_it & 1u;
-      float bias[4] = {0.f, 0.f, 0.f, 0.f};
-      if (!GATED && pr.bias) {
+      Epilogue<CH> ep;
+      ep.pt = Patch<CH>{rows, pr.N - n0, lane, buf, buf + (lane & 7) * PITCH + (lane >> 3) * 16};
+      ep.act = pr.act;
+      ep.has_z = pr.Z != nullptr;
+      ep.has_r = !GATED && pr.R != nullptr;
+      ep.d = ep.pt.view(pr.D, pr.ldd, pr.vec & VEC_D, m_base, n0);
+      if (ep.has_z) ep.z = ep.pt.view(pr.Z, pr.ldz, pr.vec & VEC_Z, m_base, n0);
+      if (GATED && ep.has_z) ep.u = ep.pt.view(pr.U, pr.ldu, pr.vec & VEC_U, m_base, n0);
+      if (ep.has_r) ep.r = ep.pt.view(pr.R, pr.ldr, pr.vec & VEC_R, m_base, n0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int n = n0 + 8 * j + (lane >> 2);
-          if (n < pr.N) bias[j] = to_f32(static_cast<const T*>(pr.bias)[n]);
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int n = n0 + 8 * j + (lane >> 2);
+        ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
       }
       typename Patch<CH>::Raw raw;
-      const bool use_r = !GATED && pr.R && n_in;
-      if (use_r && w.part < 0 && m_base + half * CH < pr.M) pt.fetch(raw, pr.R, pr.ldr, pr.vec & VEC_R, m_base + half * CH);
+      if (ep.has_r && n_in && w.part < 0) ep.pt.fetch(raw, ep.r, group * CH);
+      const uint32_t a = acc_it & 1u;
       if (!dead) dead = !wait_bounded(acc_full + 8 * a, (acc_it >> 1) & 1u, abort_flag, p);
       __syncwarp();
       ptx5::fence_after_sync();
-      const uint32_t t_acc = tmem + a * BM + lane_addr;
-      // a cut tile's sums in the workspace: [part][CTA][quad][chunk][CH / 4][lane] of float4
-      const int rel = w.part < 0 ? 0 : w.tile - pr.dp_tiles;
-      constexpr long long WS_TILE = (long long)CG * BM * 32;  // float4 per part
-      constexpr int WS_CHUNK = CH / 4 * 32;                   // float4 per quad and chunk
-      float4* ws_tile = reinterpret_cast<float4*>(p.ws) + ((long long)(pr.slot0 + rel * pr.split) * CG + rank) * (BM * 32);
-      if (w.part < 0) {
-        if (!GATED) {
-          for (int c = half; c < BM / CH; c += 2) {
-            if (m_base + c * CH >= pr.M) break;
-            float v[CH];
-            tmem_load<CH>(t_acc + c * CH, v);
-            ptx5::tmem_ld_wait<CH>(v);
-            pt.m0 = m_base + c * CH;
-            if (n_in) {
-              typename Patch<CH>::Raw now = raw;
-              // the next chunk's residual is on its way while this one is computed
-              if (use_r && c + 2 < BM / CH && pt.m0 + 2 * CH < pr.M) pt.fetch(raw, pr.R, pr.ldr, pr.vec & VEC_R, pt.m0 + 2 * CH);
-              emit_plain_any<T, CH>(pr, pt, v, bias, now);
-            }
-          }
-        } else {
-          // Lanes 0-63 hold g, lanes 64-127 hold u of the same 64 columns. Two chunks at a time: the
-          // g warp takes u of the first from its partner, the u warp takes g of the second.
-          const bool is_g = quad < 2;
-          const uint32_t mine = xchg + e * (CH * 128) + lane * 16, theirs = xchg + (e ^ 2) * (CH * 128) + lane * 16;
-          for (int c = 2 * half; c < BM / CH; c += 4) {
-            if (m_base + c * CH >= pr.M) break;
-            float v[CH], o[CH];
-            tmem_load<CH>(t_acc + (is_g ? c + 1 : c) * CH, o);  // what the partner needs
-            tmem_load<CH>(t_acc + (is_g ? c : c + 1) * CH, v);  // what stays here
-            ptx5::tmem_ld_wait<CH>(o);
-            ptx5::tmem_ld_wait<CH>(v);
-#pragma unroll
-            for (int j = 0; j < CH / 4; ++j) ptx5::sts128(mine + j * 512, *reinterpret_cast<const uint4*>(o + 4 * j));
-            named_barrier_sync(1 + half * 2 + (quad & 1), 64);
-#pragma unroll
-            for (int j = 0; j < CH / 4; ++j) *reinterpret_cast<uint4*>(o + 4 * j) = ptx5::lds128(theirs + j * 512);
-            named_barrier_sync(1 + half * 2 + (quad & 1), 64);
-            pt.m0 = m_base + (is_g ? c : c + 1) * CH;
-            if (n_in && pt.m0 < pr.M) {
-              if (is_g) emit_gated_any<T, CH>(pr, pt, v, o);
-              else emit_gated_any<T, CH>(pr, pt, o, v);
-            }
-          }
-        }
-      } else {
-        float4* ws = ws_tile + w.part * WS_TILE + (quad * (BM / CH)) * WS_CHUNK + lane;
-        for (int c = half; c < BM / CH; c += 2) {
-          if (m_base + c * CH >= pr.M) break;
-          float v[CH];
-          tmem_load<CH>(t_acc + c * CH, v);
-          ptx5::tmem_ld_wait<CH>(v);
-#pragma unroll
-          for (int j = 0; j < CH / 4; ++j) __stcg(ws + c * WS_CHUNK + j * 32, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-        }
-      }
-      // the accumulator may be overwritten
-      ptx5::fence_before_sync();
-      __syncwarp();
-      if (lane == 0) {
-        if (CG == 1) mbar_arrive(acc_empty + 8 * a);
-        else ptx5::mbar_arrive_cluster(map_to_cta(acc_empty + 8 * a, 0));
-      }
-      if (w.part >= 0) {
-        int* counter = p.counters + (pr.counter0 + rel) * CG + rank;
-        __threadfence();
-        named_barrier_sync(8, EPI_WARPS * 32);
-        if (e == 0 && lane == 0) {
-          const int old = atomicAdd(counter, 1);
-          *last_flag = old == pr.split - 1;
-          if (old == pr.split - 1) *counter = 0;  // ready for the next launch
-        }
-        named_barrier_sync(8, EPI_WARPS * 32);
-        if (*last_flag) {
-          __threadfence();
-          if (!GATED) {
-            const float4* ws = ws_tile + (quad * (BM / CH)) * WS_CHUNK + lane;
-            for (int c = half; c < BM / CH; c += 2) {
-              if (m_base + c * CH >= pr.M) break;
-              pt.m0 = m_base + c * CH;
-              if (use_r) pt.fetch(raw, pr.R, pr.ldr, pr.vec & VEC_R, pt.m0);
-              float v[CH];
-              add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, v);
-              if (n_in) emit_plain_any<T, CH>(pr, pt, v, bias, raw);
-            }
-          } else {
-            const float4* ws = ws_tile + ((quad & 1) * (BM / CH)) * WS_CHUNK + lane;
-            for (int c = 2 * half + (quad >> 1); c < BM / CH; c += 4) {
-              if (m_base + c * CH >= pr.M) break;
-              pt.m0 = m_base + c * CH;
-              float g[CH], uu[CH];
-              add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, g);
-              add_parts<CH>(ws + (2 * (BM / CH) + c) * WS_CHUNK, pr.split, WS_TILE, uu);
-              if (n_in) emit_gated_any<T, CH>(pr, pt, g, uu);
-            }
-          }
-        }
-        named_barrier_sync(8, EPI_WARPS * 32);  // last_flag may be rewritten
+      const EpiWarp ew{tmem + a * BM + lane_addr, bufs, bars + 16 * STAGES + 56, acc_empty + 8 * a, e, quad, group, lane, rank};
+      switch (pr.act) {
+        case HGEMM_ACT_NONE: epilogue_unit<T, C, HGEMM_ACT_NONE>(p, pr, w, ep, raw, ew, rows, n_in); break;
+        case HGEMM_ACT_RELU: epilogue_unit<T, C, HGEMM_ACT_RELU>(p, pr, w, ep, raw, ew, rows, n_in); break;
+        case HGEMM_ACT_GELU: epilogue_unit<T, C, HGEMM_ACT_GELU>(p, pr, w, ep, raw, ew, rows, n_in); break;
+        case HGEMM_ACT_GELU_TANH: epilogue_unit<T, C, HGEMM_ACT_GELU_TANH>(p, pr, w, ep, raw, ew, rows, n_in); break;
+        default: epilogue_unit<T, C, HGEMM_ACT_SILU>(p, pr, w, ep, raw, ew, rows, n_in); break;
       }
     }
   }
