@@ -11,7 +11,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdgemm.so")
-SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "layernorm.cu")]
+SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "hgemm_plain_f16.cu", "hgemm_plain_bf16.cu",
+                                                "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "layernorm.cu")]
 # every source, header and public header: an edit to any of them makes the built library stale
 DEPS = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh")) +
               glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))

@@ -10,7 +10,7 @@
 
 #include "../../include/hgemm.h"
 #include "hgemm_aux.cuh"
-#include "hgemm_tc.cuh"
+#include "hgemm_kernels.h"
 #include "lm_state.h"
 
 namespace {
@@ -29,45 +29,12 @@ std::mutex g_mutex;
 lm::EncodeTiledFn g_encode = nullptr;
 std::atomic<int> g_drop_limit_us{0};
 
-// ---- kernels by configuration -----------------------------------------------------------------------
+// ---- kernels by type --------------------------------------------------------------------------------
 
-struct Config {
-  int cg, bm;
-};
-constexpr Config kConfigs[] = {{1, 16}, {1, 32}, {1, 64}, {1, 128}, {2, 128}, {2, 256}};
-constexpr int kNumConfigs = sizeof(kConfigs) / sizeof(kConfigs[0]);
-
-template <typename T, int CG, int BM, bool GATED>
-bool launch_one(int clusters, cudaStream_t stream, const Params& p) {
-  return lm::launch(hgemm_tc_kernel<T, CG, BM, GATED>, dim3(clusters * CG), dim3(THREADS), (size_t)Cfg<CG, BM, GATED>::SMEM_BYTES, CG,
-                    stream, p);
-}
-template <typename T, bool GATED>
-bool launch_config(int c, int clusters, cudaStream_t stream, const Params& p) {
-  switch (c) {
-    case 0: return launch_one<T, 1, 16, GATED>(clusters, stream, p);
-    case 1: return launch_one<T, 1, 32, GATED>(clusters, stream, p);
-    case 2: return launch_one<T, 1, 64, GATED>(clusters, stream, p);
-    case 3: return launch_one<T, 1, 128, GATED>(clusters, stream, p);
-    case 4: return launch_one<T, 2, 128, GATED>(clusters, stream, p);
-    default: return launch_one<T, 2, 256, GATED>(clusters, stream, p);
-  }
-}
-bool launch_tc(int type, bool gated, int c, int clusters, cudaStream_t stream, const Params& p) {
+bool launch_tc(int type, bool gated, int act, int config, int clusters, cudaStream_t stream, const Params& p) {
   if (type == HGEMM_TYPE_BF16)
-    return gated ? launch_config<__nv_bfloat16, true>(c, clusters, stream, p) : launch_config<__nv_bfloat16, false>(c, clusters, stream, p);
-  return gated ? launch_config<__half, true>(c, clusters, stream, p) : launch_config<__half, false>(c, clusters, stream, p);
-}
-
-template <typename T, int CG, int BM, bool GATED>
-bool configure_one() {
-  return cudaFuncSetAttribute(hgemm_tc_kernel<T, CG, BM, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              Cfg<CG, BM, GATED>::SMEM_BYTES) == cudaSuccess;
-}
-template <typename T, bool GATED>
-bool configure_all() {
-  return configure_one<T, 1, 16, GATED>() && configure_one<T, 1, 32, GATED>() && configure_one<T, 1, 64, GATED>() &&
-         configure_one<T, 1, 128, GATED>() && configure_one<T, 2, 128, GATED>() && configure_one<T, 2, 256, GATED>();
+    return gated ? launch_gated_bf16(act, config, clusters, stream, p) : launch_plain_bf16(act, config, clusters, stream, p);
+  return gated ? launch_gated_f16(act, config, clusters, stream, p) : launch_plain_f16(act, config, clusters, stream, p);
 }
 
 // ---- work decomposition -------------------------------------------------------------------------------
@@ -288,7 +255,7 @@ struct Product {
   int64_t K[2];
   Matrix p[2], q[2];
   bool p_mn, q_mn;
-  int act = HGEMM_ACT_NONE;
+  int act = HGEMM_ACT_NONE;  // (the same in all products of a launch)
   const void* bias = nullptr;
   const void* R = nullptr;
   int64_t ldr = 0;
@@ -355,7 +322,6 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.units = q.units;
     d.slot0 = q.slot0;
     d.counter0 = q.counter0;
-    d.act = s.act;
     d.vec = (addressable(Matrix{s.D, s.M, s.N, s.ldd}) ? VEC_D : 0) | (addressable(Matrix{s.Z, s.M, s.N, s.ldz}) ? VEC_Z : 0) |
             (addressable(Matrix{s.U, s.M, s.N, s.ldu}) ? VEC_U : 0) | (addressable(Matrix{s.R, s.M, s.N, s.ldr}) ? VEC_R : 0);
     d.bias = s.bias;
@@ -376,7 +342,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
   p.wait_limit_ns = drop > 0 ? (unsigned long long)drop * 1000ull : kWaitLimitNs;
   p.drop = drop > 0;
   p.status = st->status;
-  return launch_tc(type, gated, pl.config, pl.clusters, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
+  return launch_tc(type, gated, pr[0]->act, pl.config, pl.clusters, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
 }
 
 // ---- validation -----------------------------------------------------------------------------------------
@@ -479,9 +445,7 @@ int device_state(DeviceState** out) {
     if (cudaGetSymbolAddress(reinterpret_cast<void**>(&st.status), g_hgemm_status_word) != cudaSuccess ||
         cudaGetSymbolAddress(reinterpret_cast<void**>(&st.counters), g_hgemm_counters) != cudaSuccess)
       return DGEMM_ERR_CUDA;
-    if (!configure_all<__half, false>() || !configure_all<__half, true>() || !configure_all<__nv_bfloat16, false>() ||
-        !configure_all<__nv_bfloat16, true>())
-      return DGEMM_ERR_CUDA;
+    if (!configure_plain_f16() || !configure_gated_f16() || !configure_plain_bf16() || !configure_gated_bf16()) return DGEMM_ERR_CUDA;
     if (!g_encode) {
       void* fn = nullptr;
       cudaDriverEntryPointQueryResult qres;

@@ -1,0 +1,30 @@
+// The tensor-core kernels by element type and kind: launchers and set-up, one source file each (they are
+// most of the library's compile time).
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "hgemm_tc.cuh"
+
+namespace hgemm {
+
+// Tile configurations: CTAs per tile and TMEM columns (rows of the output).
+struct Config {
+  int cg, bm;
+};
+constexpr Config kConfigs[] = {{1, 16}, {1, 32}, {1, 64}, {1, 128}, {2, 128}, {2, 256}};
+constexpr int kNumConfigs = sizeof(kConfigs) / sizeof(kConfigs[0]);
+
+// Launches configuration `config` for activation `act` on `clusters` tiles' worth of CTAs.
+bool launch_plain_f16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+bool launch_plain_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+bool launch_gated_f16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+bool launch_gated_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+
+// Once per device: shared-memory limits.
+bool configure_plain_f16();
+bool configure_plain_bf16();
+bool configure_gated_f16();
+bool configure_gated_bf16();
+
+}  // namespace hgemm

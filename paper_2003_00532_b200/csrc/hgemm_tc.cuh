@@ -23,6 +23,10 @@
 // a workspace; the CTA that finishes the last part of a tile (a counter per tile) adds all parts in
 // order and runs the epilogue: one launch, no CTA waits for another, same bits every time.
 //
+// The activation is a template argument of the whole kernel: with a switch over the five of them in it, the
+// registers of all shared one allocation and the epilogue without activation spilled (4096 x 9472 x 256: 50 us,
+// 40 alone).
+//
 // Roles (384 threads): warps 0 and 3 stage P and Q (one thread that issued all copies was the limit:
 // 479 ns per 64-wide k-block with four copies, against 366 ns for its MMAs; two threads with one or
 // two copies each are not), warp 1 issues the MMAs, warp 2 owns the TMEM allocation, warps 4-11 run
@@ -81,7 +85,6 @@ struct alignas(64) Problem {
   int split, kb_per_split;
   int units;               // dp_tiles + (tiles - dp_tiles) * split
   int slot0, counter0;     // first workspace slot and tile counter of the cut tiles
-  int act;
   int vec;                 // which of D, Z, U, R have 16-byte aligned rows (VEC_*)
   const void* bias;
   const void* R;
@@ -138,7 +141,7 @@ __device__ __forceinline__ void tile_to_mn(const Problem& pr, int tile, int& tm,
 
 // Polls an mbarrier phase; gives up after the limit, records the timeout and raises the CTA's abort
 // flag. Never spins without a limit.
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns, int* status) {
+__device__ __noinline__ static bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns, int* status) {
   using namespace dgemm::ptx;
   const unsigned long long t0 = globaltimer_ns();
   for (;;) {
@@ -302,7 +305,6 @@ struct Epilogue {
   Patch<CH> pt;
   typename Patch<CH>::View d, z, u, r;
   bool has_z, has_r;
-  int act;
   float bias[4];  // bias[j]: of column 8 j + lane / 4 of the patch
 };
 
@@ -385,8 +387,7 @@ __device__ __forceinline__ int lds32(uint32_t addr) {
   return v;
 }
 
-// The epilogue of one unit for one warp. Templated on the activation as a whole: a switch inside the loop over
-// the chunks cost more than the activation (4096 x 9472 x 256 without one: 51 us, 33 without the switch).
+// The epilogue of one unit for one warp.
 template <typename T, typename C, int ACT>
 __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr, const Work& w, const Epilogue<C::CH>& ep,
                                               typename Patch<C::CH>::Raw& raw, const EpiWarp& ew, int rows, bool n_in) {
@@ -501,7 +502,7 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major) {
   return (uint64_t)((addr & 0x3FFFF) >> 4) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
 }
 
-template <typename T, int CG, int BM, bool GATED>
+template <typename T, int CG, int BM, bool GATED, int ACT>
 __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_constant__ Params p) {
   using namespace dgemm::ptx;
   using C = Cfg<CG, BM, GATED>;
@@ -550,7 +551,6 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
   const uint32_t tmem = *tmem_slot;
   ptx5::launch_dependents();
   grid_dependency_wait();
-
   if ((warp == 0 || warp == 3) && lane == 0) {
     // ---- stages: warp 0 copies the P boxes, warp 3 the Q boxes; zero fill outside the matrices ----
     const bool is_p = warp == 0;
@@ -654,7 +654,6 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       const bool n_in = n0 < pr.N;  // (the whole warp: a patch beyond the last column has nothing to do)
       Epilogue<CH> ep;
       ep.pt = Patch<CH>{rows, pr.N - n0, lane, buf, buf + (lane & 7) * PITCH + (lane >> 3) * 16};
-      ep.act = pr.act;
       ep.has_z = pr.Z != nullptr;
       ep.has_r = !GATED && pr.R != nullptr;
       ep.d = ep.pt.view(pr.D, pr.ldd, pr.vec & VEC_D, m_base, n0);
@@ -673,13 +672,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       __syncwarp();
       ptx5::fence_after_sync();
       const EpiWarp ew{tmem + a * BM + lane_addr, bufs, bars + 16 * STAGES + 56, acc_empty + 8 * a, e, quad, group, lane, rank};
-      switch (pr.act) {
-        case HGEMM_ACT_NONE: epilogue_unit<T, C, HGEMM_ACT_NONE>(p, pr, w, ep, raw, ew, rows, n_in); break;
-        case HGEMM_ACT_RELU: epilogue_unit<T, C, HGEMM_ACT_RELU>(p, pr, w, ep, raw, ew, rows, n_in); break;
-        case HGEMM_ACT_GELU: epilogue_unit<T, C, HGEMM_ACT_GELU>(p, pr, w, ep, raw, ew, rows, n_in); break;
-        case HGEMM_ACT_GELU_TANH: epilogue_unit<T, C, HGEMM_ACT_GELU_TANH>(p, pr, w, ep, raw, ew, rows, n_in); break;
-        default: epilogue_unit<T, C, HGEMM_ACT_SILU>(p, pr, w, ep, raw, ew, rows, n_in); break;
-      }
+      epilogue_unit<T, C, ACT>(p, pr, w, ep, raw, ew, rows, n_in);
     }
   }
   __syncwarp();
