@@ -55,17 +55,20 @@ from .binding import (  # noqa: F401
     HGEMM_TYPE_BF16,
     HGEMM_TYPE_F16,
     HGEMM_TYPE_F32,
-    hgemm_epilogue,
-    hgemm_epilogue_bwd,
-    hgemm_gated,
-    hgemm_gated_bwd,
     hgemm_last_device_status,
     hgemm_plan,
     hgemm_set_test_drop_loads,
-    layernorm_bwd,
-    layernorm_fwd,
     lib_path,
     load_library,
     sgemm_f32,
     sgemm_last_device_status,
 )
+
+
+def __getattr__(name):
+    """hgemm_epilogue, hgemm_gated, layernorm_fwd and their backward passes: loaded on first use."""
+    from . import binding
+    if name in binding.MARSHALLED:
+        value = globals()[name] = getattr(binding, name)
+        return value
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -248,208 +248,40 @@ def sgemm_last_device_status(stream=None) -> int:
 
 # ---- 16-bit products with an epilogue, gated projections, layer norm --------------------------------
 
-_dtype_codes = None
+#: Entry points whose arguments are marshalled by the compiled module ``_marshal`` (csrc/binding_ext.cpp).
+MARSHALLED = ("hgemm_epilogue", "hgemm_epilogue_bwd", "hgemm_gated", "hgemm_gated_bwd", "layernorm_fwd", "layernorm_bwd")
 
 
-def _type_code(x, name: str) -> int:
-    """HGEMM_TYPE_* of a CUDA tensor on the current device."""
-    global _dtype_codes
-    import torch
-    if _dtype_codes is None:
-        _dtype_codes = {torch.float32: HGEMM_TYPE_F32, torch.float16: HGEMM_TYPE_F16, torch.bfloat16: HGEMM_TYPE_BF16}
-    if not isinstance(x, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor")
-    code = _dtype_codes.get(x.dtype)
-    if code is None:
-        raise TypeError(f"{name}: unsupported type {x.dtype}")
-    return code
+def _raise(rc: int, where: str):
+    raise DgemmError(rc, where)
 
 
-def _mat(x, name: str, like, rows: int, cols: int, device: int):
-    """(address, leading dimension) of an optional 2-D tensor of the type of `like` and the given shape."""
-    if x is None:
-        return None, max(cols, 1)
-    if x.dtype != like.dtype or x.dim() != 2:
-        raise TypeError(f"{name}: need a 2-D tensor of type {like.dtype}")
-    if x.get_device() != device:
-        raise ValueError(f"{name}: expected a CUDA tensor on the current device")
-    r, c = x.shape
-    if r != rows or c != cols:
-        raise ValueError(f"{name}: shape {tuple(x.shape)}, expected ({rows}, {cols})")
-    ld, one = x.stride()
-    if one != 1 and c > 1 and r > 0:
-        raise ValueError(f"{name}: columns must be contiguous (row-major)")
-    if r <= 1:
-        return x.data_ptr(), max(c, 1)
-    if ld < c:
-        raise ValueError(f"{name}: rows overlap (row stride {ld}, {c} columns)")
-    return x.data_ptr(), max(ld, 1)
+def load_marshal():
+    """The compiled marshalling module, connected to ``libdgemm.so``. Raises if either is absent."""
+    import torch  # noqa: F401  (the module uses torch's libraries)
+    lib = load_library()
+    path = os.path.join(_HERE, "_marshal.so")
+    if not os.path.exists(path):
+        raise FileNotFoundError(f"{path} not found: build it with `python -m paper_2003_00532_b200.build`; there is no fallback path")
+    from . import _marshal
+    _marshal.connect(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in MARSHALLED), _raise)
+    return _marshal
 
 
-def _vec(x, name: str, dtype, n: int, device: int):
-    """Address of an optional contiguous vector."""
-    if x is None:
-        return None
-    if x.dtype != dtype or x.dim() != 1:
-        raise TypeError(f"{name}: need a 1-D tensor of type {dtype}")
-    if x.get_device() != device:
-        raise ValueError(f"{name}: expected a CUDA tensor on the current device")
-    if x.shape[0] != n or (n > 1 and x.stride(0) != 1):
-        raise ValueError(f"{name}: expected {n} contiguous values")
-    return x.data_ptr()
+def __getattr__(name: str):
+    """The marshalled entry points, loaded on first use like the library itself."""
+    if name in MARSHALLED:
+        marshal = load_marshal()
+        for n in MARSHALLED:
+            globals()[n] = getattr(marshal, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
-def _current(stream):
-    """(current device, stream handle)."""
-    import torch
-    device = torch.cuda.current_device()
-    if stream is None:
-        return device, torch._C._cuda_getCurrentRawStream(device) or None
-    return device, _stream_handle(stream)
-
-
-def _checked(rc: int, where: str, check: bool) -> int:
-    if check and rc < 0:
+def _checked(rc: int, where: str) -> int:
+    if rc < 0:
         raise DgemmError(rc, where)
     return rc
-
-
-def _two_dims(x, name: str):
-    if x.dim() != 2:
-        raise TypeError(f"{name}: need a 2-D tensor")
-    return x.shape
-
-
-def hgemm_epilogue(A, B, D, bias=None, act: int = HGEMM_ACT_NONE, residual=None, preact=None, transa: bool = False,
-                   transb: bool = False, stream=None, check: bool = True) -> int:
-    """``Z = op(A) @ op(B) + bias``, ``D = act(Z) + residual`` on the current CUDA device, asynchronously.
-
-    ``A``, ``B``, ``D`` and the optional ``bias`` (N), ``residual`` and ``preact`` (M x N; receives ``Z``)
-    are CUDA tensors of one type, ``float16`` or ``bfloat16``; matrices have unit column stride. ``A`` and
-    ``B`` are passed as stored (K x M when ``transa``, N x K when ``transb``). ``residual`` may be ``D``.
-    Sums are binary32 and each output is rounded once.
-    """
-    code = _type_code(A, "A")
-    device, s = _current(stream)
-    M, K = _two_dims(A, "A")
-    if transa:
-        M, K = K, M
-    r, c = _two_dims(B, "B")
-    N = r if transb else c
-    pa, lda = _mat(A, "A", A, *((K, M) if transa else (M, K)), device)
-    pb, ldb = _mat(B, "B", A, *((N, K) if transb else (K, N)), device)
-    pd, ldd = _mat(D, "D", A, M, N, device)
-    pr, ldr = _mat(residual, "residual", A, M, N, device)
-    pz, ldz = _mat(preact, "preact", A, M, N, device)
-    rc = load_library().hgemm_epilogue(code, 1 if transa else 0, 1 if transb else 0, M, N, K, pa, lda, pb, ldb,
-                                       _vec(bias, "bias", A.dtype, N, device), act, pr, ldr, pd, ldd, pz, ldz, s)
-    return _checked(rc, "hgemm_epilogue", check)
-
-
-def hgemm_epilogue_bwd(A, B, dD, act: int = HGEMM_ACT_NONE, preact=None, dA=None, dB=None, dbias=None, transa: bool = False,
-                       transb: bool = False, stream=None, check: bool = True) -> int:
-    """Gradients of :func:`hgemm_epilogue` for the incoming ``dD``: ``dA`` and ``dB`` (stored as ``A`` and
-    ``B`` are) and ``dbias`` (N, ``float32``), each written if given. ``preact`` is the forward pass's and
-    may be ``None`` for ``HGEMM_ACT_NONE``. The residual's gradient is ``dD`` itself."""
-    code = _type_code(A, "A")
-    device, s = _current(stream)
-    ar, ac = _two_dims(A, "A")
-    br, bc = _two_dims(B, "B")
-    M, K = (ac, ar) if transa else (ar, ac)
-    N = br if transb else bc
-    pa, lda = _mat(A, "A", A, ar, ac, device)
-    pb, ldb = _mat(B, "B", A, *((N, K) if transb else (K, N)), device)
-    pz, ldz = _mat(preact, "preact", A, M, N, device)
-    pd, ldd = _mat(dD, "dD", A, M, N, device)
-    pda, ldda = _mat(dA, "dA", A, ar, ac, device)
-    pdb, lddb = _mat(dB, "dB", A, br, bc, device)
-    import torch
-    rc = load_library().hgemm_epilogue_bwd(code, 1 if transa else 0, 1 if transb else 0, M, N, K, pa, lda, pb, ldb, act, pz, ldz,
-                                           pd, ldd, pda, ldda, pdb, lddb, _vec(dbias, "dbias", torch.float32, N, device), s)
-    return _checked(rc, "hgemm_epilogue_bwd", check)
-
-
-def hgemm_gated(X, Wg, Wu, H, act: int = HGEMM_ACT_SILU, gate=None, up=None, transw: bool = False, stream=None,
-                check: bool = True) -> int:
-    """Gated projections ``H = act(X @ op(Wg)) * (X @ op(Wu))`` in one kernel, asynchronously.
-
-    ``X`` (M x K), ``Wg`` and ``Wu`` (K x F, or F x K when ``transw``), ``H`` (M x F): CUDA tensors of one
-    type, ``float16`` or ``bfloat16``. ``gate`` and ``up`` (both or neither) receive the two products,
-    which :func:`hgemm_gated_bwd` needs.
-    """
-    code = _type_code(X, "X")
-    device, s = _current(stream)
-    M, K = _two_dims(X, "X")
-    wr, wc = _two_dims(Wg, "Wg")
-    F = wr if transw else wc
-    shape = (F, K) if transw else (K, F)
-    px, ldx = _mat(X, "X", X, M, K, device)
-    pg, ldwg = _mat(Wg, "Wg", X, *shape, device)
-    pu, ldwu = _mat(Wu, "Wu", X, *shape, device)
-    ph, ldh = _mat(H, "H", X, M, F, device)
-    pgo, ldg = _mat(gate, "gate", X, M, F, device)
-    puo, ldu = _mat(up, "up", X, M, F, device)
-    rc = load_library().hgemm_gated(code, 1 if transw else 0, M, F, K, px, ldx, pg, ldwg, pu, ldwu, act, ph, ldh, pgo, ldg, puo, ldu, s)
-    return _checked(rc, "hgemm_gated", check)
-
-
-def hgemm_gated_bwd(X, Wg, Wu, gate, up, dH, act: int = HGEMM_ACT_SILU, dX=None, dWg=None, dWu=None, transw: bool = False,
-                    stream=None, check: bool = True) -> int:
-    """Gradients of :func:`hgemm_gated` for the incoming ``dH`` (M x F): ``dX``, ``dWg`` and ``dWu`` (stored
-    as ``Wg`` and ``Wu`` are), each written if given."""
-    code = _type_code(X, "X")
-    device, s = _current(stream)
-    M, K = _two_dims(X, "X")
-    wr, wc = _two_dims(Wg, "Wg")
-    F = wr if transw else wc
-    shape = (F, K) if transw else (K, F)
-    px, ldx = _mat(X, "X", X, M, K, device)
-    pwg, ldwg = _mat(Wg, "Wg", X, *shape, device)
-    pwu, ldwu = _mat(Wu, "Wu", X, *shape, device)
-    pg, ldg = _mat(gate, "gate", X, M, F, device)
-    pu, ldu = _mat(up, "up", X, M, F, device)
-    pd, lddh = _mat(dH, "dH", X, M, F, device)
-    pdx, lddx = _mat(dX, "dX", X, M, K, device)
-    pdg, lddwg = _mat(dWg, "dWg", X, *shape, device)
-    pdu, lddwu = _mat(dWu, "dWu", X, *shape, device)
-    rc = load_library().hgemm_gated_bwd(code, 1 if transw else 0, M, F, K, px, ldx, pwg, ldwg, pwu, ldwu, act, pg, ldg, pu, ldu,
-                                        pd, lddh, pdx, lddx, pdg, lddwg, pdu, lddwu, s)
-    return _checked(rc, "hgemm_gated_bwd", check)
-
-
-def layernorm_fwd(X, gamma, beta, Y, eps: float = 1e-5, mean=None, rstd=None, stream=None, check: bool = True) -> int:
-    """``Y = (X - mean) * rstd * gamma + beta`` over the rows of ``X``, asynchronously.
-
-    ``X``, ``Y`` (rows x cols) and ``gamma``, ``beta`` (cols, each may be ``None``): CUDA tensors of one type,
-    ``float32``, ``float16`` or ``bfloat16``. ``mean`` and ``rstd`` (rows, ``float32``) are written if given.
-    """
-    import torch
-    code = _type_code(X, "X")
-    device, s = _current(stream)
-    rows, cols = _two_dims(X, "X")
-    px, ldx = _mat(X, "X", X, rows, cols, device)
-    py, ldy = _mat(Y, "Y", X, rows, cols, device)
-    rc = load_library().layernorm_fwd(code, rows, cols, px, ldx, _vec(gamma, "gamma", X.dtype, cols, device),
-                                      _vec(beta, "beta", X.dtype, cols, device), eps, py, ldy,
-                                      _vec(mean, "mean", torch.float32, rows, device), _vec(rstd, "rstd", torch.float32, rows, device), s)
-    return _checked(rc, "layernorm_fwd", check)
-
-
-def layernorm_bwd(X, gamma, mean, rstd, dY, dX=None, dgamma=None, dbeta=None, stream=None, check: bool = True) -> int:
-    """Gradients of :func:`layernorm_fwd` for the incoming ``dY``: ``dX`` (type of ``X``), ``dgamma`` and
-    ``dbeta`` (cols, ``float32``), each written if given. ``mean`` and ``rstd`` are the forward pass's."""
-    import torch
-    code = _type_code(X, "X")
-    device, s = _current(stream)
-    rows, cols = _two_dims(X, "X")
-    px, ldx = _mat(X, "X", X, rows, cols, device)
-    pd, lddy = _mat(dY, "dY", X, rows, cols, device)
-    po, lddx = _mat(dX, "dX", X, rows, cols, device)
-    rc = load_library().layernorm_bwd(code, rows, cols, px, ldx, _vec(gamma, "gamma", X.dtype, cols, device),
-                                      _vec(mean, "mean", torch.float32, rows, device), _vec(rstd, "rstd", torch.float32, rows, device),
-                                      pd, lddy, po, lddx, _vec(dgamma, "dgamma", torch.float32, cols, device),
-                                      _vec(dbeta, "dbeta", torch.float32, cols, device), s)
-    return _checked(rc, "layernorm_bwd", check)
 
 
 HGEMM_PLAN_FIELDS = ("ctas_per_tile", "tile_rows", "tile_cols", "clusters", "kblocks", "dp_tiles", "split", "kblocks_per_part")
@@ -458,7 +290,7 @@ HGEMM_PLAN_FIELDS = ("ctas_per_tile", "tile_rows", "tile_cols", "clusters", "kbl
 def hgemm_plan(M: int, N: int, K: int, gated: bool = False, sm_count: int = 0) -> dict:
     """Tile and work decomposition of one 16-bit product of this shape (host logic only; needs no GPU)."""
     out = (ctypes.c_int * 8)()
-    _checked(load_library().hgemm_plan(int(M), int(N), int(K), int(bool(gated)), int(sm_count), out), "hgemm_plan", True)
+    _checked(load_library().hgemm_plan(int(M), int(N), int(K), int(bool(gated)), int(sm_count), out), "hgemm_plan")
     return dict(zip(HGEMM_PLAN_FIELDS, (int(v) for v in out)))
 
 
@@ -468,7 +300,7 @@ def hgemm_last_device_status(stream=None) -> int:
 
 def hgemm_set_test_drop_loads(limit_us: int) -> int:
     """Testing aid: > 0 makes the kernels' producers skip their copies, with waits limited to ``limit_us``."""
-    return _checked(load_library().hgemm_set_test_drop_loads(int(limit_us)), "hgemm_set_test_drop_loads", True)
+    return _checked(load_library().hgemm_set_test_drop_loads(int(limit_us)), "hgemm_set_test_drop_loads")
 
 
 def dgemm_f64_static_ws(A, B, C, split_k: int = 0, stream=None, check: bool = True) -> int:

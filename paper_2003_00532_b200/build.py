@@ -11,11 +11,13 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdgemm.so")
+EXT = os.path.join(HERE, "_marshal.so")  # compiled argument marshalling (csrc/binding_ext.cpp)
+EXT_SOURCE = os.path.join(CSRC, "binding_ext.cpp")
 SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "hgemm_plain_f16.cu", "hgemm_plain_bf16.cu",
                                                 "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "layernorm.cu")]
 # every source, header and public header: an edit to any of them makes the built library stale
 DEPS = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh")) +
-              glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
+              glob.glob(os.path.join(CSRC, "*.h")) + [EXT_SOURCE] + glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -29,9 +31,9 @@ def nvcc_path() -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(EXT):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(EXT))
     return any(os.path.getmtime(d) > t for d in DEPS)
 
 
@@ -77,6 +79,20 @@ def check_ptxas(log: str) -> None:
         raise RuntimeError("ptxas resource usage changed:\n  " + "\n  ".join(problems))
 
 
+def ext_command(out: str) -> list:
+    """The compiler command of the marshalling module (C++ only, against the installed torch)."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
+    inc = [*include_paths(), sysconfig.get_paths()["include"], cuda]
+    return ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *(f"-isystem{d}" for d in inc), EXT_SOURCE, "-o", out, f"-L{torch_lib}", f"-Wl,-rpath,{torch_lib}",
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
 def build(force: bool = False, verbose: bool = False, check: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; returns its path. With `check`
     the compile reports resource usage and fails if the hot kernels' registers or spills changed."""
@@ -92,6 +108,8 @@ def build(force: bool = False, verbose: bool = False, check: bool = False) -> st
                 log = open(obj + ".log", "w+")
                 jobs.append((obj, log, subprocess.Popen([nvcc_path(), *flags, "-c", "-o", obj, src], cwd=CSRC, stdout=log,
                                                         stderr=subprocess.STDOUT, text=True)))
+            ext_tmp, ext_log = EXT + ".tmp.%d" % os.getpid(), open(os.path.join(objs, "ext.log"), "w+")
+            jobs.append((None, ext_log, subprocess.Popen(ext_command(ext_tmp), cwd=CSRC, stdout=ext_log, stderr=subprocess.STDOUT, text=True)))
             failed, text = False, ""
             for obj, log, proc in jobs:
                 failed = proc.wait() != 0 or failed
@@ -99,7 +117,7 @@ def build(force: bool = False, verbose: bool = False, check: bool = False) -> st
                 text += log.read()
                 log.close()
             if not failed:
-                res = subprocess.run([nvcc_path(), *flags, "-shared", "-o", tmp, *(j[0] for j in jobs)], cwd=CSRC,
+                res = subprocess.run([nvcc_path(), *flags, "-shared", "-o", tmp, *(j[0] for j in jobs if j[0])], cwd=CSRC,
                                      capture_output=True, text=True)
                 failed = res.returncode != 0
                 text += res.stdout + res.stderr
@@ -110,6 +128,7 @@ def build(force: bool = False, verbose: bool = False, check: bool = False) -> st
         if check and not extra:
             check_ptxas(text)
         os.replace(tmp, LIB)
+        os.replace(ext_tmp, EXT)
     return LIB
 
 

@@ -152,9 +152,10 @@ double decompose(const Size* sz, int n, bool gated, int sms, int config, int len
   return clocks;
 }
 
-// The configuration and cut with the smallest estimate.
+// The configuration and cut with the smallest estimate. For one problem only the cuts around "as many parts
+// as there are idle clusters" can win; several problems of different lengths try a fixed list.
 bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
-  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
+  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
   double best_clocks = -1.0;
   int64_t max_m = 0;
   int kmax = 1;
@@ -163,9 +164,26 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
     if (sz[i].kblocks > kmax) kmax = sz[i].kblocks;
   }
   for (int c = 0; c < kNumConfigs; ++c) {
-    if (c > 0 && kConfigs[c - 1].cg == 1 && kConfigs[c - 1].bm >= max_m && kConfigs[c].bm > 16) continue;  // only more padding
-    for (int cut : kCuts) {
-      if (cut > kmax) break;
+    if (c > 0 && kConfigs[c - 1].cg == 1 && kConfigs[c - 1].bm >= max_m) break;  // only more padding
+    int cuts[sizeof(kCuts) / sizeof(kCuts[0])], ncuts = 0;
+    if (n == 1) {
+      const int nt = (gated ? 64 : 128) * kConfigs[c].cg, clusters = sms / kConfigs[c].cg;
+      const int64_t rest = ((sz[0].N + nt - 1) / nt) * ((sz[0].M + kConfigs[c].bm - 1) / kConfigs[c].bm) % clusters;
+      cuts[ncuts++] = 1;
+      if (rest > 0) {
+        const int fit = (int)(clusters / rest);
+        if (fit > 1) cuts[ncuts++] = fit;
+        cuts[ncuts++] = fit + 1;
+        cuts[ncuts++] = 2 * fit + 1;
+      }
+    } else {
+      for (int cut : kCuts) cuts[ncuts++] = cut;
+    }
+    int last = 0;
+    for (int j = 0; j < ncuts; ++j) {
+      const int cut = cuts[j] < kmax ? cuts[j] : kmax;
+      if (cut == last) break;
+      last = cut;
       Plan pl;
       const double t = decompose(sz, n, gated, sms, c, (kmax + cut - 1) / cut, &pl);
       if (t >= 0.0 && (best_clocks < 0.0 || t < best_clocks)) {
