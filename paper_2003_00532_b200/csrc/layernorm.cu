@@ -1,4 +1,5 @@
 // C ABI of layer norm (include/layernorm.h): validation, choice of kernel, launches.
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -35,42 +36,62 @@ struct Shape {
   bool longer;  // does not fit in registers
 };
 // A warp takes a row of up to 4 vectors per lane (no block barrier); longer rows take a block, each thread
-// holding as few vectors as 256 threads (or `max_threads`, for rows that need it) allow, at most `most`.
-// `spread`: as many threads as possible instead (few rows: the latency of one row counts).
-Shape shape_for(int64_t cols, int vec, int most, int max_threads, bool spread) {
+// holding as few vectors as 256 threads allow, at most `most`, and then as many threads as needed (`limit` of
+// the values a thread holds). `spread`: as many threads as possible instead (few rows: the latency of one
+// row counts).
+Shape shape_for(int64_t cols, int vec, int most, int (*limit)(int), bool spread) {
   const int64_t nv = (cols + vec - 1) / vec;
   const int warp_items = most < 4 ? most : 4;
   if (nv <= 32 * warp_items && !(spread && nv > 64)) return Shape{nv <= 32 ? 1 : nv <= 64 ? 2 : 4, 32, false};
   int items = 1;
-  while (items < most && nv > (int64_t)(spread ? max_threads : 256) * items) items *= 2;
+  while (items < most && nv > (int64_t)(spread ? limit(items * vec) : 256) * items) items *= 2;
   const int64_t threads = (nv + items - 1) / items;
-  if (threads > max_threads) return Shape{0, 1024, true};
+  if (threads > limit(items * vec)) return Shape{0, 1024, true};
   return Shape{items, (int)((threads + 31) / 32 * 32), false};
+}
+int fwd_limit(int values) { return fwd_threads(values); }
+int bwd_limit(int) { return BWD_THREADS; }
+
+// Blocks of one kernel (one instance of this function per kernel) that fit on the device at once, or fewer
+// for few rows.
+template <typename K, K kernel>
+unsigned resident_blocks(int sms, int threads, int64_t need) {
+  static std::atomic<int> known[33];  // by warps per block; the same on every device of this kind
+  int per_sm = known[threads / 32].load();
+  if (per_sm == 0) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
+    known[threads / 32].store(per_sm);
+  }
+  return (unsigned)(need < (int64_t)sms * per_sm ? need : (int64_t)sms * per_sm);
 }
 
 template <typename T, int VEC, int ITEMS>
-bool launch_fwd(const Shape& s, const Params& p, cudaStream_t stream) {
+bool launch_fwd(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
   if constexpr (ITEMS <= 4)
-    if (s.threads == 32)
-      return lm::launch(fwd_kernel<T, VEC, ITEMS, true>, dim3((unsigned)((p.rows + 7) / 8)), dim3(256), 0, 1, stream, p);
-  return lm::launch(fwd_kernel<T, VEC, ITEMS, false>, dim3((unsigned)p.rows), dim3(s.threads), 0, 1, stream, p);
+    if (s.threads == 32) {
+      const unsigned blocks = resident_blocks<decltype(&fwd_kernel<T, VEC, ITEMS, true>), &fwd_kernel<T, VEC, ITEMS, true>>(sms, 256, (p.rows + 7) / 8);
+      return lm::launch(fwd_kernel<T, VEC, ITEMS, true>, dim3(blocks), dim3(256), 0, 1, stream, p);
+    }
+  const unsigned blocks = resident_blocks<decltype(&fwd_kernel<T, VEC, ITEMS, false>), &fwd_kernel<T, VEC, ITEMS, false>>(sms, s.threads, p.rows);
+  return lm::launch(fwd_kernel<T, VEC, ITEMS, false>, dim3(blocks), dim3(s.threads), 0, 1, stream, p);
 }
 template <typename T, int VEC>
-bool launch_fwd_items(const Shape& s, const Params& p, cudaStream_t stream) {
+bool launch_fwd_items(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
   switch (s.items) {
-    case 1: return launch_fwd<T, VEC, 1>(s, p, stream);
-    case 2: return launch_fwd<T, VEC, 2>(s, p, stream);
-    case 4: return launch_fwd<T, VEC, 4>(s, p, stream);
-    case 8: return VEC == 1 && launch_fwd<T, 1, 8>(s, p, stream);
-    default: return VEC == 1 && launch_fwd<T, 1, 16>(s, p, stream);
+    case 1: return launch_fwd<T, VEC, 1>(sms, s, p, stream);
+    case 2: return launch_fwd<T, VEC, 2>(sms, s, p, stream);
+    case 4: return launch_fwd<T, VEC, 4>(sms, s, p, stream);
+    case 8: return VEC <= 4 && launch_fwd<T, VEC <= 4 ? VEC : 1, 8>(sms, s, p, stream);
+    case 16: return VEC == 1 && launch_fwd<T, 1, 16>(sms, s, p, stream);
+    default: return VEC == 1 && launch_fwd<T, 1, 32>(sms, s, p, stream);
   }
 }
 template <typename T, int VEC>
 bool run_fwd(int sms, bool aligned, const Params& p, cudaStream_t stream) {
   const bool spread = p.rows <= sms;
-  const Shape s = aligned ? shape_for(p.cols, VEC, 4, 1024, spread) : shape_for(p.cols, 1, 16, 1024, spread);
+  const Shape s = aligned ? shape_for(p.cols, VEC, 32 / VEC, fwd_limit, spread) : shape_for(p.cols, 1, 32, fwd_limit, spread);
   if (s.longer) return lm::launch(fwd_long_kernel<T>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p);
-  return aligned ? launch_fwd_items<T, VEC>(s, p, stream) : launch_fwd_items<T, 1>(s, p, stream);
+  return aligned ? launch_fwd_items<T, VEC>(sms, s, p, stream) : launch_fwd_items<T, 1>(sms, s, p, stream);
 }
 
 // Blocks of the backward pass: persistent, two per SM, or fewer for few rows.
@@ -193,7 +214,7 @@ int layernorm_bwd(int type, int64_t rows, int64_t cols, const void* X, int64_t l
   const bool aligned = rows_aligned(type, X, ldx) && rows_aligned(type, dY, lddy) && (!dX || rows_aligned(type, dX, lddx)) &&
                        ((uintptr_t)gamma & 15) == 0;
   const int vec = type == HGEMM_TYPE_F32 ? 4 : 8;
-  const Shape shape = aligned ? shape_for(cols, vec, 16 / vec, BWD_THREADS, false) : shape_for(cols, 1, 16, BWD_THREADS, false);
+  const Shape shape = aligned ? shape_for(cols, vec, 16 / vec, bwd_limit, false) : shape_for(cols, 1, 16, bwd_limit, false);
   const int blocks = bwd_blocks(st->sm_count, shape, rows);
   scratch::Hold hold(st->scratch, s);
   if (p.want_params) {

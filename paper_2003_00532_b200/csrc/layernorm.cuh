@@ -1,16 +1,20 @@
 // Layer norm, forward and backward. Bound by memory: each kernel reads its rows once, holds them in
-// registers through both sums, and writes once.
+// registers through all sums, and writes once.
 //
 // A row belongs to one warp (short rows: no block barrier at all) or to one block; a thread holds ITEMS
 // vectors of VEC values (VEC = 16 bytes where the rows are 16-byte aligned, else single values) at
-// columns (item * threads + thread) * VEC. The mean is summed first and the variance from the centred
-// values that are still in registers. Rows too long for that are streamed (three passes, the
-// second and third mostly from L2).
+// columns (item * threads + thread) * VEC. Blocks are persistent: a thread keeps its columns' gamma and beta in
+// registers from row to row, and the next row's loads are in flight while a row is computed.
 //
-// Backward: blocks are persistent; while a block walks over its rows, each thread also keeps
-// dgamma and dbeta of its own columns in registers, the next row's loads in flight. The blocks' sums go
-// to a partial matrix [block][column] that a second kernel adds in order of the blocks: no atomics,
-// same bits every time.
+// Forward: mean and variance in one block barrier. Each warp takes the mean and the sum of squares about that
+// mean of its own part of the row (both from registers); the parts are then combined as
+// M2 = sum_w M2_w + n_w (mean_w - mean)^2, so no large sums are ever subtracted.
+//
+// Backward: while a block walks over its rows, each thread also keeps dgamma and dbeta of its own columns
+// in registers. The blocks' sums go to a partial matrix [block][column] that a second kernel adds in
+// order of the blocks: no atomics, same bits every time.
+//
+// Rows too long for the registers are streamed (later passes mostly from L2).
 #pragma once
 
 #include <cstdint>
@@ -46,9 +50,15 @@ template <> __device__ __forceinline__ __half rnd<__half>(float x) { return __fl
 template <> __device__ __forceinline__ __nv_bfloat16 rnd<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 // VEC values as one access of VEC * sizeof(T) bytes (16, or one value).
+template <int BYTES> struct Bits;
+template <> struct Bits<16> { using type = uint4; };
+template <> struct Bits<4> { using type = uint32_t; };
+template <> struct Bits<2> { using type = uint16_t; };
 template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) Vec {
-  T v[VEC];
+struct Vec {
+  typename Bits<sizeof(T) * VEC>::type bits;
+  __device__ __forceinline__ T get(int i) const { return reinterpret_cast<const T*>(&bits)[i]; }
+  __device__ __forceinline__ void set(int i, T x) { reinterpret_cast<T*>(&bits)[i] = x; }
 };
 
 // VEC values at column c; beyond `cols` they read as `fill`.
@@ -56,21 +66,21 @@ template <typename T, int VEC>
 __device__ __forceinline__ Vec<T, VEC> load(const T* row, int c, int cols, float fill) {
   Vec<T, VEC> r;
   if (c + VEC <= cols) {
-    r = *reinterpret_cast<const Vec<T, VEC>*>(row + c);
+    r.bits = *reinterpret_cast<const decltype(r.bits)*>(row + c);
   } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) r.v[i] = c + i < cols ? row[c + i] : rnd<T>(fill);
+    for (int i = 0; i < VEC; ++i) r.set(i, c + i < cols ? row[c + i] : rnd<T>(fill));
   }
   return r;
 }
 template <typename T, int VEC>
 __device__ __forceinline__ void store(T* row, int c, int cols, const Vec<T, VEC>& r) {
   if (c + VEC <= cols) {
-    *reinterpret_cast<Vec<T, VEC>*>(row + c) = r;
+    *reinterpret_cast<typename Bits<sizeof(T) * VEC>::type*>(row + c) = r.bits;
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
-      if (c + i < cols) row[c + i] = r.v[i];
+      if (c + i < cols) row[c + i] = r.get(i);
   }
 }
 
@@ -90,61 +100,97 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
 
 // ---- forward ----------------------------------------------------------------------------------------
 
+// Most threads per row, by the values a thread holds: 1024 x 64 registers, 512 x 128.
+constexpr int fwd_threads(int values) { return values <= 8 ? 1024 : 512; }
+
 template <typename T, int VEC, int ITEMS, bool WARP_ROW>
-__global__ void __launch_bounds__(WARP_ROW ? 256 : 1024) fwd_kernel(const __grid_constant__ Params p) {
-  __shared__ float red[2][32];
+__global__ void __launch_bounds__(WARP_ROW ? 256 : fwd_threads(VEC* ITEMS)) fwd_kernel(const __grid_constant__ Params p) {
+  __shared__ float2 red[2][32];
   hgemm::ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
   const int threads = WARP_ROW ? 32 : blockDim.x;
   const int t = WARP_ROW ? threadIdx.x & 31 : threadIdx.x;
-  const long long row = WARP_ROW ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : (long long)blockIdx.x;
-  if (row >= p.rows) return;
-  const T* x = static_cast<const T*>(p.X) + row * p.ldx;
-  Vec<T, VEC> raw[ITEMS];
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) raw[i] = load<T, VEC>(x, (i * threads + t) * VEC, p.cols, 0.f);
-  float v[ITEMS][VEC], s = 0.f;
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      v[i][j] = cvt(raw[i].v[j]);
-      s += v[i][j];
-    }
-  const float n = (float)p.cols;
-  const float mean = (WARP_ROW ? warp_sum(s) : block_sum(s, red[0])) / n;
-  s = 0.f;
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      v[i][j] -= mean;
-      if ((i * threads + t) * VEC + j < p.cols) s += v[i][j] * v[i][j];
-    }
-  const float var = (WARP_ROW ? warp_sum(s) : block_sum(s, red[1])) / n;
-  const float rstd = 1.f / sqrtf(var + p.eps);
-  if (t == 0) {
-    if (p.mean) p.mean[row] = mean;
-    if (p.rstd) p.rstd[row] = rstd;
-  }
-  T* y = static_cast<T*>(p.out) + row * p.ldo;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long first = WARP_ROW ? (long long)blockIdx.x * 8 + warp : (long long)blockIdx.x;
+  const long long step = WARP_ROW ? (long long)gridDim.x * 8 : (long long)gridDim.x;
+  if (first >= p.rows) return;
+  const T* X = static_cast<const T*>(p.X);
   const T* gamma = static_cast<const T*>(p.gamma);
   const T* beta = static_cast<const T*>(p.beta);
+  Vec<T, VEC> g[ITEMS], b[ITEMS], raw[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) raw[i] = load<T, VEC>(X + first * p.ldx, (i * threads + t) * VEC, p.cols, 0.f);
+  int mine = 0;  // columns of this thread
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
     const int c = (i * threads + t) * VEC;
-    if (c >= p.cols) continue;
-    Vec<T, VEC> g, b, o;
-    if (gamma) g = load<T, VEC>(gamma, c, p.cols, 1.f);
-    if (beta) b = load<T, VEC>(beta, c, p.cols, 0.f);
+    mine += max(0, min(VEC, p.cols - c));
+    if (gamma) g[i] = load<T, VEC>(gamma, c, p.cols, 1.f);
+    if (beta) b[i] = load<T, VEC>(beta, c, p.cols, 0.f);
+  }
+  const float inv_n = 1.f / (float)p.cols;
+  // columns of this warp, and of warp number `lane` (exact in binary32: at most 2^15)
+  const float n_warp = WARP_ROW ? (float)p.cols : warp_sum((float)mine);
+  const float inv_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
+  float n_lane = 0.f;
+  if (!WARP_ROW) {
+    if (lane == 0) red[1][warp].x = n_warp;
+    __syncthreads();
+    if (lane < (int)(blockDim.x >> 5)) n_lane = red[1][lane].x;
+    __syncthreads();
+  }
+  int parity = 0;
+  for (long long row = first; row < p.rows; row += step, parity ^= 1) {
+    float v[ITEMS][VEC], s = 0.f;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      float a = v[i][j] * rstd;
-      if (gamma) a *= cvt(g.v[j]);
-      if (beta) a += cvt(b.v[j]);
-      o.v[j] = rnd<T>(a);
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        v[i][j] = cvt(raw[i].get(j));
+        s += v[i][j];
+      }
+    if (row + step < p.rows) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) raw[i] = load<T, VEC>(X + (row + step) * p.ldx, (i * threads + t) * VEC, p.cols, 0.f);
     }
-    store<T, VEC>(y, c, p.cols, o);
+    float mean = warp_sum(s) * inv_warp;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float d = v[i][j] - mean;
+        if ((i * threads + t) * VEC + j < p.cols) s += d * d;
+      }
+    float m2 = warp_sum(s);
+    if (!WARP_ROW) {
+      if (lane == 0) red[parity][warp] = make_float2(mean, m2);
+      __syncthreads();  // one per row: a warp can be one row ahead, and writes the other half of `red` then
+      const float2 part = lane < (int)(blockDim.x >> 5) ? red[parity][lane] : make_float2(0.f, 0.f);
+      mean = warp_sum(part.x * n_lane) * inv_n;
+      const float d = part.x - mean;
+      m2 = warp_sum(part.y + n_lane * d * d);
+    }
+    const float rstd = 1.f / sqrtf(m2 * inv_n + p.eps);
+    if (t == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
+    T* y = static_cast<T*>(p.out) + row * p.ldo;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int c = (i * threads + t) * VEC;
+      if (c >= p.cols) continue;
+      Vec<T, VEC> o;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        float a = (v[i][j] - mean) * rstd;
+        if (gamma) a *= cvt(g[i].get(j));
+        if (beta) a += cvt(b[i].get(j));
+        o.set(j, rnd<T>(a));
+      }
+      store<T, VEC>(y, c, p.cols, o);
+    }
   }
 }
 
@@ -207,7 +253,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
       g[i] = load<T, VEC>(gamma, c, p.cols, 0.f);
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) g[i].v[j] = rnd<T>(1.f);
+      for (int j = 0; j < VEC; ++j) g[i].set(j, rnd<T>(1.f));
     }
 #pragma unroll
     for (int j = 0; j < VEC; ++j) dg[i][j] = db[i][j] = 0.f;
@@ -231,11 +277,11 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float dy = cvt(dr[i].v[j]);
-        xh[i][j] = (cvt(xr[i].v[j]) - mean) * rstd;
+        const float dy = cvt(dr[i].get(j));
+        xh[i][j] = (cvt(xr[i].get(j)) - mean) * rstd;
         // a column beyond the row takes no part, whatever mean and rstd are
         if ((i * threads + t) * VEC + j >= p.cols) xh[i][j] = 0.f;
-        w[i][j] = dy * cvt(g[i].v[j]);
+        w[i][j] = dy * cvt(g[i].get(j));
         dg[i][j] += dy * xh[i][j];
         db[i][j] += dy;
         s1 += w[i][j];
@@ -275,7 +321,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
       if (c >= p.cols) continue;
       Vec<T, VEC> o;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) o.v[j] = rnd<T>(rs * (w[i][j] - s1 - xh[i][j] * s2));
+      for (int j = 0; j < VEC; ++j) o.set(j, rnd<T>(rs * (w[i][j] - s1 - xh[i][j] * s2)));
       store<T, VEC>(dx, c, p.cols, o);
     }
   }
