@@ -35,95 +35,155 @@ struct Shape {
   int items, threads;
   bool longer;  // does not fit in registers
 };
-// A warp takes a row of up to 4 vectors per lane (no block barrier); longer rows take a block, each thread
-// holding as few vectors as 256 threads allow, at most `most`, and then as many threads as needed (`limit` of
-// the values a thread holds). `spread`: as many threads as possible instead (few rows: the latency of one
-// row counts).
-Shape shape_for(int64_t cols, int vec, int most, int (*limit)(int), bool spread) {
-  const int64_t nv = (cols + vec - 1) / vec;
-  const int warp_items = most < 4 ? most : 4;
-  if (nv <= 32 * warp_items && !(spread && nv > 64)) return Shape{nv <= 32 ? 1 : nv <= 64 ? 2 : 4, 32, false};
-  int items = 1;
-  while (items < most && nv > (int64_t)(spread ? limit(items * vec) : 256) * items) items *= 2;
-  const int64_t threads = (nv + items - 1) / items;
-  if (threads > limit(items * vec)) return Shape{0, 1024, true};
-  return Shape{items, (int)((threads + 31) / 32 * 32), false};
+// Smallest power of two >= n.
+int pow2(int64_t n) {
+  int p = 1;
+  while (p < n) p *= 2;
+  return p;
 }
-int fwd_limit(int values) { return fwd_threads(values); }
-int bwd_limit(int) { return BWD_THREADS; }
+// Threads of a block that covers nv vectors with `items` per thread (a warp covers 32 items vectors).
+int threads_for(int64_t nv, int items) { return (int)((nv + 32 * items - 1) / (32 * items) * 32); }
+
+// Forward: a warp for rows of up to 32 values per lane; a block with 16 values per thread beyond (or up to 32, for rows
+// that need them). Few rows are spread over as many threads as there are vectors, because then the latency of
+// one row counts.
+Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms) {
+  const int64_t nv = (cols + vec - 1) / vec;
+  const int most = 32 / vec;
+  const bool spread = rows * ((nv + 32 * most - 1) / (32 * most)) < (int64_t)sms * 16;  // warps in all
+  if (nv <= 32 || (!spread && nv <= 32 * most)) return Shape{pow2((nv + 31) / 32), 32, false};
+  int items = spread ? 1 : 16 / vec;
+  while (items < most && threads_for(nv, items) > fwd_threads(items * vec)) items *= 2;
+  const int threads = threads_for(nv, items);
+  if (threads > fwd_threads(items * vec)) return Shape{0, 1024, true};
+  return Shape{items, threads, false};
+}
+// Backward: a warp for rows of up to 16 values per lane; a block with 16 values per thread beyond; 32 (`WIDE`, sums in
+// shared memory) for rows that need them.
+Shape bwd_shape(int64_t cols, int vec) {
+  const int64_t nv = (cols + vec - 1) / vec;
+  const int most = 16 / vec;
+  if (nv <= 32 * most) return Shape{pow2((nv + 31) / 32), 32, false};
+  for (int items = most; items <= 2 * most; items *= 2)
+    if (threads_for(nv, items) <= BWD_THREADS) return Shape{items, threads_for(nv, items), false};
+  return Shape{0, 1024, true};
+}
 
 // Blocks of one kernel (one instance of this function per kernel) that fit on the device at once, or fewer
-// for few rows.
+// for few rows. `smem` is the most that the kernel is launched with.
 template <typename K, K kernel>
-unsigned resident_blocks(int sms, int threads, int64_t need) {
+unsigned resident_blocks(int sms, int threads, size_t smem, int64_t need) {
   static std::atomic<int> known[33];  // by warps per block; the same on every device of this kind
   int per_sm = known[threads / 32].load();
   if (per_sm == 0) {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) per_sm = 1;
     known[threads / 32].store(per_sm);
   }
   return (unsigned)(need < (int64_t)sms * per_sm ? need : (int64_t)sms * per_sm);
 }
 
-template <typename T, int VEC, int ITEMS>
-bool launch_fwd(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
-  if constexpr (ITEMS <= 4)
-    if (s.threads == 32) {
-      const unsigned blocks = resident_blocks<decltype(&fwd_kernel<T, VEC, ITEMS, true>), &fwd_kernel<T, VEC, ITEMS, true>>(sms, 256, (p.rows + 7) / 8);
-      return lm::launch(fwd_kernel<T, VEC, ITEMS, true>, dim3(blocks), dim3(256), 0, 1, stream, p);
+template <typename T, int VEC, int ITEMS, bool WARP_ROW>
+bool launch_fwd(int sms, int threads, const Params& p, cudaStream_t stream) {
+  constexpr auto kernel = &fwd_kernel<T, VEC, ITEMS, WARP_ROW>;
+  const size_t smem = (size_t)((p.cols + VEC - 1) / VEC) * VEC * 8;              // gamma and beta
+  const size_t most = (size_t)(WARP_ROW ? 32 : threads) * ITEMS * VEC * 8;  // ... for the longest row of this shape
+  if (most > 48 * 1024) {
+    static std::atomic<bool> configured[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if (!configured[dev].load()) {
+      constexpr int limit = fwd_threads(VEC * ITEMS) * ITEMS * VEC * 8;
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return false;
+      configured[dev].store(true);
     }
-  const unsigned blocks = resident_blocks<decltype(&fwd_kernel<T, VEC, ITEMS, false>), &fwd_kernel<T, VEC, ITEMS, false>>(sms, s.threads, p.rows);
-  return lm::launch(fwd_kernel<T, VEC, ITEMS, false>, dim3(blocks), dim3(s.threads), 0, 1, stream, p);
+  }
+  const int64_t need = WARP_ROW ? (p.rows + 3) / 4 : p.rows;
+  const unsigned blocks = resident_blocks<decltype(kernel), kernel>(sms, threads, most, need);
+  return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p);
+}
+template <typename T, int VEC, int ITEMS>
+bool launch_fwd_items(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
+  if (s.threads == 32) return launch_fwd<T, VEC, ITEMS, true>(sms, 128, p, stream);
+  return launch_fwd<T, VEC, ITEMS, false>(sms, s.threads, p, stream);
 }
 template <typename T, int VEC>
-bool launch_fwd_items(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
+bool run_fwd_vec(int sms, const Params& p, cudaStream_t stream) {
+  const Shape s = fwd_shape(p.rows, p.cols, VEC, sms);
+  if (s.longer) return lm::launch(fwd_long_kernel<T>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p);
   switch (s.items) {
-    case 1: return launch_fwd<T, VEC, 1>(sms, s, p, stream);
-    case 2: return launch_fwd<T, VEC, 2>(sms, s, p, stream);
-    case 4: return launch_fwd<T, VEC, 4>(sms, s, p, stream);
-    case 8: return VEC <= 4 && launch_fwd<T, VEC <= 4 ? VEC : 1, 8>(sms, s, p, stream);
-    case 16: return VEC == 1 && launch_fwd<T, 1, 16>(sms, s, p, stream);
-    default: return VEC == 1 && launch_fwd<T, 1, 32>(sms, s, p, stream);
+    case 1: return launch_fwd_items<T, VEC, 1>(sms, s, p, stream);
+    case 2: return launch_fwd_items<T, VEC, 2>(sms, s, p, stream);
+    case 4: return launch_fwd_items<T, VEC, 4>(sms, s, p, stream);
+    case 8: return VEC <= 4 && launch_fwd_items<T, VEC <= 4 ? VEC : 1, 8>(sms, s, p, stream);
+    case 16: return VEC == 1 && launch_fwd_items<T, 1, 16>(sms, s, p, stream);
+    default: return VEC == 1 && launch_fwd_items<T, 1, 32>(sms, s, p, stream);
   }
 }
 template <typename T, int VEC>
 bool run_fwd(int sms, bool aligned, const Params& p, cudaStream_t stream) {
-  const bool spread = p.rows <= sms;
-  const Shape s = aligned ? shape_for(p.cols, VEC, 32 / VEC, fwd_limit, spread) : shape_for(p.cols, 1, 32, fwd_limit, spread);
-  if (s.longer) return lm::launch(fwd_long_kernel<T>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p);
-  return aligned ? launch_fwd_items<T, VEC>(sms, s, p, stream) : launch_fwd_items<T, 1>(sms, s, p, stream);
+  return aligned ? run_fwd_vec<T, VEC>(sms, p, stream) : run_fwd_vec<T, 1>(sms, p, stream);
 }
 
-// Blocks of the backward pass: persistent, two per SM, or fewer for few rows.
-int bwd_blocks(int sms, const Shape& s, int64_t rows) {
-  const int64_t need = s.longer ? (rows + 15) / 16 : s.threads == 32 ? (rows + 7) / 8 : rows;
-  return (int)(need < sms * 2 ? need : sms * 2);
+// Blocks of the backward pass: as many as fit at once, but for few rows at least eight rows each (every block leaves
+// its own sums to be added), down to one per SM.
+template <typename K, K kernel>
+int bwd_blocks(int sms, int threads, size_t smem, int64_t rows, int rows_per_block) {
+  const int64_t need = (rows + rows_per_block - 1) / rows_per_block;
+  const int64_t some = (int)resident_blocks<K, kernel>(sms, threads, smem, need);
+  const int64_t eighth = (rows + 8 * rows_per_block - 1) / (8 * rows_per_block);
+  const int64_t want = eighth > sms ? eighth : sms;
+  return (int)(some < want ? some : want);
 }
 
-template <typename T, int VEC, int ITEMS>
-bool launch_bwd(const Shape& s, int blocks, const Params& p, cudaStream_t stream) {
-  if constexpr (ITEMS <= 4)
-    if (s.threads == 32)
-      return lm::launch(bwd_kernel<T, VEC, ITEMS, true>, dim3(blocks), dim3(256), p.want_params ? (size_t)p.cols * 8 : 0, 1, stream, p);
-  return lm::launch(bwd_kernel<T, VEC, ITEMS, false>, dim3(blocks), dim3(s.threads), 0, 1, stream, p);
-}
-template <typename T, int VEC>
-bool launch_bwd_items(const Shape& s, int blocks, const Params& p, cudaStream_t stream) {
-  switch (s.items) {
-    case 1: return launch_bwd<T, VEC, 1>(s, blocks, p, stream);
-    case 2: return launch_bwd<T, VEC, 2>(s, blocks, p, stream);
-    case 4: return VEC <= 4 && launch_bwd<T, VEC <= 4 ? VEC : 1, 4>(s, blocks, p, stream);
-    case 8: return VEC == 1 && launch_bwd<T, 1, 8>(s, blocks, p, stream);
-    default: return VEC == 1 && launch_bwd<T, 1, 16>(s, blocks, p, stream);
+// Runs the row kernel; `partial` is asked for the matrix of the blocks' sums. Returns the number of blocks, 0 on failure.
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE, typename F>
+int launch_bwd(int sms, int threads, Params& p, cudaStream_t stream, F partial) {
+  constexpr auto kernel = &bwd_kernel<T, VEC, ITEMS, WARP_ROW, WIDE>;
+  const size_t smem = WIDE ? (size_t)threads * ITEMS * VEC * 12 : WARP_ROW && p.want_params ? (size_t)p.cols * 8 : 0;
+  if (WIDE) {
+    static std::atomic<bool> configured[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (!configured[dev].load()) {
+      constexpr int limit = BWD_THREADS * ITEMS * VEC * 12;
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return 0;
+      configured[dev].store(true);
+    }
   }
+  const size_t most = WIDE ? smem : WARP_ROW ? (size_t)32 * ITEMS * VEC * 8 : 0;
+  const int blocks = bwd_blocks<decltype(kernel), kernel>(sms, threads, most, p.rows, WARP_ROW ? 8 : 1);
+  if (!partial(blocks)) return 0;
+  return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p) ? blocks : 0;
 }
-template <typename T, int VEC>
-bool run_bwd(const Shape& s, int blocks, bool aligned, const Params& p, cudaStream_t stream) {
+template <typename T, int VEC, typename F>
+int run_bwd_vec(int sms, Params& p, cudaStream_t stream, F partial) {
+  const Shape s = bwd_shape(p.cols, VEC);
   if (s.longer) {
-    if (p.out && !lm::launch(bwd_long_kernel<T>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p)) return false;
-    return !p.want_params || lm::launch(bwd_long_params_kernel<T>, dim3((unsigned)((p.cols + 255) / 256), blocks), dim3(256), 0, 1, stream, p);
+    const int chunks = (int)((p.rows + 15) / 16 < sms * 2 ? (p.rows + 15) / 16 : sms * 2);
+    if (!partial(chunks)) return 0;
+    if (p.out && !lm::launch(bwd_long_kernel<T>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p)) return 0;
+    if (p.want_params && !lm::launch(bwd_long_params_kernel<T>, dim3((unsigned)((p.cols + 255) / 256), chunks), dim3(256), 0, 1, stream, p))
+      return 0;
+    return chunks;
   }
-  return aligned ? launch_bwd_items<T, VEC>(s, blocks, p, stream) : launch_bwd_items<T, 1>(s, blocks, p, stream);
+  constexpr int MOST = 16 / VEC;
+  if (s.threads == 32) {
+    if (s.items == 1) return launch_bwd<T, VEC, 1, true, false>(sms, 256, p, stream, partial);
+    if (s.items == 2) return launch_bwd<T, VEC, 2, true, false>(sms, 256, p, stream, partial);
+    if constexpr (MOST >= 4)
+      if (s.items == 4) return launch_bwd<T, VEC, 4, true, false>(sms, 256, p, stream, partial);
+    if constexpr (MOST >= 16) {
+      if (s.items == 8) return launch_bwd<T, VEC, 8, true, false>(sms, 256, p, stream, partial);
+      if (s.items == 16) return launch_bwd<T, VEC, 16, true, false>(sms, 256, p, stream, partial);
+    }
+    return 0;
+  }
+  if (s.items == MOST) return launch_bwd<T, VEC, MOST, false, false>(sms, s.threads, p, stream, partial);
+  return launch_bwd<T, VEC, 2 * MOST, false, true>(sms, s.threads, p, stream, partial);
+}
+template <typename T, int VEC, typename F>
+int run_bwd(int sms, bool aligned, Params& p, cudaStream_t stream, F partial) {
+  return aligned ? run_bwd_vec<T, VEC>(sms, p, stream, partial) : run_bwd_vec<T, 1>(sms, p, stream, partial);
 }
 
 bool bad_type(int type) { return type != HGEMM_TYPE_F32 && type != HGEMM_TYPE_F16 && type != HGEMM_TYPE_BF16; }
@@ -213,19 +273,16 @@ int layernorm_bwd(int type, int64_t rows, int64_t cols, const void* X, int64_t l
   p.want_params = dgamma || dbeta;
   const bool aligned = rows_aligned(type, X, ldx) && rows_aligned(type, dY, lddy) && (!dX || rows_aligned(type, dX, lddx)) &&
                        ((uintptr_t)gamma & 15) == 0;
-  const int vec = type == HGEMM_TYPE_F32 ? 4 : 8;
-  const Shape shape = aligned ? shape_for(cols, vec, 16 / vec, bwd_limit, false) : shape_for(cols, 1, 16, bwd_limit, false);
-  const int blocks = bwd_blocks(st->sm_count, shape, rows);
   scratch::Hold hold(st->scratch, s);
-  if (p.want_params) {
-    p.partial = static_cast<float*>(hold.workspace((size_t)2 * blocks * cols * 4));
-    if (!p.partial) return DGEMM_ERR_CUDA;
-  }
-  const bool ok = type == HGEMM_TYPE_F32   ? run_bwd<float, 4>(shape, blocks, aligned, p, s)
-                  : type == HGEMM_TYPE_F16 ? run_bwd<__half, 8>(shape, blocks, aligned, p, s)
-                                           : run_bwd<__nv_bfloat16, 8>(shape, blocks, aligned, p, s);
-  if (!ok) return DGEMM_ERR_CUDA;
-  if (p.want_params && !lm::launch(bwd_reduce_kernel, dim3((unsigned)((cols + 31) / 32), 2), dim3(256), 0, 1, s,
+  const auto partial = [&](int blocks) {
+    if (p.want_params) p.partial = static_cast<float*>(hold.workspace((size_t)2 * blocks * cols * 4));
+    return !p.want_params || p.partial != nullptr;
+  };
+  const int blocks = type == HGEMM_TYPE_F32   ? run_bwd<float, 4>(st->sm_count, aligned, p, s, partial)
+                     : type == HGEMM_TYPE_F16 ? run_bwd<__half, 8>(st->sm_count, aligned, p, s, partial)
+                                              : run_bwd<__nv_bfloat16, 8>(st->sm_count, aligned, p, s, partial);
+  if (blocks == 0) return DGEMM_ERR_CUDA;
+  if (p.want_params && !lm::launch(bwd_reduce_kernel, dim3((unsigned)((cols + 31) / 32), 2), dim3(512), 0, 1, s,
                                    (const float*)p.partial, blocks, (int)cols, dgamma, dbeta))
     return DGEMM_ERR_CUDA;
   return DGEMM_OK;

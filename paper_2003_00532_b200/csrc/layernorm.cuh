@@ -84,10 +84,125 @@ __device__ __forceinline__ void store(T* row, int c, int cols, const Vec<T, VEC>
   }
 }
 
+// Two binary32 values per instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(r)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(r)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// A thread's VEC * ITEMS values as pairs, in order of their columns (an odd count is padded with 0): pair k is
+// values 2 k and 2 k + 1, value f belongs to item f / VEC.
+template <typename T, int VEC, int ITEMS>
+struct Pairs {
+  static constexpr int N = (VEC * ITEMS + 1) / 2;
+  float2 v[N];
+  __device__ __forceinline__ void unpack(const Vec<T, VEC> (&raw)[ITEMS]) {
+    if constexpr (VEC == 8 && sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const uint32_t w[4] = {raw[i].bits.x, raw[i].bits.y, raw[i].bits.z, raw[i].bits.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * i + j] = unpack_pair(w[j], T());
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        v[k].x = cvt(raw[2 * k / VEC].get(2 * k % VEC));
+        v[k].y = 2 * k + 1 < VEC * ITEMS ? cvt(raw[(2 * k + 1 < VEC * ITEMS ? 2 * k + 1 : 0) / VEC].get((2 * k + 1) % VEC)) : 0.f;
+      }
+    }
+  }
+  // Item i rounded to T.
+  __device__ __forceinline__ Vec<T, VEC> pack(int i) const {
+    Vec<T, VEC> o;
+    if constexpr (VEC == 8 && sizeof(T) == 2) {
+      o.bits = make_uint4(pack_pair(v[4 * i], T()), pack_pair(v[4 * i + 1], T()), pack_pair(v[4 * i + 2], T()), pack_pair(v[4 * i + 3], T()));
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const int f = i * VEC + j;
+        o.set(j, rnd<T>(f % 2 ? v[f / 2].y : v[f / 2].x));
+      }
+    }
+    return o;
+  }
+  static __device__ __forceinline__ float2 unpack_pair(uint32_t w, __nv_bfloat16) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  static __device__ __forceinline__ float2 unpack_pair(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+  static __device__ __forceinline__ uint32_t pack_pair(float2 x, __nv_bfloat16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t pack_pair(float2 x, __half) {
+    const __half2 h = __floats2half2_rn(x.x, x.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+};
+
+// A thread's part of a row: ITEMS vectors 32 vectors apart, so that a warp covers 32 ITEMS vectors and every offset
+// from the thread's first one is a constant. `full`: all of them lie inside the row.
+template <typename T, int VEC, int ITEMS>
+__device__ __forceinline__ void load_row(Vec<T, VEC> (&raw)[ITEMS], const T* at, int c0, int cols, bool full) {
+  if (full) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) raw[i].bits = *reinterpret_cast<const decltype(raw[i].bits)*>(at + i * 32 * VEC);
+  } else {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) raw[i] = load<T, VEC>(at + i * 32 * VEC, 0, cols - c0 - i * 32 * VEC, 0.f);
+  }
+}
+template <typename T, int VEC, int ITEMS>
+__device__ __forceinline__ void store_row(T* at, const Pairs<T, VEC, ITEMS>& v, int c0, int cols, bool full) {
+  if (full) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) *reinterpret_cast<decltype(v.pack(0).bits)*>(at + i * 32 * VEC) = v.pack(i).bits;
+  } else {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) store<T, VEC>(at + i * 32 * VEC, 0, cols - c0 - i * 32 * VEC, v.pack(i));
+  }
+}
+// Values per vector and plane of a parameter kept in shared memory as binary32: value j of vector v at
+// [plane j / 4][v][j % 4], so that 16-byte accesses are free of conflicts.
+template <int VEC>
+__device__ __forceinline__ int plane_at(int c, int nv) {
+  constexpr int LOW = VEC < 4 ? VEC : 4;
+  return ((c % VEC / LOW) * nv + c / VEC) * LOW + c % VEC % LOW;
+}
+
+// 1 / sqrt(x): the approximation (2 units in the last place) and one Newton step. x = 0 gives infinity.
+__device__ __forceinline__ float inv_sqrt(float x) {
+  const float r = rsqrtf(x);
+  return x > 0.f && r < __int_as_float(0x7f800000) && r > 0.f ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
+}
+
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
+}
+// Two sums over the warp with six shuffles instead of ten: the halves of the warp each take one of them.
+__device__ __forceinline__ float2 warp_sum_pair(float a, float b) {
+  const bool low = (threadIdx.x & 16) == 0;
+  float x = (low ? a : b) + __shfl_xor_sync(0xffffffffu, low ? b : a, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  const float y = __shfl_xor_sync(0xffffffffu, x, 16);
+  return low ? make_float2(x, y) : make_float2(y, x);
 }
 // Sum over the block; `red` holds one value per warp and may be reused after the next barrier.
 __device__ __forceinline__ float block_sum(float x, float* red) {
@@ -100,97 +215,112 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
 
 // ---- forward ----------------------------------------------------------------------------------------
 
-// Most threads per row, by the values a thread holds: 1024 x 64 registers, 512 x 128.
+// Most threads per row, by the values a thread holds.
 constexpr int fwd_threads(int values) { return values <= 8 ? 1024 : 512; }
 
+// WARP_ROW: four rows per block of 128 threads, one warp each; otherwise one row per block. gamma and beta wait in
+// shared memory. What the shuffles, the barrier and the combination of the warps' parts cost per row is shared by 16
+// values per thread; 8 leave them half of all instructions, with 32 too few warps fit on an SM.
 template <typename T, int VEC, int ITEMS, bool WARP_ROW>
-__global__ void __launch_bounds__(WARP_ROW ? 256 : fwd_threads(VEC* ITEMS)) fwd_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_kernel(const __grid_constant__ Params p) {
+  constexpr int PLANES = (VEC + 3) / 4, LOW = VEC < 4 ? VEC : 4;
+  extern __shared__ uint4 smem[];
   __shared__ float2 red[2][32];
   hgemm::ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
-  const int threads = WARP_ROW ? 32 : blockDim.x;
-  const int t = WARP_ROW ? threadIdx.x & 31 : threadIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long first = WARP_ROW ? (long long)blockIdx.x * 8 + warp : (long long)blockIdx.x;
-  const long long step = WARP_ROW ? (long long)gridDim.x * 8 : (long long)gridDim.x;
-  if (first >= p.rows) return;
-  const T* X = static_cast<const T*>(p.X);
-  const T* gamma = static_cast<const T*>(p.gamma);
-  const T* beta = static_cast<const T*>(p.beta);
-  Vec<T, VEC> g[ITEMS], b[ITEMS], raw[ITEMS];
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) raw[i] = load<T, VEC>(X + first * p.ldx, (i * threads + t) * VEC, p.cols, 0.f);
-  int mine = 0;  // columns of this thread
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int c = (i * threads + t) * VEC;
-    mine += max(0, min(VEC, p.cols - c));
-    if (gamma) g[i] = load<T, VEC>(gamma, c, p.cols, 1.f);
-    if (beta) b[i] = load<T, VEC>(beta, c, p.cols, 0.f);
+  const int v0 = (WARP_ROW ? 0 : warp * ITEMS * 32) + lane, c0 = v0 * VEC;  // first vector and column of this thread
+  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
+  const long long step = WARP_ROW ? (long long)gridDim.x * 4 : (long long)gridDim.x;
+  long long row = WARP_ROW ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  T* y_at = static_cast<T*>(p.out) + row * p.ldo + c0;
+  Vec<T, VEC> raw[ITEMS];
+  if (row < p.rows) load_row<T, VEC, ITEMS>(raw, x_at, c0, p.cols, full);
+  const int nv = (p.cols + VEC - 1) / VEC;
+  float* sg = reinterpret_cast<float*>(smem);
+  float* sb = sg + nv * VEC;
+  for (int c = threadIdx.x; c < nv * VEC; c += blockDim.x) {
+    const bool in = c < p.cols;
+    sg[plane_at<VEC>(c, nv)] = p.gamma && in ? cvt(static_cast<const T*>(p.gamma)[c]) : 1.f;
+    sb[plane_at<VEC>(c, nv)] = p.beta && in ? cvt(static_cast<const T*>(p.beta)[c]) : 0.f;
   }
+  using P = Pairs<T, VEC, ITEMS>;
+  constexpr int N = P::N;
+  const bool plain = full && VEC * ITEMS % 2 == 0;
   const float inv_n = 1.f / (float)p.cols;
-  // columns of this warp, and of warp number `lane` (exact in binary32: at most 2^15)
-  const float n_warp = WARP_ROW ? (float)p.cols : warp_sum((float)mine);
-  const float inv_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
-  float n_lane = 0.f;
-  if (!WARP_ROW) {
-    if (lane == 0) red[1][warp].x = n_warp;
-    __syncthreads();
-    if (lane < (int)(blockDim.x >> 5)) n_lane = red[1][lane].x;
-    __syncthreads();
-  }
+  // columns of this warp, and of warp number `lane`
+  const auto columns = [&](int w) { return (float)max(0, min(32 * ITEMS * VEC, p.cols - w * 32 * ITEMS * VEC)); };
+  const float n_warp = WARP_ROW ? (float)p.cols : columns(warp), inv_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
+  const float n_lane = !WARP_ROW && lane < (int)(blockDim.x >> 5) ? columns(lane) : 0.f;
+  __syncthreads();
   int parity = 0;
-  for (long long row = first; row < p.rows; row += step, parity ^= 1) {
-    float v[ITEMS][VEC], s = 0.f;
+  for (; row < p.rows; parity ^= 1) {
+    P x;
+    x.unpack(raw);
+    const long long at = row;
+    row += step;
+    x_at += step * p.ldx;
+    if (row < p.rows) load_row<T, VEC, ITEMS>(raw, x_at, c0, p.cols, full);
+    float2 s = both(0.f);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
+    for (int k = 0; k < N; ++k) s = add2(s, x.v[k]);
+    float mean = warp_sum(s.x + s.y) * inv_warp;
+    s = both(0.f);
+    const float2 minus = both(-mean);
+    if (plain) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        v[i][j] = cvt(raw[i].get(j));
-        s += v[i][j];
+      for (int k = 0; k < N; ++k) {
+        x.v[k] = add2(x.v[k], minus);
+        s = fma2(x.v[k], x.v[k], s);
       }
-    if (row + step < p.rows) {
+    } else {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i) raw[i] = load<T, VEC>(X + (row + step) * p.ldx, (i * threads + t) * VEC, p.cols, 0.f);
+      for (int f = 0; f < VEC * ITEMS; ++f) {
+        float& d = f % 2 ? x.v[f / 2].y : x.v[f / 2].x;
+        d -= mean;
+        if (c0 + f / VEC * 32 * VEC + f % VEC < p.cols) s.x += d * d;
+      }
     }
-    float mean = warp_sum(s) * inv_warp;
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float d = v[i][j] - mean;
-        if ((i * threads + t) * VEC + j < p.cols) s += d * d;
-      }
-    float m2 = warp_sum(s);
+    float m2 = warp_sum(s.x + s.y);
+    float shift = 0.f;  // row mean minus the mean that x is centred by
     if (!WARP_ROW) {
       if (lane == 0) red[parity][warp] = make_float2(mean, m2);
       __syncthreads();  // one per row: a warp can be one row ahead, and writes the other half of `red` then
       const float2 part = lane < (int)(blockDim.x >> 5) ? red[parity][lane] : make_float2(0.f, 0.f);
+      const float warp_mean = mean;
       mean = warp_sum(part.x * n_lane) * inv_n;
-      const float d = part.x - mean;
-      m2 = warp_sum(part.y + n_lane * d * d);
+      const float off = part.x - mean;
+      m2 = warp_sum(part.y + n_lane * off * off);
+      shift = mean - warp_mean;
     }
-    const float rstd = 1.f / sqrtf(m2 * inv_n + p.eps);
-    if (t == 0) {
-      if (p.mean) p.mean[row] = mean;
-      if (p.rstd) p.rstd[row] = rstd;
+    const float rstd = inv_sqrt(m2 * inv_n + p.eps);
+    if (lane == 0 && (WARP_ROW || warp == 0)) {
+      if (p.mean) p.mean[at] = mean;
+      if (p.rstd) p.rstd[at] = rstd;
     }
-    T* y = static_cast<T*>(p.out) + row * p.ldo;
+    // x was centred before it is scaled: a mean far above the deviation costs no accuracy
+    const float bias = -shift * rstd;
+#pragma unroll
+    for (int k = 0; k < N; ++k) x.v[k] = fma2(x.v[k], both(rstd), both(bias));
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * threads + t) * VEC;
-      if (c >= p.cols) continue;
-      Vec<T, VEC> o;
+      const int v = min(v0 + i * 32, nv - 1);  // (beyond the row: any value, it is not stored)
+      if constexpr (VEC > 1) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        float a = (v[i][j] - mean) * rstd;
-        if (gamma) a *= cvt(g[i].get(j));
-        if (beta) a += cvt(b[i].get(j));
-        o.set(j, rnd<T>(a));
+        for (int h = 0; h < PLANES; ++h) {
+          const float4 g = *reinterpret_cast<const float4*>(sg + (h * nv + v) * LOW), b = *reinterpret_cast<const float4*>(sb + (h * nv + v) * LOW);
+          const int k = i * VEC / 2 + 2 * h;
+          x.v[k] = fma2(x.v[k], make_float2(g.x, g.y), make_float2(b.x, b.y));
+          x.v[k + 1] = fma2(x.v[k + 1], make_float2(g.z, g.w), make_float2(b.z, b.w));
+        }
+      } else {
+        float& d = i % 2 ? x.v[i / 2].y : x.v[i / 2].x;
+        d = d * sg[v] + sb[v];
       }
-      store<T, VEC>(y, c, p.cols, o);
     }
+    store_row<T, VEC, ITEMS>(y_at, x, c0, p.cols, full);
+    y_at += step * p.ldo;
   }
 }
 
@@ -210,7 +340,7 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
     const float d = cvt(x[c]) - mean;
     s += d * d;
   }
-  const float rstd = 1.f / sqrtf(block_sum(s, red[1]) / (float)p.cols + p.eps);
+  const float rstd = inv_sqrt(block_sum(s, red[1]) / (float)p.cols + p.eps);
   if (threadIdx.x == 0) {
     if (p.mean) p.mean[blockIdx.x] = mean;
     if (p.rstd) p.rstd[blockIdx.x] = rstd;
@@ -227,137 +357,173 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
 
 // ---- backward ---------------------------------------------------------------------------------------
 
-constexpr int BWD_THREADS = 512;  // most threads per row: 128 registers each hold 16 columns and their sums
+// Most threads per row: 512 with 16 values each in 128 registers.
+constexpr int BWD_THREADS = 512;
 
-template <typename T, int VEC, int ITEMS, bool WARP_ROW>
+// WARP_ROW: eight rows per block, one warp each; otherwise one row per block. WIDE: 32 values per thread, gamma and the
+// sums for dgamma and dbeta in shared memory (each thread's own entries) instead of registers.
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE>
 __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const __grid_constant__ Params p) {
-  extern __shared__ float sums[];  // WARP_ROW with parameter gradients: [cols] twice
-  __shared__ float red[2][2][32];
+  constexpr int LOW = VEC < 4 ? VEC : 4;
+  extern __shared__ uint4 smem[];  // WARP_ROW with parameter gradients: [cols] twice; WIDE: gamma, dgamma, dbeta
+  __shared__ float2 red[2][32];
   hgemm::ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
-  const int threads = WARP_ROW ? 32 : blockDim.x;
-  const int t = WARP_ROW ? threadIdx.x & 31 : threadIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long first = WARP_ROW ? (long long)blockIdx.x * 8 + warp : (long long)blockIdx.x;
+  const int v0 = (WARP_ROW ? 0 : warp * ITEMS * 32) + lane, c0 = v0 * VEC;  // first vector and column of this thread
+  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const long long step = WARP_ROW ? (long long)gridDim.x * 8 : (long long)gridDim.x;
-  const T* X = static_cast<const T*>(p.X);
-  const T* dY = static_cast<const T*>(p.dY);
+  long long row = WARP_ROW ? (long long)blockIdx.x * 8 + warp : (long long)blockIdx.x;
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  const T* d_at = static_cast<const T*>(p.dY) + row * p.ldy + c0;
+  T* o_at = static_cast<T*>(p.out) + row * p.ldo + c0;
   const T* gamma = static_cast<const T*>(p.gamma);
   const float inv_n = 1.f / (float)p.cols;
-  Vec<T, VEC> g[ITEMS], xr[ITEMS], dr[ITEMS];
-  float dg[ITEMS][VEC], db[ITEMS][VEC];
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int c = (i * threads + t) * VEC;
+  using P = Pairs<T, VEC, ITEMS>;
+  constexpr int N = P::N;
+  const int nv = (int)(blockDim.x >> 5) * ITEMS * 32;  // WIDE: vectors of the whole block, inside the row or not
+  float* sums = reinterpret_cast<float*>(smem);
+  float* w_g = sums;
+  float* w_dg = sums + nv * VEC;
+  float* w_db = sums + 2 * nv * VEC;
+  Vec<T, VEC> xr[ITEMS], dr[ITEMS];
+  P g, dg, db;
+  if (WIDE) {
+    for (int c = threadIdx.x; c < nv * VEC; c += blockDim.x) {
+      const int at = plane_at<VEC>(c, nv);
+      w_g[at] = gamma && c < p.cols ? cvt(gamma[c]) : 1.f;
+      w_dg[at] = w_db[at] = 0.f;
+    }
+    __syncthreads();
+  } else {
     if (gamma) {
-      g[i] = load<T, VEC>(gamma, c, p.cols, 0.f);
+      load_row<T, VEC, ITEMS>(xr, gamma + c0, c0, p.cols, full);
+      g.unpack(xr);
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) g[i].set(j, rnd<T>(1.f));
+      for (int k = 0; k < N; ++k) g.v[k] = both(1.f);
     }
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) dg[i][j] = db[i][j] = 0.f;
+    for (int k = 0; k < N; ++k) dg.v[k] = db.v[k] = both(0.f);
   }
   float mean = 0.f, rstd = 0.f;
-  if (first < p.rows) {
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * threads + t) * VEC;
-      xr[i] = load<T, VEC>(X + first * p.ldx, c, p.cols, 0.f);
-      dr[i] = load<T, VEC>(dY + first * p.ldy, c, p.cols, 0.f);
-    }
-    mean = p.mean[first];
-    rstd = p.rstd[first];
+  if (row < p.rows) {
+    load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
+    load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
+    mean = p.mean[row];
+    rstd = p.rstd[row];
   }
   int parity = 0;
-  for (long long row = first; row < p.rows; row += step, parity ^= 1) {
-    // xh and w = dy gamma of this row; beyond `cols` dy is 0 and so is every sum's term
-    float xh[ITEMS][VEC], w[ITEMS][VEC], s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float dy = cvt(dr[i].get(j));
-        xh[i][j] = (cvt(xr[i].get(j)) - mean) * rstd;
-        // a column beyond the row takes no part, whatever mean and rstd are
-        if ((i * threads + t) * VEC + j >= p.cols) xh[i][j] = 0.f;
-        w[i][j] = dy * cvt(g[i].get(j));
-        dg[i][j] += dy * xh[i][j];
-        db[i][j] += dy;
-        s1 += w[i][j];
-        s2 += w[i][j] * xh[i][j];
-      }
-    const float rs = rstd;
-    const long long next = row + step;
-    if (next < p.rows) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * threads + t) * VEC;
-        xr[i] = load<T, VEC>(X + next * p.ldx, c, p.cols, 0.f);
-        dr[i] = load<T, VEC>(dY + next * p.ldy, c, p.cols, 0.f);
-      }
-      mean = p.mean[next];
-      rstd = p.rstd[next];
+  for (; row < p.rows; parity ^= 1) {
+    // xh and w = dy gamma of this row. Beyond `cols` dy is 0, and so is every term of the sums
+    P xh, w;
+    xh.unpack(xr);
+    w.unpack(dr);
+    const float rs = rstd, mu = mean;
+    row += step;
+    x_at += step * p.ldx;
+    d_at += step * p.ldy;
+    if (row < p.rows) {
+      load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
+      load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
+      mean = p.mean[row];
+      rstd = p.rstd[row];
     }
-    if (!p.out) continue;
-    s1 = warp_sum(s1);
-    s2 = warp_sum(s2);
-    if (!WARP_ROW) {
-      if (lane == 0) {
-        red[parity][0][warp] = s1;
-        red[parity][1][warp] = s2;
+    float2 t1 = both(0.f), t2 = both(0.f);
+    if (!WIDE) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        xh.v[k] = mul2(add2(xh.v[k], both(-mu)), both(rs));
+        dg.v[k] = fma2(w.v[k], xh.v[k], dg.v[k]);
+        db.v[k] = add2(db.v[k], w.v[k]);
+        w.v[k] = mul2(w.v[k], g.v[k]);
+        t1 = add2(t1, w.v[k]);
+        t2 = fma2(w.v[k], xh.v[k], t2);
       }
-      __syncthreads();  // one barrier per row: the other parity's values are read before the next one
-      const int warps = (blockDim.x + 31) >> 5;
-      s1 = warp_sum(lane < warps ? red[parity][0][lane] : 0.f);
-      s2 = warp_sum(lane < warps ? red[parity][1][lane] : 0.f);
+    } else {
+      // LOW values at a time; with VEC == 1 the pairs span two vectors, so single values are used
+#pragma unroll
+      for (int q = 0; q < VEC * ITEMS / LOW; ++q) {
+        const int at = ((q % (VEC / LOW)) * nv + v0 + q / (VEC / LOW) * 32) * LOW;
+        if constexpr (LOW == 4) {
+          float4 a = *reinterpret_cast<float4*>(w_dg + at), b = *reinterpret_cast<float4*>(w_db + at);
+          const float4 gg = *reinterpret_cast<const float4*>(w_g + at);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int k = 2 * q + h;
+            float2& da = reinterpret_cast<float2*>(&a)[h];
+            float2& dbb = reinterpret_cast<float2*>(&b)[h];
+            xh.v[k] = mul2(add2(xh.v[k], both(-mu)), both(rs));
+            da = fma2(w.v[k], xh.v[k], da);
+            dbb = add2(dbb, w.v[k]);
+            w.v[k] = mul2(w.v[k], reinterpret_cast<const float2*>(&gg)[h]);
+            t1 = add2(t1, w.v[k]);
+            t2 = fma2(w.v[k], xh.v[k], t2);
+          }
+          *reinterpret_cast<float4*>(w_dg + at) = a;
+          *reinterpret_cast<float4*>(w_db + at) = b;
+        } else {
+          float& h = q % 2 ? xh.v[q / 2].y : xh.v[q / 2].x;
+          float& d = q % 2 ? w.v[q / 2].y : w.v[q / 2].x;
+          h = (h - mu) * rs;
+          w_dg[at] += d * h;
+          w_db[at] += d;
+          d *= w_g[at];
+          t1.x += d;
+          t2.x += d * h;
+        }
+      }
     }
-    s1 *= inv_n;
-    s2 *= inv_n;
-    T* dx = static_cast<T*>(p.out) + row * p.ldo;
+    if (p.out) {
+      float2 both_sums = warp_sum_pair(t1.x + t1.y, t2.x + t2.y);
+      if (!WARP_ROW) {
+        if (lane == 0) red[parity][warp] = both_sums;
+        __syncthreads();  // one barrier per row: the other parity's values are read before the next one
+        both_sums = lane < (int)(blockDim.x >> 5) ? red[parity][lane] : both(0.f);
+        both_sums = warp_sum_pair(both_sums.x, both_sums.y);
+      }
+      const float s1 = both_sums.x * inv_n, s2 = both_sums.y * inv_n;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int c = (i * threads + t) * VEC;
-      if (c >= p.cols) continue;
-      Vec<T, VEC> o;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) o.set(j, rnd<T>(rs * (w[i][j] - s1 - xh[i][j] * s2)));
-      store<T, VEC>(dx, c, p.cols, o);
+      for (int k = 0; k < N; ++k) w.v[k] = mul2(add2(fma2(xh.v[k], both(-s2), w.v[k]), both(-s1)), both(rs));
+      store_row<T, VEC, ITEMS>(o_at, w, c0, p.cols, full);
+      o_at += step * p.ldo;
     }
   }
   if (!p.want_params) return;
-  if (!WARP_ROW) {
-    float* out = p.partial + (long long)blockIdx.x * p.cols;
-    const long long half = (long long)gridDim.x * p.cols;
+  float* out = p.partial + (long long)blockIdx.x * p.cols;
+  const long long half = (long long)gridDim.x * p.cols;
+  const auto value = [](const P& x, int f) { return f % 2 ? x.v[f / 2].y : x.v[f / 2].x; };
+  if (WIDE) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
+      out[c] = w_dg[plane_at<VEC>(c, nv)];
+      out[half + c] = w_db[plane_at<VEC>(c, nv)];
+    }
+  } else if (!WARP_ROW) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const int c = (i * threads + t) * VEC + j;
-        if (c < p.cols) {
-          out[c] = dg[i][j];
-          out[half + c] = db[i][j];
-        }
+    for (int f = 0; f < VEC * ITEMS; ++f) {
+      const int c = c0 + f / VEC * 32 * VEC + f % VEC;
+      if (c < p.cols) {
+        out[c] = value(dg, f);
+        out[half + c] = value(db, f);
       }
+    }
   } else {
     // the eight warps add their sums one after the other, in order
     for (int k = 0; k < 8; ++k) {
       if (warp == k) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const int c = (i * 32 + t) * VEC + j;
-            if (c < p.cols) {
-              sums[c] = k ? sums[c] + dg[i][j] : dg[i][j];
-              sums[p.cols + c] = k ? sums[p.cols + c] + db[i][j] : db[i][j];
-            }
+        for (int f = 0; f < VEC * ITEMS; ++f) {
+          const int c = c0 + f / VEC * 32 * VEC + f % VEC;
+          if (c < p.cols) {
+            const float a = value(dg, f), b = value(db, f);
+            sums[c] = k ? sums[c] + a : a;
+            sums[p.cols + c] = k ? sums[p.cols + c] + b : b;
           }
+        }
       }
       __syncthreads();
     }
-    float* out = p.partial + (long long)blockIdx.x * p.cols;
-    const long long half = (long long)gridDim.x * p.cols;
     for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
       out[c] = sums[c];
       out[half + c] = sums[p.cols + c];
@@ -409,10 +575,10 @@ __global__ void __launch_bounds__(256) bwd_long_params_kernel(const __grid_const
   p.partial[((long long)gridDim.y + blockIdx.y) * p.cols + c] = db;
 }
 
-// Adds the blocks' sums in order: blockIdx.y 0 = dgamma, 1 = dbeta. 32 columns per block; eight warps
-// take an eighth of the blocks each.
-__global__ void __launch_bounds__(256) bwd_reduce_kernel(const float* partial, int blocks, int cols, float* dgamma, float* dbeta) {
-  __shared__ float red[8][32];
+// Adds the blocks' sums in order: blockIdx.y 0 = dgamma, 1 = dbeta. 32 columns per block; sixteen warps
+// take a sixteenth of the blocks each, eight loads in flight.
+__global__ void __launch_bounds__(512) bwd_reduce_kernel(const float* partial, int blocks, int cols, float* dgamma, float* dbeta) {
+  __shared__ float red[16][32];
   hgemm::ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
   float* out = blockIdx.y ? dbeta : dgamma;
@@ -420,15 +586,25 @@ __global__ void __launch_bounds__(256) bwd_reduce_kernel(const float* partial, i
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;
   const float* src = partial + (long long)blockIdx.y * blocks * cols;
-  const int per = (blocks + 7) / 8;
+  const int per = (blocks + 15) / 16;
+  const int b1 = min(blocks, (warp + 1) * per);
   float s = 0.f;
-  if (c < cols)
-    for (int b = warp * per; b < min(blocks, (warp + 1) * per); ++b) s += __ldcg(src + (long long)b * cols + c);
+  if (c < cols) {
+    int b = warp * per;
+    for (; b + 8 <= b1; b += 8) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __ldcg(src + (long long)(b + j) * cols + c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[j];
+    }
+    for (; b < b1; ++b) s += __ldcg(src + (long long)b * cols + c);
+  }
   red[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < cols) {
     s = red[0][lane];
-    for (int w = 1; w < 8; ++w) s += red[w][lane];
+    for (int w = 1; w < 16; ++w) s += red[w][lane];
     out[c] = s;
   }
 }
