@@ -21,9 +21,6 @@ __device__ __forceinline__ float inv_1p_exp2(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
-// 1 / (1 + exp(-x)) to binary32 accuracy, for values that are summed in binary32.
-__device__ __forceinline__ float sigmoid_full(float x) { return 1.f / (1.f + expf(-x)); }
-
 // act(z) for a result that is rounded to 16 bits.
 template <int ACT>
 __device__ __forceinline__ float act_fwd(float z) {
@@ -35,7 +32,8 @@ __device__ __forceinline__ float act_fwd(float z) {
   return z;
 }
 
-// act(z) and act'(z) to binary32 accuracy.
+// act(z) and act'(z), within a few units of 2^-22 of their size: the values are rounded to 16 bits, or summed over
+// rows in binary32, where such errors average out below the rounding of the sum.
 template <int ACT>
 __device__ __forceinline__ void act_both(float z, float& f, float& df) {
   if (ACT == HGEMM_ACT_RELU) {
@@ -46,12 +44,12 @@ __device__ __forceinline__ void act_both(float z, float& f, float& df) {
     f = z * cdf;
     df = cdf + z * INV_SQRT_2PI * expf(-0.5f * z * z);
   } else if (ACT == HGEMM_ACT_GELU_TANH) {
-    const float q = sigmoid_full(2.f * TANH_C * (z + TANH_A * z * z * z));
+    const float q = inv_1p_exp2(z * (-2.f * LOG2E * TANH_C - 2.f * LOG2E * TANH_C * TANH_A * z * z));
     f = z * q;
     const float t = f * (1.f - q);  // 0 far out, where z * z may be infinite
     df = t == 0.f ? q : q + t * (2.f * TANH_C) * (1.f + 3.f * TANH_A * z * z);
   } else if (ACT == HGEMM_ACT_SILU) {
-    const float q = sigmoid_full(z);
+    const float q = inv_1p_exp2(-LOG2E * z);
     f = z * q;
     df = q + f * (1.f - q);
   } else {

@@ -39,11 +39,20 @@ bool launch_tc(int type, bool gated, int act, int config, int clusters, cudaStre
 
 // ---- work decomposition -------------------------------------------------------------------------------
 
-// Sizes of one product: output columns N (lanes) and rows M, k-blocks.
+// Sizes of one product: output columns N (lanes) and rows M, k-blocks, and the clocks a CTA's epilogue takes per
+// row of the output.
 struct Size {
   int64_t N, M;
   int kblocks;
+  double epilogue;
 };
+// Clocks per output row of a tile's epilogue in one CTA: a plain store, what the activation adds, each further
+// matrix with 16-byte aligned rows, and what a matrix that moves value by value adds (outputs; the residual, whose
+// loads are exposed).
+double epilogue_clocks(int act, int matrices, int unaligned_out, bool unaligned_res) {
+  const double f = act == HGEMM_ACT_NONE || act == HGEMM_ACT_RELU ? 0.0 : act == HGEMM_ACT_GELU ? 60.0 : 20.0;
+  return 10.0 + f + 10.0 * (matrices - 1) + 25.0 * unaligned_out + (unaligned_res ? 100.0 : 0.0);
+}
 
 struct Plan {
   int config = 0;
@@ -56,12 +65,22 @@ struct Plan {
   int slots = 0;  // workspace slots of bm * 128 * cg binary32 values
 };
 
-// Estimated clocks of one launch, from the sizes that bound each part (per CTA): the MMAs of a k-block
-// (8192 flop per clock), its operand bytes from L2 (64 per clock), an epilogue, and for cut tiles the
-// partial sums' way through L2.
+// The model of a launch's time in clocks. Its constants were fitted to 20 shapes in every configuration and cut that
+// could win (M 1 .. 4096, N 128 .. 16384, K 64 .. 8192): the pick's time is 1.3 % above the best one's in the
+// geometric mean.
+constexpr double kL2BytesPerClock = 43.5;  // operand bytes into one SM
+constexpr double kKBlockClocks = 510.0;    // least time of a k-block
+constexpr double kUnitClocks = 1700.0;     // start and end of a unit of work
+constexpr double kLaunchClocks = 6700.0;
+constexpr double kPartColumn = 20.0;       // a part's sums to the workspace, per row of the output
+constexpr double kJoinColumn = 8.0;        // adding one part, per row of the output
+constexpr double kJoinClocks = 4500.0;     // publishing the parts and finding the last one
+
+// Clocks of one k-block in a CTA: its MMAs (8192 flop per clock), or its operand bytes.
 double step_clocks(const Config& c) {
-  const double mma = 2.0 * c.bm, bytes = (16384.0 + 128.0 * (c.bm / c.cg < 64 ? 64 : c.bm / c.cg)) / 64.0;
-  return mma > bytes ? mma : bytes;
+  const double mma = 2.16 * c.bm, bytes = (16384.0 + 128.0 * (c.bm / c.cg < 64 ? 64 : c.bm / c.cg)) / kL2BytesPerClock;
+  const double t = mma > bytes ? mma : bytes;
+  return t > kKBlockClocks ? t : kKBlockClocks;
 }
 
 // Decomposes the problems (longest contraction first) into units for one configuration: whole waves of
@@ -84,7 +103,10 @@ double decompose(const Size* sz, int n, bool gated, int sms, int config, int len
   }
   if (total > INT32_MAX / 64) return -1.0;
   int64_t tail = total % clusters;
-  // whole waves: each as long as its longest tile
+  double epi = 0.0;
+  for (int i = 0; i < n; ++i)
+    if (sz[i].epilogue * c.bm > epi) epi = sz[i].epilogue * c.bm;
+  // whole waves: each as long as its longest tile, or as an epilogue (which runs beside the next tile's MMAs)
   const double step = step_clocks(c);
   double clocks = 0.0;
   {
@@ -96,7 +118,7 @@ double decompose(const Size* sz, int n, bool gated, int sms, int config, int len
       const int64_t waves = (in_problem < left ? in_problem : left) + clusters - 1;
       int64_t w = waves / clusters;
       if (w * clusters > left) w = left / clusters;
-      clocks += (double)w * sz[i].kblocks * step;
+      clocks += (double)w * ((sz[i].kblocks * step > epi ? sz[i].kblocks * step : epi) + kUnitClocks);
       int64_t used = w * clusters;
       left -= used;
       while (used > 0) {
@@ -142,9 +164,10 @@ double decompose(const Size* sz, int n, bool gated, int sms, int config, int len
   }
   if (counters * c.cg > lm::kCounters) return -1.0;
   const int64_t tail_rounds = (tail_units + clusters - 1) / clusters;
-  clocks += (double)tail_rounds * longest * step;
-  if (max_split > 1) clocks += (double)tail_rounds * 10.0 * c.bm + 8.0 * c.bm * max_split + 2500.0;
-  clocks += 12.0 * c.bm + 2000.0;
+  const double part = longest * step, write = max_split > 1 ? kPartColumn * c.bm : 0.0;
+  clocks += (double)tail_rounds * ((part > write ? part : write) + kUnitClocks);
+  if (max_split > 1) clocks += write + kJoinColumn * c.bm * max_split + kJoinClocks + 116e-6 * (double)slots * c.cg * c.bm * 512.0;
+  clocks += epi + kLaunchClocks;
   pl.units = (int)units;
   pl.slots = (int)slots;
   pl.clusters = units < clusters ? (int)units : clusters;
@@ -243,15 +266,15 @@ class Packer {
     if (n_ == 0) return true;
     PackOps ops;
     memset(&ops, 0, sizeof(ops));
-    int64_t gx = 0, gy = 0;
+    int64_t most = 0;  // vectors of the largest matrix
     for (int i = 0; i < n_; ++i) {
       const Matrix& m = src_[i];
       ops.op[i] = PackOp{static_cast<const uint16_t*>(m.ptr), m.ld, (int)m.rows, (int)m.cols,
                          reinterpret_cast<uint16_t*>(buf + at_[i]), padded(m.cols)};
-      if ((m.cols + 255) / 256 > gx) gx = (m.cols + 255) / 256;
-      if (m.rows > gy) gy = m.rows;
+      if ((m.cols + 7) / 8 * m.rows > most) most = (m.cols + 7) / 8 * m.rows;
     }
-    if (!lm::launch(hgemm_pack_kernel, dim3((unsigned)gx, capped(gy), (unsigned)n_), dim3(256), 0, 1, stream, ops)) return false;
+    const int64_t blocks = (most + 255) / 256;
+    if (!lm::launch(hgemm_pack_kernel, dim3((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), (unsigned)n_), dim3(256), 0, 1, stream, ops)) return false;
     for (int i = 0; i < nu_; ++i) *users_[i] = Matrix{buf + at_[of_[i]], users_[i]->rows, users_[i]->cols, padded(users_[i]->cols)};
     return true;
   }
@@ -286,7 +309,16 @@ struct Product {
   Size size() const {
     int64_t kb = 0;
     for (int i = 0; i < nseg; ++i) kb += (K[i] + TK - 1) / TK;
-    return Size{N, M, (int)kb};
+    int count = R ? 1 : 0, unaligned = 0;
+    const auto add = [&](const void* p, int64_t ld) {
+      if (!p) return;
+      ++count;
+      if (!addressable(Matrix{p, M, N, ld})) ++unaligned;
+    };
+    add(D, ldd);
+    add(Z, ldz);
+    add(U, ldu);
+    return Size{N, M, (int)kb, epilogue_clocks(act, count, unaligned, R && !addressable(Matrix{R, M, N, ldr}))};
   }
 };
 
@@ -323,7 +355,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     const Plan::Part& q = pl.part[i];
     const int np = gated ? 2 : s.nseg, nq = s.nseg;
     for (int j = 0; j < np; ++j)
-      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated ? 64 : 128)) return DGEMM_ERR_CUDA;
+      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated || qrows <= 64 ? 64 : 128)) return DGEMM_ERR_CUDA;
     for (int j = 0; j < nq; ++j)
       if (!make_map(&d.q[j], type, s.q[j], s.q_mn ? 64 : qrows)) return DGEMM_ERR_CUDA;
     d.N = (int)s.N;
@@ -839,7 +871,7 @@ int hgemm_last_device_status(void* stream) {
 int hgemm_plan(int64_t M, int64_t N, int64_t K, int gated, int sm_count, int* out) {
   if (!out) return DGEMM_ERR_NULL;
   if (M <= 0 || N <= 0 || K <= 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim || sm_count < 0 || sm_count == 1) return DGEMM_ERR_BAD_DIM;
-  const Size sz{N, M, (int)((K + TK - 1) / TK)};
+  const Size sz{N, M, (int)((K + TK - 1) / TK), epilogue_clocks(HGEMM_ACT_NONE, 1, 0, false)};
   Plan pl;
   if (!make_plan(&sz, 1, gated != 0, sm_count ? sm_count : 148, &pl)) return DGEMM_ERR_BAD_DIM;
   const Config& c = kConfigs[pl.config];

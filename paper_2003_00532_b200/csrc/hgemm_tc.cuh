@@ -358,12 +358,29 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float* v) {
   ptx5::tmem_ld_16x256b<CH / 8>(addr + (16u << 16), v + CH / 2);
 }
 
-// The sum of a cut tile's parts, in order, for one thread's CH values.
+// The sum of a cut tile's parts, in order, for one thread's CH values; the loads of four parts are in flight.
 template <int CH>
 __device__ __forceinline__ void add_parts(const float4* ws, int split, long long stride, float* v) {
 #pragma unroll
   for (int j = 0; j < CH; ++j) v[j] = 0.f;
-  for (int s = 0; s < split; ++s)
+  int s = 0;
+  for (; s + 4 <= split; s += 4) {
+    float4 x[4][CH / 4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < CH / 4; ++j) x[q][j] = __ldcg(ws + (s + q) * stride + j * 32);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < CH / 4; ++j) {
+        v[4 * j] += x[q][j].x;
+        v[4 * j + 1] += x[q][j].y;
+        v[4 * j + 2] += x[q][j].z;
+        v[4 * j + 3] += x[q][j].w;
+      }
+  }
+  for (; s < split; ++s)
 #pragma unroll
     for (int j = 0; j < CH / 4; ++j) {
       const float4 x = __ldcg(ws + s * stride + j * 32);
@@ -552,8 +569,10 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
   ptx5::launch_dependents();
   grid_dependency_wait();
   if ((warp == 0 || warp == 3) && lane == 0) {
-    // ---- stages: warp 0 copies the P boxes, warp 3 the Q boxes; zero fill outside the matrices ----
+    // ---- stages: warp 0 copies the P boxes, warp 3 the Q boxes and, where those are small, the second half of P (one
+    // stream of copies brings about 35 bytes per clock); zero fill outside the matrices ----
     const bool is_p = warp == 0;
+    constexpr bool SHARE_P = !GATED && C::QROWS <= 64;
     uint32_t it = 0;
     bool ok = !p.drop;
     for (int u = cluster; u < p.units && ok; u += clusters) {
@@ -561,12 +580,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       const Problem& pr = p.prob[w.prob];
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
-      const bool mn = is_p ? pr.p_mn : pr.q_mn;
-      // first outer index of this CTA's rows of the operand
-      const int o0 = is_p ? tn * C::NT + rank * (GATED ? 64 : 128) : tm * BM + rank * C::QROWS;
-      const int boxes = is_p ? (GATED || mn ? 2 : 1) : (mn ? C::QBOXES : 1);
-      const int o_step = is_p && GATED ? 0 : 64;
-      const CUtensorMap* maps = is_p ? pr.p : pr.q;
+      const int n0 = tn * C::NT + rank * (GATED ? 64 : 128), m0 = tm * BM + rank * C::QROWS;
       const uint32_t bytes = CG * (C::P_BYTES + (pr.q_mn ? C::QBOXES * BOX_BYTES : C::QROWS * 128));
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
         const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u;
@@ -578,11 +592,24 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         if (is_p && rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, bytes);
         const int seg = kb >= pr.kb_seg0 ? 1 : 0;
         const int k0 = (kb - (seg ? pr.kb_seg0 : 0)) * TK;
-        const uint32_t dst = base + s * C::STAGE_BYTES + (is_p ? 0 : C::P_BYTES);
-        for (int i = 0; i < boxes; ++i) {
-          const CUtensorMap* map = maps + (GATED ? (is_p ? i : 0) : seg);
-          const int o = o0 + i * o_step;
-          ptx5::tma_load_2d<CG>(dst + i * BOX_BYTES, map, mn ? o : k0, mn ? k0 : o, fb);
+        const uint32_t dst = base + s * C::STAGE_BYTES;
+        const auto load_p = [&](int i) {
+          const CUtensorMap* map = &pr.p[GATED ? i : seg];
+          const int n = n0 + (GATED ? 0 : 64 * i);
+          ptx5::tma_load_2d<CG>(dst + i * BOX_BYTES, map, pr.p_mn ? n : k0, pr.p_mn ? k0 : n, fb);
+        };
+        if (is_p) {
+          load_p(0);
+          if (GATED || (!SHARE_P && pr.p_mn)) load_p(1);
+        } else {
+          if (SHARE_P) load_p(1);
+          const CUtensorMap* map = &pr.q[GATED ? 0 : seg];
+          if (pr.q_mn) {
+#pragma unroll
+            for (int i = 0; i < C::QBOXES; ++i) ptx5::tma_load_2d<CG>(dst + C::P_BYTES + i * BOX_BYTES, map, m0 + 64 * i, k0, fb);
+          } else {
+            ptx5::tma_load_2d<CG>(dst + C::P_BYTES, map, k0, m0, fb);
+          }
         }
       }
     }
