@@ -111,8 +111,9 @@ DGEMM_API int hgemm_last_device_status(void *stream);
 /*
  * What the library would do with one product (or, `gated` != 0, gated projection) of op(A) M x K and
  * op(B) K x N, without touching a device. `sm_count`: 0 = 148. Writes 8 ints to `out`: CTAs per tile
- * (1, or 2 for a pair), tile rows, tile columns, clusters launched, k-blocks (64 values each), tiles
- * run whole, parts each remaining tile's k-blocks are cut into, k-blocks per part.
+ * (1, or 2 for a pair), tile rows, tile columns, clusters launched, k-blocks (64 values each), whole
+ * rounds of tiles over the clusters, tiles left over, and the k-blocks of those that each cluster
+ * takes as one span (0: they run whole, too).
  */
 DGEMM_API int hgemm_plan(int64_t M, int64_t N, int64_t K, int gated, int sm_count, int *out);
 

@@ -284,7 +284,7 @@ def _checked(rc: int, where: str) -> int:
     return rc
 
 
-HGEMM_PLAN_FIELDS = ("ctas_per_tile", "tile_rows", "tile_cols", "clusters", "kblocks", "dp_tiles", "split", "kblocks_per_part")
+HGEMM_PLAN_FIELDS = ("ctas_per_tile", "tile_rows", "tile_cols", "clusters", "kblocks", "rounds", "rest", "span")
 
 
 def hgemm_plan(M: int, N: int, K: int, gated: bool = False, sm_count: int = 0) -> dict:

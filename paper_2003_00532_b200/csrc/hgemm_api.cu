@@ -57,12 +57,13 @@ double epilogue_clocks(int act, int matrices, int unaligned_out, bool unaligned_
 struct Plan {
   int config = 0;
   int clusters = 0;
-  int units = 0;
   int nt = 0;
   struct Part {
-    int tiles_n, tiles_m, dp_tiles, split, kb_per_split, units, slot0, counter0;
+    int tiles_n, tiles_m, rounds, rest, span_len;
   } part[MAX_PROBLEMS];
-  int slots = 0;  // workspace slots of bm * 128 * cg binary32 values
+  int rounds = 0, rest = 0;
+  int span = 0, span_total = 0;  // k-blocks per cluster and in all of the tiles left over; span 0: run whole
+  size_t workspace = 0;          // bytes
 };
 
 // The model of a launch's time in clocks. Its constants were fitted to 20 shapes in every configuration and cut that
@@ -83,139 +84,122 @@ double step_clocks(const Config& c) {
   return t > kKBlockClocks ? t : kKBlockClocks;
 }
 
-// Decomposes the problems (longest contraction first) into units for one configuration: whole waves of
-// tiles run whole; the tiles of the last partial wave are cut into parts of at most `len` k-blocks.
-double decompose(const Size* sz, int n, bool gated, int sms, int config, int len, Plan* out) {
+// Decomposes the problems (longest contraction first) for one configuration and returns the estimated clocks: whole
+// rounds of tiles, then the tiles left over, whole or as spans of `span` k-blocks per cluster. -1: too many tiles.
+struct Layout {
+  int64_t tiles[MAX_PROBLEMS], rounds[MAX_PROBLEMS], rest[MAX_PROBLEMS];
+  int64_t left, left_kblocks;
+  int clusters, nt, longest;  // longest: k-blocks of the longest tile left over
+  double step, epi, fixed;    // fixed: all but the tiles left over
+};
+bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out) {
   const Config& c = kConfigs[config];
-  const int clusters = sms / c.cg;
-  const int nt = (gated ? 64 : 128) * c.cg;
-  Plan pl;
-  pl.config = config;
-  pl.nt = nt;
-  int64_t tiles[MAX_PROBLEMS], total = 0;
-  for (int i = 0; i < n; ++i) {
-    const int64_t tn = (sz[i].N + nt - 1) / nt, tm = (sz[i].M + c.bm - 1) / c.bm;
-    tiles[i] = tn * tm;
-    if (tiles[i] > INT32_MAX / 64) return -1.0;
-    pl.part[i].tiles_n = (int)tn;
-    pl.part[i].tiles_m = (int)tm;
-    total += tiles[i];
-  }
-  if (total > INT32_MAX / 64) return -1.0;
-  int64_t tail = total % clusters;
-  double epi = 0.0;
+  Layout l;
+  l.clusters = sms / c.cg;
+  l.nt = (gated ? 64 : 128) * c.cg;
+  l.step = step_clocks(c);
+  l.epi = 0.0;
+  l.left = l.left_kblocks = 0;
+  l.longest = 0;
   for (int i = 0; i < n; ++i)
-    if (sz[i].epilogue * c.bm > epi) epi = sz[i].epilogue * c.bm;
-  // whole waves: each as long as its longest tile, or as an epilogue (which runs beside the next tile's MMAs)
-  const double step = step_clocks(c);
+    if (sz[i].epilogue * c.bm > l.epi) l.epi = sz[i].epilogue * c.bm;
+  l.fixed = kLaunchClocks + l.epi;
+  for (int i = 0; i < n; ++i) {
+    l.tiles[i] = ((sz[i].N + l.nt - 1) / l.nt) * ((sz[i].M + c.bm - 1) / c.bm);
+    if (l.tiles[i] > INT32_MAX / 64) return false;
+    l.rounds[i] = l.tiles[i] / l.clusters;
+    l.rest[i] = l.tiles[i] % l.clusters;
+    l.left += l.rest[i];
+    l.left_kblocks += l.rest[i] * sz[i].kblocks;
+    if (l.rest[i] > 0 && sz[i].kblocks > l.longest) l.longest = sz[i].kblocks;
+    // a round is as long as a tile's MMAs, or as an epilogue (which runs beside the next tile's MMAs)
+    const double mma = sz[i].kblocks * l.step;
+    l.fixed += (double)l.rounds[i] * ((mma > l.epi ? mma : l.epi) + kUnitClocks);
+  }
+  *out = l;
+  return true;
+}
+// The tiles left over, run whole: rounds over the clusters, each as long as its longest tile.
+double whole_clocks(const Layout& l, const Size* sz, int n) {
   double clocks = 0.0;
-  {
-    int i = 0;
-    int64_t left = total - tail, in_problem = tiles[0];
-    while (left > 0) {
-      while (in_problem == 0) in_problem = tiles[++i];
-      // waves that start inside problem i
-      const int64_t waves = (in_problem < left ? in_problem : left) + clusters - 1;
-      int64_t w = waves / clusters;
-      if (w * clusters > left) w = left / clusters;
-      clocks += (double)w * ((sz[i].kblocks * step > epi ? sz[i].kblocks * step : epi) + kUnitClocks);
-      int64_t used = w * clusters;
-      left -= used;
-      while (used > 0) {
-        const int64_t d = used < in_problem ? used : in_problem;
-        in_problem -= d;
-        used -= d;
-        if (in_problem == 0 && i + 1 < n) in_problem = tiles[++i];
-        else if (in_problem == 0) break;
-      }
-    }
+  int64_t at = 0;
+  int i = 0;
+  int64_t end = l.rest[0];
+  while (at < l.left) {
+    while (at >= end) end += l.rest[++i];
+    const double mma = sz[i].kblocks * l.step;
+    clocks += (mma > l.epi || at + l.clusters >= l.left ? mma : l.epi) + kUnitClocks;
+    at += l.clusters;
   }
-  int64_t units = 0, slots = 0, tail_units = 0;
-  int counters = 0, longest = 0, max_split = 1;
-  for (int i = n - 1; i >= 0; --i) {
-    const int64_t t = tail < tiles[i] ? tail : tiles[i];
-    tail -= t;
-    Plan::Part& q = pl.part[i];
-    int kps = sz[i].kblocks < len ? sz[i].kblocks : len;
-    int split = (sz[i].kblocks + kps - 1) / kps;
-    kps = (sz[i].kblocks + split - 1) / split;
-    split = (sz[i].kblocks + kps - 1) / kps;
-    if (split == 1 || t == 0) {
-      q.dp_tiles = (int)tiles[i];
-      q.split = 1;
-      q.kb_per_split = sz[i].kblocks;
-      if (t > 0 && sz[i].kblocks > longest) longest = sz[i].kblocks;
-      tail_units += t;
-    } else {
-      q.dp_tiles = (int)(tiles[i] - t);
-      q.split = split;
-      q.kb_per_split = kps;
-      if (kps > longest) longest = kps;
-      if (split > max_split) max_split = split;
-      tail_units += t * split;
-      q.slot0 = (int)slots;
-      q.counter0 = counters;
-      slots += t * split;
-      counters += (int)t;
-    }
-    q.units = (int)(q.dp_tiles + (tiles[i] - q.dp_tiles) * q.split);
-    units += q.units;
-    if (q.split == 1) q.slot0 = q.counter0 = 0;
-  }
-  if (counters * c.cg > lm::kCounters) return -1.0;
-  const int64_t tail_rounds = (tail_units + clusters - 1) / clusters;
-  const double part = longest * step, write = max_split > 1 ? kPartColumn * c.bm : 0.0;
-  clocks += (double)tail_rounds * ((part > write ? part : write) + kUnitClocks);
-  if (max_split > 1) clocks += write + kJoinColumn * c.bm * max_split + kJoinClocks + 116e-6 * (double)slots * c.cg * c.bm * 512.0;
-  clocks += epi + kLaunchClocks;
-  pl.units = (int)units;
-  pl.slots = (int)slots;
-  pl.clusters = units < clusters ? (int)units : clusters;
-  *out = pl;
   return clocks;
 }
+// ... or in spans. `even`: every tile is cut alike, each part by a cluster of its own; otherwise a span holds the end of
+// one tile, whole ones and the beginning of another.
+double span_clocks(const Layout& l, const Config& c, int64_t span, bool even) {
+  const double write = kPartColumn * c.bm, mma = span * l.step;
+  const int64_t parts = (l.longest + span - 1) / span + (even ? 0 : 1);
+  const int64_t pieces = even ? 1 : 1 + (span * l.left + l.left_kblocks - 1) / l.left_kblocks;
+  return (mma > write ? mma : write) + pieces * kUnitClocks + write + kJoinColumn * c.bm * parts + kJoinClocks;
+}
 
-// The configuration and cut with the smallest estimate. For one problem only the cuts around "as many parts
-// as there are idle clusters" can win; several problems of different lengths try a fixed list.
+// The configuration and cut with the smallest estimate.
 bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
-  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
   double best_clocks = -1.0;
   int64_t max_m = 0;
-  int kmax = 1;
-  for (int i = 0; i < n; ++i) {
+  for (int i = 0; i < n; ++i)
     if (sz[i].M > max_m) max_m = sz[i].M;
-    if (sz[i].kblocks > kmax) kmax = sz[i].kblocks;
-  }
+  Layout pick;
+  int config = -1;
+  int64_t pick_span = 0;
+  bool pick_even = false;
   for (int c = 0; c < kNumConfigs; ++c) {
     if (c > 0 && kConfigs[c - 1].cg == 1 && kConfigs[c - 1].bm >= max_m) break;  // only more padding
-    int cuts[sizeof(kCuts) / sizeof(kCuts[0])], ncuts = 0;
-    if (n == 1) {
-      const int nt = (gated ? 64 : 128) * kConfigs[c].cg, clusters = sms / kConfigs[c].cg;
-      const int64_t rest = ((sz[0].N + nt - 1) / nt) * ((sz[0].M + kConfigs[c].bm - 1) / kConfigs[c].bm) % clusters;
-      cuts[ncuts++] = 1;
-      if (rest > 0) {
-        const int fit = (int)(clusters / rest);
-        if (fit > 1) cuts[ncuts++] = fit;
-        cuts[ncuts++] = fit + 1;
-        cuts[ncuts++] = 2 * fit + 1;
-      }
-    } else {
-      for (int cut : kCuts) cuts[ncuts++] = cut;
+    Layout l;
+    if (!lay_out(sz, n, gated, sms, c, &l)) continue;
+    const auto consider = [&](double t, int64_t span, bool even) {
+      if (best_clocks >= 0.0 && t >= best_clocks) return;
+      best_clocks = t;
+      pick = l;
+      config = c;
+      pick_span = span;
+      pick_even = even;
+    };
+    consider(l.fixed + (l.left > 0 ? whole_clocks(l, sz, n) : 0.0), 0, false);
+    if (l.left == 0 || l.left * kConfigs[c].cg > lm::kCounters || l.left_kblocks > INT32_MAX / 2) continue;
+    // equal spans over all clusters, or over half or a quarter of them where joining many parts costs more
+    for (int divide = 1; divide <= 4; divide *= 2) {
+      int64_t span = (l.left_kblocks * divide + l.clusters - 1) / l.clusters;
+      if (span >= l.longest) break;
+      consider(l.fixed + span_clocks(l, kConfigs[c], span, false), span, false);
     }
-    int last = 0;
-    for (int j = 0; j < ncuts; ++j) {
-      const int cut = cuts[j] < kmax ? cuts[j] : kmax;
-      if (cut == last) break;
-      last = cut;
-      Plan pl;
-      const double t = decompose(sz, n, gated, sms, c, (kmax + cut - 1) / cut, &pl);
-      if (t >= 0.0 && (best_clocks < 0.0 || t < best_clocks)) {
-        best_clocks = t;
-        *best = pl;
-      }
+    const int64_t cut = l.clusters / l.left;
+    if (n == 1 && cut > 1 && l.longest > 1) {
+      const int64_t span = (l.longest + cut - 1) / cut;
+      if (span < l.longest) consider(l.fixed + span_clocks(l, kConfigs[c], span, true), span, true);
     }
   }
-  return best_clocks >= 0.0;
+  if (config < 0) return false;
+  const Config& c = kConfigs[config];
+  Plan pl;
+  pl.config = config;
+  pl.nt = pick.nt;
+  for (int i = 0; i < n; ++i) {
+    Plan::Part& q = pl.part[i];
+    q.tiles_n = (int)((sz[i].N + pick.nt - 1) / pick.nt);
+    q.tiles_m = (int)((sz[i].M + c.bm - 1) / c.bm);
+    q.rounds = (int)pick.rounds[i];
+    q.rest = (int)pick.rest[i];
+    q.span_len = (int)(pick_even ? (sz[i].kblocks + pick_span - 1) / pick_span * pick_span : sz[i].kblocks);
+    pl.rounds += q.rounds;
+    pl.rest += q.rest;
+    if (pick_span > 0) pl.span_total += q.rest * q.span_len;
+  }
+  pl.span = (int)pick_span;
+  const int64_t used = pick_span > 0 ? (pl.span_total + pick_span - 1) / pick_span : pick.left;
+  pl.clusters = pl.rounds > 0 || used > pick.clusters ? pick.clusters : (int)used;
+  if (pick_span > 0) pl.workspace = (size_t)2 * pl.clusters * c.cg * c.bm * 128 * sizeof(float);
+  *best = pl;
+  return true;
 }
 
 // ---- operands -----------------------------------------------------------------------------------------
@@ -322,11 +306,6 @@ struct Product {
   }
 };
 
-size_t workspace_bytes(const Plan& pl) {
-  const Config& c = kConfigs[pl.config];
-  return (size_t)pl.slots * c.cg * c.bm * 128 * sizeof(float);
-}
-
 // Longest contraction first (the schedule assumes it), stable.
 void order(Product** pr, int n) {
   for (int i = 1; i < n; ++i)
@@ -366,12 +345,9 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.kb_seg0 = (int)((s.K[0] + TK - 1) / TK);
     d.p_mn = s.p_mn;
     d.q_mn = s.q_mn;
-    d.dp_tiles = q.dp_tiles;
-    d.split = q.split;
-    d.kb_per_split = q.kb_per_split;
-    d.units = q.units;
-    d.slot0 = q.slot0;
-    d.counter0 = q.counter0;
+    d.rounds = q.rounds;
+    d.rest = q.rest;
+    d.span_len = q.span_len;
     d.vec = (addressable(Matrix{s.D, s.M, s.N, s.ldd}) ? VEC_D : 0) | (addressable(Matrix{s.Z, s.M, s.N, s.ldz}) ? VEC_Z : 0) |
             (addressable(Matrix{s.U, s.M, s.N, s.ldu}) ? VEC_U : 0) | (addressable(Matrix{s.R, s.M, s.N, s.ldr}) ? VEC_R : 0);
     d.bias = s.bias;
@@ -385,7 +361,10 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.ldu = s.ldu;
   }
   p.nprob = n;
-  p.units = pl.units;
+  p.rounds = pl.rounds;
+  p.rest = pl.rest;
+  p.span = pl.span;
+  p.span_total = pl.span_total;
   p.ws = ws;
   p.counters = counters;
   const int drop = g_drop_limit_us.load();
@@ -463,8 +442,8 @@ int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
     if (!buf || !pack.launch(buf, stream)) return DGEMM_ERR_CUDA;
   }
   float* ws = nullptr;
-  if (pl.slots > 0) {
-    ws = static_cast<float*>(hold.workspace(workspace_bytes(pl)));
+  if (pl.workspace > 0) {
+    ws = static_cast<float*>(hold.workspace(pl.workspace));
     if (!ws) return DGEMM_ERR_CUDA;
   }
   return run_products(type, gated, &prod, 1, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, stream);
@@ -665,7 +644,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     ap.lddz = lddz;
     ap.act = act;
   }
-  size_t ws_bytes = n > 0 ? workspace_bytes(pl) : 0;
+  size_t ws_bytes = n > 0 ? pl.workspace : 0;
   if (dbias && chunks > 1 && (size_t)chunks * N * 4 > ws_bytes) ws_bytes = (size_t)chunks * N * 4;
   float* ws = nullptr;
   if (ws_bytes > 0 && !(ws = static_cast<float*>(hold.workspace(ws_bytes)))) return DGEMM_ERR_CUDA;
@@ -817,7 +796,7 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes()));
   if (!buf) return DGEMM_ERR_CUDA;
   float* ws = nullptr;
-  if (pl.slots > 0 && !(ws = static_cast<float*>(hold.workspace(workspace_bytes(pl))))) return DGEMM_ERR_CUDA;
+  if (pl.workspace > 0 && !(ws = static_cast<float*>(hold.workspace(pl.workspace)))) return DGEMM_ERR_CUDA;
   GatedBwdParams gp;
   memset(&gp, 0, sizeof(gp));
   gp.M = (int)M;
@@ -876,7 +855,7 @@ int hgemm_plan(int64_t M, int64_t N, int64_t K, int gated, int sm_count, int* ou
   if (!make_plan(&sz, 1, gated != 0, sm_count ? sm_count : 148, &pl)) return DGEMM_ERR_BAD_DIM;
   const Config& c = kConfigs[pl.config];
   const Plan::Part& q = pl.part[0];
-  const int v[8] = {c.cg, c.bm, pl.nt, pl.clusters, sz.kblocks, q.dp_tiles, q.split, q.kb_per_split};
+  const int v[8] = {c.cg, c.bm, pl.nt, pl.clusters, sz.kblocks, q.rounds, q.rest, pl.span};
   memcpy(out, v, sizeof(v));
   return DGEMM_OK;
 }

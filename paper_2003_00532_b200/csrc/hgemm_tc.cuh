@@ -18,10 +18,12 @@
 // bytes, 128-byte swizzle, 8 KB) and the MMA descriptors say which of the two a box holds, so all four
 // transpositions run the same code without a transposing pass.
 //
-// Work. One launch covers up to three problems (the gradients of one operator), each cut into tiles;
-// tiles beyond the whole waves may have their k-blocks cut into parts, whose binary32 sums go to
-// a workspace; the CTA that finishes the last part of a tile (a counter per tile) adds all parts in
-// order and runs the epilogue: one launch, no CTA waits for another, same bits every time.
+// Work. One launch covers up to three problems (the gradients of one operator). Of each problem's tiles as many as make
+// whole rounds over the clusters run whole. The tiles left over, of all problems together, are either dealt out whole
+// as well, or their k-blocks are laid end to end and cut into equal spans, one per cluster: then a tile may be
+// computed in parts, whose binary32 sums go to a workspace, and the CTA that finishes the last part of a tile (a
+// counter per tile) adds all parts in order and runs the epilogue: one launch, no CTA waits for another, same bits
+// every time.
 //
 // The activation is a template argument of the whole kernel: with a switch over the five of them in it, the
 // registers of all shared one allocation and the epilogue without activation spilled (4096 x 9472 x 256: 50 us,
@@ -81,10 +83,9 @@ struct alignas(64) Problem {
   int tiles_n, tiles_m;
   int kblocks, kb_seg0;    // k-blocks in all, and of the first segment
   int p_mn, q_mn;          // operand stored MN-major
-  int dp_tiles;            // tiles run whole; the others are cut into `split` parts of kb_per_split k-blocks
-  int split, kb_per_split;
-  int units;               // dp_tiles + (tiles - dp_tiles) * split
-  int slot0, counter0;     // first workspace slot and tile counter of the cut tiles
+  int rounds;              // tiles run whole in rounds over all clusters; the first `rounds` x clusters tiles
+  int rest;                // tiles left over
+  int span_len;            // positions that such a tile takes among the spans: its k-blocks, or a multiple of the span
   int vec;                 // which of D, Z, U, R have 16-byte aligned rows (VEC_*)
   const void* bias;
   const void* R;
@@ -97,36 +98,78 @@ struct alignas(64) Problem {
 struct Params {
   Problem prob[MAX_PROBLEMS];
   int nprob;
-  int units;
-  float* ws;
-  int* counters;
+  int rounds;              // of all problems
+  int span;                // k-blocks per cluster of the tiles left over, 0: they run whole
+  int span_total;          // positions of all tiles left over
+  int rest;                // tiles left over
+  float* ws;               // two slots of CG x BM x 128 sums per cluster
+  int* counters;           // one per tile left over and CTA of a pair; zero between launches
   unsigned long long wait_limit_ns;
   int* status;
   int drop;  // testing aid: the producers skip their copies
 };
 
+// One unit of work: k-blocks kb0 .. kb1 of a tile. For a part of a cut tile: its slot in the workspace, the tile's index
+// among those left over, the clusters that share it and the first one's slot.
 struct Work {
-  int prob, tile, kb0, kb1, part;  // part: -1 = whole tile
+  int prob, tile, kb0, kb1;
+  int slot;  // -1: the whole tile
+  int left, parts, first_slot, next_slot;
 };
 
-__device__ __forceinline__ Work get_work(const Params& p, int u) {
-  Work w;
-  w.prob = 0;
-  while (w.prob + 1 < p.nprob && u >= p.prob[w.prob].units) u -= p.prob[w.prob++].units;
-  const Problem& pr = p.prob[w.prob];
-  if (u < pr.dp_tiles) {
-    w.tile = u;
+// Unit number j of `cluster`; false after its last one.
+__device__ __forceinline__ bool get_work(const Params& p, int cluster, int clusters, int j, Work& w) {
+  w.slot = -1;
+  if (j < p.rounds) {
+    w.prob = 0;
+    while (j >= p.prob[w.prob].rounds) j -= p.prob[w.prob++].rounds;
+    w.tile = j * clusters + cluster;
     w.kb0 = 0;
-    w.kb1 = pr.kblocks;
-    w.part = -1;
-  } else {
-    const int v = u - pr.dp_tiles;
-    w.tile = pr.dp_tiles + v / pr.split;
-    w.part = v % pr.split;
-    w.kb0 = w.part * pr.kb_per_split;
-    w.kb1 = min(pr.kblocks, w.kb0 + pr.kb_per_split);
+    w.kb1 = p.prob[w.prob].kblocks;
+    return true;
   }
-  return w;
+  j -= p.rounds;
+  if (p.span == 0) {
+    int left = j * clusters + cluster;
+    if (left >= p.rest) return false;
+    w.prob = 0;
+    while (left >= p.prob[w.prob].rest) left -= p.prob[w.prob++].rest;
+    w.tile = p.prob[w.prob].rounds * clusters + left;
+    w.kb0 = 0;
+    w.kb1 = p.prob[w.prob].kblocks;
+    return true;
+  }
+  // the span's pieces: up to the end of a tile each
+  int pos = cluster * p.span;
+  const int end = min(pos + p.span, p.span_total);
+  for (;; --j) {
+    if (pos >= end) return false;
+    int base = 0, left = 0;  // position and index of the problem's first tile left over
+    w.prob = 0;
+    while (pos >= base + p.prob[w.prob].rest * p.prob[w.prob].span_len) {
+      base += p.prob[w.prob].rest * p.prob[w.prob].span_len;
+      left += p.prob[w.prob++].rest;
+    }
+    const int kb = p.prob[w.prob].kblocks, len = p.prob[w.prob].span_len, t = (pos - base) / len;
+    const int lo = base + t * len, hi = lo + len;
+    const int stop = min(hi, end);
+    if (j == 0) {
+      w.tile = p.prob[w.prob].rounds * clusters + t;
+      w.kb0 = pos - lo;
+      w.kb1 = min(stop - lo, kb);
+      if (w.kb1 - w.kb0 < kb) {
+        const int c0 = lo / p.span;
+        w.left = left + t;
+        w.parts = (hi - 1) / p.span - c0 + 1;
+        // a cluster whose span begins inside the tile uses its first slot, the one whose span runs into it the second
+        w.first_slot = 2 * c0 + (c0 * p.span >= lo ? 0 : 1);
+        w.next_slot = 2 * c0 + 2;
+        w.slot = cluster == c0 ? w.first_slot : 2 * cluster;
+      }
+      return true;
+    }
+    pos = stop;
+  }
 }
 
 // Grouped raster: 8 tile rows of lanes (n) at a time, so that the tiles in flight share operands in L2.
@@ -358,13 +401,14 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float* v) {
   ptx5::tmem_ld_16x256b<CH / 8>(addr + (16u << 16), v + CH / 2);
 }
 
-// The sum of a cut tile's parts, in order, for one thread's CH values; the loads of four parts are in flight.
+// The sum of a cut tile's parts, in order, for one thread's CH values: the first at `first`, the others `stride` apart
+// from `ws`; the loads of four parts are in flight.
 template <int CH>
-__device__ __forceinline__ void add_parts(const float4* ws, int split, long long stride, float* v) {
+__device__ __forceinline__ void add_parts(const float4* first, const float4* ws, int others, long long stride, float* v) {
 #pragma unroll
-  for (int j = 0; j < CH; ++j) v[j] = 0.f;
+  for (int j = 0; j < CH / 4; ++j) *reinterpret_cast<float4*>(v + 4 * j) = __ldcg(first + j * 32);
   int s = 0;
-  for (; s + 4 <= split; s += 4) {
+  for (; s + 4 <= others; s += 4) {
     float4 x[4][CH / 4];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -380,7 +424,7 @@ __device__ __forceinline__ void add_parts(const float4* ws, int split, long long
         v[4 * j + 3] += x[q][j].w;
       }
   }
-  for (; s < split; ++s)
+  for (; s < others; ++s)
 #pragma unroll
     for (int j = 0; j < CH / 4; ++j) {
       const float4 x = __ldcg(ws + s * stride + j * 32);
@@ -411,11 +455,10 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
   using namespace dgemm::ptx;
   constexpr int CG = C::CG, BM = C::BM, CH = C::CH, GROUPS = EPI_WARPS / 4;
   constexpr bool GATED = C::GATED;
-  // a cut tile's sums in the workspace: [part][CTA][quarter][chunk][CH / 4][lane] of float4
-  const int rel = w.part < 0 ? 0 : w.tile - pr.dp_tiles;
-  constexpr long long WS_TILE = (long long)CG * BM * 32;  // float4 per part
+  // a part's sums in the workspace: [slot][CTA][quarter][chunk][CH / 4][lane] of float4
+  constexpr long long WS_SLOT = (long long)CG * BM * 32;  // float4 per slot
   constexpr int WS_CHUNK = CH / 4 * 32;                   // float4 per quarter and chunk
-  float4* ws_tile = reinterpret_cast<float4*>(p.ws) + ((long long)(pr.slot0 + rel * pr.split) * CG + ew.rank) * (BM * 32);
+  float4* const ws_cta = reinterpret_cast<float4*>(p.ws) + ew.rank * (BM * 32) + ew.lane;
   // the accumulator may be overwritten: called once this warp's last load of it has been waited for
   bool released = false;
   const auto release = [&]() {
@@ -427,7 +470,7 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
     }
     released = true;
   };
-  if (w.part < 0) {
+  if (w.slot < 0) {
     if (!GATED) {
       for (int c = ew.group; c * CH < rows; c += GROUPS) {
         float v[CH];
@@ -467,7 +510,7 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
       }
     }
   } else {
-    float4* ws = ws_tile + w.part * WS_TILE + (ew.quad * (BM / CH)) * WS_CHUNK + ew.lane;
+    float4* ws = ws_cta + w.slot * WS_SLOT + (ew.quad * (BM / CH)) * WS_CHUNK;
     for (int c = ew.group; c * CH < rows; c += GROUPS) {
       float v[CH];
       tmem_load<CH>(ew.acc + c * CH, v);
@@ -477,32 +520,35 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
     }
   }
   if (!released) release();
-  if (w.part >= 0) {
-    int* counter = p.counters + (pr.counter0 + rel) * CG + ew.rank;
+  if (w.slot >= 0) {
+    int* counter = p.counters + w.left * CG + ew.rank;
     __threadfence();
     named_barrier_sync(15, EPI_WARPS * 32);
     if (ew.e == 0 && ew.lane == 0) {
       const int old = atomicAdd(counter, 1);
-      sts32(ew.last_flag, old == pr.split - 1);
-      if (old == pr.split - 1) *counter = 0;  // ready for the next launch
+      sts32(ew.last_flag, old == w.parts - 1);
+      if (old == w.parts - 1) *counter = 0;  // ready for the next launch
     }
     named_barrier_sync(15, EPI_WARPS * 32);
     if (lds32(ew.last_flag)) {
       __threadfence();
       if (!GATED) {
-        const float4* ws = ws_tile + (ew.quad * (BM / CH)) * WS_CHUNK + ew.lane;
+        const float4* first = ws_cta + w.first_slot * WS_SLOT + (ew.quad * (BM / CH)) * WS_CHUNK;
+        const float4* next = ws_cta + w.next_slot * WS_SLOT + (ew.quad * (BM / CH)) * WS_CHUNK;
         for (int c = ew.group; c * CH < rows; c += GROUPS) {
           if (ep.has_r && n_in) ep.pt.fetch(raw, ep.r, c * CH);
           float v[CH];
-          add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, v);
+          add_parts<CH>(first + c * WS_CHUNK, next + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, v);
           if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw);
         }
       } else {
-        const float4* ws = ws_tile + ((ew.quad & 1) * (BM / CH)) * WS_CHUNK + ew.lane;
+        const float4* first = ws_cta + w.first_slot * WS_SLOT + ((ew.quad & 1) * (BM / CH)) * WS_CHUNK;
+        const float4* next = ws_cta + w.next_slot * WS_SLOT + ((ew.quad & 1) * (BM / CH)) * WS_CHUNK;
+        constexpr int UP = 2 * (BM / CH) * WS_CHUNK;  // the up projection's quarters
         for (int c = 2 * ew.group + (ew.quad >> 1); c * CH < rows; c += 2 * GROUPS) {
           float g[CH], uu[CH];
-          add_parts<CH>(ws + c * WS_CHUNK, pr.split, WS_TILE, g);
-          add_parts<CH>(ws + (2 * (BM / CH) + c) * WS_CHUNK, pr.split, WS_TILE, uu);
+          add_parts<CH>(first + c * WS_CHUNK, next + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, g);
+          add_parts<CH>(first + UP + c * WS_CHUNK, next + UP + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, uu);
           if (n_in) emit_gated<T, CH, ACT>(ep, c * CH, g, uu);
         }
       }
@@ -575,8 +621,8 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     constexpr bool SHARE_P = !GATED && C::QROWS <= 64;
     uint32_t it = 0;
     bool ok = !p.drop;
-    for (int u = cluster; u < p.units && ok; u += clusters) {
-      const Work w = get_work(p, u);
+    Work w;
+    for (int j = 0; ok && get_work(p, cluster, clusters, j, w); ++j) {
       const Problem& pr = p.prob[w.prob];
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
@@ -629,8 +675,8 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     constexpr uint32_t idesc0 = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(BM >> 3) << 17) | ((uint32_t)((128 * CG) >> 4) << 24);
     uint32_t it = 0, acc_it = 0;
     bool ok = true;
-    for (int u = cluster; u < p.units && ok; u += clusters, ++acc_it) {
-      const Work w = get_work(p, u);
+    Work w;
+    for (; ok && get_work(p, cluster, clusters, (int)acc_it, w); ++acc_it) {
       const Problem& pr = p.prob[w.prob];
       const uint32_t idesc = idesc0 | ((uint32_t)pr.p_mn << 15) | ((uint32_t)pr.q_mn << 16);
       const uint32_t p_step = pr.p_mn ? 2048 >> 4 : 32 >> 4, q_step = pr.q_mn ? 2048 >> 4 : 32 >> 4;
@@ -671,8 +717,8 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     // After a wait has given up, the warps still walk through the rest of the units together (without
     // waiting again), so that every named barrier below is met by all of its warps.
     bool dead = false;
-    for (int u = cluster; u < p.units; u += clusters, ++acc_it) {
-      const Work w = get_work(p, u);
+    Work w;
+    for (; get_work(p, cluster, clusters, (int)acc_it, w); ++acc_it) {
       const Problem& pr = p.prob[w.prob];
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
@@ -693,7 +739,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
       }
       typename Patch<CH>::Raw raw;
-      if (ep.has_r && n_in && w.part < 0) ep.pt.fetch(raw, ep.r, group * CH);
+      if (ep.has_r && n_in && w.slot < 0) ep.pt.fetch(raw, ep.r, group * CH);
       const uint32_t a = acc_it & 1u;
       if (!dead) dead = !wait_bounded(acc_full + 8 * a, (acc_it >> 1) & 1u, abort_flag, p);
       __syncwarp();

@@ -120,7 +120,7 @@ def test_repeated_calls_give_the_same_bits():
     g = _gen(3)
     for M, N, K in ((1, 1024, 8192), (300, 700, 6000)):
         A, B = _draw(g, M, K, torch.bfloat16), _draw(g, N, K, torch.bfloat16, K ** -0.5)
-        assert dg.hgemm_plan(M, N, K)["split"] > 1
+        assert dg.hgemm_plan(M, N, K)["span"] > 0
         first = None
         for _ in range(20):
             D = _out(M, N, torch.bfloat16)

@@ -123,14 +123,14 @@ def test_plan_covers_every_tile_and_k_block_once(sms, gated):
         p = dg.hgemm_plan(M, N, K, gated=gated, sm_count=sms)
         assert p["kblocks"] == -(-K // 64)
         tiles = -(-M // p["tile_rows"]) * -(-N // p["tile_cols"])
-        assert 0 <= p["dp_tiles"] <= tiles
-        rest = tiles - p["dp_tiles"]
-        if rest:
-            # the parts are non-empty and cover all k-blocks
-            assert p["split"] >= 2
-            assert (p["split"] - 1) * p["kblocks_per_part"] < p["kblocks"] <= p["split"] * p["kblocks_per_part"]
-        else:
-            assert p["split"] == 1
-        units = p["dp_tiles"] + rest * p["split"]
         limit = (sms or 148) // p["ctas_per_tile"]
-        assert p["clusters"] == min(units, limit)
+        # whole rounds take one tile per cluster each; what is left over is less than a round
+        assert p["rounds"] * limit + p["rest"] == tiles and 0 <= p["rest"] < limit
+        if p["span"] == 0:
+            assert p["clusters"] == (limit if p["rounds"] else p["rest"])
+        else:
+            # equal spans that cover all k-blocks left over, each shorter than a tile, none empty
+            # (end to end, or every tile cut alike into parts of its own)
+            assert 0 < p["span"] < p["kblocks"]
+            used = {-(-p["rest"] * p["kblocks"] // p["span"]), p["rest"] * -(-p["kblocks"] // p["span"])}
+            assert min(used) <= limit and p["clusters"] in ({limit} if p["rounds"] else used)
