@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libdgemm.so")
 EXT = os.path.join(HERE, "_marshal.so")  # compiled argument marshalling (csrc/binding_ext.cpp)
 EXT_SOURCE = os.path.join(CSRC, "binding_ext.cpp")
 SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "hgemm_plain_f16.cu", "hgemm_plain_bf16.cu",
-                                                "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "layernorm.cu")]
+                                                "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "hgemm_token.cu", "layernorm.cu")]
 # every source, header and public header: an edit to any of them makes the built library stale
 DEPS = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh")) +
               glob.glob(os.path.join(CSRC, "*.h")) + [EXT_SOURCE] + glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))

@@ -426,10 +426,45 @@ int run_empty(int type, int64_t M, int64_t N, const void* bias, int act, const v
   return ok ? DGEMM_OK : DGEMM_ERR_CUDA;
 }
 
+// Whether a product runs on the kernels for one or two rows.
+bool by_token(const Product& s, bool gated) {
+  return s.M <= TOKEN_ROWS && !s.p_mn && addressable(s.p[0]) && (!gated || addressable(s.p[1])) &&
+         s.M * ((s.K[0] + 7) / 8 * 8) * 2 <= (int64_t)TOKEN_SMEM && g_drop_limit_us.load() == 0;
+}
+int run_token(int type, bool gated, const Product& s, int sms, cudaStream_t stream) {
+  TokenParams p;
+  memset(&p, 0, sizeof(p));
+  p.M = (int)s.M;
+  p.N = (int)s.N;
+  p.K = (int)s.K[0];
+  p.X = s.q[0].ptr;
+  p.ldx = s.q[0].ld;
+  p.x_trans = s.q_mn;
+  p.x_vec = !s.q_mn && addressable(s.q[0]);
+  p.W[0] = s.p[0].ptr;
+  p.ldw[0] = s.p[0].ld;
+  if (gated) {
+    p.W[1] = s.p[1].ptr;
+    p.ldw[1] = s.p[1].ld;
+  }
+  p.act = s.act;
+  p.bias = s.bias;
+  p.R = s.R;
+  p.D = s.D;
+  p.Z = s.Z;
+  p.U = s.U;
+  p.ldr = s.ldr;
+  p.ldd = s.ldd;
+  p.ldz = s.ldz;
+  p.ldu = s.ldu;
+  return launch_token(type, gated, sms, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
+}
+
 // Packs what needs it and runs the products: the whole of a forward call.
 int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
   lm::DeviceState* st = nullptr;
   HGEMM_TRY(lm::device_state(&st));
+  if (by_token(*prod, gated)) return run_token(type, gated, *prod, st->sm_count, stream);
   Plan pl;
   if (!plan_products(&prod, 1, gated, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
   scratch::Hold hold(st->scratch, stream);

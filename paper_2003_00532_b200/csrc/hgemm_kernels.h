@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include "hgemm_tc.cuh"
+#include "hgemm_token.cuh"
 
 namespace hgemm {
 
@@ -20,6 +21,11 @@ bool launch_plain_f16(int act, int config, int clusters, cudaStream_t stream, co
 bool launch_plain_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
 bool launch_gated_f16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
 bool launch_gated_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+
+// Products of at most TOKEN_ROWS rows with 16-byte aligned weights stored N x K (hgemm_token.cuh). The tokens must fit in
+// TOKEN_SMEM bytes of shared memory.
+constexpr size_t TOKEN_SMEM = 160 * 1024;
+bool launch_token(int type, bool gated, int sms, cudaStream_t stream, const TokenParams& p);
 
 // Once per device: shared-memory limits.
 bool configure_plain_f16();

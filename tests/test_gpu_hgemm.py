@@ -84,6 +84,16 @@ def test_linear_exact_on_integers(shape, transa, transb, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transa,transb", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (8, 0), (3, 0), (0, 1)])
+@pytest.mark.parametrize("shape", [(1, 4096, 333), (2, 3001, 200), (3, 3333, 77), (4, 3500, 700), (4, 5, 9001), (1, 70, 20000), (3, 1, 8)])
+def test_linear_of_few_rows(shape, pad, offset, transa, transb, dtype):
+    """One to four rows; one and two have a kernel of their own for aligned weights stored N x K."""
+    _linear_case(*shape, dtype, transa, transb, ref.NONE, True, True, True, seed=sum(shape), integer=True, pad=pad, offset=offset)
+    _linear_case(*shape, dtype, transa, transb, ref.SILU, True, False, False, seed=1, pad=pad, offset=offset)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("act", ref.ACTS)
 @pytest.mark.parametrize("shape", [(1, 300, 500), (130, 200, 300), (600, 520, 96)])
 def test_linear_activations(shape, act, dtype):
@@ -279,6 +289,15 @@ def _gated_case(M, F, K, dtype, transw, act, save, seed=0, pad=0, offset=0):
                                    (129, 257, 65), (300, 260, 200), (1000, 777, 515)])
 def test_gated(shape, transw, dtype):
     _gated_case(*shape, dtype, transw, ref.SILU, True, seed=sum(shape))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transw", [False, True])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (3, 0), (0, 1)])
+@pytest.mark.parametrize("shape", [(1, 3100, 130), (2, 4096, 515), (4, 3001, 300), (3, 40, 9000)])
+def test_gated_of_few_rows(shape, pad, offset, transw, dtype):
+    _gated_case(*shape, dtype, transw, ref.SILU, True, seed=sum(shape), pad=pad, offset=offset)
+    _gated_case(*shape, dtype, transw, ref.GELU, False, seed=2, pad=pad, offset=offset)
 
 
 @pytest.mark.parametrize("act", ref.ACTS)
