@@ -651,21 +651,16 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
   const bool want_act = want_dz || dbias;
   ActBwdParams ap;
   memset(&ap, 0, sizeof(ap));
-  int vec = 1;
   int64_t strips = 0, chunks = 1;
   if (want_act) {
-    const Matrix z{act != HGEMM_ACT_NONE ? Z : dD, M, N, act != HGEMM_ACT_NONE ? ldz : lddd};
-    vec = addressable(dz) && addressable(z) ? 8 : 1;
-    strips = (N + 32 * vec - 1) / (32 * vec);
-    // enough blocks for the machine, at least 32 rows each (8 warps x 4 rows)
-    chunks = ((int64_t)st->sm_count * 8 + strips - 1) / strips;
+    strips = (N + 255) / 256;
+    ap.vec_d = addressable(dz);
+    ap.vec_z = addressable(Matrix{Z, M, N, ldz});
+    // four blocks per SM, at least 32 rows each (8 warps x 4 rows)
+    chunks = ((int64_t)st->sm_count * 4 + strips - 1) / strips;
     if (chunks > (M + 31) / 32) chunks = (M + 31) / 32;
     if (chunks > 1 && strips > lm::kCounters) chunks = 1;
     if (chunks > 256) chunks = 256;
-    if (!dbias) {
-      chunks = (M + 31) / 32;
-      if (chunks > 65535) chunks = 65535;
-    }
     ap.rows_per_chunk = (int)((M + chunks - 1) / chunks);
     chunks = (M + ap.rows_per_chunk - 1) / ap.rows_per_chunk;
     ap.M = (int)M;
@@ -688,13 +683,8 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     ap.partial = ws;
     ap.counters = counters;
     const dim3 grid((unsigned)strips, (unsigned)chunks);
-    bool ok;
-    if (type == HGEMM_TYPE_BF16)
-      ok = vec == 8 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, 1, s, ap)
-                    : lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, 1, s, ap);
-    else
-      ok = vec == 8 ? lm::launch(hgemm_act_bwd_kernel<__half, 8>, grid, dim3(256), 0, 1, s, ap)
-                    : lm::launch(hgemm_act_bwd_kernel<__half, 1>, grid, dim3(256), 0, 1, s, ap);
+    const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, ap)
+                                            : lm::launch(hgemm_act_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, ap);
     if (!ok) return DGEMM_ERR_CUDA;
   }
   if (n == 0) return DGEMM_OK;
@@ -848,17 +838,14 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   gp.act = act;
   dgu[0].ptr = gp.dG;
   dgu[1].ptr = gp.dU;
-  const int vec = addressable(Matrix{G, M, F, ldg}) && addressable(Matrix{U, M, F, ldu}) && addressable(Matrix{dH, M, F, lddh}) ? 8 : 1;
-  int64_t blocks = ((F + vec - 1) / vec * M + 255) / 256;
+  gp.vec_g = addressable(Matrix{G, M, F, ldg});
+  gp.vec_u = addressable(Matrix{U, M, F, ldu});
+  gp.vec_h = addressable(Matrix{dH, M, F, lddh});
+  int64_t blocks = ((F + 7) / 8 * M + 255) / 256;
   if (blocks > (int64_t)st->sm_count * 16) blocks = (int64_t)st->sm_count * 16;
   const dim3 grid((unsigned)blocks);
-  bool ok;
-  if (type == HGEMM_TYPE_BF16)
-    ok = vec == 8 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, 1, s, gp)
-                  : lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, 1, s, gp);
-  else
-    ok = vec == 8 ? lm::launch(hgemm_gated_bwd_kernel<__half, 8>, grid, dim3(256), 0, 1, s, gp)
-                  : lm::launch(hgemm_gated_bwd_kernel<__half, 1>, grid, dim3(256), 0, 1, s, gp);
+  const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, gp)
+                                          : lm::launch(hgemm_gated_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, gp);
   if (!ok || !pack.launch(buf, s)) return DGEMM_ERR_CUDA;
   for (int i = 0; i < 2; ++i) {
     px.p[i] = w[i];

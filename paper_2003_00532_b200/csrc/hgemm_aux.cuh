@@ -23,9 +23,48 @@ struct PackOps {
   PackOp op[3];
 };
 
-// Copies up to three matrices (blockIdx.y) into 16-byte aligned rows. A thread writes 8 values as one vector; it reads
-// them as five aligned words shifted by the row's misalignment, or, where those would reach beyond the row, one by one.
-// (One value per thread and block row: 17 us for 1000 x 777 and 777 x 1537.)
+// 8 values of 16 bits at src[0 .. 8), the columns c .. of a row of `cols`; those beyond the row are zero. An aligned vector
+// where it can be one (`vec`); else five aligned words shifted by the row's misalignment, or, where those would
+// reach beyond the row, one value after the other.
+__device__ __forceinline__ uint4 load8(const uint16_t* src, int c, int cols, bool vec) {
+  if (vec && c + 8 <= cols) return *reinterpret_cast<const uint4*>(src);
+  uint4 v;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  const bool half = (reinterpret_cast<uintptr_t>(src) & 2) != 0;  // the first value is the upper half of its word
+  if (c + 9 <= cols && (!half || c > 0)) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(src - (half ? 1 : 0));
+    uint32_t x[5];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = p[j];
+    x[4] = half ? p[4] : 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = half ? __funnelshift_r(x[j], x[j + 1], 16) : x[j];
+  } else {
+    uint16_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = c + j < cols ? src[j] : (uint16_t)0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)e[2 * j] | (uint32_t)e[2 * j + 1] << 16;
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint4& raw, float* v) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = unpack2<T>(w[j]);
+    v[2 * j] = f.x;
+    v[2 * j + 1] = f.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack8(const float* v) {
+  return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+}
+
+// Copies up to three matrices (blockIdx.y) into 16-byte aligned rows, a vector of 8 values per thread. (One value per
+// thread and block row: 17 us for 1000 x 777 and 777 x 1537, this 4 us.)
 __global__ void __launch_bounds__(256) hgemm_pack_kernel(const __grid_constant__ PackOps ops) {
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
@@ -35,24 +74,7 @@ __global__ void __launch_bounds__(256) hgemm_pack_kernel(const __grid_constant__
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
     const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 8;
     const uint16_t* src = o.src + r * o.ld_src + c;
-    uint4 v;
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-    const bool half = (reinterpret_cast<uintptr_t>(src) & 2) != 0;  // the first value is the upper half of its word
-    if (c + 9 <= o.cols && (!half || c > 0)) {
-      const uint32_t* p = reinterpret_cast<const uint32_t*>(src - (half ? 1 : 0));
-      uint32_t x[5];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = p[j];
-      x[4] = half ? p[4] : 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = half ? __funnelshift_r(x[j], x[j + 1], 16) : x[j];
-    } else {
-      uint16_t e[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = c + j < o.cols ? src[j] : (uint16_t)0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = (uint32_t)e[2 * j] | (uint32_t)e[2 * j + 1] << 16;
-    }
+    const uint4 v = load8(src, c, o.cols, false);
     *reinterpret_cast<uint4*>(o.dst + r * o.ld_dst + c) = v;
   }
 }
@@ -84,94 +106,83 @@ __global__ void hgemm_empty_kernel(int M, int N, const T* bias, int act, const T
 
 // ---- gradient at the activation -------------------------------------------------------------------
 
-// VEC consecutive 16-bit values as one access.
-template <int VEC> struct Raw;
-template <> struct Raw<8> { using type = uint4; };
-template <> struct Raw<1> { using type = uint16_t; };
-
-template <typename T, int VEC>
-__device__ __forceinline__ void load_vec(const T* p, float* v) {
-  typename Raw<VEC>::type raw = *reinterpret_cast<const typename Raw<VEC>::type*>(p);
-  const T* t = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) v[i] = to_f32(t[i]);
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void store_vec(T* p, const float* v) {
-  typename Raw<VEC>::type raw;
-  T* t = reinterpret_cast<T*>(&raw);
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) t[i] = from_f32<T>(v[i]);
-  *reinterpret_cast<typename Raw<VEC>::type*>(p) = raw;
-}
-
 struct ActBwdParams {
   int M, N;
   int rows_per_chunk;
   const void* Z;
   const void* dD;
-  void* dZ;         // or NULL
+  void* dZ;         // rows of 16-byte vectors (padding columns are written); or NULL
   float* dbias;     // or NULL
   float* partial;   // [chunks][N]
   int* counters;    // one per strip
   long long ldz, lddd, lddz;
   int act;
+  int vec_z, vec_d;  // 16-byte aligned rows
 };
 
-// dZ = dD act'(Z) (rounded) and dbias = column sums of the unrounded products. A block takes a strip of
-// 32 VEC columns and a chunk of rows; its eight warps take every eighth row. The blocks' column sums go
-// to `partial`; the block that finishes a strip last adds them in order of the chunks.
-template <typename T, int VEC, int ACT>
-__device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)[32 * VEC], int* last) {
+// dZ = dD act'(Z) (rounded) and dbias = column sums of the unrounded products. A block takes a strip of 256 columns (a lane
+// 8 of them) and a chunk of rows; its eight warps take every eighth row. The blocks' column sums
+// go to `partial`; the block that finishes a strip last adds them in order of the chunks.
+template <typename T, int ACT>
+__device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)[256], int* last) {
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int n = (blockIdx.x * 32 + tx) * VEC;
+  const int n = (blockIdx.x * 32 + tx) * 8;
   const int r0 = blockIdx.y * p.rows_per_chunk, r1 = min(p.M, r0 + p.rows_per_chunk);
-  const bool whole = n + VEC <= p.N;
-  float sum[VEC];
+  float sum[8];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
+  for (int i = 0; i < 8; ++i) sum[i] = 0.f;
   if (n < p.N) {
-    for (int r = r0 + ty; r < r1; r += 8) {
-      const T* pd = static_cast<const T*>(p.dD) + r * p.lddd + n;
-      const T* pz = static_cast<const T*>(p.Z) + r * p.ldz + n;
-      T* po = static_cast<T*>(p.dZ) + r * p.lddz + n;
-      float d[VEC], z[VEC];
-      if (whole) {
-        load_vec<T, VEC>(pd, d);
-        if (ACT != HGEMM_ACT_NONE) load_vec<T, VEC>(pz, z);
-      } else {
+    const uint16_t* pd = static_cast<const uint16_t*>(p.dD) + n;
+    const uint16_t* pz = static_cast<const uint16_t*>(p.Z) + n;
+    uint16_t* po = static_cast<uint16_t*>(p.dZ) + n;
+    const auto one = [&](const uint4& raw_d, const uint4& raw_z, int r) {
+      float d[8];
+      unpack8<T>(raw_d, d);
+      if (ACT != HGEMM_ACT_NONE) {
+        float z[8];
+        unpack8<T>(raw_z, z);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          d[i] = n + i < p.N ? to_f32(pd[i]) : 0.f;
-          z[i] = ACT != HGEMM_ACT_NONE && n + i < p.N ? to_f32(pz[i]) : 0.f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        if (ACT != HGEMM_ACT_NONE) {
+        for (int i = 0; i < 8; ++i) {
           float f, df;
           act_both<ACT>(z[i], f, df);
           d[i] *= df;
         }
-        sum[i] += d[i];
       }
-      if (p.dZ) {
-        if (whole) {
-          store_vec<T, VEC>(po, d);
-        } else {
 #pragma unroll
-          for (int i = 0; i < VEC; ++i)
-            if (n + i < p.N) po[i] = from_f32<T>(d[i]);
+      for (int i = 0; i < 8; ++i) sum[i] += d[i];
+      if (p.dZ) *reinterpret_cast<uint4*>(po + r * p.lddz) = pack8<T>(d);
+    };
+    int r = r0 + ty;
+    // two rows at a time where both are aligned vectors: no condition between the loads, or they would wait for one
+    // another (four rows made so much straight code that fetching it was the limit)
+    if (n + 8 <= p.N && p.vec_d && (ACT == HGEMM_ACT_NONE || p.vec_z)) {
+#pragma unroll 1
+      for (; r + 8 < r1; r += 16) {
+        uint4 d[2], z[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          d[i] = *reinterpret_cast<const uint4*>(pd + (r + 8 * i) * p.lddd);
+          if (ACT != HGEMM_ACT_NONE) z[i] = *reinterpret_cast<const uint4*>(pz + (r + 8 * i) * p.ldz);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) one(d[i], z[i], r + 8 * i);
       }
+    }
+#pragma unroll 1
+    for (; r < r1; r += 8) {
+      const uint4 d = load8(pd + r * p.lddd, n, p.N, p.vec_d);
+      uint4 z = d;
+      if (ACT != HGEMM_ACT_NONE) z = load8(pz + r * p.ldz, n, p.N, p.vec_z);
+      one(d, z, r);
     }
   }
   if (!p.dbias) return;
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) red[ty][tx * VEC + i] = sum[i];
+  for (int i = 0; i < 8; ++i) red[ty][tx * 8 + i] = sum[i];
   __syncthreads();
-  const int c0 = blockIdx.x * 32 * VEC;
-  for (int c = threadIdx.x; c < 32 * VEC && c0 + c < p.N; c += blockDim.x) {
+  const int c0 = blockIdx.x * 256, c = threadIdx.x;
+  const bool in = c0 + c < p.N;
+  if (in) {
     float s = 0.f;
     for (int w = 0; w < 8; ++w) s += red[w][c];
     if (gridDim.y == 1) p.dbias[c0 + c] = s;
@@ -186,27 +197,33 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
     if (*last) p.counters[blockIdx.x] = 0;
   }
   __syncthreads();
-  if (!*last) return;
+  if (!*last || !in) return;
   __threadfence();
-  for (int c = threadIdx.x; c < 32 * VEC && c0 + c < p.N; c += blockDim.x) {
-    float s = 0.f;
-    for (int k = 0; k < (int)gridDim.y; ++k) s += __ldcg(p.partial + (long long)k * p.N + c0 + c);
-    p.dbias[c0 + c] = s;
+  float s = 0.f;
+  int k = 0;
+  for (; k + 8 <= (int)gridDim.y; k += 8) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __ldcg(p.partial + (long long)(k + j) * p.N + c0 + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[j];
   }
+  for (; k < (int)gridDim.y; ++k) s += __ldcg(p.partial + (long long)k * p.N + c0 + c);
+  p.dbias[c0 + c] = s;
 }
 
-template <typename T, int VEC>
+template <typename T>
 __global__ void __launch_bounds__(256) hgemm_act_bwd_kernel(const __grid_constant__ ActBwdParams p) {
-  __shared__ float red[8][32 * VEC];
+  __shared__ float red[8][256];
   __shared__ int last;
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
   switch (p.act) {
-    case HGEMM_ACT_RELU: act_bwd_body<T, VEC, HGEMM_ACT_RELU>(p, red, &last); break;
-    case HGEMM_ACT_GELU: act_bwd_body<T, VEC, HGEMM_ACT_GELU>(p, red, &last); break;
-    case HGEMM_ACT_GELU_TANH: act_bwd_body<T, VEC, HGEMM_ACT_GELU_TANH>(p, red, &last); break;
-    case HGEMM_ACT_SILU: act_bwd_body<T, VEC, HGEMM_ACT_SILU>(p, red, &last); break;
-    default: act_bwd_body<T, VEC, HGEMM_ACT_NONE>(p, red, &last); break;
+    case HGEMM_ACT_RELU: act_bwd_body<T, HGEMM_ACT_RELU>(p, red, &last); break;
+    case HGEMM_ACT_GELU: act_bwd_body<T, HGEMM_ACT_GELU>(p, red, &last); break;
+    case HGEMM_ACT_GELU_TANH: act_bwd_body<T, HGEMM_ACT_GELU_TANH>(p, red, &last); break;
+    case HGEMM_ACT_SILU: act_bwd_body<T, HGEMM_ACT_SILU>(p, red, &last); break;
+    default: act_bwd_body<T, HGEMM_ACT_NONE>(p, red, &last); break;
   }
 }
 
@@ -215,70 +232,60 @@ struct GatedBwdParams {
   const void* G;
   const void* U;
   const void* dH;
-  void* dG;
+  void* dG;  // rows of 16-byte vectors (padding columns are written)
   void* dU;
   long long ldg, ldu, lddh, ldo;  // ldo: of dG and dU
   int act;
+  int vec_g, vec_u, vec_h;  // 16-byte aligned rows
 };
 
-// dG = dH U act'(G), dU = dH act(G); both rounded. One thread per VEC columns of a row.
-template <typename T, int VEC, int ACT>
+// dG = dH U act'(G), dU = dH act(G); both rounded. One thread per 8 columns of a row.
+template <typename T, int ACT>
 __device__ __forceinline__ void gated_bwd_body(const GatedBwdParams& p) {
-  const int per_row = (p.F + VEC - 1) / VEC;
+  const int per_row = (p.F + 7) / 8;
+  const bool vec = p.vec_g && p.vec_u && p.vec_h;
   const long long total = (long long)per_row * p.M;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
-    const int r = (int)(i / per_row), f = (int)(i - (long long)r * per_row) * VEC;
-    const T* pg = static_cast<const T*>(p.G) + r * p.ldg + f;
-    const T* pu = static_cast<const T*>(p.U) + r * p.ldu + f;
-    const T* pd = static_cast<const T*>(p.dH) + r * p.lddh + f;
-    T* og = static_cast<T*>(p.dG) + r * p.ldo + f;
-    T* ou = static_cast<T*>(p.dU) + r * p.ldo + f;
-    float g[VEC], u[VEC], d[VEC];
-    const bool whole = f + VEC <= p.F;
-    if (whole) {
-      load_vec<T, VEC>(pg, g);
-      load_vec<T, VEC>(pu, u);
-      load_vec<T, VEC>(pd, d);
+    const int r = (int)(i / per_row), f = (int)(i - (long long)r * per_row) * 8;
+    const uint16_t* pg = static_cast<const uint16_t*>(p.G) + r * p.ldg + f;
+    const uint16_t* pu = static_cast<const uint16_t*>(p.U) + r * p.ldu + f;
+    const uint16_t* pd = static_cast<const uint16_t*>(p.dH) + r * p.lddh + f;
+    uint4 rg, ru, rd;
+    if (vec && f + 8 <= p.F) {  // one condition for the three loads, or they would wait for one another
+      rg = *reinterpret_cast<const uint4*>(pg);
+      ru = *reinterpret_cast<const uint4*>(pu);
+      rd = *reinterpret_cast<const uint4*>(pd);
     } else {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const bool in = f + j < p.F;
-        g[j] = in ? to_f32(pg[j]) : 0.f;
-        u[j] = in ? to_f32(pu[j]) : 0.f;
-        d[j] = in ? to_f32(pd[j]) : 0.f;
-      }
+      rg = load8(pg, f, p.F, p.vec_g);
+      ru = load8(pu, f, p.F, p.vec_u);
+      rd = load8(pd, f, p.F, p.vec_h);
     }
+    float g[8], u[8], d[8];
+    unpack8<T>(rg, g);
+    unpack8<T>(ru, u);
+    unpack8<T>(rd, d);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
+    for (int j = 0; j < 8; ++j) {
       float a, da;
       act_both<ACT>(g[j], a, da);
       g[j] = d[j] * u[j] * da;
       u[j] = d[j] * a;
     }
-    if (whole) {
-      store_vec<T, VEC>(og, g);
-      store_vec<T, VEC>(ou, u);
-    } else {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j)
-        if (f + j < p.F) {
-          og[j] = from_f32<T>(g[j]);
-          ou[j] = from_f32<T>(u[j]);
-        }
-    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dG) + r * p.ldo + f) = pack8<T>(g);
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dU) + r * p.ldo + f) = pack8<T>(u);
   }
 }
 
-template <typename T, int VEC>
+template <typename T>
 __global__ void __launch_bounds__(256) hgemm_gated_bwd_kernel(const __grid_constant__ GatedBwdParams p) {
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
   switch (p.act) {
-    case HGEMM_ACT_RELU: gated_bwd_body<T, VEC, HGEMM_ACT_RELU>(p); break;
-    case HGEMM_ACT_GELU: gated_bwd_body<T, VEC, HGEMM_ACT_GELU>(p); break;
-    case HGEMM_ACT_GELU_TANH: gated_bwd_body<T, VEC, HGEMM_ACT_GELU_TANH>(p); break;
-    case HGEMM_ACT_SILU: gated_bwd_body<T, VEC, HGEMM_ACT_SILU>(p); break;
-    default: gated_bwd_body<T, VEC, HGEMM_ACT_NONE>(p); break;
+    case HGEMM_ACT_RELU: gated_bwd_body<T, HGEMM_ACT_RELU>(p); break;
+    case HGEMM_ACT_GELU: gated_bwd_body<T, HGEMM_ACT_GELU>(p); break;
+    case HGEMM_ACT_GELU_TANH: gated_bwd_body<T, HGEMM_ACT_GELU_TANH>(p); break;
+    case HGEMM_ACT_SILU: gated_bwd_body<T, HGEMM_ACT_SILU>(p); break;
+    default: gated_bwd_body<T, HGEMM_ACT_NONE>(p); break;
   }
 }
 
