@@ -85,9 +85,8 @@ unsigned resident_blocks(int sms, int threads, size_t smem, int64_t need) {
 template <typename T, int VEC, int ITEMS, bool WARP_ROW>
 bool launch_fwd(int sms, int threads, const Params& p, cudaStream_t stream) {
   constexpr auto kernel = &fwd_kernel<T, VEC, ITEMS, WARP_ROW>;
-  const size_t smem = (size_t)((p.cols + VEC - 1) / VEC) * VEC * 8;              // gamma and beta
-  const size_t most = (size_t)(WARP_ROW ? 32 : threads) * ITEMS * VEC * 8;  // ... for the longest row of this shape
-  if (most > 48 * 1024) {
+  const size_t smem = (size_t)(WARP_ROW ? 32 : threads) * ITEMS * VEC * 8;  // gamma and beta
+  if (smem > 48 * 1024) {
     static std::atomic<bool> configured[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
@@ -98,7 +97,7 @@ bool launch_fwd(int sms, int threads, const Params& p, cudaStream_t stream) {
     }
   }
   const int64_t need = WARP_ROW ? (p.rows + 3) / 4 : p.rows;
-  const unsigned blocks = resident_blocks<decltype(kernel), kernel>(sms, threads, most, need);
+  const unsigned blocks = resident_blocks<decltype(kernel), kernel>(sms, threads, smem, need);
   return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p);
 }
 template <typename T, int VEC, int ITEMS>

@@ -235,25 +235,48 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
   long long row = WARP_ROW ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
   const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
   T* y_at = static_cast<T*>(p.out) + row * p.ldo + c0;
-  Vec<T, VEC> raw[ITEMS];
-  if (row < p.rows) load_row<T, VEC, ITEMS>(raw, x_at, c0, p.cols, full);
-  const int nv = (p.cols + VEC - 1) / VEC;
-  float* sg = reinterpret_cast<float*>(smem);
-  float* sb = sg + nv * VEC;
-  for (int c = threadIdx.x; c < nv * VEC; c += blockDim.x) {
-    const bool in = c < p.cols;
-    sg[plane_at<VEC>(c, nv)] = p.gamma && in ? cvt(static_cast<const T*>(p.gamma)[c]) : 1.f;
-    sb[plane_at<VEC>(c, nv)] = p.beta && in ? cvt(static_cast<const T*>(p.beta)[c]) : 0.f;
-  }
   using P = Pairs<T, VEC, ITEMS>;
   constexpr int N = P::N;
+  Vec<T, VEC> raw[ITEMS];
+  const int nv = (int)(WARP_ROW ? 1 : blockDim.x >> 5) * ITEMS * 32;  // vectors of the whole block, inside the row or not
+  float* sg = reinterpret_cast<float*>(smem);
+  float* sb = sg + nv * VEC;
+  {
+    // every thread puts down what it will read itself (WARP_ROW: the four warps the same values)
+    Vec<T, VEC> raw_b[ITEMS];
+    if (p.gamma) load_row<T, VEC, ITEMS>(raw, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+    if (p.beta) load_row<T, VEC, ITEMS>(raw_b, static_cast<const T*>(p.beta) + c0, c0, p.cols, full);
+    P g, b;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      g.v[k] = both(1.f);
+      b.v[k] = both(0.f);
+    }
+    if (p.gamma) g.unpack(raw);
+    if (p.beta) b.unpack(raw_b);
+    if (row < p.rows) load_row<T, VEC, ITEMS>(raw, x_at, c0, p.cols, full);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int v = v0 + i * 32;
+      if constexpr (VEC > 1) {
+#pragma unroll
+        for (int h = 0; h < PLANES; ++h) {
+          const int k = i * VEC / 2 + 2 * h;
+          *reinterpret_cast<float4*>(sg + (h * nv + v) * LOW) = make_float4(g.v[k].x, g.v[k].y, g.v[k + 1].x, g.v[k + 1].y);
+          *reinterpret_cast<float4*>(sb + (h * nv + v) * LOW) = make_float4(b.v[k].x, b.v[k].y, b.v[k + 1].x, b.v[k + 1].y);
+        }
+      } else {
+        sg[v] = i % 2 ? g.v[i / 2].y : g.v[i / 2].x;
+        sb[v] = i % 2 ? b.v[i / 2].y : b.v[i / 2].x;
+      }
+    }
+  }
   const bool plain = full && VEC * ITEMS % 2 == 0;
   const float inv_n = 1.f / (float)p.cols;
   // columns of this warp, and of warp number `lane`
   const auto columns = [&](int w) { return (float)max(0, min(32 * ITEMS * VEC, p.cols - w * 32 * ITEMS * VEC)); };
   const float n_warp = WARP_ROW ? (float)p.cols : columns(warp), inv_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
   const float n_lane = !WARP_ROW && lane < (int)(blockDim.x >> 5) ? columns(lane) : 0.f;
-  __syncthreads();
   int parity = 0;
   for (; row < p.rows; parity ^= 1) {
     P x;
@@ -305,7 +328,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
     for (int k = 0; k < N; ++k) x.v[k] = fma2(x.v[k], both(rstd), both(bias));
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int v = min(v0 + i * 32, nv - 1);  // (beyond the row: any value, it is not stored)
+      const int v = v0 + i * 32;
       if constexpr (VEC > 1) {
 #pragma unroll
         for (int h = 0; h < PLANES; ++h) {
