@@ -418,23 +418,24 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
       w_dg[at] = w_db[at] = 0.f;
     }
     __syncthreads();
-  } else {
-    if (gamma) {
-      load_row<T, VEC, ITEMS>(xr, gamma + c0, c0, p.cols, full);
-      g.unpack(xr);
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k) g.v[k] = both(1.f);
-    }
-#pragma unroll
-    for (int k = 0; k < N; ++k) dg.v[k] = db.v[k] = both(0.f);
   }
+  // gamma's loads and the first row's are in flight together
+  Vec<T, VEC> gr[ITEMS];
+  if (!WIDE && gamma) load_row<T, VEC, ITEMS>(gr, gamma + c0, c0, p.cols, full);
   float mean = 0.f, rstd = 0.f;
   if (row < p.rows) {
     load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
     load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
     mean = p.mean[row];
     rstd = p.rstd[row];
+  }
+  if (!WIDE) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      g.v[k] = both(1.f);
+      dg.v[k] = db.v[k] = both(0.f);
+    }
+    if (gamma) g.unpack(gr);
   }
   int parity = 0;
   for (; row < p.rows; parity ^= 1) {
@@ -521,6 +522,14 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
     for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
       out[c] = w_dg[plane_at<VEC>(c, nv)];
       out[half + c] = w_db[plane_at<VEC>(c, nv)];
+    }
+  } else if (!WARP_ROW && VEC >= 4 && full && p.cols % 4 == 0) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      const int c = c0 + 2 * k / VEC * 32 * VEC + 2 * k % VEC;
+      const int l = k + 1 < N ? k + 1 : k;
+      *reinterpret_cast<float4*>(out + c) = make_float4(dg.v[k].x, dg.v[k].y, dg.v[l].x, dg.v[l].y);
+      *reinterpret_cast<float4*>(out + half + c) = make_float4(db.v[k].x, db.v[k].y, db.v[l].x, db.v[l].y);
     }
   } else if (!WARP_ROW) {
 #pragma unroll
