@@ -77,8 +77,14 @@ constexpr double kPartColumn = 20.0;       // a part's sums to the workspace, pe
 constexpr double kJoinColumn = 8.0;        // adding one part, per row of the output
 constexpr double kJoinClocks = 4500.0;     // publishing the parts and finding the last one
 
+constexpr double kWideKBlockClocks = 1270.0;  // of a 512 x 256 tile
+// A 512 x 256 tile's two accumulators fill TMEM: its epilogue stands beside little of the next tile's MMAs. Per row of
+// the output: a part of its own and most of an ordinary epilogue, for each of the two.
+constexpr double kWideEpilogue = 20.0, kWideShare = 0.85;
+
 // Clocks of one k-block in a CTA: its MMAs (8192 flop per clock), or its operand bytes.
 double step_clocks(const Config& c) {
+  if (c.nb == 2) return kWideKBlockClocks;
   const double mma = 2.16 * c.bm, bytes = (16384.0 + 128.0 * (c.bm / c.cg < 64 ? 64 : c.bm / c.cg)) / kL2BytesPerClock;
   const double t = mma > bytes ? mma : bytes;
   return t > kKBlockClocks ? t : kKBlockClocks;
@@ -96,7 +102,7 @@ bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out
   const Config& c = kConfigs[config];
   Layout l;
   l.clusters = sms / c.cg;
-  l.nt = (gated ? 64 : 128) * c.cg;
+  l.nt = (gated ? 64 : 128) * c.cg * c.nb;
   l.step = step_clocks(c);
   l.epi = 0.0;
   l.left = l.left_kblocks = 0;
@@ -114,10 +120,23 @@ bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out
     if (l.rest[i] > 0 && sz[i].kblocks > l.longest) l.longest = sz[i].kblocks;
     // a round is as long as a tile's MMAs, or as an epilogue (which runs beside the next tile's MMAs)
     const double mma = sz[i].kblocks * l.step;
-    l.fixed += (double)l.rounds[i] * ((mma > l.epi ? mma : l.epi) + kUnitClocks);
+    if (c.nb == 2) l.fixed += (double)l.rounds[i] * (mma + 2 * c.bm * (kWideEpilogue + kWideShare * sz[i].epilogue));
+    else l.fixed += (double)l.rounds[i] * ((mma > l.epi ? mma : l.epi) + kUnitClocks);
   }
   *out = l;
   return true;
+}
+// Whether 512 x 256 tiles are worth a thought: they move a quarter less from L2 per product, which pays where the power
+// limit holds the clock down for long, and lose where tiles are few or short. Sustained, against 256 x 256: 8192 x
+// 4096 x 8192 466 -> 447 us, gated gradients 4096 x 8192 x 2048 548 -> 503, gated 8192 x 4096 x 8192 880 -> 755; but
+// 4096 x 9472 x 4096 (64 k-blocks) 243 -> 297, 2048 x 2048 x 8192 (half a round) 60 -> 93.
+bool wide_tiles(const Layout& l, const Size* sz, int n) {
+  int64_t tiles = 0, kblocks = 0;
+  for (int i = 0; i < n; ++i) {
+    tiles += l.tiles[i];
+    kblocks += l.tiles[i] * sz[i].kblocks;
+  }
+  return tiles >= 3 * (int64_t)l.clusters && kblocks >= 96 * tiles;
 }
 // The tiles left over, run whole: rounds over the clusters, each as long as its longest tile.
 double whole_clocks(const Layout& l, const Size* sz, int n) {
@@ -155,7 +174,7 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
   for (int c = 0; c < kNumConfigs; ++c) {
     if (c > 0 && kConfigs[c - 1].cg == 1 && kConfigs[c - 1].bm >= max_m) break;  // only more padding
     Layout l;
-    if (!lay_out(sz, n, gated, sms, c, &l)) continue;
+    if (!lay_out(sz, n, gated, sms, c, &l) || (kConfigs[c].nb == 2 && !wide_tiles(l, sz, n))) continue;
     const auto consider = [&](double t, int64_t span, bool even) {
       if (best_clocks >= 0.0 && t >= best_clocks) return;
       best_clocks = t;
@@ -165,7 +184,7 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
       pick_even = even;
     };
     consider(l.fixed + (l.left > 0 ? whole_clocks(l, sz, n) : 0.0), 0, false);
-    if (l.left == 0 || l.left * kConfigs[c].cg > lm::kCounters || l.left_kblocks > INT32_MAX / 2) continue;
+    if (l.left == 0 || l.left * kConfigs[c].cg * kConfigs[c].nb > lm::kCounters || l.left_kblocks > INT32_MAX / 2) continue;
     // equal spans over all clusters, or over half or a quarter of them where joining many parts costs more
     for (int divide = 1; divide <= 4; divide *= 2) {
       int64_t span = (l.left_kblocks * divide + l.clusters - 1) / l.clusters;
@@ -197,7 +216,7 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
   pl.span = (int)pick_span;
   const int64_t used = pick_span > 0 ? (pl.span_total + pick_span - 1) / pick_span : pick.left;
   pl.clusters = pl.rounds > 0 || used > pick.clusters ? pick.clusters : (int)used;
-  if (pick_span > 0) pl.workspace = (size_t)2 * pl.clusters * c.cg * c.bm * 128 * sizeof(float);
+  if (pick_span > 0) pl.workspace = (size_t)2 * pl.clusters * c.cg * c.nb * c.bm * 128 * sizeof(float);
   *best = pl;
   return true;
 }
@@ -334,7 +353,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     const Plan::Part& q = pl.part[i];
     const int np = gated ? 2 : s.nseg, nq = s.nseg;
     for (int j = 0; j < np; ++j)
-      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated || qrows <= 64 ? 64 : 128)) return DGEMM_ERR_CUDA;
+      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated || c.nb == 1 ? 64 : 128)) return DGEMM_ERR_CUDA;
     for (int j = 0; j < nq; ++j)
       if (!make_map(&d.q[j], type, s.q[j], s.q_mn ? 64 : qrows)) return DGEMM_ERR_CUDA;
     d.N = (int)s.N;

@@ -8,8 +8,8 @@ namespace hgemm {
 
 template <typename T, bool GATED, int I, int ACT>
 bool launch_one(int clusters, cudaStream_t stream, const Params& p) {
-  constexpr int CG = kConfigs[I].cg, BM = kConfigs[I].bm;
-  return lm::launch(hgemm_tc_kernel<T, CG, BM, GATED, ACT>, dim3(clusters * CG), dim3(THREADS), (size_t)Cfg<CG, BM, GATED>::SMEM_BYTES, CG,
+  constexpr int CG = kConfigs[I].cg, BM = kConfigs[I].bm, NB = kConfigs[I].nb;
+  return lm::launch(hgemm_tc_kernel<T, CG, BM, NB, GATED, ACT>, dim3(clusters * CG), dim3(THREADS), (size_t)Cfg<CG, BM, NB, GATED>::SMEM_BYTES, CG,
                     stream, p);
 }
 template <typename T, bool GATED, int I>
@@ -31,9 +31,9 @@ bool launch_config(int act, int config, int clusters, cudaStream_t stream, const
 
 template <typename T, bool GATED, int I, int ACT = 0>
 bool configure_config() {
-  constexpr int CG = kConfigs[I].cg, BM = kConfigs[I].bm;
-  if (cudaFuncSetAttribute(hgemm_tc_kernel<T, CG, BM, GATED, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           Cfg<CG, BM, GATED>::SMEM_BYTES) != cudaSuccess)
+  constexpr int CG = kConfigs[I].cg, BM = kConfigs[I].bm, NB = kConfigs[I].nb;
+  if (cudaFuncSetAttribute(hgemm_tc_kernel<T, CG, BM, NB, GATED, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           Cfg<CG, BM, NB, GATED>::SMEM_BYTES) != cudaSuccess)
     return false;
   if constexpr (ACT + 1 < HGEMM_ACT_COUNT) return configure_config<T, GATED, I, ACT + 1>();
   return true;

@@ -9,11 +9,11 @@
 
 namespace hgemm {
 
-// Tile configurations: CTAs per tile and TMEM columns (rows of the output).
+// Tile configurations: CTAs per tile, TMEM columns (rows of the output), blocks of 128 lanes per CTA.
 struct Config {
-  int cg, bm;
+  int cg, bm, nb;
 };
-constexpr Config kConfigs[] = {{1, 16}, {1, 32}, {1, 64}, {1, 128}, {2, 128}, {2, 256}};
+constexpr Config kConfigs[] = {{1, 16, 1}, {1, 32, 1}, {1, 64, 1}, {1, 128, 1}, {2, 128, 1}, {2, 256, 1}, {2, 256, 2}};
 constexpr int kNumConfigs = sizeof(kConfigs) / sizeof(kConfigs[0]);
 
 // Launches configuration `config` for activation `act` on `clusters` tiles' worth of CTAs.

@@ -29,10 +29,10 @@
 // registers of all shared one allocation and the epilogue without activation spilled (4096 x 9472 x 256: 50 us,
 // 40 alone).
 //
-// Roles (384 threads): warps 0 and 3 stage P and Q (one thread that issued all copies was the limit:
-// 479 ns per 64-wide k-block with four copies, against 366 ns for its MMAs; two threads with one or
-// two copies each are not), warp 1 issues the MMAs, warp 2 owns the TMEM allocation, warps 4-11 run
-// the epilogue of one accumulator while the MMAs fill the other. In a pair the MMAs of both CTAs are issued by the leader; each CTA stages its own 128 lanes and its half of Q.
+// Roles (384 threads): warps 0 and 2 stage halves of P, warp 3 stages Q (one thread that issued all copies was the
+// limit: 479 ns per 64-wide k-block with four copies, against 366 ns for its MMAs), warp 1 issues the MMAs, warp 2 also
+// owns the TMEM allocation, warps 4-11 run the epilogue of one accumulator while the MMAs fill the other. In a
+// pair the MMAs of both CTAs are issued by the leader; each CTA stages its own lanes and its half of Q.
 #pragma once
 
 #include <cstdint>
@@ -56,14 +56,16 @@ constexpr int PITCH = 80;  // bytes per patch row in shared memory: 64 + 16, no 
 constexpr int MAX_SMEM = 232448;  // 227 KB
 constexpr int MAX_PROBLEMS = 3;
 
-// CG: CTAs per tile (1, or a pair); BM: TMEM columns of the tile (rows of the output).
-template <int CG_, int BM_, bool GATED_>
+// CG: CTAs per tile (1, or a pair); BM: TMEM columns of the tile (rows of the output); NB: blocks of 128 lanes per CTA.
+// With NB = 1 the two accumulators are two tiles', filled and drained in turn; with NB = 2 they are the two lane
+// blocks of one tile, which share each staged Q.
+template <int CG_, int BM_, int NB_, bool GATED_>
 struct Cfg {
-  static constexpr int CG = CG_, BM = BM_;
+  static constexpr int CG = CG_, BM = BM_, NB = NB_;
   static constexpr bool GATED = GATED_;
   static constexpr int QROWS = BM / CG;  // rows of Q that one CTA stages
   static constexpr int QBOXES = (QROWS + 63) / 64;
-  static constexpr int P_BYTES = 2 * BOX_BYTES;
+  static constexpr int P_BYTES = NB * 2 * BOX_BYTES;
   static constexpr int STAGE_BYTES = P_BYTES + QBOXES * BOX_BYTES;
   static constexpr int CH = GATED ? (BM < 32 ? 8 : 16) : 16;  // TMEM columns one warp takes at a time
   // Each epilogue warp's buffer: a patch of the output or, before that, the values it hands to its partner.
@@ -74,7 +76,8 @@ struct Cfg {
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + BUFS_BYTES + CTRL_BYTES + 1024;
   static constexpr int TMEM_COLS = 2 * BM < 32 ? 32 : 2 * BM;  // two accumulators (a power of two)
-  static constexpr int NT = (GATED ? 64 : 128) * CG;           // output columns per tile
+  static constexpr int BLOCK = GATED ? 64 : 128;               // output columns of one accumulator
+  static constexpr int NT = BLOCK * CG * NB;                   // output columns per tile
 };
 
 struct alignas(64) Problem {
@@ -102,8 +105,8 @@ struct Params {
   int span;                // k-blocks per cluster of the tiles left over, 0: they run whole
   int span_total;          // positions of all tiles left over
   int rest;                // tiles left over
-  float* ws;               // two slots of CG x BM x 128 sums per cluster
-  int* counters;           // one per tile left over and CTA of a pair; zero between launches
+  float* ws;               // two slots of CG x NB x BM x 128 sums per cluster
+  int* counters;           // CG x NB per tile left over; zero between launches
   unsigned long long wait_limit_ns;
   int* status;
   int drop;  // testing aid: the producers skip their copies
@@ -438,7 +441,7 @@ __device__ __forceinline__ void add_parts(const float4* first, const float4* ws,
 // One epilogue warp: its accumulator quarter, buffers and place.
 struct EpiWarp {
   uint32_t acc, bufs, last_flag, acc_empty;
-  int e, quad, group, lane, rank;
+  int e, quad, group, lane, block;  // block: of 128 lanes among the tile's CG x NB
 };
 
 __device__ __forceinline__ void sts32(uint32_t addr, int v) { asm volatile("st.shared.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
@@ -453,12 +456,12 @@ template <typename T, typename C, int ACT>
 __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr, const Work& w, const Epilogue<C::CH>& ep,
                                               typename Patch<C::CH>::Raw& raw, const EpiWarp& ew, int rows, bool n_in) {
   using namespace dgemm::ptx;
-  constexpr int CG = C::CG, BM = C::BM, CH = C::CH, GROUPS = EPI_WARPS / 4;
+  constexpr int CG = C::CG, BM = C::BM, CH = C::CH, BLOCKS = C::CG * C::NB, GROUPS = EPI_WARPS / 4;
   constexpr bool GATED = C::GATED;
-  // a part's sums in the workspace: [slot][CTA][quarter][chunk][CH / 4][lane] of float4
-  constexpr long long WS_SLOT = (long long)CG * BM * 32;  // float4 per slot
+  // a part's sums in the workspace: [slot][block][quarter][chunk][CH / 4][lane] of float4
+  constexpr long long WS_SLOT = (long long)BLOCKS * BM * 32;  // float4 per slot
   constexpr int WS_CHUNK = CH / 4 * 32;                   // float4 per quarter and chunk
-  float4* const ws_cta = reinterpret_cast<float4*>(p.ws) + ew.rank * (BM * 32) + ew.lane;
+  float4* const ws_cta = reinterpret_cast<float4*>(p.ws) + ew.block * (BM * 32) + ew.lane;
   // the accumulator may be overwritten: called once this warp's last load of it has been waited for
   bool released = false;
   const auto release = [&]() {
@@ -521,7 +524,7 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
   }
   if (!released) release();
   if (w.slot >= 0) {
-    int* counter = p.counters + w.left * CG + ew.rank;
+    int* counter = p.counters + w.left * BLOCKS + ew.block;
     __threadfence();
     named_barrier_sync(15, EPI_WARPS * 32);
     if (ew.e == 0 && ew.lane == 0) {
@@ -565,10 +568,10 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major) {
   return (uint64_t)((addr & 0x3FFFF) >> 4) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
 }
 
-template <typename T, int CG, int BM, bool GATED, int ACT>
+template <typename T, int CG, int BM, int NB, bool GATED, int ACT>
 __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_constant__ Params p) {
   using namespace dgemm::ptx;
-  using C = Cfg<CG, BM, GATED>;
+  using C = Cfg<CG, BM, NB, GATED>;
   constexpr int STAGES = C::STAGES, CH = C::CH;
 
   extern __shared__ uint8_t smem_raw[];
@@ -614,11 +617,11 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
   const uint32_t tmem = *tmem_slot;
   ptx5::launch_dependents();
   grid_dependency_wait();
-  if ((warp == 0 || warp == 3) && lane == 0) {
-    // ---- stages: warp 0 copies the P boxes, warp 3 the Q boxes and, where those are small, the second half of P (one
-    // stream of copies brings about 35 bytes per clock); zero fill outside the matrices ----
-    const bool is_p = warp == 0;
-    constexpr bool SHARE_P = !GATED && C::QROWS <= 64;
+  if ((warp == 0 || warp == 2 || warp == 3) && lane == 0) {
+    // ---- stages: warps 0 and 2 copy half of the P boxes each, warp 3 the Q boxes: one stream of copies brings about 35
+    // bytes per clock. Zero fill outside the matrices ----
+    const bool is_p = warp != 3;
+    const int half = warp == 2 ? 1 : 0;
     uint32_t it = 0;
     bool ok = !p.drop;
     Work w;
@@ -626,7 +629,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       const Problem& pr = p.prob[w.prob];
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
-      const int n0 = tn * C::NT + rank * (GATED ? 64 : 128), m0 = tm * BM + rank * C::QROWS;
+      const int n0 = tn * C::NT + rank * NB * C::BLOCK, m0 = tm * BM + rank * C::QROWS;
       const uint32_t bytes = CG * (C::P_BYTES + (pr.q_mn ? C::QBOXES * BOX_BYTES : C::QROWS * 128));
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
         const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u;
@@ -635,20 +638,19 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
           break;
         }
         const uint32_t fb = CG == 1 ? full_bar + 8 * s : map_to_cta(full_bar + 8 * s, 0);
-        if (is_p && rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, bytes);
+        if (warp == 0 && rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, bytes);
         const int seg = kb >= pr.kb_seg0 ? 1 : 0;
         const int k0 = (kb - (seg ? pr.kb_seg0 : 0)) * TK;
         const uint32_t dst = base + s * C::STAGE_BYTES;
         const auto load_p = [&](int i) {
-          const CUtensorMap* map = &pr.p[GATED ? i : seg];
-          const int n = n0 + (GATED ? 0 : 64 * i);
+          const CUtensorMap* map = &pr.p[GATED ? i & 1 : seg];
+          const int n = n0 + 64 * (GATED ? i >> 1 : i);
           ptx5::tma_load_2d<CG>(dst + i * BOX_BYTES, map, pr.p_mn ? n : k0, pr.p_mn ? k0 : n, fb);
         };
         if (is_p) {
-          load_p(0);
-          if (GATED || (!SHARE_P && pr.p_mn)) load_p(1);
+          load_p(NB * half);
+          if (NB == 2 && (GATED || pr.p_mn)) load_p(NB * half + 1);
         } else {
-          if (SHARE_P) load_p(1);
           const CUtensorMap* map = &pr.q[GATED ? 0 : seg];
           if (pr.q_mn) {
 #pragma unroll
@@ -661,7 +663,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     }
     // After a normal run every copy has been consumed. After an abort let the copies in flight land
     // (bounded); the leader's barriers count the bytes of both CTAs of a pair.
-    if (!ok && !p.drop && is_p && rank == 0) {
+    if (!ok && !p.drop && warp == 0 && rank == 0) {
       const uint32_t n_inflight = it < (uint32_t)STAGES ? it : (uint32_t)STAGES;
       for (uint32_t j = it - n_inflight; j < it; ++j) {
         const unsigned long long t0 = globaltimer_ns();
@@ -680,27 +682,60 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       const Problem& pr = p.prob[w.prob];
       const uint32_t idesc = idesc0 | ((uint32_t)pr.p_mn << 15) | ((uint32_t)pr.q_mn << 16);
       const uint32_t p_step = pr.p_mn ? 2048 >> 4 : 32 >> 4, q_step = pr.q_mn ? 2048 >> 4 : 32 >> 4;
-      const uint32_t a = acc_it & 1u;
-      if (!wait_bounded(acc_empty + 8 * a, ((acc_it >> 1) & 1u) ^ 1u, abort_flag, p)) {
-        ok = false;
-        break;
-      }
-      ptx5::fence_after_sync();
-      const uint32_t d = tmem + a * BM;
-      for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-        const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u;
-        if (!wait_bounded(full_bar + 8 * s, ph, abort_flag, p)) {
+      const auto mmas = [&](uint32_t stage, uint32_t d, int block, bool first) {
+        const uint32_t src = base + stage * C::STAGE_BYTES;
+        const uint64_t pd = smem_desc(src + block * 2 * BOX_BYTES, pr.p_mn), qd = smem_desc(src + C::P_BYTES, pr.q_mn);
+#pragma unroll
+        for (int k = 0; k < TK / 16; ++k) ptx5::mma_f16<CG>(d, pd + k * p_step, qd + k * q_step, idesc, !first || k > 0);
+      };
+      const auto staged = [&](uint32_t i) {
+        if (!wait_bounded(full_bar + 8 * (i % STAGES), (i / STAGES) & 1u, abort_flag, p)) return false;
+        ptx5::fence_after_sync();
+        return true;
+      };
+      if constexpr (NB == 1) {
+        const uint32_t a = acc_it & 1u;
+        if (!wait_bounded(acc_empty + 8 * a, ((acc_it >> 1) & 1u) ^ 1u, abort_flag, p)) {
           ok = false;
           break;
         }
         ptx5::fence_after_sync();
-        const uint32_t src = base + s * C::STAGE_BYTES;
-        const uint64_t pd = smem_desc(src, pr.p_mn), qd = smem_desc(src + C::P_BYTES, pr.q_mn);
-#pragma unroll
-        for (int k = 0; k < TK / 16; ++k) ptx5::mma_f16<CG>(d, pd + k * p_step, qd + k * q_step, idesc, kb > w.kb0 || k > 0);
-        ptx5::mma_commit<CG>(empty_bar + 8 * s);
+        for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+          if (!staged(it)) {
+            ok = false;
+            break;
+          }
+          mmas(it % STAGES, tmem + a * BM, 0, kb == w.kb0);
+          ptx5::mma_commit<CG>(empty_bar + 8 * (it % STAGES));
+        }
+        if (ok) ptx5::mma_commit<CG>(acc_full + 8 * a);
+      } else {
+        // The first block's accumulator is drained first: its MMAs on all staged k-blocks run while the second one's is
+        // still being read; then the second block catches up.
+        const int nkb = w.kb1 - w.kb0, ahead = min(nkb, STAGES);
+        if (!wait_bounded(acc_empty, (acc_it & 1u) ^ 1u, abort_flag, p)) ok = false;
+        ptx5::fence_after_sync();
+        for (int i = 0; ok && i < ahead; ++i) {
+          if (!(ok = staged(it + i))) break;
+          mmas((it + i) % STAGES, tmem, 0, i == 0);
+        }
+        if (ok && ahead == nkb) ptx5::mma_commit<CG>(acc_full);
+        if (ok && !wait_bounded(acc_empty + 8, (acc_it & 1u) ^ 1u, abort_flag, p)) ok = false;
+        ptx5::fence_after_sync();
+        for (int i = 0; ok && i < ahead; ++i) {
+          mmas((it + i) % STAGES, tmem + BM, 1, i == 0);
+          ptx5::mma_commit<CG>(empty_bar + 8 * ((it + i) % STAGES));
+        }
+        for (int i = ahead; ok && i < nkb; ++i) {
+          if (!(ok = staged(it + i))) break;
+          mmas((it + i) % STAGES, tmem, 0, false);
+          if (i == nkb - 1) ptx5::mma_commit<CG>(acc_full);
+          mmas((it + i) % STAGES, tmem + BM, 1, false);
+          ptx5::mma_commit<CG>(empty_bar + 8 * ((it + i) % STAGES));
+        }
+        if (ok) ptx5::mma_commit<CG>(acc_full + 8);
+        it += nkb;
       }
-      if (ok) ptx5::mma_commit<CG>(acc_full + 8 * a);
     }
     if (!ok) {  // leave no MMA in flight (bounded)
       ptx5::mma_commit<CG>(drain_bar);
@@ -723,29 +758,31 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
       int tm, tn;
       tile_to_mn(pr, w.tile, tm, tn);
       const int m_base = tm * BM, rows = min(pr.M - m_base, BM);
-      const int n0 = tn * C::NT + (GATED ? rank * 64 + (quad & 1) * 32 : rank * 128 + quad * 32);
-      const bool n_in = n0 < pr.N;  // (the whole warp: a patch beyond the last column has nothing to do)
-      Epilogue<CH> ep;
-      ep.pt = Patch<CH>{rows, pr.N - n0, lane, buf, buf + (lane & 7) * PITCH + (lane >> 3) * 16};
-      ep.has_z = pr.Z != nullptr;
-      ep.has_r = !GATED && pr.R != nullptr;
-      ep.d = ep.pt.view(pr.D, pr.ldd, pr.vec & VEC_D, m_base, n0);
-      if (ep.has_z) ep.z = ep.pt.view(pr.Z, pr.ldz, pr.vec & VEC_Z, m_base, n0);
-      if (GATED && ep.has_z) ep.u = ep.pt.view(pr.U, pr.ldu, pr.vec & VEC_U, m_base, n0);
-      if (ep.has_r) ep.r = ep.pt.view(pr.R, pr.ldr, pr.vec & VEC_R, m_base, n0);
+      for (int h = 0; h < NB; ++h) {
+        const int n0 = tn * C::NT + (rank * NB + h) * C::BLOCK + (GATED ? (quad & 1) * 32 : quad * 32);
+        const bool n_in = n0 < pr.N;  // (the whole warp: a patch beyond the last column has nothing to do)
+        Epilogue<CH> ep;
+        ep.pt = Patch<CH>{rows, pr.N - n0, lane, buf, buf + (lane & 7) * PITCH + (lane >> 3) * 16};
+        ep.has_z = pr.Z != nullptr;
+        ep.has_r = !GATED && pr.R != nullptr;
+        ep.d = ep.pt.view(pr.D, pr.ldd, pr.vec & VEC_D, m_base, n0);
+        if (ep.has_z) ep.z = ep.pt.view(pr.Z, pr.ldz, pr.vec & VEC_Z, m_base, n0);
+        if (GATED && ep.has_z) ep.u = ep.pt.view(pr.U, pr.ldu, pr.vec & VEC_U, m_base, n0);
+        if (ep.has_r) ep.r = ep.pt.view(pr.R, pr.ldr, pr.vec & VEC_R, m_base, n0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int n = n0 + 8 * j + (lane >> 2);
-        ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
+        for (int j = 0; j < 4; ++j) {
+          const int n = n0 + 8 * j + (lane >> 2);
+          ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
       }
       typename Patch<CH>::Raw raw;
       if (ep.has_r && n_in && w.slot < 0) ep.pt.fetch(raw, ep.r, group * CH);
-      const uint32_t a = acc_it & 1u;
-      if (!dead) dead = !wait_bounded(acc_full + 8 * a, (acc_it >> 1) & 1u, abort_flag, p);
+      const uint32_t a = NB == 1 ? acc_it & 1u : (uint32_t)h;
+      if (!dead) dead = !wait_bounded(acc_full + 8 * a, (NB == 1 ? acc_it >> 1 : acc_it) & 1u, abort_flag, p);
       __syncwarp();
       ptx5::fence_after_sync();
-      const EpiWarp ew{tmem + a * BM + lane_addr, bufs, bars + 16 * STAGES + 56, acc_empty + 8 * a, e, quad, group, lane, rank};
+      const EpiWarp ew{tmem + a * BM + lane_addr, bufs, bars + 16 * STAGES + 56, acc_empty + 8 * a, e, quad, group, lane, rank * NB + h};
       epilogue_unit<T, C, ACT>(p, pr, w, ep, raw, ew, rows, n_in);
+      }
     }
   }
   __syncwarp();

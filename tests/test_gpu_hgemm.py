@@ -125,6 +125,27 @@ def test_linear_large(shape, dtype):
     _linear_case(*shape, dtype, False, True, ref.GELU_TANH, True, False, True, seed=11)
 
 
+WIDE = (3700, 7900, 6300)  # long contraction, several rounds of 512 x 256 tiles, ragged in every direction
+
+
+@pytest.mark.parametrize("transa,transb", [(False, True), (True, False)])
+def test_linear_wide_tiles(transa, transb):
+    assert dg.hgemm_plan(*WIDE)["tile_cols"] == 512
+    _linear_case(*WIDE, torch.bfloat16, transa, transb, ref.NONE, True, True, True, seed=1, integer=True)
+
+
+def test_gated_wide_tiles():
+    M, F, K = 3700, 4000, 6300
+    assert dg.hgemm_plan(M, F, K, gated=True)["tile_cols"] == 256
+    _gated_case(M, F, K, torch.float16, True, ref.SILU, True, seed=2)
+    _gated_case(M, F, K, torch.bfloat16, False, ref.GELU_TANH, False, seed=3)
+
+
+def test_gradients_wide_tiles():
+    _gated_grad_case(6200, 8100, 1000, torch.bfloat16, False, ref.SILU, seed=4)
+    _linear_grad_case(7000, 6700, 7100, torch.float16, False, True, ref.NONE, seed=5)
+
+
 def test_repeated_calls_give_the_same_bits():
     """Cut tiles are added in a fixed order, whichever part finishes last."""
     g = _gen(3)
