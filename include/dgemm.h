@@ -295,8 +295,8 @@ DGEMM_API int dgemm_last_device_status(void *stream);
 /*
  * Gives the device memory the library holds on the current device back to the system: every
  * scratch lease (an 80 MiB split-K workspace and a packing buffer of up to 2.5 GiB each, as large
- * as the largest packed problem so far; up to four leases) and what the memory pool of
- * dgemm_f64_host keeps mapped (up to 1.5 GiB).
+ * as the largest packed problem so far; up to four leases), those of the operators of hgemm.h and
+ * layernorm.h, and what the memory pool of dgemm_f64_host keeps mapped (up to 1.5 GiB).
  * All of it comes back on demand. Synchronises the device first (a kernel of an earlier call may
  * still be using the memory), so it must not be called while a stream is being captured. Returns
  * DGEMM_OK, DGEMM_ERR_DEVICE or DGEMM_ERR_CUDA. No counterpart in the paper.

@@ -45,6 +45,8 @@ PTXAS_EXPECT = [
     ("dgemm_dmma_ws_kernelILb1ELi128ELb0ELb0EE", 168, 128),
     ("dgemm_dmma_ws_kernelILb1ELi64ELb0ELb0EE", 128, 128),
     ("dgemm_dmma_kernelILb1ELi64ELi64ELi128ELi0ELb0ELb0EE", 255, 64),
+    ("hgemm_tc_kernelI13__nv_bfloat16Li2ELi256ELi1ELb0ELi0EE", 168, 0),
+    ("hgemm_tc_kernelI13__nv_bfloat16Li2ELi256ELi1ELb1ELi4EE", 164, 0),
 ]
 
 

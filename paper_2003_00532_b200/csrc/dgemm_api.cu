@@ -18,6 +18,7 @@
 #include "dgemm_dmma.cuh"
 #include "dgemm_cluster.cuh"
 #include "dgemm_bulk_epi.cuh"
+#include "lm_state.h"
 #include "scratch_pool.h"
 
 namespace {
@@ -1463,6 +1464,7 @@ int dgemm_release_scratch(void) {
     return DGEMM_ERR_CUDA;
   }
   bool ok = scratch::release_all(st->scratch);
+  ok = lm::release_scratch() && ok;
   std::lock_guard<std::mutex> lock(g_mutex);
   if (st->host_pool) ok = cudaMemPoolTrimTo(st->host_pool, 0) == cudaSuccess && ok;
   if (!ok) (void)cudaGetLastError();

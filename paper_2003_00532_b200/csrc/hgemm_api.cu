@@ -507,7 +507,11 @@ int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
 
 namespace lm {
 
-EncodeTiledFn encode_tiled() { return g_encode; }
+bool release_scratch() {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
+  return !g_dev[dev].ready || scratch::release_all(g_dev[dev].scratch);
+}
 
 int device_state(DeviceState** out) {
   int dev = -1;
@@ -884,7 +888,10 @@ int hgemm_last_device_status(void* stream) {
   }
   int v = 0;
   if (cudaMemcpy(&v, st->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return DGEMM_ERR_CUDA;
-  if (v != 0 && cudaMemset(st->status, 0, sizeof(int)) != cudaSuccess) return DGEMM_ERR_CUDA;
+  // a kernel that gave up may have left tile counters behind
+  if (v != 0 && (cudaMemset(st->status, 0, sizeof(int)) != cudaSuccess ||
+                 cudaMemset(st->counters, 0, sizeof(int) * scratch::kMaxLeases * lm::kCounters) != cudaSuccess))
+    return DGEMM_ERR_CUDA;
   return v;
 }
 

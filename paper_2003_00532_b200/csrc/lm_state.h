@@ -27,10 +27,12 @@ struct DeviceState {
 // The current device's state, set up on first use. DGEMM_OK or an error code.
 int device_state(DeviceState** out);
 
+// Frees the current device's scratch leases (it has been synchronised). False if a free failed.
+bool release_scratch();
+
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                    const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                    CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled();
 
 // Launch with programmatic stream serialization (every kernel of these files waits for its
 // predecessor before its first global access); `cluster` CTAs per cluster.

@@ -142,7 +142,7 @@ def test_gated_wide_tiles():
 
 
 def test_gradients_wide_tiles():
-    _gated_grad_case(6200, 8100, 1000, torch.bfloat16, False, ref.SILU, seed=4)
+    _gated_grad_case(6200, 8100, 2000, torch.bfloat16, False, ref.SILU, seed=4)
     _linear_grad_case(7000, 6700, 7100, torch.float16, False, True, ref.NONE, seed=5)
 
 
