@@ -51,7 +51,7 @@ struct Size {
 // loads are exposed).
 double epilogue_clocks(int act, int matrices, int unaligned_out, bool unaligned_res) {
   const double f = act == HGEMM_ACT_NONE || act == HGEMM_ACT_RELU ? 0.0 : act == HGEMM_ACT_GELU ? 60.0 : 20.0;
-  return 10.0 + f + 10.0 * (matrices - 1) + 25.0 * unaligned_out + (unaligned_res ? 100.0 : 0.0);
+  return 10.0 + f + 10.0 * (matrices - 1) + 25.0 * unaligned_out + (unaligned_res ? 25.0 : 0.0);
 }
 
 struct Plan {
@@ -59,10 +59,10 @@ struct Plan {
   int clusters = 0;
   int nt = 0;
   struct Part {
-    int tiles_n, tiles_m, rounds, rest, span_len;
+    int tiles_n, tiles_m, rounds, rest, skip, span_len;
   } part[MAX_PROBLEMS];
   int rounds = 0, rest = 0;
-  int span = 0, span_total = 0;  // k-blocks per cluster and in all of the tiles left over; span 0: run whole
+  int span = 0, span_total = 0;  // positions per cluster and in all of the tiles left over; span 0: run whole
   size_t workspace = 0;          // bytes
 };
 
@@ -91,11 +91,15 @@ double step_clocks(const Config& c) {
 }
 
 // Decomposes the problems (longest contraction first) for one configuration and returns the estimated clocks: whole
-// rounds of tiles, then the tiles left over, whole or as spans of `span` k-blocks per cluster. -1: too many tiles.
+// rounds of tiles, then the tiles left over, whole or as spans of `span` positions per cluster. -1: too many tiles.
+// A position is a k-block; where products of unlike lengths share a launch, a tile whose k-blocks take less time than its
+// epilogue has positions for the rest of that time (`skip`, before its k-blocks), or a cluster's span would be a dozen
+// epilogues long and another's none (gated gradients 1 x 4485 x 1312: 91 -> 39 us, linear gradients 16 x 4096 x 4096: 80 -> 33).
 struct Layout {
   int64_t tiles[MAX_PROBLEMS], rounds[MAX_PROBLEMS], rest[MAX_PROBLEMS];
-  int64_t left, left_kblocks;
-  int clusters, nt, longest;  // longest: k-blocks of the longest tile left over
+  int64_t left, left_positions;
+  int skip[MAX_PROBLEMS], most_skip;
+  int clusters, nt, longest;  // longest: positions of the longest tile left over
   double step, epi, fixed;    // fixed: all but the tiles left over
 };
 bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out) {
@@ -105,8 +109,8 @@ bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out
   l.nt = (gated ? 64 : 128) * c.cg * c.nb;
   l.step = step_clocks(c);
   l.epi = 0.0;
-  l.left = l.left_kblocks = 0;
-  l.longest = 0;
+  l.left = l.left_positions = 0;
+  l.longest = l.most_skip = 0;
   for (int i = 0; i < n; ++i)
     if (sz[i].epilogue * c.bm > l.epi) l.epi = sz[i].epilogue * c.bm;
   l.fixed = kLaunchClocks + l.epi;
@@ -116,8 +120,11 @@ bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out
     l.rounds[i] = l.tiles[i] / l.clusters;
     l.rest[i] = l.tiles[i] % l.clusters;
     l.left += l.rest[i];
-    l.left_kblocks += l.rest[i] * sz[i].kblocks;
-    if (l.rest[i] > 0 && sz[i].kblocks > l.longest) l.longest = sz[i].kblocks;
+    const int least = (int)((sz[i].epilogue * c.bm + kUnitClocks) / l.step);
+    l.skip[i] = n > 1 && sz[i].kblocks < least ? least - sz[i].kblocks : 0;
+    l.left_positions += l.rest[i] * (sz[i].kblocks + l.skip[i]);
+    if (l.rest[i] > 0 && sz[i].kblocks + l.skip[i] > l.longest) l.longest = sz[i].kblocks + l.skip[i];
+    if (l.skip[i] > l.most_skip) l.most_skip = l.skip[i];
     // a round is as long as a tile's MMAs, or as an epilogue (which runs beside the next tile's MMAs)
     const double mma = sz[i].kblocks * l.step;
     if (c.nb == 2) l.fixed += (double)l.rounds[i] * (mma + 2 * c.bm * (kWideEpilogue + kWideShare * sz[i].epilogue));
@@ -157,7 +164,7 @@ double whole_clocks(const Layout& l, const Size* sz, int n) {
 double span_clocks(const Layout& l, const Config& c, int64_t span, bool even) {
   const double write = kPartColumn * c.bm, mma = span * l.step;
   const int64_t parts = (l.longest + span - 1) / span + (even ? 0 : 1);
-  const int64_t pieces = even ? 1 : 1 + (span * l.left + l.left_kblocks - 1) / l.left_kblocks;
+  const int64_t pieces = even ? 1 : 1 + (span * l.left + l.left_positions - 1) / l.left_positions;
   return (mma > write ? mma : write) + pieces * kUnitClocks + write + kJoinColumn * c.bm * parts + kJoinClocks;
 }
 
@@ -184,12 +191,13 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
       pick_even = even;
     };
     consider(l.fixed + (l.left > 0 ? whole_clocks(l, sz, n) : 0.0), 0, false);
-    if (l.left == 0 || l.left * kConfigs[c].cg * kConfigs[c].nb > lm::kCounters || l.left_kblocks > INT32_MAX / 2) continue;
+    if (l.left == 0 || l.left * kConfigs[c].cg * kConfigs[c].nb > lm::kCounters || l.left_positions > INT32_MAX / 2) continue;
     // equal spans over all clusters, or over half or a quarter of them where joining many parts costs more
     for (int divide = 1; divide <= 4; divide *= 2) {
-      int64_t span = (l.left_kblocks * divide + l.clusters - 1) / l.clusters;
+      int64_t span = (l.left_positions * divide + l.clusters - 1) / l.clusters;
       if (span >= l.longest) break;
-      consider(l.fixed + span_clocks(l, kConfigs[c], span, false), span, false);
+      if (span > l.most_skip)  // (no span without a k-block)
+        consider(l.fixed + span_clocks(l, kConfigs[c], span, false), span, false);
     }
     const int64_t cut = l.clusters / l.left;
     if (n == 1 && cut > 1 && l.longest > 1) {
@@ -208,7 +216,8 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
     q.tiles_m = (int)((sz[i].M + c.bm - 1) / c.bm);
     q.rounds = (int)pick.rounds[i];
     q.rest = (int)pick.rest[i];
-    q.span_len = (int)(pick_even ? (sz[i].kblocks + pick_span - 1) / pick_span * pick_span : sz[i].kblocks);
+    q.skip = pick_even ? 0 : pick.skip[i];
+    q.span_len = (int)(pick_even ? (sz[i].kblocks + pick_span - 1) / pick_span * pick_span : q.skip + sz[i].kblocks);
     pl.rounds += q.rounds;
     pl.rest += q.rest;
     if (pick_span > 0) pl.span_total += q.rest * q.span_len;
@@ -366,6 +375,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.q_mn = s.q_mn;
     d.rounds = q.rounds;
     d.rest = q.rest;
+    d.skip = q.skip;
     d.span_len = q.span_len;
     d.vec = (addressable(Matrix{s.D, s.M, s.N, s.ldd}) ? VEC_D : 0) | (addressable(Matrix{s.Z, s.M, s.N, s.ldz}) ? VEC_Z : 0) |
             (addressable(Matrix{s.U, s.M, s.N, s.ldu}) ? VEC_U : 0) | (addressable(Matrix{s.R, s.M, s.N, s.ldr}) ? VEC_R : 0);

@@ -88,7 +88,8 @@ struct alignas(64) Problem {
   int p_mn, q_mn;          // operand stored MN-major
   int rounds;              // tiles run whole in rounds over all clusters; the first `rounds` x clusters tiles
   int rest;                // tiles left over
-  int span_len;            // positions that such a tile takes among the spans: its k-blocks, or a multiple of the span
+  int skip;                // positions before such a tile's k-blocks in the spans, which stand for its epilogue's time
+  int span_len;            // positions that it takes in all: skip + its k-blocks, or a multiple of the span
   int vec;                 // which of D, Z, U, R have 16-byte aligned rows (VEC_*)
   const void* bias;
   const void* R;
@@ -102,7 +103,7 @@ struct Params {
   Problem prob[MAX_PROBLEMS];
   int nprob;
   int rounds;              // of all problems
-  int span;                // k-blocks per cluster of the tiles left over, 0: they run whole
+  int span;                // positions per cluster of the tiles left over, 0: they run whole
   int span_total;          // positions of all tiles left over
   int rest;                // tiles left over
   float* ws;               // two slots of CG x NB x BM x 128 sums per cluster
@@ -145,7 +146,7 @@ __device__ __forceinline__ bool get_work(const Params& p, int cluster, int clust
   // the span's pieces: up to the end of a tile each
   int pos = cluster * p.span;
   const int end = min(pos + p.span, p.span_total);
-  for (;; --j) {
+  for (;;) {
     if (pos >= end) return false;
     int base = 0, left = 0;  // position and index of the problem's first tile left over
     w.prob = 0;
@@ -155,13 +156,13 @@ __device__ __forceinline__ bool get_work(const Params& p, int cluster, int clust
     }
     const int kb = p.prob[w.prob].kblocks, len = p.prob[w.prob].span_len, t = (pos - base) / len;
     const int lo = base + t * len, hi = lo + len;
-    const int stop = min(hi, end);
-    if (j == 0) {
+    const int k0 = lo + p.prob[w.prob].skip, stop = min(hi, end);
+    if (stop > k0 && j-- == 0) {
       w.tile = p.prob[w.prob].rounds * clusters + t;
-      w.kb0 = pos - lo;
-      w.kb1 = min(stop - lo, kb);
+      w.kb0 = max(pos - k0, 0);
+      w.kb1 = min(stop - k0, kb);
       if (w.kb1 - w.kb0 < kb) {
-        const int c0 = lo / p.span;
+        const int c0 = k0 / p.span;
         w.left = left + t;
         w.parts = (hi - 1) / p.span - c0 + 1;
         // a cluster whose span begins inside the tile uses its first slot, the one whose span runs into it the second
@@ -275,10 +276,12 @@ struct Patch {
         o += 8 * out.ld;
       }
     } else if (lane < cols) {
+      uint16_t x[CH];
+#pragma unroll
+      for (int r = 0; r < CH; ++r) x[r] = ptx5::lds16(buf + r * PITCH + lane * 2);
 #pragma unroll
       for (int r = 0; r < CH; ++r) {
-        const uint16_t x = ptx5::lds16(buf + r * PITCH + lane * 2);
-        if (m + r < rows) *reinterpret_cast<uint16_t*>(o) = x;
+        if (m + r < rows) *reinterpret_cast<uint16_t*>(o) = x[r];
         o += out.ld;
       }
     }
@@ -290,29 +293,33 @@ struct Patch {
   struct Raw {
     uint32_t w[CH / 2];
   };
-  __device__ __forceinline__ void fetch(Raw& raw, const View& in, int m) const {
-    const char* s = in.p + m * in.ld;
-    if (in.vec) {
+  __device__ __forceinline__ void fetch(Raw& raw, const View& view, int m) const {
+    const long long in_ld = view.ld;
+    if (view.vec) {
+      const char* s = view.p + m * in_ld;
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
         uint4 x = make_uint4(0, 0, 0, 0);
         if (m + 8 * i + (lane >> 2) < rows) x = *reinterpret_cast<const uint4*>(s);
-        s += 8 * in.ld;
+        s += 8 * in_ld;
         raw.w[4 * i] = x.x;
         raw.w[4 * i + 1] = x.y;
         raw.w[4 * i + 2] = x.z;
         raw.w[4 * i + 3] = x.w;
       }
     } else {
+      // Rows beyond the matrix read its last row (a warp's first patch may begin there): no condition between the
+      // loads, or they would wait for one another.
+      const char* s = view.p + min(m, rows - 1) * in_ld;
+      uint16_t x[CH];
+      const bool in = lane < cols;
 #pragma unroll
-      for (int r = 0; r < CH; r += 2) {
-        uint32_t lo = 0, hi = 0;
-        if (m + r < rows && lane < cols) lo = *reinterpret_cast<const uint16_t*>(s);
-        s += in.ld;
-        if (m + r + 1 < rows && lane < cols) hi = *reinterpret_cast<const uint16_t*>(s);
-        s += in.ld;
-        raw.w[r / 2] = lo | hi << 16;
+      for (int r = 0; r < CH; ++r) {
+        x[r] = in ? *reinterpret_cast<const uint16_t*>(s) : (uint16_t)0;
+        if (m + r + 1 < rows) s += in_ld;
       }
+#pragma unroll
+      for (int r = 0; r < CH; r += 2) raw.w[r / 2] = (uint32_t)x[r] | (uint32_t)x[r + 1] << 16;
     }
   }
   __device__ __forceinline__ void take(const Raw& raw, bool vec, uint32_t* q) const {
