@@ -109,24 +109,29 @@ __global__ void hgemm_empty_kernel(int M, int N, const T* bias, int act, const T
 struct ActBwdParams {
   int M, N;
   int rows_per_chunk;
+  int lane_bits;    // 2^lane_bits threads to a row, 32 at most
   const void* Z;
   const void* dD;
   void* dZ;         // rows of 16-byte vectors (padding columns are written); or NULL
   float* dbias;     // or NULL
-  float* partial;   // [chunks][N]
+  float* partial;   // [chunks][N rounded up to 8]
   int* counters;    // one per strip
   long long ldz, lddd, lddz;
   int act;
   int vec_z, vec_d;  // 16-byte aligned rows
 };
 
-// dZ = dD act'(Z) (rounded) and dbias = column sums of the unrounded products. A block takes a strip of 256 columns (a lane
-// 8 of them) and a chunk of rows; its eight warps take every eighth row. The blocks' column sums
-// go to `partial`; the block that finishes a strip last adds them in order of the chunks.
+// dZ = dD act'(Z) (rounded) and dbias = column sums of the unrounded products. A block takes a strip of 64 or 256 columns
+// (a thread 8 of them; of fewer columns, fewer threads to a row and more rows at a time) and a chunk of rows. The blocks'
+// column sums go to `partial`; the block that finishes a strip last adds them up, its threads every R-th chunk each, in an
+// order that depends on the sizes alone (one thread per column for all chunks, eight rows at a time: 5451 x 280 15.4 us
+// for 8.3 now, 7269 x 70 18.6 for 9.1). Large ones stand near half of the copy rate (2088 x 4096: 18 us), held by the
+// activation's arithmetic, small ones wait for the chain load - sum - partial - join.
 template <typename T, int ACT>
 __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)[256], int* last) {
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int n = (blockIdx.x * 32 + tx) * 8;
+  const int W = 1 << p.lane_bits, R = 256 >> p.lane_bits;
+  const int tx = threadIdx.x & (W - 1), ty = threadIdx.x >> p.lane_bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = ((blockIdx.x << p.lane_bits) + tx) * 8;
   const int r0 = blockIdx.y * p.rows_per_chunk, r1 = min(p.M, r0 + p.rows_per_chunk);
   float sum[8];
 #pragma unroll
@@ -157,19 +162,19 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
     // another (four rows made so much straight code that fetching it was the limit)
     if (n + 8 <= p.N && p.vec_d && (ACT == HGEMM_ACT_NONE || p.vec_z)) {
 #pragma unroll 1
-      for (; r + 8 < r1; r += 16) {
+      for (; r + R < r1; r += 2 * R) {
         uint4 d[2], z[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          d[i] = *reinterpret_cast<const uint4*>(pd + (r + 8 * i) * p.lddd);
-          if (ACT != HGEMM_ACT_NONE) z[i] = *reinterpret_cast<const uint4*>(pz + (r + 8 * i) * p.ldz);
+          d[i] = *reinterpret_cast<const uint4*>(pd + (r + R * i) * p.lddd);
+          if (ACT != HGEMM_ACT_NONE) z[i] = *reinterpret_cast<const uint4*>(pz + (r + R * i) * p.ldz);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) one(d[i], z[i], r + 8 * i);
+        for (int i = 0; i < 2; ++i) one(d[i], z[i], r + R * i);
       }
     }
 #pragma unroll 1
-    for (; r < r1; r += 8) {
+    for (; r < r1; r += R) {
       const uint4 d = load8(pd + r * p.lddd, n, p.N, p.vec_d);
       uint4 z = d;
       if (ACT != HGEMM_ACT_NONE) z = load8(pz + r * p.ldz, n, p.N, p.vec_z);
@@ -177,18 +182,31 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
     }
   }
   if (!p.dbias) return;
+  // the sum over the rows of threads, of column threadIdx.x of the strip
+  const auto over_rows = [&]() {
+    for (int o = W; o < 32; o *= 2) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) red[ty][tx * 8 + i] = sum[i];
-  __syncthreads();
-  const int c0 = blockIdx.x * 256, c = threadIdx.x;
-  const bool in = c0 + c < p.N;
-  if (in) {
-    float s = 0.f;
-    for (int w = 0; w < 8; ++w) s += red[w][c];
-    if (gridDim.y == 1) p.dbias[c0 + c] = s;
-    else __stcg(p.partial + (long long)blockIdx.y * p.N + c0 + c, s);
+      for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+    }
+    if (lane < W) {
+      *reinterpret_cast<float4*>(&red[warp][8 * lane]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+      *reinterpret_cast<float4*>(&red[warp][8 * lane + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+    }
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) t += red[w][threadIdx.x];
+    return t;
+  };
+  const int c0 = (blockIdx.x << p.lane_bits) * 8 + threadIdx.x;
+  const bool in = (int)threadIdx.x < 8 * W && c0 < p.N;
+  const long long ld = (p.N + 7) / 8 * 8;
+  const float t = over_rows();
+  if (gridDim.y == 1) {
+    if (in) p.dbias[c0] = t;
+    return;
   }
-  if (gridDim.y == 1) return;
+  if (in) __stcg(p.partial + blockIdx.y * ld + c0, t);
   __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -197,24 +215,26 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
     if (*last) p.counters[blockIdx.x] = 0;
   }
   __syncthreads();
-  if (!*last || !in) return;
+  if (!*last) return;
   __threadfence();
-  float s = 0.f;
-  int k = 0;
-  for (; k + 8 <= (int)gridDim.y; k += 8) {
-    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = __ldcg(p.partial + (long long)(k + j) * p.N + c0 + c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s += v[j];
+  for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+  if (n < p.N) {  // (the columns beyond N, of the last 8, hold anything and are dropped)
+#pragma unroll 8
+    for (int k = ty; k < (int)gridDim.y; k += R) {
+      const float4 a = __ldcg(reinterpret_cast<const float4*>(p.partial + k * ld + n));
+      const float4 b = __ldcg(reinterpret_cast<const float4*>(p.partial + k * ld + n + 4));
+      sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w;
+      sum[4] += b.x, sum[5] += b.y, sum[6] += b.z, sum[7] += b.w;
+    }
   }
-  for (; k < (int)gridDim.y; ++k) s += __ldcg(p.partial + (long long)k * p.N + c0 + c);
-  p.dbias[c0 + c] = s;
+  const float s = over_rows();
+  if (in) p.dbias[c0] = s;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256) hgemm_act_bwd_kernel(const __grid_constant__ ActBwdParams p) {
-  __shared__ float red[8][256];
+  __shared__ __align__(16) float red[8][256];
   __shared__ int last;
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
