@@ -73,6 +73,8 @@ constexpr double kL2BytesPerClock = 43.5;  // operand bytes into one SM
 constexpr double kKBlockClocks = 510.0;    // least time of a k-block
 constexpr double kUnitClocks = 1700.0;     // start and end of a unit of work
 constexpr double kLaunchClocks = 6700.0;
+constexpr double kRoundColumn = 10.0;      // what an epilogue takes more while other tiles are on their way, per row
+                                           // (one k-block per tile: 2800, 4100, 6500 clocks a round for 64, 128, 256 rows)
 constexpr double kPartColumn = 20.0;       // a part's sums to the workspace, per row of the output
 constexpr double kJoinColumn = 8.0;        // adding one part, per row of the output
 constexpr double kJoinClocks = 4500.0;     // publishing the parts and finding the last one
@@ -94,7 +96,8 @@ double step_clocks(const Config& c) {
 // rounds of tiles, then the tiles left over, whole or as spans of `span` positions per cluster. -1: too many tiles.
 // A position is a k-block; where products of unlike lengths share a launch, a tile whose k-blocks take less time than its
 // epilogue has positions for the rest of that time (`skip`, before its k-blocks), or a cluster's span would be a dozen
-// epilogues long and another's none (gated gradients 1 x 4485 x 1312: 91 -> 39 us, linear gradients 16 x 4096 x 4096: 80 -> 33).
+// epilogues long and another's none (gated gradients 1 x 4485 x 1312: 91 -> 39 us, linear
+// gradients 16 x 4096 x 4096: 80 -> 30, 5451 x 280 x 7032: 128 -> 79).
 struct Layout {
   int64_t tiles[MAX_PROBLEMS], rounds[MAX_PROBLEMS], rest[MAX_PROBLEMS];
   int64_t left, left_positions;
@@ -114,13 +117,14 @@ bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out
   for (int i = 0; i < n; ++i)
     if (sz[i].epilogue * c.bm > l.epi) l.epi = sz[i].epilogue * c.bm;
   l.fixed = kLaunchClocks + l.epi;
+  l.epi += kRoundColumn * c.bm;
   for (int i = 0; i < n; ++i) {
     l.tiles[i] = ((sz[i].N + l.nt - 1) / l.nt) * ((sz[i].M + c.bm - 1) / c.bm);
     if (l.tiles[i] > INT32_MAX / 64) return false;
     l.rounds[i] = l.tiles[i] / l.clusters;
     l.rest[i] = l.tiles[i] % l.clusters;
     l.left += l.rest[i];
-    const int least = (int)((sz[i].epilogue * c.bm + kUnitClocks) / l.step);
+    const int least = (int)(((sz[i].epilogue + kRoundColumn) * c.bm + kUnitClocks) / l.step);
     l.skip[i] = n > 1 && sz[i].kblocks < least ? least - sz[i].kblocks : 0;
     l.left_positions += l.rest[i] * (sz[i].kblocks + l.skip[i]);
     if (l.rest[i] > 0 && sz[i].kblocks + l.skip[i] > l.longest) l.longest = sz[i].kblocks + l.skip[i];
