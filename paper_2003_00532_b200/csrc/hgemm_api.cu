@@ -51,7 +51,7 @@ struct Size {
 // loads are exposed).
 double epilogue_clocks(int act, int matrices, int unaligned_out, bool unaligned_res) {
   const double f = act == HGEMM_ACT_NONE || act == HGEMM_ACT_RELU ? 0.0 : act == HGEMM_ACT_GELU ? 60.0 : 20.0;
-  return 10.0 + f + 10.0 * (matrices - 1) + 25.0 * unaligned_out + (unaligned_res ? 25.0 : 0.0);
+  return 10.0 + f + 10.0 * (matrices - 1) + 16.0 * unaligned_out + (unaligned_res ? 13.0 : 0.0);
 }
 
 struct Plan {
@@ -278,25 +278,30 @@ class Packer {
     of_[nu_++] = n_++;
   }
   size_t bytes() const { return bytes_; }
-  bool launch(char* buf, cudaStream_t stream) {
-    if (n_ == 0) return true;
+  // The copies into `buf`, a block for 256 vectors each up to eight blocks per SM; from here on the operands are the copies.
+  PackOps finish(char* buf) {
     PackOps ops;
     memset(&ops, 0, sizeof(ops));
-    int64_t most = 0;  // vectors of the largest matrix
     for (int i = 0; i < n_; ++i) {
       const Matrix& m = src_[i];
       ops.op[i] = PackOp{static_cast<const uint16_t*>(m.ptr), m.ld, (int)m.rows, (int)m.cols,
                          reinterpret_cast<uint16_t*>(buf + at_[i]), padded(m.cols)};
-      if ((m.cols + 7) / 8 * m.rows > most) most = (m.cols + 7) / 8 * m.rows;
+      const int64_t blocks = ((m.cols + 7) / 8 * m.rows + 255) / 256;
+      blocks_ += (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
+      ops.end[i] = blocks_;
     }
-    const int64_t blocks = (most + 255) / 256;
-    if (!lm::launch(hgemm_pack_kernel, dim3((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), (unsigned)n_), dim3(256), 0, 1, stream, ops)) return false;
     for (int i = 0; i < nu_; ++i) *users_[i] = Matrix{buf + at_[of_[i]], users_[i]->rows, users_[i]->cols, padded(users_[i]->cols)};
-    return true;
+    return ops;
+  }
+  unsigned blocks() const { return blocks_; }  // after finish()
+  bool launch(char* buf, cudaStream_t stream) {
+    const PackOps ops = finish(buf);
+    return blocks_ == 0 || lm::launch(hgemm_pack_kernel, dim3(blocks_), dim3(256), 0, 1, stream, ops);
   }
 
  private:
   size_t bytes_;
+  unsigned blocks_ = 0;
   int n_ = 0, nu_ = 0;
   Matrix src_[3];
   size_t at_[3];
@@ -727,9 +732,13 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
   if (want_act) {
     ap.partial = ws;
     ap.counters = counters;
-    const dim3 grid((unsigned)strips, (unsigned)chunks);
-    const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, ap)
-                                            : lm::launch(hgemm_act_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, ap);
+    // the operands that TMA cannot address are copied by further blocks of the same launch
+    ap.strips = (unsigned)strips;
+    ap.chunks = (unsigned)chunks;
+    const PackOps ops = pack.finish(buf);
+    const dim3 grid((unsigned)(strips * chunks) + pack.blocks());
+    const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, ap, ops)
+                                            : lm::launch(hgemm_act_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, ap, ops);
     if (!ok) return DGEMM_ERR_CUDA;
   }
   if (n == 0) return DGEMM_OK;
@@ -738,7 +747,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     if (want_a) (transa ? pa.p[0] : pa.q[0]) = packed;
     if (want_b) (transb ? pb.q[0] : pb.p[0]) = packed;
   }
-  if (!pack.launch(buf, s)) return DGEMM_ERR_CUDA;
+  if (!want_act && !pack.launch(buf, s)) return DGEMM_ERR_CUDA;
   return run_products(type, false, list, n, pl, st, ws, counters, s);
 }
 
@@ -888,10 +897,12 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   gp.vec_h = addressable(Matrix{dH, M, F, lddh});
   int64_t blocks = ((F + 7) / 8 * M + 255) / 256;
   if (blocks > (int64_t)st->sm_count * 16) blocks = (int64_t)st->sm_count * 16;
-  const dim3 grid((unsigned)blocks);
-  const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, gp)
-                                          : lm::launch(hgemm_gated_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, gp);
-  if (!ok || !pack.launch(buf, s)) return DGEMM_ERR_CUDA;
+  gp.blocks = (unsigned)blocks;
+  const PackOps ops = pack.finish(buf);  // copied by further blocks of the same launch
+  const dim3 grid((unsigned)blocks + pack.blocks());
+  const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, gp, ops)
+                                          : lm::launch(hgemm_gated_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, gp, ops);
+  if (!ok) return DGEMM_ERR_CUDA;
   for (int i = 0; i < 2; ++i) {
     px.p[i] = w[i];
     px.q[i] = dgu[i];

@@ -21,6 +21,7 @@ struct PackOp {
 };
 struct PackOps {
   PackOp op[3];
+  unsigned end[3];  // the first block that is not op i's (nor an earlier one's)
 };
 
 // 8 values of 16 bits at src[0 .. 8), the columns c .. of a row of `cols`; those beyond the row are zero. An aligned vector
@@ -63,20 +64,28 @@ __device__ __forceinline__ uint4 pack8(const float* v) {
   return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
 }
 
-// Copies up to three matrices (blockIdx.y) into 16-byte aligned rows, a vector of 8 values per thread. (One value per
-// thread and block row: 17 us for 1000 x 777 and 777 x 1537, this 4 us.)
-__global__ void __launch_bounds__(256) hgemm_pack_kernel(const __grid_constant__ PackOps ops) {
-  ptx5::launch_dependents();
-  dgemm::ptx::grid_dependency_wait();
-  const PackOp& o = ops.op[blockIdx.y];
+// Copies up to three matrices into 16-byte aligned rows, a vector of 8 values per thread; `block` counts the blocks of all of
+// them. (One value per thread and block row: 17 us for 1000 x 777 and 777 x 1537, this 4 us.)
+__device__ __forceinline__ void pack_body(const PackOps& ops, unsigned block) {
+  int k = 0;
+  while (block >= ops.end[k]) ++k;
+  const unsigned first = k ? ops.end[k - 1] : 0;
+  const PackOp& o = ops.op[k];
   const int per_row = (o.cols + 7) / 8;
-  const long long total = (long long)per_row * o.rows;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+  const long long total = (long long)per_row * o.rows, step = (long long)(ops.end[k] - first) * blockDim.x;
+  for (long long i = (long long)(block - first) * blockDim.x + threadIdx.x; i < total; i += step) {
     const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 8;
     const uint16_t* src = o.src + r * o.ld_src + c;
     const uint4 v = load8(src, c, o.cols, false);
     *reinterpret_cast<uint4*>(o.dst + r * o.ld_dst + c) = v;
   }
+}
+// (Forward. The gradients' copies are blocks of the element-wise kernels below: a launch of their own cost 2 to 3 us,
+// 333 x 1537 x 1000 29.1 -> 27.2, 24 x 138 x 512 9.5 -> 7.1.)
+__global__ void __launch_bounds__(256) hgemm_pack_kernel(const __grid_constant__ PackOps ops) {
+  ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  pack_body(ops, blockIdx.x);
 }
 
 // ---- empty sums -----------------------------------------------------------------------------------
@@ -110,6 +119,7 @@ struct ActBwdParams {
   int M, N;
   int rows_per_chunk;
   int lane_bits;    // 2^lane_bits threads to a row, 32 at most
+  unsigned strips, chunks;  // one block each; the blocks beyond copy operands
   const void* Z;
   const void* dD;
   void* dZ;         // rows of 16-byte vectors (padding columns are written); or NULL
@@ -129,10 +139,11 @@ struct ActBwdParams {
 // activation's arithmetic, small ones wait for the chain load - sum - partial - join.
 template <typename T, int ACT>
 __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)[256], int* last) {
+  const unsigned strip = blockIdx.x % p.strips, chunk = blockIdx.x / p.strips;
   const int W = 1 << p.lane_bits, R = 256 >> p.lane_bits;
   const int tx = threadIdx.x & (W - 1), ty = threadIdx.x >> p.lane_bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int n = ((blockIdx.x << p.lane_bits) + tx) * 8;
-  const int r0 = blockIdx.y * p.rows_per_chunk, r1 = min(p.M, r0 + p.rows_per_chunk);
+  const int n = ((strip << p.lane_bits) + tx) * 8;
+  const int r0 = chunk * p.rows_per_chunk, r1 = min(p.M, r0 + p.rows_per_chunk);
   float sum[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum[i] = 0.f;
@@ -198,21 +209,21 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
     for (int w = 0; w < 8; ++w) t += red[w][threadIdx.x];
     return t;
   };
-  const int c0 = (blockIdx.x << p.lane_bits) * 8 + threadIdx.x;
+  const int c0 = (strip << p.lane_bits) * 8 + threadIdx.x;
   const bool in = (int)threadIdx.x < 8 * W && c0 < p.N;
   const long long ld = (p.N + 7) / 8 * 8;
   const float t = over_rows();
-  if (gridDim.y == 1) {
+  if (p.chunks == 1) {
     if (in) p.dbias[c0] = t;
     return;
   }
-  if (in) __stcg(p.partial + blockIdx.y * ld + c0, t);
+  if (in) __stcg(p.partial + chunk * ld + c0, t);
   __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) {
-    const int old = atomicAdd(p.counters + blockIdx.x, 1);
-    *last = old == (int)gridDim.y - 1;
-    if (*last) p.counters[blockIdx.x] = 0;
+    const int old = atomicAdd(p.counters + strip, 1);
+    *last = old == (int)p.chunks - 1;
+    if (*last) p.counters[strip] = 0;
   }
   __syncthreads();
   if (!*last) return;
@@ -221,7 +232,7 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
   for (int i = 0; i < 8; ++i) sum[i] = 0.f;
   if (n < p.N) {  // (the columns beyond N, of the last 8, hold anything and are dropped)
 #pragma unroll 8
-    for (int k = ty; k < (int)gridDim.y; k += R) {
+    for (int k = ty; k < (int)p.chunks; k += R) {
       const float4 a = __ldcg(reinterpret_cast<const float4*>(p.partial + k * ld + n));
       const float4 b = __ldcg(reinterpret_cast<const float4*>(p.partial + k * ld + n + 4));
       sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w;
@@ -233,11 +244,15 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) hgemm_act_bwd_kernel(const __grid_constant__ ActBwdParams p) {
+__global__ void __launch_bounds__(256) hgemm_act_bwd_kernel(const __grid_constant__ ActBwdParams p, const __grid_constant__ PackOps ops) {
   __shared__ __align__(16) float red[8][256];
   __shared__ int last;
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
+  if (blockIdx.x >= p.strips * p.chunks) {
+    pack_body(ops, blockIdx.x - p.strips * p.chunks);
+    return;
+  }
   switch (p.act) {
     case HGEMM_ACT_RELU: act_bwd_body<T, HGEMM_ACT_RELU>(p, red, &last); break;
     case HGEMM_ACT_GELU: act_bwd_body<T, HGEMM_ACT_GELU>(p, red, &last); break;
@@ -257,6 +272,7 @@ struct GatedBwdParams {
   long long ldg, ldu, lddh, ldo;  // ldo: of dG and dU
   int act;
   int vec_g, vec_u, vec_h;  // 16-byte aligned rows
+  unsigned blocks;          // the blocks beyond copy operands
 };
 
 // dG = dH U act'(G), dU = dH act(G); both rounded. One thread per 8 columns of a row.
@@ -265,7 +281,7 @@ __device__ __forceinline__ void gated_bwd_body(const GatedBwdParams& p) {
   const int per_row = (p.F + 7) / 8;
   const bool vec = p.vec_g && p.vec_u && p.vec_h;
   const long long total = (long long)per_row * p.M;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)p.blocks * blockDim.x) {
     const int r = (int)(i / per_row), f = (int)(i - (long long)r * per_row) * 8;
     const uint16_t* pg = static_cast<const uint16_t*>(p.G) + r * p.ldg + f;
     const uint16_t* pu = static_cast<const uint16_t*>(p.U) + r * p.ldu + f;
@@ -297,9 +313,13 @@ __device__ __forceinline__ void gated_bwd_body(const GatedBwdParams& p) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) hgemm_gated_bwd_kernel(const __grid_constant__ GatedBwdParams p) {
+__global__ void __launch_bounds__(256) hgemm_gated_bwd_kernel(const __grid_constant__ GatedBwdParams p, const __grid_constant__ PackOps ops) {
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
+  if (blockIdx.x >= p.blocks) {
+    pack_body(ops, blockIdx.x - p.blocks);
+    return;
+  }
   switch (p.act) {
     case HGEMM_ACT_RELU: gated_bwd_body<T, HGEMM_ACT_RELU>(p); break;
     case HGEMM_ACT_GELU: gated_bwd_body<T, HGEMM_ACT_GELU>(p); break;

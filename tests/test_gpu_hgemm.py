@@ -383,6 +383,23 @@ def test_gated_gradients_large():
     _gated_grad_case(2048, 4096, 1024, torch.bfloat16, True, ref.SILU, seed=2)
 
 
+@pytest.mark.parametrize("transw", [False, True])
+@pytest.mark.parametrize("shape", [(1, 1485, 1312), (12, 2408, 1874), (130, 3100, 200), (700, 130, 2600)])
+def test_gradients_of_unlike_contractions_share_a_launch(shape, transw):
+    """Few long sums beside many tiles of one or two k-blocks, and the other way round: spans that hold several tiles."""
+    M, F, K = shape
+    _gated_grad_case(M, F, K, torch.bfloat16, transw, ref.SILU, seed=M)
+    _linear_grad_case(M, F, K, torch.float16, False, transw, ref.GELU_TANH, seed=M)
+    _linear_grad_case(M, F, K, torch.float16, True, transw, ref.RELU, seed=M, integer=True, pad=3)
+
+
+@pytest.mark.parametrize("N", [1, 8, 9, 63, 64, 65, 130, 520])
+@pytest.mark.parametrize("M", [1, 31, 600, 9000])
+def test_bias_gradient_over_strips_and_chunks(M, N):
+    _linear_grad_case(M, N, 16, torch.bfloat16, False, True, ref.RELU, seed=N, integer=True, want=("dA", "dbias"))
+    _linear_grad_case(M, N, 16, torch.float16, False, True, ref.SILU, seed=N, want=("dbias",), pad=1)
+
+
 # ---- streams, refusals, abort path -----------------------------------------------------------------------
 
 def test_calls_on_several_streams_do_not_share_scratch():
