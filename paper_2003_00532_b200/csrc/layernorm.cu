@@ -270,19 +270,21 @@ int layernorm_bwd(int type, int64_t rows, int64_t cols, const void* X, int64_t l
   p.mean = const_cast<float*>(mean);
   p.rstd = const_cast<float*>(rstd);
   p.want_params = dgamma || dbeta;
+  p.ldp = (cols + 3) / 4 * 4;
   const bool aligned = rows_aligned(type, X, ldx) && rows_aligned(type, dY, lddy) && (!dX || rows_aligned(type, dX, lddx)) &&
                        ((uintptr_t)gamma & 15) == 0;
   scratch::Hold hold(st->scratch, s);
   const auto partial = [&](int blocks) {
-    if (p.want_params) p.partial = static_cast<float*>(hold.workspace((size_t)2 * blocks * cols * 4));
+    if (p.want_params) p.partial = static_cast<float*>(hold.workspace((size_t)2 * blocks * p.ldp * 4));
     return !p.want_params || p.partial != nullptr;
   };
   const int blocks = type == HGEMM_TYPE_F32   ? run_bwd<float, 4>(st->sm_count, aligned, p, s, partial)
                      : type == HGEMM_TYPE_F16 ? run_bwd<__half, 8>(st->sm_count, aligned, p, s, partial)
                                               : run_bwd<__nv_bfloat16, 8>(st->sm_count, aligned, p, s, partial);
   if (blocks == 0) return DGEMM_ERR_CUDA;
-  if (p.want_params && !lm::launch(bwd_reduce_kernel, dim3((unsigned)((cols + 31) / 32), 2), dim3(512), 0, 1, s,
-                                   (const float*)p.partial, blocks, (int)cols, dgamma, dbeta))
+  const bool many = blocks > MANY_BLOCKS;
+  if (p.want_params && !lm::launch(many ? bwd_reduce_kernel<32> : bwd_reduce_kernel<16>, dim3((unsigned)((cols + 31) / 32), 2),
+                                   dim3(many ? 1024 : 512), 0, 1, s, (const float*)p.partial, blocks, (int)cols, (int)p.ldp, dgamma, dbeta))
     return DGEMM_ERR_CUDA;
   return DGEMM_OK;
 }
