@@ -69,14 +69,28 @@ Shape bwd_shape(int64_t cols, int vec) {
   return Shape{0, 1024, true};
 }
 
+// Raises the kernel's limit of dynamic shared memory to `bytes`, the most that any call asks for, once per device and before
+// its first launch or occupancy query whatever that one asks for: without it static and dynamic memory together stop at 48 KB.
+template <typename K, K kernel>
+bool allow_smem(int bytes) {
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  if (!done[dev].load()) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done[dev].store(true);
+  }
+  return true;
+}
+
 // Blocks of one kernel (one instance of this function per kernel) that fit on the device at once, or fewer
-// for few rows. `smem` is the most that the kernel is launched with.
+// for few rows; 0 on failure. `smem` is the most that the kernel is launched with.
 template <typename K, K kernel>
 unsigned resident_blocks(int sms, int threads, size_t smem, int64_t need) {
   static std::atomic<int> known[33];  // by warps per block; the same on every device of this kind
   int per_sm = known[threads / 32].load();
   if (per_sm == 0) {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) per_sm = 1;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) return 0;
     known[threads / 32].store(per_sm);
   }
   return (unsigned)(need < (int64_t)sms * per_sm ? need : (int64_t)sms * per_sm);
@@ -86,19 +100,10 @@ template <typename T, int VEC, int ITEMS, bool WARP_ROW>
 bool launch_fwd(int sms, int threads, const Params& p, cudaStream_t stream) {
   constexpr auto kernel = &fwd_kernel<T, VEC, ITEMS, WARP_ROW>;
   const size_t smem = (size_t)(WARP_ROW ? 32 : threads) * ITEMS * VEC * 8;  // gamma and beta
-  if (smem > 48 * 1024) {
-    static std::atomic<bool> configured[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
-    if (!configured[dev].load()) {
-      constexpr int limit = fwd_threads(VEC * ITEMS) * ITEMS * VEC * 8;
-      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return false;
-      configured[dev].store(true);
-    }
-  }
+  if (!WARP_ROW && !allow_smem<decltype(kernel), kernel>(fwd_threads(VEC * ITEMS) * ITEMS * VEC * 8)) return false;
   const int64_t need = WARP_ROW ? (p.rows + 3) / 4 : p.rows;
   const unsigned blocks = resident_blocks<decltype(kernel), kernel>(sms, threads, smem, need);
-  return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p);
+  return blocks > 0 && lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p);
 }
 template <typename T, int VEC, int ITEMS>
 bool launch_fwd_items(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
@@ -139,19 +144,10 @@ template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE, typename F>
 int launch_bwd(int sms, int threads, Params& p, cudaStream_t stream, F partial) {
   constexpr auto kernel = &bwd_kernel<T, VEC, ITEMS, WARP_ROW, WIDE>;
   const size_t smem = WIDE ? (size_t)threads * ITEMS * VEC * 12 : WARP_ROW && p.want_params ? (size_t)p.cols * 8 : 0;
-  if (WIDE) {
-    static std::atomic<bool> configured[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    if (!configured[dev].load()) {
-      constexpr int limit = BWD_THREADS * ITEMS * VEC * 12;
-      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return 0;
-      configured[dev].store(true);
-    }
-  }
+  if (WIDE && !allow_smem<decltype(kernel), kernel>(BWD_THREADS * ITEMS * VEC * 12)) return 0;
   const size_t most = WIDE ? smem : WARP_ROW ? (size_t)32 * ITEMS * VEC * 8 : 0;
   const int blocks = bwd_blocks<decltype(kernel), kernel>(sms, threads, most, p.rows, WARP_ROW ? 8 : 1);
-  if (!partial(blocks)) return 0;
+  if (blocks == 0 || !partial(blocks)) return 0;
   return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p) ? blocks : 0;
 }
 template <typename T, int VEC, typename F>
