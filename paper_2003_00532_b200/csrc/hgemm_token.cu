@@ -9,12 +9,10 @@ namespace hgemm {
 
 namespace {
 
-constexpr size_t kStatic = 48 * 1024;
-
-// Raises the kernel's shared-memory limit once per device where a call needs it.
+// Raises the kernel's limit of dynamic shared memory to the most that a call asks for, once per device and before its first
+// launch whatever that one asks for: without it static and dynamic memory together stop at 48 KB.
 template <typename K, K kernel>
-bool allow(size_t smem) {
-  if (smem <= kStatic) return true;
+bool allow_smem() {
   static std::atomic<bool> done[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
@@ -29,7 +27,7 @@ template <typename T, int MT, bool GATED>
 bool run(TokenParams p, int sms, cudaStream_t stream) {
   constexpr auto kernel = &hgemm_token_kernel<T, MT, GATED>;
   const size_t smem = (size_t)MT * ((p.K + 7) / 8 * 8) * sizeof(T);
-  if (!allow<decltype(kernel), kernel>(smem)) return false;
+  if (!allow_smem<decltype(kernel), kernel>()) return false;
   // enough warps for 16 per SM; a warp's share of k is at least one load of every lane
   const int cols = GATED ? 1 : 2;
   const long long pairs = (p.N + cols - 1) / cols;
