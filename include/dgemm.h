@@ -111,7 +111,9 @@ enum {
  * stream outside stream capture. As long as all calls on a device come from one stream nothing
  * else synchronises; the first call on a second stream synchronises the device once. Calls
  * recorded into a CUDA graph use the lease their stream had at capture time; replays of the graph
- * are not covered by the guarantee above and must not overlap other calls that use scratch.
+ * are not covered by the guarantee above and must not overlap other calls that use scratch. The
+ * scratch that a recorded call uses stays allocated, whatever later calls need, until
+ * dgemm_release_scratch; no graph recorded before that call may be replayed after it.
  *
  * The kernels are launched with programmatic stream serialization: their thread blocks may be
  * scheduled while the previous kernel in `stream` is finishing, but they wait for its completion
@@ -298,7 +300,8 @@ DGEMM_API int dgemm_last_device_status(void *stream);
  * as the largest packed problem so far; up to four leases), those of the operators of hgemm.h and
  * layernorm.h, and what the memory pool of dgemm_f64_host keeps mapped (up to 1.5 GiB).
  * All of it comes back on demand. Synchronises the device first (a kernel of an earlier call may
- * still be using the memory), so it must not be called while a stream is being captured. Returns
+ * still be using the memory), so it must not be called while a stream is being captured, and graphs
+ * captured before it must not be replayed after it (they hold the freed addresses). Returns
  * DGEMM_OK, DGEMM_ERR_DEVICE or DGEMM_ERR_CUDA. No counterpart in the paper.
  */
 DGEMM_API int dgemm_release_scratch(void);

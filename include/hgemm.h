@@ -13,7 +13,8 @@
  * address (16-byte aligned, leading dimension a multiple of 8) are used where they lie; others are
  * first rewritten into scratch memory of the library (leased per call as for dgemm_f64: calls may be
  * in flight on several streams; it is grown with a synchronising cudaMalloc, so make a stream's
- * first call of a size outside stream capture; dgemm_release_scratch frees it). Only the logical part of a matrix is read or written.
+ * first call of a size outside stream capture; what a captured call uses stays allocated, whatever later calls need, until
+ * dgemm_release_scratch, after which the graph must not be replayed). Only the logical part of a matrix is read or written.
  * All calls are asynchronous on `stream` (a cudaStream_t passed as void*; NULL is the legacy default
  * stream) and give the same bits every time for the same arguments.
  */

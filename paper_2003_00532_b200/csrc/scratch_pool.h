@@ -18,7 +18,9 @@
 //
 // Stream capture: no event is recorded or queried on a capturing stream and nothing is allocated
 // (allocation would invalidate the capture): a captured call uses the lease of its stream, or
-// the first lease, as it stands. Replays of such a graph are outside the guarantee above.
+// the first lease, as it stands. Replays of such a graph are outside the guarantee above. The graph
+// keeps the addresses that the call was given, so a buffer that was handed to a captured call is never
+// freed when its lease grows: it is set aside until release_all.
 //
 // Host only; plain CUDA runtime calls. Used by the FP64 and the FP32 halves of the library, each
 // with a pool array of its own.
@@ -26,6 +28,7 @@
 
 #include <cstddef>
 #include <mutex>
+#include <new>
 
 #include <cuda_runtime.h>
 
@@ -38,11 +41,18 @@ struct Lease {
   size_t workspace_bytes = 0;
   void* pack = nullptr;
   size_t pack_bytes = 0;
+  bool captured[2] = {false, false};  // workspace, pack: a graph may hold the buffer's address
   cudaEvent_t done = nullptr;       // behind the last kernel that used the lease (multi-stream mode only)
   bool recorded = false;            // `done` has been recorded at least once since the lease was last free for sure
   cudaStream_t last_stream = nullptr;
   bool used = false;
   unsigned long long tick = 0;      // order of last use
+};
+
+// A buffer that a lease has outgrown and a graph may still refer to.
+struct Retired {
+  void* buf;
+  Retired* next;
 };
 
 struct Pool {
@@ -53,6 +63,7 @@ struct Pool {
   cudaStream_t only_stream = nullptr;
   bool any_use = false;
   unsigned long long tick = 0;
+  Retired* retired = nullptr;
 };
 
 enum Kind { kWorkspace = 0, kPack = 1 };
@@ -117,6 +128,7 @@ class Hold {
   bool acquire(Kind kind, size_t bytes) {
     pool_.mu.lock();
     Lease* pick = nullptr;
+    in_capture_ = is_capturing();
     if (!pool_.multi_stream) {
       if (!pool_.any_use || stream_ == pool_.only_stream) {
         // (a first-ever call under capture will fail at its allocation, like any allocation under capture)
@@ -125,7 +137,7 @@ class Hold {
           pool_.any_use = true;
           pool_.only_stream = stream_;
         }
-      } else if ((capturing_ = is_capturing())) {
+      } else if ((capturing_ = in_capture_)) {
         pick = pool_.count > 0 ? &pool_.lease[0] : new_lease();
       } else {
         // A second stream. Nothing has recorded events so far, so let everything issued up to now
@@ -142,7 +154,7 @@ class Hold {
         }
       }
     } else {
-      capturing_ = is_capturing();
+      capturing_ = in_capture_;
     }
     if (!pick && capturing_) {
       for (int i = 0; i < pool_.count && !pick; ++i)
@@ -202,34 +214,51 @@ class Hold {
     return true;
   }
 
+  // Sets `buf` aside until release_all. False if there is no host memory left for the note of it.
+  bool retire(void* buf) {
+    Retired* r = new (std::nothrow) Retired{buf, pool_.retired};
+    if (r) pool_.retired = r;
+    return r != nullptr;
+  }
+
   void* get(Kind kind, size_t bytes, size_t head_room) {
     if (!lease_ && !acquire(kind, bytes)) return nullptr;
     void*& buf = kind == kWorkspace ? lease_->workspace : lease_->pack;
     size_t& have = kind == kWorkspace ? lease_->workspace_bytes : lease_->pack_bytes;
-    if (have >= bytes) return buf;
-    if (capturing_) return nullptr;  // growing means allocating, which a capture does not survive
-    if (buf) {
-      // the buffer being replaced may still be read by this stream's earlier kernels (no other
-      // stream can hold this lease): let them finish before it is freed
-      if (cudaStreamSynchronize(stream_) != cudaSuccess) (void)cudaGetLastError();
-      cudaFree(buf);
-      buf = nullptr;
-      have = 0;
+    bool& captured = lease_->captured[kind];
+    if (have < bytes) {
+      if (capturing_) return nullptr;  // growing means allocating, which a capture does not survive
+      if (buf && !captured && !in_capture_) {
+        // the buffer being replaced may still be read by this stream's earlier kernels (no other
+        // stream can hold this lease): let them finish before it is freed
+        if (cudaStreamSynchronize(stream_) != cudaSuccess) (void)cudaGetLastError();
+        cudaFree(buf);
+        buf = nullptr;
+        have = 0;
+      }
+      const size_t want = bytes + head_room;
+      void* grown = nullptr;
+      if (cudaMalloc(&grown, want) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return nullptr;
+      }
+      if (buf && !retire(buf)) {
+        cudaFree(grown);
+        return nullptr;
+      }
+      buf = grown;
+      have = want;
+      captured = false;
     }
-    const size_t want = bytes + head_room;
-    if (cudaMalloc(&buf, want) != cudaSuccess) {
-      (void)cudaGetLastError();
-      buf = nullptr;
-      return nullptr;
-    }
-    have = want;
+    if (in_capture_) captured = true;
     return buf;
   }
 
   Pool& pool_;
   cudaStream_t stream_;
   Lease* lease_ = nullptr;
-  bool capturing_ = false;
+  bool in_capture_ = false;  // the stream is being captured
+  bool capturing_ = false;   // ... and it is not the only stream that the pool has seen: nothing but a lease as it stands is used
 };
 
 // Frees everything the pool holds and returns it to its initial single-stream state. The caller
@@ -243,6 +272,12 @@ inline bool release_all(Pool& pool) {
     if (l.pack) ok = cudaFree(l.pack) == cudaSuccess && ok;
     if (l.done) ok = cudaEventDestroy(l.done) == cudaSuccess && ok;
     l = Lease();
+  }
+  while (pool.retired) {
+    Retired* r = pool.retired;
+    pool.retired = r->next;
+    ok = cudaFree(r->buf) == cudaSuccess && ok;
+    delete r;
   }
   pool.count = 0;
   pool.multi_stream = false;
