@@ -73,7 +73,9 @@ DGEMM_API int hgemm_epilogue(int type, int transa, int transb, int64_t M, int64_
  *   dA, dB, dbias  outputs, each NULL if not wanted; dbias is N binary32 values, summed in binary32
  *
  * dZ enters the products rounded to `type`: the tensor cores take 16-bit operands. That rounding is
- * of the size of the outputs' own; dbias sums the unrounded values.
+ * of the size of the outputs' own; dbias sums the unrounded values. In binary16 a dZ whose largest finite
+ * magnitude lies outside [2^-4, 65520) is scaled by a power of two before it is rounded, and the products
+ * back, so that its range is no limit of theirs (values below 2^-28 of the largest lose bits).
  * M == 0 gives dB = 0 and dbias = 0, N == 0 gives dA = 0.
  */
 DGEMM_API int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, int64_t K,
@@ -97,7 +99,8 @@ DGEMM_API int hgemm_gated(int type, int transw, int64_t M, int64_t F, int64_t K,
  * Gradients of hgemm_gated for an incoming dH (M x F):
  *   dG = dH * U * act'(G),  dU = dH * act(G),
  *   dX = dG op(Wg)^T + dU op(Wu)^T (one sum, rounded once),  dWg = X^T dG,  dWu = X^T dU (stored as Wg and Wu are).
- * dX, dWg, dWu: outputs, each NULL if not wanted. dG and dU enter the products rounded to `type`.
+ * dX, dWg, dWu: outputs, each NULL if not wanted. dG and dU enter the products rounded to `type`, in
+ * binary16 scaled together as dZ above.
  */
 DGEMM_API int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K,
                               const void *X, int64_t ldx, const void *Wg, int64_t ldwg, const void *Wu, int64_t ldwu,

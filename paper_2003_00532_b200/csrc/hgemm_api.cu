@@ -365,7 +365,7 @@ bool plan_products(Product** pr, int n, bool gated, int sms, Plan* pl) {
 }
 
 int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::DeviceState* st, float* ws, int* counters,
-                 cudaStream_t stream) {
+                 cudaStream_t stream, const float* unscale = nullptr) {
   const Config& c = kConfigs[pl.config];
   Params p;
   memset(&p, 0, sizeof(p));
@@ -414,6 +414,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
   p.wait_limit_ns = drop > 0 ? (unsigned long long)drop * 1000ull : kWaitLimitNs;
   p.drop = drop > 0;
   p.status = st->status;
+  p.unscale = unscale;
   return launch_tc(type, gated, pr[0]->act, pl.config, pl.clusters, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
 }
 
@@ -501,6 +502,15 @@ int run_token(int type, bool gated, const Product& s, int sms, cudaStream_t stre
   p.ldz = s.ldz;
   p.ldu = s.ldu;
   return launch_token(type, gated, sms, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
+}
+
+// The range of a binary16 gradient part stored by `blocks` blocks takes range_bytes of scratch at the 4-byte aligned `at`.
+size_t range_bytes(int64_t blocks) { return (size_t)(blocks + 1) * 4; }
+PartRange range_at(char* at) { return PartRange{reinterpret_cast<float*>(at), reinterpret_cast<unsigned*>(at) + 1}; }
+// Blocks of the kernel that scales it.
+unsigned rescale_blocks(const lm::DeviceState* st, int64_t rows, int64_t cols) {
+  const int64_t need = ((cols + 7) / 8 * rows + 255) / 256, most = (int64_t)st->sm_count * 4;
+  return (unsigned)(need < most ? need : most);
 }
 
 // Packs what needs it and runs the products: the whole of a forward call.
@@ -691,8 +701,6 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
   Packer pack(want_dz ? (size_t)M * lddz * 2 : 0);
   if (want_a) pack.add(transa ? &pa.q[0] : &pa.p[0]);
   if (want_b) pack.add(transb ? &pb.p[0] : &pb.q[0]);
-  char* buf = nullptr;
-  if (pack.bytes() > 0 && !(buf = static_cast<char*>(hold.pack_buffer(pack.bytes())))) return DGEMM_ERR_CUDA;
 
   // dZ and dbias
   const bool want_act = want_dz || dbias;
@@ -717,13 +725,19 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     ap.N = (int)N;
     ap.Z = act != HGEMM_ACT_NONE ? Z : nullptr;
     ap.dD = dD;
-    ap.dZ = want_dz ? buf : nullptr;
     ap.dbias = dbias;
     ap.ldz = ldz;
     ap.lddd = lddd;
     ap.lddz = lddz;
     ap.act = act;
   }
+  // (without activation or with ReLU dZ's values are dD's own or zero)
+  const bool ranged = want_dz && type == HGEMM_TYPE_F16 && act != HGEMM_ACT_NONE && act != HGEMM_ACT_RELU;
+  const size_t pack_bytes = pack.bytes() + (ranged ? range_bytes(strips * chunks) : 0);
+  char* buf = nullptr;
+  if (pack_bytes > 0 && !(buf = static_cast<char*>(hold.pack_buffer(pack_bytes)))) return DGEMM_ERR_CUDA;
+  if (want_dz) ap.dZ = buf;
+  if (ranged) ap.range = range_at(buf + pack.bytes());
   size_t ws_bytes = n > 0 ? pl.workspace : 0;
   if (dbias && chunks > 1 && (size_t)chunks * (N + 7) * 4 > ws_bytes) ws_bytes = (size_t)chunks * (N + 7) * 4;
   float* ws = nullptr;
@@ -740,6 +754,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, ap, ops)
                                             : lm::launch(hgemm_act_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, ap, ops);
     if (!ok) return DGEMM_ERR_CUDA;
+    if (ranged && !lm::launch(hgemm_act_rescale_kernel, dim3(rescale_blocks(st, M, N)), dim3(256), 0, 1, s, ap)) return DGEMM_ERR_CUDA;
   }
   if (n == 0) return DGEMM_OK;
   if (want_dz) {
@@ -748,7 +763,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     if (want_b) (transb ? pb.q[0] : pb.p[0]) = packed;
   }
   if (!want_act && !pack.launch(buf, s)) return DGEMM_ERR_CUDA;
-  return run_products(type, false, list, n, pl, st, ws, counters, s);
+  return run_products(type, false, list, n, pl, st, ws, counters, s, ap.range.inverse);
 }
 
 int hgemm_gated(int type, int transw, int64_t M, int64_t F, int64_t K, const void* X, int64_t ldx, const void* Wg, int64_t ldwg,
@@ -872,7 +887,10 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
     pack.add(&w[0]);
     pack.add(&w[1]);
   }
-  char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes()));
+  int64_t blocks = ((F + 7) / 8 * M + 255) / 256;
+  if (blocks > (int64_t)st->sm_count * 16) blocks = (int64_t)st->sm_count * 16;
+  const bool ranged = type == HGEMM_TYPE_F16;
+  char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes() + (ranged ? range_bytes(blocks) : 0)));
   if (!buf) return DGEMM_ERR_CUDA;
   float* ws = nullptr;
   if (pl.workspace > 0 && !(ws = static_cast<float*>(hold.workspace(pl.workspace)))) return DGEMM_ERR_CUDA;
@@ -895,21 +913,22 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   gp.vec_g = addressable(Matrix{G, M, F, ldg});
   gp.vec_u = addressable(Matrix{U, M, F, ldu});
   gp.vec_h = addressable(Matrix{dH, M, F, lddh});
-  int64_t blocks = ((F + 7) / 8 * M + 255) / 256;
-  if (blocks > (int64_t)st->sm_count * 16) blocks = (int64_t)st->sm_count * 16;
   gp.blocks = (unsigned)blocks;
+  if (ranged) gp.range = range_at(buf + pack.bytes());
   const PackOps ops = pack.finish(buf);  // copied by further blocks of the same launch
   const dim3 grid((unsigned)blocks + pack.blocks());
   const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, gp, ops)
                                           : lm::launch(hgemm_gated_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, gp, ops);
   if (!ok) return DGEMM_ERR_CUDA;
+  if (ranged && !lm::launch(hgemm_gated_rescale_kernel, dim3(rescale_blocks(st, M, F)), dim3(256), 0, 1, s, gp)) return DGEMM_ERR_CUDA;
   for (int i = 0; i < 2; ++i) {
     px.p[i] = w[i];
     px.q[i] = dgu[i];
     pw[i].p[0] = transw ? x : dgu[i];
     pw[i].q[0] = transw ? dgu[i] : x;
   }
-  return run_products(type, false, list, n, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, s);
+  return run_products(type, false, list, n, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, s,
+                      gp.range.inverse);
 }
 
 int hgemm_last_device_status(void* stream) {

@@ -113,6 +113,49 @@ __global__ void hgemm_empty_kernel(int M, int N, const T* bias, int act, const T
   }
 }
 
+// ---- range of the gradients' element-wise part ------------------------------------------------------
+
+// dZ, dG and dU enter the products in 16 bits. bfloat16 has binary32's range; binary16 has not: dH = 1500 and U = 50 make
+// 75000, beyond its largest number, where the products' results may lie well inside, and gradients without loss scaling
+// fall below its smallest. So the binary16 kernels also leave the largest finite magnitude of what each block stores, and
+// a second kernel looks at the largest of all: where it lies outside [2^-4, 65520) it stores the part once more, times the
+// power of two that brings it into [2^14, 2^15), and the products' sums are multiplied by the inverse (both exact). One power
+// serves the whole part, because each product sums over another of its dimensions; values below 2^-28 of the largest lose
+// bits to it. Down to a largest value of 2^-4 the part stays as it is: there bits are lost below 2^-10 of the largest, in
+// steps of 2^-20 of it, under the rounding of the larger ones.
+// Where the part stays as it is this costs 2 to 3 us, the second kernel's launch (64 x 512 x 512 with SiLU 9.3 -> 11.4 us,
+// 2088 x 4096 x 2088 101.4 -> 104.5); a pass that takes the largest magnitude first would read every call's inputs twice.
+struct PartRange {
+  float* inverse;   // what the products' sums are multiplied by: written by the second kernel
+  unsigned* top;    // bits of each block's largest magnitude
+};
+__device__ __forceinline__ unsigned finite_magnitude(float x) {
+  const unsigned m = __float_as_uint(x) & 0x7fffffffu;
+  return m < 0x7f800000u ? m : 0u;
+}
+// The largest of the block's values, in every thread (256 of them).
+__device__ __forceinline__ unsigned block_max(unsigned top) {
+  __shared__ unsigned most[8];
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) top = max(top, most[w]);
+  return top;
+}
+// Second kernel: the power of two that the part is to be multiplied by, from the `blocks` blocks of the first.
+__device__ __forceinline__ float part_scale(const PartRange& r, unsigned blocks) {
+  unsigned top = 0;
+#pragma unroll 4
+  for (unsigned i = threadIdx.x; i < blocks; i += 256) top = max(top, __ldcg(r.top + i));
+  top = block_max(top);
+  const float t = __uint_as_float(top);
+  int e = 0;
+  if (top != 0 && !(t >= 0.0625f && t < 65520.f)) e = min(14 + 127 - (int)(top >> 23), 100);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *r.inverse = __int_as_float((127 - e) << 23);
+  return __int_as_float((127 + e) << 23);
+}
+
 // ---- gradient at the activation -------------------------------------------------------------------
 
 struct ActBwdParams {
@@ -129,6 +172,7 @@ struct ActBwdParams {
   long long ldz, lddd, lddz;
   int act;
   int vec_z, vec_d;  // 16-byte aligned rows
+  PartRange range;   // of a binary16 dZ; or NULLs
 };
 
 // dZ = dD act'(Z) (rounded) and dbias = column sums of the unrounded products. A block takes a strip of 64 or 256 columns
@@ -144,6 +188,8 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
   const int tx = threadIdx.x & (W - 1), ty = threadIdx.x >> p.lane_bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = ((strip << p.lane_bits) + tx) * 8;
   const int r0 = chunk * p.rows_per_chunk, r1 = min(p.M, r0 + p.rows_per_chunk);
+  constexpr bool RANGED = std::is_same<T, __half>::value && ACT != HGEMM_ACT_NONE && ACT != HGEMM_ACT_RELU;
+  unsigned top = 0;
   float sum[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum[i] = 0.f;
@@ -165,7 +211,10 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
         }
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += d[i];
+      for (int i = 0; i < 8; ++i) {
+        sum[i] += d[i];
+        if (RANGED) top = max(top, finite_magnitude(d[i]));
+      }
       if (p.dZ) *reinterpret_cast<uint4*>(po + r * p.lddz) = pack8<T>(d);
     };
     int r = r0 + ty;
@@ -191,6 +240,10 @@ __device__ __forceinline__ void act_bwd_body(const ActBwdParams& p, float (*red)
       if (ACT != HGEMM_ACT_NONE) z = load8(pz + r * p.ldz, n, p.N, p.vec_z);
       one(d, z, r);
     }
+  }
+  if (RANGED && p.range.top) {
+    top = block_max(top);
+    if (threadIdx.x == 0) p.range.top[blockIdx.x] = top;
   }
   if (!p.dbias) return;
   // the sum over the rows of threads, of column threadIdx.x of the strip
@@ -273,15 +326,19 @@ struct GatedBwdParams {
   int act;
   int vec_g, vec_u, vec_h;  // 16-byte aligned rows
   unsigned blocks;          // the blocks beyond copy operands
+  PartRange range;          // of a binary16 dG and dU; or NULLs
 };
 
-// dG = dH U act'(G), dU = dH act(G); both rounded. One thread per 8 columns of a row.
-template <typename T, int ACT>
-__device__ __forceinline__ void gated_bwd_body(const GatedBwdParams& p) {
+// dG = dH U act'(G), dU = dH act(G); both rounded, AGAIN: times `scale` first. One thread per 8 columns of a row.
+template <typename T, int ACT, bool AGAIN = false>
+__device__ __forceinline__ void gated_bwd_body(const GatedBwdParams& p, float scale = 1.f) {
+  constexpr bool RANGED = std::is_same<T, __half>::value && !AGAIN;
+  unsigned top = 0;
   const int per_row = (p.F + 7) / 8;
   const bool vec = p.vec_g && p.vec_u && p.vec_h;
   const long long total = (long long)per_row * p.M;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)p.blocks * blockDim.x) {
+  const unsigned blocks = AGAIN ? gridDim.x : p.blocks;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)blocks * blockDim.x) {
     const int r = (int)(i / per_row), f = (int)(i - (long long)r * per_row) * 8;
     const uint16_t* pg = static_cast<const uint16_t*>(p.G) + r * p.ldg + f;
     const uint16_t* pu = static_cast<const uint16_t*>(p.U) + r * p.ldu + f;
@@ -306,9 +363,18 @@ __device__ __forceinline__ void gated_bwd_body(const GatedBwdParams& p) {
       act_both<ACT>(g[j], a, da);
       g[j] = d[j] * u[j] * da;
       u[j] = d[j] * a;
+      if (RANGED) top = max(top, max(finite_magnitude(g[j]), finite_magnitude(u[j])));
+      if (AGAIN) {
+        g[j] *= scale;
+        u[j] *= scale;
+      }
     }
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dG) + r * p.ldo + f) = pack8<T>(g);
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dU) + r * p.ldo + f) = pack8<T>(u);
+  }
+  if (RANGED && p.range.top) {
+    top = block_max(top);
+    if (threadIdx.x == 0) p.range.top[blockIdx.x] = top;
   }
 }
 
@@ -326,6 +392,50 @@ __global__ void __launch_bounds__(256) hgemm_gated_bwd_kernel(const __grid_const
     case HGEMM_ACT_GELU_TANH: gated_bwd_body<T, HGEMM_ACT_GELU_TANH>(p); break;
     case HGEMM_ACT_SILU: gated_bwd_body<T, HGEMM_ACT_SILU>(p); break;
     default: gated_bwd_body<T, HGEMM_ACT_NONE>(p); break;
+  }
+}
+
+// The second pass over a binary16 part outside the range: the same values times the chosen power of two.
+__global__ void __launch_bounds__(256) hgemm_gated_rescale_kernel(const __grid_constant__ GatedBwdParams p) {
+  ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  const float scale = part_scale(p.range, p.blocks);
+  if (scale == 1.f) return;
+  switch (p.act) {
+    case HGEMM_ACT_RELU: gated_bwd_body<__half, HGEMM_ACT_RELU, true>(p, scale); break;
+    case HGEMM_ACT_GELU: gated_bwd_body<__half, HGEMM_ACT_GELU, true>(p, scale); break;
+    case HGEMM_ACT_GELU_TANH: gated_bwd_body<__half, HGEMM_ACT_GELU_TANH, true>(p, scale); break;
+    case HGEMM_ACT_SILU: gated_bwd_body<__half, HGEMM_ACT_SILU, true>(p, scale); break;
+    default: gated_bwd_body<__half, HGEMM_ACT_NONE, true>(p, scale); break;
+  }
+}
+template <int ACT>
+__device__ __forceinline__ void act_rescale_body(const ActBwdParams& p, float scale) {
+  const int per_row = (p.N + 7) / 8;
+  const long long total = (long long)per_row * p.M;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+    const int r = (int)(i / per_row), n = (int)(i - (long long)r * per_row) * 8;
+    float d[8], z[8];
+    unpack8<__half>(load8(static_cast<const uint16_t*>(p.dD) + r * p.lddd + n, n, p.N, p.vec_d), d);
+    unpack8<__half>(load8(static_cast<const uint16_t*>(p.Z) + r * p.ldz + n, n, p.N, p.vec_z), z);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float f, df;
+      act_both<ACT>(z[j], f, df);
+      d[j] = d[j] * df * scale;
+    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.dZ) + r * p.lddz + n) = pack8<__half>(d);
+  }
+}
+__global__ void __launch_bounds__(256) hgemm_act_rescale_kernel(const __grid_constant__ ActBwdParams p) {
+  ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  const float scale = part_scale(p.range, p.strips * p.chunks);
+  if (scale == 1.f) return;
+  switch (p.act) {
+    case HGEMM_ACT_GELU: act_rescale_body<HGEMM_ACT_GELU>(p, scale); break;
+    case HGEMM_ACT_GELU_TANH: act_rescale_body<HGEMM_ACT_GELU_TANH>(p, scale); break;
+    default: act_rescale_body<HGEMM_ACT_SILU>(p, scale); break;
   }
 }
 

@@ -110,6 +110,7 @@ struct Params {
   int* counters;           // CG x NB per tile left over; zero between launches
   unsigned long long wait_limit_ns;
   int* status;
+  const float* unscale;  // gradients in binary16: what the sums are multiplied by (a power of two), or NULL
   int drop;  // testing aid: the producers skip their copies
 };
 
@@ -358,12 +359,21 @@ struct Epilogue {
   Patch<CH> pt;
   typename Patch<CH>::View d, z, u, r;
   bool has_z, has_r;
+  float unscale;  // see Params (read by the binary16 kernel without activation alone)
   float bias[4];  // bias[j]: of column 8 j + lane / 4 of the patch
 };
 
+// The gradients' products, whose operand may have been scaled, run without activation; bfloat16 needs no scaling.
+template <typename T, int ACT>
+constexpr bool UNSCALED = std::is_same<T, __half>::value && ACT == HGEMM_ACT_NONE;
+
 template <typename T, int CH, int ACT>
-__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, const float* v, const typename Patch<CH>::Raw& raw) {
+__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, float* v, const typename Patch<CH>::Raw& raw) {
   constexpr int MB = CH / 8;
+  if (UNSCALED<T, ACT> && ep.unscale != 1.f) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) v[i] *= ep.unscale;
+  }
   uint32_t q[CH / 2], r[CH / 2];
   if (ep.has_r) ep.pt.take(raw, ep.r.vec, r);
   if (ep.has_z) {
@@ -759,6 +769,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     // After a wait has given up, the warps still walk through the rest of the units together (without
     // waiting again), so that every named barrier below is met by all of its warps.
     bool dead = false;
+    const float unscale = !GATED && UNSCALED<T, ACT> && p.unscale ? __ldcg(p.unscale) : 1.f;
     Work w;
     for (; get_work(p, cluster, clusters, (int)acc_it, w); ++acc_it) {
       const Problem& pr = p.prob[w.prob];
@@ -770,6 +781,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         const bool n_in = n0 < pr.N;  // (the whole warp: a patch beyond the last column has nothing to do)
         Epilogue<CH> ep;
         ep.pt = Patch<CH>{rows, pr.N - n0, lane, buf, buf + (lane & 7) * PITCH + (lane >> 3) * 16};
+        ep.unscale = unscale;
         ep.has_z = pr.Z != nullptr;
         ep.has_r = !GATED && pr.R != nullptr;
         ep.d = ep.pt.view(pr.D, pr.ldd, pr.vec & VEC_D, m_base, n0);
