@@ -1,4 +1,6 @@
-"""Builds ``libdgemm.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds ``libdgemm.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU), and ``_marshal.so``, the compiled
+argument marshalling of some Python entry points, with g++ against the installed torch. Nothing in the library uses torch:
+without torch it is built alone, and those entry points say what is missing when they are first used."""
 from __future__ import annotations
 
 import glob
@@ -13,11 +15,15 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdgemm.so")
 EXT = os.path.join(HERE, "_marshal.so")  # compiled argument marshalling (csrc/binding_ext.cpp)
 EXT_SOURCE = os.path.join(CSRC, "binding_ext.cpp")
+EXT_STAMP = EXT + ".torch"  # the torch and the Python that it was built against
 SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "hgemm_plain_f16.cu", "hgemm_plain_bf16.cu",
                                                 "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "hgemm_token.cu", "layernorm.cu")]
-# every source, header and public header: an edit to any of them makes the built library stale
-DEPS = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh")) +
-              glob.glob(os.path.join(CSRC, "*.h")) + [EXT_SOURCE] + glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
+HEADERS = sorted(glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) +
+                 glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))
+# every source, header and public header: an edit to any of them makes what is built from them stale
+LIB_DEPS = sorted(glob.glob(os.path.join(CSRC, "*.cu"))) + HEADERS
+EXT_DEPS = [EXT_SOURCE] + HEADERS
+DEPS = LIB_DEPS + [EXT_SOURCE]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -30,11 +36,33 @@ def nvcc_path() -> str:
     return cand if os.path.exists(cand) else "nvcc"
 
 
-def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(EXT):
+def _older(built: str, deps: list) -> bool:
+    return not os.path.exists(built) or any(os.path.getmtime(d) > os.path.getmtime(built) for d in deps)
+
+
+def torch_version() -> str | None:
+    """The installed torch's version and this Python's, or None without torch."""
+    import importlib.metadata
+    import importlib.util
+    if "torch" in sys.modules and sys.modules["torch"] is None or importlib.util.find_spec("torch") is None:
+        return None
+    return "torch %s, %s" % (importlib.metadata.version("torch"), sys.version.split()[0])
+
+
+def lib_is_stale() -> bool:
+    return _older(LIB, LIB_DEPS)
+
+
+def ext_is_stale() -> bool:
+    """Missing, older than its sources, or built against another torch or Python than the installed ones."""
+    if _older(EXT, EXT_DEPS) or not os.path.exists(EXT_STAMP):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(EXT))
-    return any(os.path.getmtime(d) > t for d in DEPS)
+    with open(EXT_STAMP) as f:
+        return f.read() != torch_version()
+
+
+def is_stale() -> bool:
+    return lib_is_stale() or (torch_version() is not None and ext_is_stale())
 
 
 # What ptxas must report for the kernels whose speed hangs on their register allocation: (substring
@@ -95,42 +123,54 @@ def ext_command(out: str) -> list:
             "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
 
 
+def _compile_all(commands: list) -> tuple:
+    """Runs the commands side by side; (whether all succeeded, their output)."""
+    jobs = []
+    for cmd in commands:
+        log = tempfile.TemporaryFile("w+")
+        jobs.append((log, subprocess.Popen(cmd, cwd=CSRC, stdout=log, stderr=subprocess.STDOUT, text=True)))
+    ok, text = True, ""
+    for log, proc in jobs:
+        ok = proc.wait() == 0 and ok
+        log.seek(0)
+        text += log.read()
+        log.close()
+    return ok, text
+
+
 def build(force: bool = False, verbose: bool = False, check: bool = False) -> str:
-    """Compile the library if it is missing or older than its sources; returns its path. With `check`
+    """Compile what is missing or older than its sources; returns the library's path. With `check`
     the compile reports resource usage and fails if the hot kernels' registers or spills changed."""
-    if force or is_stale():
-        tmp = LIB + ".tmp.%d" % os.getpid()
-        extra = shlex.split(os.environ.get("DGEMM_NVCC_FLAGS", ""))  # e.g. -D switches for experiments
-        flags = [*NVCC_FLAGS, *extra, *(["-Xptxas", "-v"] if (verbose or check) else [])]
-        with tempfile.TemporaryDirectory() as objs:
-            # one compiler process per source, side by side
-            jobs = []
-            for src in SOURCES:
-                obj = os.path.join(objs, os.path.basename(src) + ".o")
-                log = open(obj + ".log", "w+")
-                jobs.append((obj, log, subprocess.Popen([nvcc_path(), *flags, "-c", "-o", obj, src], cwd=CSRC, stdout=log,
-                                                        stderr=subprocess.STDOUT, text=True)))
-            ext_tmp, ext_log = EXT + ".tmp.%d" % os.getpid(), open(os.path.join(objs, "ext.log"), "w+")
-            jobs.append((None, ext_log, subprocess.Popen(ext_command(ext_tmp), cwd=CSRC, stdout=ext_log, stderr=subprocess.STDOUT, text=True)))
-            failed, text = False, ""
-            for obj, log, proc in jobs:
-                failed = proc.wait() != 0 or failed
-                log.seek(0)
-                text += log.read()
-                log.close()
-            if not failed:
-                res = subprocess.run([nvcc_path(), *flags, "-shared", "-o", tmp, *(j[0] for j in jobs if j[0])], cwd=CSRC,
-                                     capture_output=True, text=True)
-                failed = res.returncode != 0
-                text += res.stdout + res.stderr
-        if verbose or failed:
-            sys.stderr.write(text)
-        if failed:
-            raise RuntimeError("nvcc failed building libdgemm.so")
+    do_lib = force or lib_is_stale()
+    version = torch_version()
+    do_ext = version is not None and (force or ext_is_stale())
+    extra = shlex.split(os.environ.get("DGEMM_NVCC_FLAGS", ""))  # e.g. -D switches for experiments
+    flags = [*NVCC_FLAGS, *extra, *(["-Xptxas", "-v"] if (verbose or check) else [])]
+    lib_tmp, ext_tmp = LIB + ".tmp.%d" % os.getpid(), EXT + ".tmp.%d" % os.getpid()
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        compiles = [[nvcc_path(), *flags, "-c", "-o", obj, src] for obj, src in zip(objs, SOURCES)] if do_lib else []
+        ok, text = _compile_all(compiles + ([ext_command(ext_tmp)] if do_ext else []))
+        if ok and do_lib:
+            ok, linked = _compile_all([[nvcc_path(), *flags, "-shared", "-o", lib_tmp, *objs]])
+            text += linked
+    if verbose or not ok:
+        sys.stderr.write(text)
+    if not ok:
+        for path in (lib_tmp, ext_tmp):
+            if os.path.exists(path):
+                os.remove(path)
+        raise RuntimeError("the compiler failed building " + " and ".join(n for n, d in (("libdgemm.so", do_lib), ("_marshal.so", do_ext)) if d))
+    if do_lib:
         if check and not extra:
             check_ptxas(text)
-        os.replace(tmp, LIB)
+        os.replace(lib_tmp, LIB)
+    if do_ext:
         os.replace(ext_tmp, EXT)
+        with open(EXT_STAMP, "w") as f:
+            f.write(version)
+    if version is None:
+        sys.stderr.write("torch is not installed: libdgemm.so is built, the Python module _marshal is not\n")
     return LIB
 
 
