@@ -440,7 +440,8 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
   }
   int parity = 0;
   for (; row < p.rows; parity ^= 1) {
-    // xh and w = dy gamma of this row. Beyond `cols` dy is 0, and so is every term of the sums
+    // xh and w = dy gamma of this row. Beyond `cols` dy is 0, and so is every term of the sums: t2 adds w (x - mean) and is
+    // scaled at the end, because (0 - mean) rstd may be infinite there
     P xh, w;
     xh.unpack(xr);
     w.unpack(dr);
@@ -458,12 +459,13 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
     if (!WIDE) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        xh.v[k] = mul2(add2(xh.v[k], both(-mu)), both(rs));
+        const float2 d = add2(xh.v[k], both(-mu));
+        xh.v[k] = mul2(d, both(rs));
         dg.v[k] = fma2(w.v[k], xh.v[k], dg.v[k]);
         db.v[k] = add2(db.v[k], w.v[k]);
         w.v[k] = mul2(w.v[k], g.v[k]);
         t1 = add2(t1, w.v[k]);
-        t2 = fma2(w.v[k], xh.v[k], t2);
+        t2 = fma2(w.v[k], d, t2);
       }
     } else {
       // LOW values at a time; with VEC == 1 the pairs span two vectors, so single values are used
@@ -478,24 +480,26 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
             const int k = 2 * q + h;
             float2& da = reinterpret_cast<float2*>(&a)[h];
             float2& dbb = reinterpret_cast<float2*>(&b)[h];
-            xh.v[k] = mul2(add2(xh.v[k], both(-mu)), both(rs));
+            const float2 d = add2(xh.v[k], both(-mu));
+            xh.v[k] = mul2(d, both(rs));
             da = fma2(w.v[k], xh.v[k], da);
             dbb = add2(dbb, w.v[k]);
             w.v[k] = mul2(w.v[k], reinterpret_cast<const float2*>(&gg)[h]);
             t1 = add2(t1, w.v[k]);
-            t2 = fma2(w.v[k], xh.v[k], t2);
+            t2 = fma2(w.v[k], d, t2);
           }
           *reinterpret_cast<float4*>(w_dg + at) = a;
           *reinterpret_cast<float4*>(w_db + at) = b;
         } else {
           float& h = q % 2 ? xh.v[q / 2].y : xh.v[q / 2].x;
           float& d = q % 2 ? w.v[q / 2].y : w.v[q / 2].x;
-          h = (h - mu) * rs;
+          const float off = h - mu;
+          h = off * rs;
           w_dg[at] += d * h;
           w_db[at] += d;
           d *= w_g[at];
           t1.x += d;
-          t2.x += d * h;
+          t2.x += d * off;
         }
       }
     }
@@ -507,7 +511,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
         both_sums = lane < (int)(blockDim.x >> 5) ? red[parity][lane] : both(0.f);
         both_sums = warp_sum_pair(both_sums.x, both_sums.y);
       }
-      const float s1 = both_sums.x * inv_n, s2 = both_sums.y * inv_n;
+      const float s1 = both_sums.x * inv_n, s2 = both_sums.y * rs * inv_n;
 #pragma unroll
       for (int k = 0; k < N; ++k) w.v[k] = mul2(add2(fma2(xh.v[k], both(-s2), w.v[k]), both(-s1)), both(rs));
       store_row<T, VEC, ITEMS>(o_at, w, c0, p.cols, full);
