@@ -376,9 +376,9 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     const Plan::Part& q = pl.part[i];
     const int np = gated ? 2 : s.nseg, nq = s.nseg;
     for (int j = 0; j < np; ++j)
-      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated || c.nb == 1 ? 64 : 128)) return DGEMM_ERR_CUDA;
+      if (!make_map(&d.p[j], type, s.p[j], s.p_mn || gated || c.nb == 1 ? 64 : 128)) return lm::cuda_failed();
     for (int j = 0; j < nq; ++j)
-      if (!make_map(&d.q[j], type, s.q[j], s.q_mn ? 64 : qrows)) return DGEMM_ERR_CUDA;
+      if (!make_map(&d.q[j], type, s.q[j], s.q_mn ? 64 : qrows)) return lm::cuda_failed();
     d.N = (int)s.N;
     d.M = (int)s.M;
     d.tiles_n = q.tiles_n;
@@ -415,7 +415,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
   p.drop = drop > 0;
   p.status = st->status;
   p.unscale = unscale;
-  return launch_tc(type, gated, pr[0]->act, pl.config, pl.clusters, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
+  return launch_tc(type, gated, pr[0]->act, pl.config, pl.clusters, stream, p) ? DGEMM_OK : lm::cuda_failed();
 }
 
 // ---- validation -----------------------------------------------------------------------------------------
@@ -467,7 +467,7 @@ int run_empty(int type, int64_t M, int64_t N, const void* bias, int act, const v
               int64_t ldz, cudaStream_t stream) {
   const bool ok = type == HGEMM_TYPE_BF16 ? launch_empty<__nv_bfloat16>(M, N, bias, act, R, ldr, D, ldd, Z, ldz, stream)
                                           : launch_empty<__half>(M, N, bias, act, R, ldr, D, ldd, Z, ldz, stream);
-  return ok ? DGEMM_OK : DGEMM_ERR_CUDA;
+  return ok ? DGEMM_OK : lm::cuda_failed();
 }
 
 // Whether a product runs on the kernels for one or two rows.
@@ -501,7 +501,7 @@ int run_token(int type, bool gated, const Product& s, int sms, cudaStream_t stre
   p.ldd = s.ldd;
   p.ldz = s.ldz;
   p.ldu = s.ldu;
-  return launch_token(type, gated, sms, stream, p) ? DGEMM_OK : DGEMM_ERR_CUDA;
+  return launch_token(type, gated, sms, stream, p) ? DGEMM_OK : lm::cuda_failed();
 }
 
 // The range of a binary16 gradient part stored by `blocks` blocks takes range_bytes of scratch at the 4-byte aligned `at`.
@@ -527,12 +527,12 @@ int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
   pack.add(&prod->q[0]);
   if (pack.bytes() > 0) {
     char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes()));
-    if (!buf || !pack.launch(buf, stream)) return DGEMM_ERR_CUDA;
+    if (!buf || !pack.launch(buf, stream)) return lm::cuda_failed();
   }
   float* ws = nullptr;
   if (pl.workspace > 0) {
     ws = static_cast<float*>(hold.workspace(pl.workspace));
-    if (!ws) return DGEMM_ERR_CUDA;
+    if (!ws) return lm::cuda_failed();
   }
   return run_products(type, gated, &prod, 1, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, stream);
 }
@@ -565,14 +565,14 @@ int device_state(DeviceState** out) {
     if (major != 10) return DGEMM_ERR_DEVICE;
     if (cudaGetSymbolAddress(reinterpret_cast<void**>(&st.status), g_hgemm_status_word) != cudaSuccess ||
         cudaGetSymbolAddress(reinterpret_cast<void**>(&st.counters), g_hgemm_counters) != cudaSuccess)
-      return DGEMM_ERR_CUDA;
-    if (!configure_plain_f16() || !configure_gated_f16() || !configure_plain_bf16() || !configure_gated_bf16()) return DGEMM_ERR_CUDA;
+      return lm::cuda_failed();
+    if (!configure_plain_f16() || !configure_gated_f16() || !configure_plain_bf16() || !configure_gated_bf16()) return lm::cuda_failed();
     if (!g_encode) {
       void* fn = nullptr;
       cudaDriverEntryPointQueryResult qres;
       if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn ||
           qres != cudaDriverEntryPointSuccess)
-        return DGEMM_ERR_CUDA;
+        return lm::cuda_failed();
       g_encode = reinterpret_cast<EncodeTiledFn>(fn);
     }
     st.sm_count = sms;
@@ -655,7 +655,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
   // empty sums
   if (dA && N == 0 && M > 0 && K > 0) HGEMM_TRY(run_empty(type, ar, ac, nullptr, HGEMM_ACT_NONE, nullptr, 0, dA, ldda, nullptr, 0, s));
   if (dB && M == 0 && N > 0 && K > 0) HGEMM_TRY(run_empty(type, br, bc, nullptr, HGEMM_ACT_NONE, nullptr, 0, dB, lddb, nullptr, 0, s));
-  if (dbias && M == 0 && N > 0 && cudaMemsetAsync(dbias, 0, (size_t)N * 4, s) != cudaSuccess) return DGEMM_ERR_CUDA;
+  if (dbias && M == 0 && N > 0 && cudaMemsetAsync(dbias, 0, (size_t)N * 4, s) != cudaSuccess) return lm::cuda_failed();
   if (M == 0 || N == 0) return DGEMM_OK;
   const bool want_a = dA && K > 0, want_b = dB && K > 0;
   if (!want_a && !want_b && !dbias) return DGEMM_OK;
@@ -735,13 +735,13 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
   const bool ranged = want_dz && type == HGEMM_TYPE_F16 && act != HGEMM_ACT_NONE && act != HGEMM_ACT_RELU;
   const size_t pack_bytes = pack.bytes() + (ranged ? range_bytes(strips * chunks) : 0);
   char* buf = nullptr;
-  if (pack_bytes > 0 && !(buf = static_cast<char*>(hold.pack_buffer(pack_bytes)))) return DGEMM_ERR_CUDA;
+  if (pack_bytes > 0 && !(buf = static_cast<char*>(hold.pack_buffer(pack_bytes)))) return lm::cuda_failed();
   if (want_dz) ap.dZ = buf;
   if (ranged) ap.range = range_at(buf + pack.bytes());
   size_t ws_bytes = n > 0 ? pl.workspace : 0;
   if (dbias && chunks > 1 && (size_t)chunks * (N + 7) * 4 > ws_bytes) ws_bytes = (size_t)chunks * (N + 7) * 4;
   float* ws = nullptr;
-  if (ws_bytes > 0 && !(ws = static_cast<float*>(hold.workspace(ws_bytes)))) return DGEMM_ERR_CUDA;
+  if (ws_bytes > 0 && !(ws = static_cast<float*>(hold.workspace(ws_bytes)))) return lm::cuda_failed();
   int* counters = st->counters + hold.lease_index() * lm::kCounters;
   if (want_act) {
     ap.partial = ws;
@@ -753,8 +753,8 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     const dim3 grid((unsigned)(strips * chunks) + pack.blocks());
     const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_act_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, ap, ops)
                                             : lm::launch(hgemm_act_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, ap, ops);
-    if (!ok) return DGEMM_ERR_CUDA;
-    if (ranged && !lm::launch(hgemm_act_rescale_kernel, dim3(rescale_blocks(st, M, N)), dim3(256), 0, 1, s, ap)) return DGEMM_ERR_CUDA;
+    if (!ok) return lm::cuda_failed();
+    if (ranged && !lm::launch(hgemm_act_rescale_kernel, dim3(rescale_blocks(st, M, N)), dim3(256), 0, 1, s, ap)) return lm::cuda_failed();
   }
   if (n == 0) return DGEMM_OK;
   if (want_dz) {
@@ -762,7 +762,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
     if (want_a) (transa ? pa.p[0] : pa.q[0]) = packed;
     if (want_b) (transb ? pb.q[0] : pb.p[0]) = packed;
   }
-  if (!want_act && !pack.launch(buf, s)) return DGEMM_ERR_CUDA;
+  if (!want_act && !pack.launch(buf, s)) return lm::cuda_failed();
   return run_products(type, false, list, n, pl, st, ws, counters, s, ap.range.inverse);
 }
 
@@ -891,9 +891,9 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   if (blocks > (int64_t)st->sm_count * 16) blocks = (int64_t)st->sm_count * 16;
   const bool ranged = type == HGEMM_TYPE_F16;
   char* buf = static_cast<char*>(hold.pack_buffer(pack.bytes() + (ranged ? range_bytes(blocks) : 0)));
-  if (!buf) return DGEMM_ERR_CUDA;
+  if (!buf) return lm::cuda_failed();
   float* ws = nullptr;
-  if (pl.workspace > 0 && !(ws = static_cast<float*>(hold.workspace(pl.workspace)))) return DGEMM_ERR_CUDA;
+  if (pl.workspace > 0 && !(ws = static_cast<float*>(hold.workspace(pl.workspace)))) return lm::cuda_failed();
   GatedBwdParams gp;
   memset(&gp, 0, sizeof(gp));
   gp.M = (int)M;
@@ -919,8 +919,8 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   const dim3 grid((unsigned)blocks + pack.blocks());
   const bool ok = type == HGEMM_TYPE_BF16 ? lm::launch(hgemm_gated_bwd_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, s, gp, ops)
                                           : lm::launch(hgemm_gated_bwd_kernel<__half>, grid, dim3(256), 0, 1, s, gp, ops);
-  if (!ok) return DGEMM_ERR_CUDA;
-  if (ranged && !lm::launch(hgemm_gated_rescale_kernel, dim3(rescale_blocks(st, M, F)), dim3(256), 0, 1, s, gp)) return DGEMM_ERR_CUDA;
+  if (!ok) return lm::cuda_failed();
+  if (ranged && !lm::launch(hgemm_gated_rescale_kernel, dim3(rescale_blocks(st, M, F)), dim3(256), 0, 1, s, gp)) return lm::cuda_failed();
   for (int i = 0; i < 2; ++i) {
     px.p[i] = w[i];
     px.q[i] = dgu[i];
@@ -935,14 +935,13 @@ int hgemm_last_device_status(void* stream) {
   lm::DeviceState* st = nullptr;
   HGEMM_TRY(lm::device_state(&st));
   if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return DGEMM_ERR_CUDA;
+    return lm::cuda_failed();
   }
   int v = 0;
-  if (cudaMemcpy(&v, st->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return DGEMM_ERR_CUDA;
+  if (cudaMemcpy(&v, st->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return lm::cuda_failed();
   // The word alone: the counters of cut tiles belong to calls that may be in flight on other streams, and a kernel that gave
   // up has still counted every part (its epilogue walks through all units), so they are zero after it like after any other.
-  if (v != 0 && cudaMemset(st->status, 0, sizeof(int)) != cudaSuccess) return DGEMM_ERR_CUDA;
+  if (v != 0 && cudaMemset(st->status, 0, sizeof(int)) != cudaSuccess) return lm::cuda_failed();
   return v;
 }
 

@@ -222,7 +222,7 @@ int layernorm_fwd(int type, int64_t rows, int64_t cols, const void* X, int64_t l
   const bool ok = type == HGEMM_TYPE_F32   ? run_fwd<float, 4>(st->sm_count, aligned, p, s)
                   : type == HGEMM_TYPE_F16 ? run_fwd<__half, 8>(st->sm_count, aligned, p, s)
                                            : run_fwd<__nv_bfloat16, 8>(st->sm_count, aligned, p, s);
-  return ok ? DGEMM_OK : DGEMM_ERR_CUDA;
+  return ok ? DGEMM_OK : lm::cuda_failed();
 }
 
 int layernorm_bwd(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const void* gamma, const float* mean,
@@ -248,7 +248,7 @@ int layernorm_bwd(int type, int64_t rows, int64_t cols, const void* X, int64_t l
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (rows == 0) {
     for (float* out : {dgamma, dbeta})
-      if (out && cudaMemsetAsync(out, 0, (size_t)cols * 4, s) != cudaSuccess) return DGEMM_ERR_CUDA;
+      if (out && cudaMemsetAsync(out, 0, (size_t)cols * 4, s) != cudaSuccess) return lm::cuda_failed();
     return DGEMM_OK;
   }
   if (!dX && !dgamma && !dbeta) return DGEMM_OK;
@@ -277,11 +277,11 @@ int layernorm_bwd(int type, int64_t rows, int64_t cols, const void* X, int64_t l
   const int blocks = type == HGEMM_TYPE_F32   ? run_bwd<float, 4>(st->sm_count, aligned, p, s, partial)
                      : type == HGEMM_TYPE_F16 ? run_bwd<__half, 8>(st->sm_count, aligned, p, s, partial)
                                               : run_bwd<__nv_bfloat16, 8>(st->sm_count, aligned, p, s, partial);
-  if (blocks == 0) return DGEMM_ERR_CUDA;
+  if (blocks == 0) return lm::cuda_failed();
   const bool many = blocks > MANY_BLOCKS;
   if (p.want_params && !lm::launch(many ? bwd_reduce_kernel<32> : bwd_reduce_kernel<16>, dim3((unsigned)((cols + 31) / 32), 2),
                                    dim3(many ? 1024 : 512), 0, 1, s, (const float*)p.partial, blocks, (int)cols, (int)p.ldp, dgamma, dbeta))
-    return DGEMM_ERR_CUDA;
+    return lm::cuda_failed();
   return DGEMM_OK;
 }
 

@@ -27,6 +27,12 @@ struct DeviceState {
 // The current device's state, set up on first use. DGEMM_OK or an error code.
 int device_state(DeviceState** out);
 
+// DGEMM_ERR_CUDA, with the runtime's last error cleared: the next call, of any part of the library, must not find it.
+inline int cuda_failed() {
+  (void)cudaGetLastError();
+  return DGEMM_ERR_CUDA;
+}
+
 // Frees the current device's scratch leases (it has been synchronised). False if a free failed.
 bool release_scratch();
 
