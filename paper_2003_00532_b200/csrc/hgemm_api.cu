@@ -262,7 +262,7 @@ inline unsigned capped(int64_t n) { return (unsigned)(n < 65535 ? n : 65535); }
 // Operands that need rewriting, collected so that one launch and one buffer serve them all.
 class Packer {
  public:
-  explicit Packer(size_t first_free = 0) : bytes_(first_free) {}
+  explicit Packer(int sms, size_t first_free = 0) : most_(8u * sms), bytes_(first_free) {}
   void add(Matrix* m) {
     if (addressable(*m)) return;
     for (int i = 0; i < n_; ++i)
@@ -287,7 +287,7 @@ class Packer {
       ops.op[i] = PackOp{static_cast<const uint16_t*>(m.ptr), m.ld, (int)m.rows, (int)m.cols,
                          reinterpret_cast<uint16_t*>(buf + at_[i]), padded(m.cols)};
       const int64_t blocks = ((m.cols + 7) / 8 * m.rows + 255) / 256;
-      blocks_ += (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
+      blocks_ += (unsigned)(blocks < most_ ? blocks : most_);
       ops.end[i] = blocks_;
     }
     for (int i = 0; i < nu_; ++i) *users_[i] = Matrix{buf + at_[of_[i]], users_[i]->rows, users_[i]->cols, padded(users_[i]->cols)};
@@ -300,6 +300,7 @@ class Packer {
   }
 
  private:
+  unsigned most_;  // blocks per operand
   size_t bytes_;
   unsigned blocks_ = 0;
   int n_ = 0, nu_ = 0;
@@ -521,7 +522,7 @@ int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
   Plan pl;
   if (!plan_products(&prod, 1, gated, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
   scratch::Hold hold(st->scratch, stream);
-  Packer pack;
+  Packer pack(st->sm_count);
   pack.add(&prod->p[0]);
   if (gated) pack.add(&prod->p[1]);
   pack.add(&prod->q[0]);
@@ -698,7 +699,7 @@ int hgemm_epilogue_bwd(int type, int transa, int transb, int64_t M, int64_t N, i
 
   scratch::Hold hold(st->scratch, s);
   const int64_t lddz = padded(N);
-  Packer pack(want_dz ? (size_t)M * lddz * 2 : 0);
+  Packer pack(st->sm_count, want_dz ? (size_t)M * lddz * 2 : 0);
   if (want_a) pack.add(transa ? &pa.q[0] : &pa.p[0]);
   if (want_b) pack.add(transb ? &pb.p[0] : &pb.q[0]);
 
@@ -881,7 +882,7 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   if (!plan_products(list, n, false, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
 
   scratch::Hold hold(st->scratch, s);
-  Packer pack(2 * half_bytes);
+  Packer pack(st->sm_count, 2 * half_bytes);
   if (need_x) pack.add(&x);
   if (dX) {
     pack.add(&w[0]);

@@ -792,15 +792,15 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         for (int j = 0; j < 4; ++j) {
           const int n = n0 + 8 * j + (lane >> 2);
           ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
-      }
-      typename Patch<CH>::Raw raw;
-      if (ep.has_r && n_in && w.slot < 0) ep.pt.fetch(raw, ep.r, group * CH);
-      const uint32_t a = NB == 1 ? acc_it & 1u : (uint32_t)h;
-      if (!dead) dead = !wait_bounded(acc_full + 8 * a, (NB == 1 ? acc_it >> 1 : acc_it) & 1u, abort_flag, p);
-      __syncwarp();
-      ptx5::fence_after_sync();
-      const EpiWarp ew{tmem + a * BM + lane_addr, bufs, bars + 16 * STAGES + 56, acc_empty + 8 * a, e, quad, group, lane, rank * NB + h};
-      epilogue_unit<T, C, ACT>(p, pr, w, ep, raw, ew, rows, n_in);
+        }
+        typename Patch<CH>::Raw raw;
+        if (ep.has_r && n_in && w.slot < 0) ep.pt.fetch(raw, ep.r, group * CH);
+        const uint32_t a = NB == 1 ? acc_it & 1u : (uint32_t)h;
+        if (!dead) dead = !wait_bounded(acc_full + 8 * a, (NB == 1 ? acc_it >> 1 : acc_it) & 1u, abort_flag, p);
+        __syncwarp();
+        ptx5::fence_after_sync();
+        const EpiWarp ew{tmem + a * BM + lane_addr, bufs, bars + 16 * STAGES + 56, acc_empty + 8 * a, e, quad, group, lane, rank * NB + h};
+        epilogue_unit<T, C, ACT>(p, pr, w, ep, raw, ew, rows, n_in);
       }
     }
   }
