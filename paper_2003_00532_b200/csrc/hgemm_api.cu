@@ -49,6 +49,8 @@ struct Size {
 // Clocks per output row of a tile's epilogue in one CTA: a plain store, what the activation adds, each further
 // matrix with 16-byte aligned rows, and what a matrix that moves value by value adds (outputs; the residual). For the
 // last two the time of 1000 x 1536 x 64 rises by 0.9 us; 13 to 25 clocks give the same time within 0.4 % over 99 ragged sizes.
+// GELU's exact form takes 1.4 of what its tanh form adds (4096 x 9472 x 64: 34.6 us without activation, 59.5, 52.8), SiLU 0.83;
+// as an estimate 60 serves it better than 30 (15 shapes with GELU: 16.70 us in the geometric mean against 16.86, 45 16.77).
 double epilogue_clocks(int act, int matrices, int unaligned_out, bool unaligned_res) {
   const double f = act == HGEMM_ACT_NONE || act == HGEMM_ACT_RELU ? 0.0 : act == HGEMM_ACT_GELU ? 60.0 : 20.0;
   return 10.0 + f + 10.0 * (matrices - 1) + 16.0 * unaligned_out + (unaligned_res ? 13.0 : 0.0);
@@ -140,7 +142,10 @@ bool lay_out(const Size* sz, int n, bool gated, int sms, int config, Layout* out
 // Whether 512 x 256 tiles are worth a thought: they move a quarter less from L2 per product, which pays where the power
 // limit holds the clock down for long, and lose where tiles are few or short. Sustained, against 256 x 256: 8192 x
 // 4096 x 8192 466 -> 447 us, gated gradients 4096 x 8192 x 2048 548 -> 503, gated 8192 x 4096 x 8192 880 -> 755; but
-// 4096 x 9472 x 4096 (64 k-blocks) 243 -> 297, 2048 x 2048 x 8192 (half a round) 60 -> 93.
+// 4096 x 9472 x 4096 (64 k-blocks) 243 -> 297, 2048 x 2048 x 8192 (half a round) 60 -> 93. Between 64 and 128 k-blocks, over
+// three shapes, where the estimate takes them (sustained): 8192 x 8192 at 88 650 -> 621, 96 708 -> 666, 128 938 -> 870; 4096 x
+// 7168 at 112 390 -> 368, 128 444 -> 420; gated 8192 x 4096 at 72 505 -> 466, 96 670 -> 624, 128 906 -> 831; below those the
+// estimate leaves them aside (level within 0.5 %). So they would already pay from 72 on, by 4 to 8 %, where the rule waits for 96.
 bool wide_tiles(const Layout& l, const Size* sz, int n) {
   int64_t tiles = 0, kblocks = 0;
   for (int i = 0; i < n; ++i) {
@@ -345,8 +350,8 @@ struct Product {
 };
 
 // The element-wise gradient kernel's strips: 64 columns, so that its bias gradient has fewer partial sums in a row to add
-// (5451 x 280: 13.2 -> 8.3 us, 20000 x 128: 14.6 -> 11.2), or, from this many values on, 256, as memory likes it better
-// (8192 x 4096: 60 us against 80, 2088 x 4096: 18.0 against 18.9; 4096 x 1024 level).
+// (bias gradient alone, GELU's tanh form, 256 and 64 columns: 5451 x 280 11.6 and 7.1 us, 20000 x 128 11.3 and 9.5, 4096 x 1024
+// 10.2 and 8.8), or, from this many values on, 256, as memory likes it better (2088 x 4096 13.9 and 20.9, 8192 x 4096 35.5 and 59.4).
 constexpr int64_t kWideStrips = 6ll << 20;
 
 // Longest contraction first (the schedule assumes it), stable.

@@ -2,13 +2,16 @@
 // fused multiply-adds from registers; no tensor cores, no TMEM set-up, no workspace.
 //
 // A warp takes two weight rows (gated: the gate and the up row of one column), a lane 8 consecutive k (16 bytes) of
-// each, up to eight steps of loads in flight; WK warps of a block share the rows' k where there are too few rows for
+// each, in turns of up to eight steps without a condition between their loads. A turn of eight would need 64 registers for its
+// loads alone; the kernels are compiled to 54 (one row; gated 48, with 12 bytes of spills) and 64 (two rows, 8 bytes), so its loads
+// leave in two or more portions, each a trip to memory. WK warps of a block share the rows' k where there are too few rows for
 // all SMs. The tokens wait in shared memory. Sums are binary32: per lane in ascending k, then over the lanes by
 // shuffles, then over the warps in order: the same bits every time.
 //
-// Measured against the tensor-core kernel (4096 x 4096 bf16): 9.2 us for one row, 10.4 for two, against 12; four rows
-// 23 us (bound by the arithmetic), and a kernel of this kind for weights stored K x N 13.4 us, so that those and rows
-// that are not 16-byte aligned go to the tensor-core kernel.
+// Measured against the tensor-core kernel (4096 x 4096 bf16, bias and residual, calls back to back, weights rotating through
+// more than L2): 10.0 to 10.3 us for one row, 11.0 for two, against 12; four rows 23 us (bound by the arithmetic), and a kernel of
+// this kind for weights stored K x N 13.4 us against 12.6, so that those and rows that are not 16-byte aligned go to the
+// tensor-core kernel.
 #pragma once
 
 #include <cstdint>
