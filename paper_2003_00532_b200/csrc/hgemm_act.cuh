@@ -20,6 +20,14 @@ __device__ __forceinline__ float inv_1p_exp2(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
+// ... and what it leaves of 1, without cancellation: 2^x / (1 + 2^x) where that is the smaller one.
+__device__ __forceinline__ float inv_1p_exp2(float x, float& rest) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  rest = e < 1.f ? e * r : 1.f - r;
+  return r;
+}
 // The normal distribution function of z, and exp(-z^2 / 2). With y = |z|: Phi(-y) = exp(-y^2 / 2) q(1 / (1 + 0.4 y)), where q is
 // the polynomial of degree 8 whose largest relative error over 0 <= y <= 13.3 is smallest (7e-8; fitted by exchange of the
 // extrema), beyond which the exponential is 0. In binary32 the relative error is 3.3e-7 near 0 and grows with the exponent's rounding,
@@ -67,14 +75,16 @@ __device__ __forceinline__ void act_both(float z, float& f, float& df) {
     f = z * cdf;
     df = cdf + z * INV_SQRT_2PI * e;
   } else if (ACT == HGEMM_ACT_GELU_TANH) {
-    const float q = inv_1p_exp2(z * (-2.f * LOG2E * TANH_C - 2.f * LOG2E * TANH_C * TANH_A * z * z));
+    float rest;
+    const float q = inv_1p_exp2(z * (-2.f * LOG2E * TANH_C - 2.f * LOG2E * TANH_C * TANH_A * z * z), rest);
     f = z * q;
-    const float t = f * (1.f - q);  // 0 far out, where z * z may be infinite
+    const float t = f * rest;  // 0 far out, where z * z may be infinite
     df = t == 0.f ? q : q + t * (2.f * TANH_C) * (1.f + 3.f * TANH_A * z * z);
   } else if (ACT == HGEMM_ACT_SILU) {
-    const float q = inv_1p_exp2(-LOG2E * z);
+    float rest;
+    const float q = inv_1p_exp2(-LOG2E * z, rest);
     f = z * q;
-    df = q + f * (1.f - q);
+    df = q + f * rest;
   } else {
     f = z;
     df = 1.f;
