@@ -260,19 +260,18 @@ def _to_eight(y):
 
 
 def _keep(rows, cols, p, seed, offset, device):
-    """The mask of dropout: word i % 4 of Philox4x32-10 (Salmon et al., SC 2011) with counter (i / 4, offset) and key seed, for value
-    number i of the matrix, against p 2^32. 64-bit integers hold the 32-bit words; a product's high half is bits 32 to 63."""
+    """The mask of dropout: word c % 4 of Philox4x32-10 (Salmon et al., SC 2011) with the counter (c / 4, row, offset's halves) and the
+    key seed, for column c, against p 2^32. 64-bit integers hold the 32-bit words; a product's high half is bits 32 to 63."""
     low = 0xFFFFFFFF
-    n = rows * cols
-    block = torch.arange((n + 3) // 4, dtype=torch.int64, device=device)
-    a, b = block & low, block >> 32
+    a = torch.arange((cols + 3) // 4, dtype=torch.int64, device=device).expand(rows, -1)
+    b = torch.arange(rows, dtype=torch.int64, device=device)[:, None].expand_as(a)
     c, d = torch.full_like(a, offset & low), torch.full_like(a, offset >> 32 & low)
     k0, k1 = seed & low, seed >> 32 & low
     for _ in range(10):
         x, y = a * 0xD2511F53, c * 0xCD9E8D57
         a, b, c, d = ((y >> 32) & low) ^ b ^ k0, y & low, ((x >> 32) & low) ^ d ^ k1, x & low
         k0, k1 = (k0 + 0x9E3779B9) & low, (k1 + 0xBB67AE85) & low
-    words = torch.stack((a, b, c, d), 1).reshape(-1)[:n].reshape(rows, cols)
+    words = torch.stack((a, b, c, d), 2).reshape(rows, -1)[:, :cols]
     return words >= int(p * 2.0 ** 32 + 0.5)
 
 
@@ -333,17 +332,17 @@ def _eight_exact(y):
 
 
 def _mask_exact(case, seed, offset):
-    """The same generator in numpy's unsigned integers: the four words of a block as rows of one array."""
-    n = case["rows"] * case["cols"]
-    block = np.arange(-(-n // 4), dtype=np.uint64)
+    """The same generator in numpy's unsigned integers."""
+    rows, cols = case["rows"], case["cols"]
+    row, block = (a.ravel() for a in np.mgrid[0:rows, 0:-(-cols // 4)].astype(np.uint64))
     half, word = np.uint64(32), np.uint64(0xFFFFFFFF)
-    w = [block & word, block >> half, np.uint64(offset & 0xFFFFFFFF), np.uint64((offset >> 32) & 0xFFFFFFFF)]
+    w = [block, row, np.uint64(offset & 0xFFFFFFFF), np.uint64((offset >> 32) & 0xFFFFFFFF)]
     for i in range(10):
         key = [np.uint64(((seed >> 32 * j) + i * step) & 0xFFFFFFFF) for j, step in enumerate((0x9E3779B9, 0xBB67AE85))]
         p, q = w[0] * np.uint64(0xD2511F53), w[2] * np.uint64(0xCD9E8D57)
         w = [(q >> half) ^ w[1] ^ key[0], q & word, (p >> half) ^ w[3] ^ key[1], p & word]
-    words = np.stack(np.broadcast_arrays(*w), axis=1).ravel()[:n]
-    return words.astype(np.float64).reshape(case["rows"], case["cols"]) / 2.0 ** 32 >= round(case["p"] * 2 ** 32) / 2.0 ** 32
+    words = np.stack(np.broadcast_arrays(*w), axis=1).reshape(rows, -1)[:, :cols]
+    return words.astype(np.float64) / 2.0 ** 32 >= round(case["p"] * 2 ** 32) / 2.0 ** 32
 
 
 def _phi(z, act):
