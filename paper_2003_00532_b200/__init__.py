@@ -66,7 +66,7 @@ from .binding import (  # noqa: F401
 
 
 def __getattr__(name):
-    """hgemm_epilogue, hgemm_gated, layernorm_fwd and their backward passes: loaded on first use."""
+    """hgemm_epilogue, qgemm_epilogue, layernorm_fwd, rmsnorm_fwd, dropout_fwd and the like: loaded on first use."""
     from . import binding
     if name in binding.MARSHALLED:
         value = globals()[name] = getattr(binding, name)

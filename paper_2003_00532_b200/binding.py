@@ -110,7 +110,18 @@ def load_library() -> ctypes.CDLL:
             lib.hgemm_set_test_drop_loads.argtypes = [ctypes.c_int]
             lib.layernorm_fwd.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, vp, ctypes.c_float, vp, i64, vp, vp, vp]
             lib.layernorm_bwd.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp]
-            for name in ("hgemm_epilogue", "hgemm_epilogue_bwd", "hgemm_gated", "hgemm_gated_bwd", "hgemm_plan",
+            u64, dbl = ctypes.c_uint64, ctypes.c_double
+            lib.rmsnorm_fwd.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, i64, vp, ctypes.c_float, vp, i64, vp, i64, vp, vp]
+            lib.rmsnorm_fwd_e4m3.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, i64, vp, ctypes.c_float, vp, i64, vp, i64, vp, vp, vp]
+            lib.quantize_rows_e4m3.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, i64, vp, vp]
+            lib.rmsnorm_bwd.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp]
+            lib.dropout_fwd.argtypes = [ctypes.c_int, i64, i64, vp, i64, vp, i64, dbl, u64, u64, vp, vp, i64, vp]
+            lib.dropout_bwd.argtypes = [ctypes.c_int, i64, i64, vp, i64, dbl, u64, u64, vp, vp, i64, vp]
+            lib.qgemm_epilogue.argtypes = [ctypes.c_int] + [i64] * 3 + [vp, i64, vp] * 2 + [vp, ctypes.c_int] + [vp, i64] * 3 + [vp]
+            lib.qgemm_gated.argtypes = [ctypes.c_int] + [i64] * 3 + [vp, i64, vp] * 3 + [ctypes.c_int] + [vp, i64] * 3 + [vp]
+            for name in ("rmsnorm_fwd", "rmsnorm_fwd_e4m3", "quantize_rows_e4m3", "rmsnorm_bwd", "dropout_fwd", "dropout_bwd",
+                         "qgemm_epilogue", "qgemm_gated",
+                         "hgemm_epilogue", "hgemm_epilogue_bwd", "hgemm_gated", "hgemm_gated_bwd", "hgemm_plan",
                          "hgemm_last_device_status", "hgemm_set_test_drop_loads", "layernorm_fwd", "layernorm_bwd"):
                 getattr(lib, name).restype = ctypes.c_int
             lib.dgemm_plan.argtypes = [i64, i64, i64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]
@@ -246,10 +257,12 @@ def sgemm_last_device_status(stream=None) -> int:
     return int(load_library().sgemm_last_device_status(_stream_handle(stream)))
 
 
-# ---- 16-bit products with an epilogue, gated projections, layer norm --------------------------------
+# ---- 16-bit and 8-bit products with an epilogue, gated projections, norms, dropout -------------------
 
 #: Entry points whose arguments are marshalled by the compiled module ``_marshal`` (csrc/binding_ext.cpp).
-MARSHALLED = ("hgemm_epilogue", "hgemm_epilogue_bwd", "hgemm_gated", "hgemm_gated_bwd", "layernorm_fwd", "layernorm_bwd")
+MARSHALLED = ("hgemm_epilogue", "hgemm_epilogue_bwd", "hgemm_gated", "hgemm_gated_bwd", "layernorm_fwd", "layernorm_bwd",
+              "rmsnorm_fwd", "rmsnorm_fwd_e4m3", "quantize_rows_e4m3", "rmsnorm_bwd", "dropout_fwd", "dropout_bwd",
+              "qgemm_epilogue", "qgemm_gated")
 
 
 def _raise(rc: int, where: str):

@@ -1,5 +1,5 @@
-// Compiled argument marshalling of the 16-bit products and layer norm: the Python names of
-// include/hgemm.h and include/layernorm.h as builtins that unpack torch tensors, check shapes, types,
+// Compiled argument marshalling of the 16-bit and 8-bit products, the norms and dropout: the Python names of
+// include/hgemm.h, qgemm.h, layernorm.h, rmsnorm.h and dropout.h as builtins that unpack torch tensors, check shapes, types,
 // strides and device, and call the C ABI. No arithmetic and no CUDA kernels here. Reached through the
 // interpreter, the same checks cost 8 to 15 us per call, more than the kernels of a single token take.
 //
@@ -17,8 +17,11 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include "../../include/dropout.h"
 #include "../../include/hgemm.h"
 #include "../../include/layernorm.h"
+#include "../../include/qgemm.h"
+#include "../../include/rmsnorm.h"
 
 namespace {
 
@@ -28,6 +31,14 @@ decltype(&hgemm_gated) f_gated = nullptr;
 decltype(&hgemm_gated_bwd) f_gated_bwd = nullptr;
 decltype(&layernorm_fwd) f_ln_fwd = nullptr;
 decltype(&layernorm_bwd) f_ln_bwd = nullptr;
+decltype(&rmsnorm_fwd) f_rms_fwd = nullptr;
+decltype(&rmsnorm_fwd_e4m3) f_rms_e4m3 = nullptr;
+decltype(&quantize_rows_e4m3) f_rows_e4m3 = nullptr;
+decltype(&rmsnorm_bwd) f_rms_bwd = nullptr;
+decltype(&dropout_fwd) f_drop_fwd = nullptr;
+decltype(&dropout_bwd) f_drop_bwd = nullptr;
+decltype(&qgemm_epilogue) f_q_epilogue = nullptr;
+decltype(&qgemm_gated) f_q_gated = nullptr;
 PyObject* on_error = nullptr;
 
 // Arguments by position or name. `names` ends with nullptr; the first `required` must be given.
@@ -106,6 +117,7 @@ struct Call {
   int device = 0;
   void* stream = nullptr;
   bool check = true;
+  const char* others = "the type of the first operand";  // what the other operands have to be of
 
   // Element type from the first operand; device and stream; the check flag.
   bool begin(const at::Tensor& first, const char* name, PyObject* stream_arg, PyObject* check_arg) {
@@ -143,12 +155,20 @@ struct Call {
 
   // Address and leading dimension of a rows x cols matrix of the call's type.
   bool matrix(PyObject* o, const char* name, int64_t rows, int64_t cols, bool optional, void** ptr, int64_t* ld) const {
+    return matrix_of(type, others, o, name, rows, cols, optional, ptr, ld);
+  }
+  // ... of 8-bit values.
+  bool matrix8(PyObject* o, const char* name, int64_t rows, int64_t cols, void** ptr, int64_t* ld) const {
+    return matrix_of(at::kFloat8_e4m3fn, "float8_e4m3fn", o, name, rows, cols, false, ptr, ld);
+  }
+  bool matrix_of(at::ScalarType t, const char* what, PyObject* o, const char* name, int64_t rows, int64_t cols, bool optional, void** ptr,
+                 int64_t* ld) const {
     *ptr = nullptr;
     *ld = cols > 0 ? cols : 1;
     const at::Tensor* x = tensor(o, name, optional);
     if (!x) return !PyErr_Occurred();
-    if (x->scalar_type() != type || x->dim() != 2) {
-      PyErr_Format(PyExc_TypeError, "%s: need a 2-D tensor of the type of the first operand", name);
+    if (x->scalar_type() != t || x->dim() != 2) {
+      PyErr_Format(PyExc_TypeError, "%s: need a 2-D tensor of %s", name, what);
       return false;
     }
     if (!on_device(*x, name)) return false;
@@ -178,7 +198,7 @@ struct Call {
     const at::Tensor* x = tensor(o, name, optional);
     if (!x) return !PyErr_Occurred();
     if (x->scalar_type() != t || x->dim() != 1) {
-      PyErr_Format(PyExc_TypeError, "%s: need a 1-D tensor of %s", name, t == at::kFloat ? "float32" : "the type of the first operand");
+      PyErr_Format(PyExc_TypeError, "%s: need a 1-D tensor of %s", name, t == at::kFloat ? "float32" : others);
       return false;
     }
     if (!on_device(*x, name)) return false;
@@ -220,6 +240,21 @@ bool integer(PyObject* o, int fallback, int* out) {
   if (v == -1 && PyErr_Occurred()) return false;
   *out = v < -1000 ? -1000 : v > 1000 ? 1000 : (int)v;
   return true;
+}
+
+// A 64-bit word from any integer (its two's complement, modulo 2^64).
+bool word64(PyObject* o, uint64_t* out) {
+  *out = 0;
+  if (!o) return true;
+  PyObject* n = PyNumber_Index(o);
+  if (!n) return false;
+  *out = PyLong_AsUnsignedLongLongMask(n);
+  Py_DECREF(n);
+  return !PyErr_Occurred();
+}
+bool real(PyObject* o, double fallback, double* out) {
+  *out = fallback;
+  return !o || (*out = PyFloat_AsDouble(o)) != -1.0 || !PyErr_Occurred();
 }
 
 // Runs `body`, turning a C++ exception (from torch) into a Python one.
@@ -377,17 +412,222 @@ PyObject* py_ln_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject
   });
 }
 
-// connect(addresses of the six C functions in the order below, error function)
+PyObject* py_rms_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"X", "gamma", "Y", "eps", "residual", "sum", "rstd", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("rmsnorm_fwd", names, keys.keys, 3, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* X = operand(a.v[0], "X");
+    if (!X) return nullptr;
+    Call c{"rmsnorm_fwd"};
+    double eps;
+    if (!c.begin(*X, "X", a.v[7], a.v[8]) || !real(a.v[3], 1e-5, &eps)) return nullptr;
+    const int64_t rows = X->size(0), cols = X->size(1);
+    void *px, *g, *py, *pr, *ps, *rstd;
+    int64_t ldx, ldy, ldr, lds;
+    if (!c.matrix(a.v[0], "X", rows, cols, false, &px, &ldx) || !c.vector(a.v[1], "gamma", c.type, cols, true, &g) ||
+        !c.matrix(a.v[2], "Y", rows, cols, false, &py, &ldy) || !c.matrix(a.v[4], "residual", rows, cols, true, &pr, &ldr) ||
+        !c.matrix(a.v[5], "sum", rows, cols, true, &ps, &lds) || !c.vector(a.v[6], "rstd", at::kFloat, rows, true, &rstd))
+      return nullptr;
+    return c.done(f_rms_fwd(c.code, rows, cols, px, ldx, pr, ldr, g, (float)eps, ps, lds, py, ldy, static_cast<float*>(rstd), c.stream));
+  });
+}
+
+PyObject* py_rms_e4m3(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"X", "gamma", "Q", "scale", "eps", "residual", "sum", "rstd", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("rmsnorm_fwd_e4m3", names, keys.keys, 4, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* X = operand(a.v[0], "X");
+    if (!X) return nullptr;
+    Call c{"rmsnorm_fwd_e4m3"};
+    double eps;
+    if (!c.begin(*X, "X", a.v[8], a.v[9]) || !real(a.v[4], 1e-5, &eps)) return nullptr;
+    const int64_t rows = X->size(0), cols = X->size(1);
+    void *px, *g, *pq, *scale, *pr, *ps, *rstd;
+    int64_t ldx, ldq, ldr, lds;
+    if (!c.matrix(a.v[0], "X", rows, cols, false, &px, &ldx) || !c.vector(a.v[1], "gamma", c.type, cols, true, &g) ||
+        !c.matrix8(a.v[2], "Q", rows, cols, &pq, &ldq) || !c.vector(a.v[3], "scale", at::kFloat, rows, false, &scale) ||
+        !c.matrix(a.v[5], "residual", rows, cols, true, &pr, &ldr) || !c.matrix(a.v[6], "sum", rows, cols, true, &ps, &lds) ||
+        !c.vector(a.v[7], "rstd", at::kFloat, rows, true, &rstd))
+      return nullptr;
+    return c.done(f_rms_e4m3(c.code, rows, cols, px, ldx, pr, ldr, g, (float)eps, ps, lds, pq, ldq, static_cast<float*>(scale),
+                             static_cast<float*>(rstd), c.stream));
+  });
+}
+
+PyObject* py_rows_e4m3(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"X", "Q", "scale", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("quantize_rows_e4m3", names, keys.keys, 3, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* X = operand(a.v[0], "X");
+    if (!X) return nullptr;
+    Call c{"quantize_rows_e4m3"};
+    if (!c.begin(*X, "X", a.v[3], a.v[4])) return nullptr;
+    const int64_t rows = X->size(0), cols = X->size(1);
+    void *px, *pq, *scale;
+    int64_t ldx, ldq;
+    if (!c.matrix(a.v[0], "X", rows, cols, false, &px, &ldx) || !c.matrix8(a.v[1], "Q", rows, cols, &pq, &ldq) ||
+        !c.vector(a.v[2], "scale", at::kFloat, rows, false, &scale))
+      return nullptr;
+    return c.done(f_rows_e4m3(c.code, rows, cols, px, ldx, pq, ldq, static_cast<float*>(scale), c.stream));
+  });
+}
+
+PyObject* py_rms_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"S", "gamma", "rstd", "dY", "dsum", "dX", "dgamma", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("rmsnorm_bwd", names, keys.keys, 4, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* S = operand(a.v[0], "S");
+    if (!S) return nullptr;
+    Call c{"rmsnorm_bwd"};
+    if (!c.begin(*S, "S", a.v[7], a.v[8])) return nullptr;
+    const int64_t rows = S->size(0), cols = S->size(1);
+    void *ps, *g, *rstd, *pd, *pr, *dx, *dg;
+    int64_t lds, lddy, ldds, lddx;
+    if (!c.matrix(a.v[0], "S", rows, cols, false, &ps, &lds) || !c.vector(a.v[1], "gamma", c.type, cols, true, &g) ||
+        !c.vector(a.v[2], "rstd", at::kFloat, rows, true, &rstd) || !c.matrix(a.v[3], "dY", rows, cols, false, &pd, &lddy) ||
+        !c.matrix(a.v[4], "dsum", rows, cols, true, &pr, &ldds) || !c.matrix(a.v[5], "dX", rows, cols, true, &dx, &lddx) ||
+        !c.vector(a.v[6], "dgamma", at::kFloat, cols, true, &dg))
+      return nullptr;
+    return c.done(f_rms_bwd(c.code, rows, cols, ps, lds, g, static_cast<float*>(rstd), pd, lddy, pr, ldds, dx, lddx, static_cast<float*>(dg),
+                            c.stream));
+  });
+}
+
+// The device address of dropout's counter of uses: one int64 value, or None.
+bool counter(const Call& c, PyObject* o, int64_t** ptr) {
+  *ptr = nullptr;
+  const at::Tensor* x = tensor(o, "step", true);
+  if (!x) return !PyErr_Occurred();
+  if (x->scalar_type() != at::kLong || x->numel() != 1) {
+    PyErr_SetString(PyExc_TypeError, "step: need a tensor of one int64 value");
+    return false;
+  }
+  if (!c.on_device(*x, "step")) return false;
+  *ptr = static_cast<int64_t*>(x->data_ptr());
+  return true;
+}
+
+PyObject* py_drop_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"X", "Y", "p", "seed", "offset", "residual", "step", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("dropout_fwd", names, keys.keys, 4, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* X = operand(a.v[0], "X");
+    if (!X) return nullptr;
+    Call c{"dropout_fwd"};
+    double p;
+    uint64_t seed, offset;
+    if (!c.begin(*X, "X", a.v[7], a.v[8]) || !real(a.v[2], 0.0, &p) || !word64(a.v[3], &seed) || !word64(a.v[4], &offset)) return nullptr;
+    const int64_t rows = X->size(0), cols = X->size(1);
+    void *px, *py, *pr;
+    int64_t ldx, ldy, ldr, *step;
+    if (!c.matrix(a.v[0], "X", rows, cols, false, &px, &ldx) || !c.matrix(a.v[1], "Y", rows, cols, false, &py, &ldy) ||
+        !c.matrix(a.v[5], "residual", rows, cols, true, &pr, &ldr) || !counter(c, a.v[6], &step))
+      return nullptr;
+    return c.done(f_drop_fwd(c.code, rows, cols, px, ldx, pr, ldr, p, seed, offset, step, py, ldy, c.stream));
+  });
+}
+
+PyObject* py_drop_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"dY", "dX", "p", "seed", "offset", "step", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("dropout_bwd", names, keys.keys, 4, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* D = operand(a.v[0], "dY");
+    if (!D) return nullptr;
+    Call c{"dropout_bwd"};
+    double p;
+    uint64_t seed, offset;
+    if (!c.begin(*D, "dY", a.v[6], a.v[7]) || !real(a.v[2], 0.0, &p) || !word64(a.v[3], &seed) || !word64(a.v[4], &offset)) return nullptr;
+    const int64_t rows = D->size(0), cols = D->size(1);
+    void *pd, *px;
+    int64_t ldd, ldx, *step;
+    if (!c.matrix(a.v[0], "dY", rows, cols, false, &pd, &ldd) || !c.matrix(a.v[1], "dX", rows, cols, false, &px, &ldx) ||
+        !counter(c, a.v[5], &step))
+      return nullptr;
+    return c.done(f_drop_bwd(c.code, rows, cols, pd, ldd, p, seed, offset, step, px, ldx, c.stream));
+  });
+}
+
+PyObject* py_q_epilogue(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"A", "B", "D", "a_scale", "b_scale", "bias", "act", "residual", "preact", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("qgemm_epilogue", names, keys.keys, 3, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor *A = operand(a.v[0], "A"), *B = A ? operand(a.v[1], "B") : nullptr, *D = B ? operand(a.v[2], "D") : nullptr;
+    int act;
+    if (!D || !integer(a.v[6], HGEMM_ACT_NONE, &act)) return nullptr;
+    Call c{"qgemm_epilogue"};
+    c.others = "the type of the output";
+    if (!c.begin(*D, "D", a.v[9], a.v[10])) return nullptr;
+    const int64_t M = A->size(0), K = A->size(1), N = B->size(0);
+    void *pa, *pb, *pd, *pr, *pz, *sa, *sb, *bias;
+    int64_t lda, ldb, ldd, ldr, ldz;
+    if (!c.matrix8(a.v[0], "A", M, K, &pa, &lda) || !c.matrix8(a.v[1], "B", N, K, &pb, &ldb) || !c.matrix(a.v[2], "D", M, N, false, &pd, &ldd) ||
+        !c.vector(a.v[3], "a_scale", at::kFloat, M, true, &sa) || !c.vector(a.v[4], "b_scale", at::kFloat, N, true, &sb) ||
+        !c.vector(a.v[5], "bias", c.type, N, true, &bias) || !c.matrix(a.v[7], "residual", M, N, true, &pr, &ldr) ||
+        !c.matrix(a.v[8], "preact", M, N, true, &pz, &ldz))
+      return nullptr;
+    return c.done(f_q_epilogue(c.code, M, N, K, pa, lda, static_cast<float*>(sa), pb, ldb, static_cast<float*>(sb), bias, act, pr, ldr, pd, ldd,
+                               pz, ldz, c.stream));
+  });
+}
+
+PyObject* py_q_gated(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"X", "Wg", "Wu", "H", "x_scale", "g_scale", "u_scale", "act", "gate", "up", "stream", "check", nullptr};
+  static Names keys(names);
+  Args a;
+  if (!a.parse("qgemm_gated", names, keys.keys, 4, args, nargs, kwnames)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor *X = operand(a.v[0], "X"), *W = X ? operand(a.v[1], "Wg") : nullptr, *H = W ? operand(a.v[3], "H") : nullptr;
+    int act;
+    if (!H || !integer(a.v[7], HGEMM_ACT_SILU, &act)) return nullptr;
+    Call c{"qgemm_gated"};
+    c.others = "the type of the output";
+    if (!c.begin(*H, "H", a.v[10], a.v[11])) return nullptr;
+    const int64_t M = X->size(0), K = X->size(1), F = W->size(0);
+    void *px, *pg, *pu, *ph, *og, *ou, *sx, *sg, *su;
+    int64_t ldx, ldwg, ldwu, ldh, ldg, ldu;
+    if (!c.matrix8(a.v[0], "X", M, K, &px, &ldx) || !c.matrix8(a.v[1], "Wg", F, K, &pg, &ldwg) || !c.matrix8(a.v[2], "Wu", F, K, &pu, &ldwu) ||
+        !c.matrix(a.v[3], "H", M, F, false, &ph, &ldh) || !c.vector(a.v[4], "x_scale", at::kFloat, M, true, &sx) ||
+        !c.vector(a.v[5], "g_scale", at::kFloat, F, true, &sg) || !c.vector(a.v[6], "u_scale", at::kFloat, F, true, &su) ||
+        !c.matrix(a.v[8], "gate", M, F, true, &og, &ldg) || !c.matrix(a.v[9], "up", M, F, true, &ou, &ldu))
+      return nullptr;
+    return c.done(f_q_gated(c.code, M, F, K, px, ldx, static_cast<float*>(sx), pg, ldwg, static_cast<float*>(sg), pu, ldwu,
+                            static_cast<float*>(su), act, ph, ldh, og, ldg, ou, ldu, c.stream));
+  });
+}
+
+// connect(addresses of the C functions in this order, error function)
 PyObject* py_connect(PyObject*, PyObject* args) {
-  unsigned long long p[6];
-  PyObject* handler;
-  if (!PyArg_ParseTuple(args, "KKKKKKO", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &handler)) return nullptr;
-  f_epilogue = reinterpret_cast<decltype(f_epilogue)>(p[0]);
-  f_epilogue_bwd = reinterpret_cast<decltype(f_epilogue_bwd)>(p[1]);
-  f_gated = reinterpret_cast<decltype(f_gated)>(p[2]);
-  f_gated_bwd = reinterpret_cast<decltype(f_gated_bwd)>(p[3]);
-  f_ln_fwd = reinterpret_cast<decltype(f_ln_fwd)>(p[4]);
-  f_ln_bwd = reinterpret_cast<decltype(f_ln_bwd)>(p[5]);
+  void** const slots[] = {reinterpret_cast<void**>(&f_epilogue),  reinterpret_cast<void**>(&f_epilogue_bwd), reinterpret_cast<void**>(&f_gated),
+                          reinterpret_cast<void**>(&f_gated_bwd), reinterpret_cast<void**>(&f_ln_fwd),       reinterpret_cast<void**>(&f_ln_bwd),
+                          reinterpret_cast<void**>(&f_rms_fwd),   reinterpret_cast<void**>(&f_rms_e4m3),     reinterpret_cast<void**>(&f_rows_e4m3),
+                          reinterpret_cast<void**>(&f_rms_bwd),   reinterpret_cast<void**>(&f_drop_fwd),     reinterpret_cast<void**>(&f_drop_bwd),
+                          reinterpret_cast<void**>(&f_q_epilogue), reinterpret_cast<void**>(&f_q_gated)};
+  constexpr Py_ssize_t n = sizeof(slots) / sizeof(slots[0]);
+  if (PyTuple_GET_SIZE(args) != n + 1) {
+    PyErr_Format(PyExc_TypeError, "connect: takes %zd addresses and a function", n);
+    return nullptr;
+  }
+  void* p[n];
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args, i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  for (Py_ssize_t i = 0; i < n; ++i) *slots[i] = p[i];
+  PyObject* handler = PyTuple_GET_ITEM(args, n);
   Py_INCREF(handler);
   Py_XSETREF(on_error, handler);
   Py_RETURN_NONE;
@@ -427,10 +667,49 @@ PyMethodDef methods[] = {
      "layernorm_bwd(X, gamma, mean, rstd, dY, dX=None, dgamma=None, dbeta=None, stream=None, check=True)\n--\n\n"
      "Gradients of :func:`layernorm_fwd` for the incoming ``dY``: ``dX`` (type of ``X``), ``dgamma`` and ``dbeta`` (cols,\n"
      "``float32``), each written if given. ``mean`` and ``rstd`` are the forward pass's."},
+    {"rmsnorm_fwd", FAST(py_rms_fwd),
+     "rmsnorm_fwd(X, gamma, Y, eps=1e-05, residual=None, sum=None, rstd=None, stream=None, check=True)\n--\n\n"
+     "``s = X + residual``, ``Y = s * rstd * gamma`` over the rows, ``rstd = 1 / sqrt(mean(s^2) + eps)``, asynchronously.\n\n"
+     "``X``, ``Y``, ``residual``, ``sum`` (rows x cols) and ``gamma`` (cols, or ``None``): CUDA tensors of one type, ``float32``,\n"
+     "``float16`` or ``bfloat16``. ``sum`` (receives ``s``; it may be ``X`` or ``residual`` itself) and ``rstd`` (rows, ``float32``)\n"
+     "are written if given. ``Y`` and ``rstd`` are computed from ``s`` before it is rounded."},
+    {"rmsnorm_fwd_e4m3", FAST(py_rms_e4m3),
+     "rmsnorm_fwd_e4m3(X, gamma, Q, scale, eps=1e-05, residual=None, sum=None, rstd=None, stream=None, check=True)\n--\n\n"
+     ":func:`rmsnorm_fwd` with its output in 8 bits: ``scale = max(max|y|, 2^-100) / 448`` for each row (``float32``) and ``Q``\n"
+     "(rows x cols, ``float8_e4m3fn``) the nearest values to ``y / scale``."},
+    {"quantize_rows_e4m3", FAST(py_rows_e4m3),
+     "quantize_rows_e4m3(X, Q, scale, stream=None, check=True)\n--\n\n"
+     "The rows of ``X`` in 8 bits, as :func:`rmsnorm_fwd_e4m3` brings its output there."},
+    {"rmsnorm_bwd", FAST(py_rms_bwd),
+     "rmsnorm_bwd(S, gamma, rstd, dY, dsum=None, dX=None, dgamma=None, stream=None, check=True)\n--\n\n"
+     "Gradients of :func:`rmsnorm_fwd` for the incoming ``dY`` and, where the sum goes on, ``dsum``: ``dX`` (of ``X`` and of the\n"
+     "residual; it may be ``dsum`` itself) and ``dgamma`` (cols, ``float32``), each written if given. ``S`` is the forward pass's sum\n"
+     "(``X`` where there was no residual), ``rstd`` its statistics."},
+    {"dropout_fwd", FAST(py_drop_fwd),
+     "dropout_fwd(X, Y, p, seed, offset=0, residual=None, step=None, stream=None, check=True)\n--\n\n"
+     "``Y = residual + (keep ? X / (1 - p) : 0)``, asynchronously, with a mask that is a function of ``seed`` and ``offset`` (64 bits each),\n"
+     "row and column, and is never stored.\n\n"
+     "``X``, ``Y``, ``residual`` (rows x cols): CUDA tensors of one type, ``float32``, ``float16`` or ``bfloat16``; ``Y`` may be ``X`` or\n"
+     "``residual`` itself. ``step``: a CUDA tensor of one ``int64`` value that is added to ``offset`` when the kernel runs, so that a\n"
+     "captured call can have another mask in each replay."},
+    {"dropout_bwd", FAST(py_drop_bwd),
+     "dropout_bwd(dY, dX, p, seed, offset=0, step=None, stream=None, check=True)\n--\n\n"
+     "The gradient of :func:`dropout_fwd` with the same ``p``, ``seed``, ``offset`` and ``step``: ``dX = keep ? dY / (1 - p) : 0``. ``dX`` may\n"
+     "be ``dY`` itself. (The residual's gradient is ``dY``.)"},
+    {"qgemm_epilogue", FAST(py_q_epilogue),
+     "qgemm_epilogue(A, B, D, a_scale=None, b_scale=None, bias=None, act=0, residual=None, preact=None, stream=None, check=True)\n--\n\n"
+     "``Z = a_scale[:, None] * b_scale * (A @ B.T) + bias``, ``D = act(Z) + residual`` with operands of 8 bits, asynchronously.\n\n"
+     "``A`` (M x K) and ``B`` (N x K): CUDA tensors of ``float8_e4m3fn``; ``a_scale`` (M) and ``b_scale`` (N): ``float32``, ones if not\n"
+     "given; ``D`` and the optional ``bias``, ``residual`` and ``preact`` as in :func:`hgemm_epilogue`."},
+    {"qgemm_gated", FAST(py_q_gated),
+     "qgemm_gated(X, Wg, Wu, H, x_scale=None, g_scale=None, u_scale=None, act=4, gate=None, up=None, stream=None, check=True)\n--\n\n"
+     "Gated projections of 8-bit operands: ``H = act(G) * U`` with ``G = x_scale[:, None] * g_scale * (X @ Wg.T)`` and ``U`` alike.\n\n"
+     "``X`` (M x K), ``Wg`` and ``Wu`` (F x K): CUDA tensors of ``float8_e4m3fn``; scales ``float32``; ``H`` and the optional ``gate`` and\n"
+     "``up`` (both or neither) as in :func:`hgemm_gated`."},
     {"connect", py_connect, METH_VARARGS, "Addresses of the C functions and the function that raises on an error status."},
     {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Compiled argument marshalling of libdgemm's 16-bit products and layer norm.", -1, methods};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Compiled argument marshalling of libdgemm's 16-bit and 8-bit products, norms and dropout.", -1, methods};
 
 }  // namespace
 

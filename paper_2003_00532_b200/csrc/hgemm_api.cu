@@ -1,5 +1,5 @@
-// C ABI of the 16-bit products (include/hgemm.h): validation, packing of operands TMA cannot
-// address, choice of tile and work decomposition, tensor maps, launches.
+// C ABI of the 16-bit products (include/hgemm.h) and those of 8-bit operands (include/qgemm.h): validation, packing of
+// operands TMA cannot address, choice of tile and work decomposition, tensor maps, launches.
 #include <atomic>
 #include <cstdint>
 #include <cstring>
@@ -9,6 +9,7 @@
 #include <cuda_runtime.h>
 
 #include "../../include/hgemm.h"
+#include "../../include/qgemm.h"
 #include "hgemm_aux.cuh"
 #include "hgemm_kernels.h"
 #include "lm_state.h"
@@ -31,7 +32,12 @@ std::atomic<int> g_drop_limit_us{0};
 
 // ---- kernels by type --------------------------------------------------------------------------------
 
-bool launch_tc(int type, bool gated, int act, int config, int clusters, cudaStream_t stream, const Params& p) {
+bool launch_tc(int type, bool eight, bool gated, int act, int config, int clusters, cudaStream_t stream, const Params& p) {
+  if (eight) {
+    if (type == HGEMM_TYPE_BF16)
+      return gated ? launch_gated8_bf16(act, config, clusters, stream, p) : launch_plain8_bf16(act, config, clusters, stream, p);
+    return gated ? launch_gated8_f16(act, config, clusters, stream, p) : launch_plain8_f16(act, config, clusters, stream, p);
+  }
   if (type == HGEMM_TYPE_BF16)
     return gated ? launch_gated_bf16(act, config, clusters, stream, p) : launch_plain_bf16(act, config, clusters, stream, p);
   return gated ? launch_gated_f16(act, config, clusters, stream, p) : launch_plain_f16(act, config, clusters, stream, p);
@@ -241,30 +247,33 @@ bool make_plan(const Size* sz, int n, bool gated, int sms, Plan* best) {
 
 // ---- operands -----------------------------------------------------------------------------------------
 
-// A matrix as it is stored: rows x cols values, row-major.
+// A matrix as it is stored: rows x cols values of 16 bits, or of 8, row-major.
 struct Matrix {
   const void* ptr;
   int64_t rows, cols, ld;
+  bool eight = false;
+  int64_t bytes() const { return eight ? 1 : 2; }                   // of a value
+  int64_t padded_ld() const { return eight ? (cols + 127) / 128 * 128 : (cols + 63) / 64 * 64; }  // whole 128-byte rows
 };
 
 // TMA takes 16-byte aligned rows. A single row has no stride that matters.
-bool addressable(const Matrix& m) { return ((uintptr_t)m.ptr & 15) == 0 && (m.ld % 8 == 0 || m.rows == 1); }
+bool addressable(const Matrix& m) { return ((uintptr_t)m.ptr & 15) == 0 && (m.ld * m.bytes() % 16 == 0 || m.rows == 1); }
 
 bool make_map(CUtensorMap* map, int type, const Matrix& m, int box_rows) {
-  const int64_t ld = m.rows == 1 ? (m.cols + 7) / 8 * 8 : m.ld;
+  const int64_t ld = m.rows == 1 ? m.padded_ld() : m.ld;
   const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)TK, (cuuint32_t)box_rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(ld * m.bytes())};
+  const cuuint32_t box[2] = {(cuuint32_t)(m.eight ? TK8 : TK), (cuuint32_t)box_rows};
   const cuuint32_t estr[2] = {1, 1};
-  return g_encode(map, type == HGEMM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                  const_cast<void*>(m.ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return g_encode(map, m.eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : type == HGEMM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                  2, const_cast<void*>(m.ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 int64_t padded(int64_t cols) { return (cols + 63) / 64 * 64; }
 inline unsigned capped(int64_t n) { return (unsigned)(n < 65535 ? n : 65535); }
 
-// Operands that need rewriting, collected so that one launch and one buffer serve them all.
+// Operands that need rewriting (all of 16 bits, or all of 8), collected so that one launch and one buffer serve them all.
 class Packer {
  public:
   explicit Packer(int sms, size_t first_free = 0) : most_(8u * sms), bytes_(first_free) {}
@@ -278,7 +287,7 @@ class Packer {
       }
     src_[n_] = *m;
     at_[n_] = bytes_;
-    bytes_ += (size_t)m->rows * padded(m->cols) * 2;
+    bytes_ += (size_t)m->rows * m->padded_ld() * m->bytes();
     users_[nu_] = m;
     of_[nu_++] = n_++;
   }
@@ -289,19 +298,19 @@ class Packer {
     memset(&ops, 0, sizeof(ops));
     for (int i = 0; i < n_; ++i) {
       const Matrix& m = src_[i];
-      ops.op[i] = PackOp{static_cast<const uint16_t*>(m.ptr), m.ld, (int)m.rows, (int)m.cols,
-                         reinterpret_cast<uint16_t*>(buf + at_[i]), padded(m.cols)};
-      const int64_t blocks = ((m.cols + 7) / 8 * m.rows + 255) / 256;
+      ops.op[i] = PackOp{m.ptr, m.ld, (int)m.rows, (int)m.cols, buf + at_[i], m.padded_ld()};
+      const int64_t vec = 16 / m.bytes(), blocks = ((m.cols + vec - 1) / vec * m.rows + 255) / 256;
       blocks_ += (unsigned)(blocks < most_ ? blocks : most_);
       ops.end[i] = blocks_;
     }
-    for (int i = 0; i < nu_; ++i) *users_[i] = Matrix{buf + at_[of_[i]], users_[i]->rows, users_[i]->cols, padded(users_[i]->cols)};
+    for (int i = 0; i < nu_; ++i) *users_[i] = Matrix{buf + at_[of_[i]], users_[i]->rows, users_[i]->cols, users_[i]->padded_ld(), users_[i]->eight};
     return ops;
   }
   unsigned blocks() const { return blocks_; }  // after finish()
   bool launch(char* buf, cudaStream_t stream) {
     const PackOps ops = finish(buf);
-    return blocks_ == 0 || lm::launch(hgemm_pack_kernel, dim3(blocks_), dim3(256), 0, 1, stream, ops);
+    const bool eight = n_ > 0 && src_[0].eight;
+    return blocks_ == 0 || lm::launch(eight ? hgemm_pack8_kernel : hgemm_pack_kernel, dim3(blocks_), dim3(256), 0, 1, stream, ops);
   }
 
  private:
@@ -333,9 +342,13 @@ struct Product {
   int64_t ldz = 0;
   void* U = nullptr;
   int64_t ldu = 0;
+  bool eight = false;  // operands of 8 bits, with the scales of op(A)'s rows and of op(B)'s columns (gated: of both)
+  const float* row_scale = nullptr;
+  const float* col_scale[2] = {nullptr, nullptr};
+  int step() const { return eight ? TK8 : TK; }  // values of a k-block
   Size size() const {
     int64_t kb = 0;
-    for (int i = 0; i < nseg; ++i) kb += (K[i] + TK - 1) / TK;
+    for (int i = 0; i < nseg; ++i) kb += (K[i] + step() - 1) / step();
     int count = R ? 1 : 0, unaligned = 0;
     const auto add = [&](const void* p, int64_t ld) {
       if (!p) return;
@@ -390,7 +403,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.tiles_n = q.tiles_n;
     d.tiles_m = q.tiles_m;
     d.kblocks = s.size().kblocks;
-    d.kb_seg0 = (int)((s.K[0] + TK - 1) / TK);
+    d.kb_seg0 = (int)((s.K[0] + s.step() - 1) / s.step());
     d.p_mn = s.p_mn;
     d.q_mn = s.q_mn;
     d.rounds = q.rounds;
@@ -408,6 +421,9 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
     d.ldd = s.ldd;
     d.ldz = s.ldz;
     d.ldu = s.ldu;
+    d.row_scale = s.row_scale;
+    d.col_scale[0] = s.col_scale[0];
+    d.col_scale[1] = s.col_scale[1];
   }
   p.nprob = n;
   p.rounds = pl.rounds;
@@ -421,7 +437,7 @@ int run_products(int type, bool gated, Product** pr, int n, const Plan& pl, lm::
   p.drop = drop > 0;
   p.status = st->status;
   p.unscale = unscale;
-  return launch_tc(type, gated, pr[0]->act, pl.config, pl.clusters, stream, p) ? DGEMM_OK : lm::cuda_failed();
+  return launch_tc(type, pr[0]->eight, gated, pr[0]->act, pl.config, pl.clusters, stream, p) ? DGEMM_OK : lm::cuda_failed();
 }
 
 // ---- validation -----------------------------------------------------------------------------------------
@@ -442,6 +458,13 @@ int check(const void* ptr, int64_t rows, int64_t cols, int64_t ld, bool optional
   if (ld > (int64_t)1 << 38) return DGEMM_ERR_BAD_LD;
   return DGEMM_OK;
 }
+
+// The same of 8-bit values: any address, ld in bytes.
+int check8(const void* ptr, int64_t rows, int64_t cols, int64_t ld) {
+  if (ld < (cols > 0 ? cols : 1) || ld > (int64_t)1 << 38) return DGEMM_ERR_BAD_LD;
+  return ptr || rows == 0 || cols == 0 ? (int)DGEMM_OK : (int)DGEMM_ERR_NULL;
+}
+int64_t span8(int64_t rows, int64_t cols, int64_t ld) { return rows > 0 && cols > 0 ? (rows - 1) * ld + cols : 0; }
 
 struct Range {
   const void* ptr;
@@ -478,7 +501,7 @@ int run_empty(int type, int64_t M, int64_t N, const void* bias, int act, const v
 
 // Whether a product runs on the kernels for one or two rows.
 bool by_token(const Product& s, bool gated) {
-  return s.M <= TOKEN_ROWS && !s.p_mn && addressable(s.p[0]) && (!gated || addressable(s.p[1])) &&
+  return !s.eight && s.M <= TOKEN_ROWS && !s.p_mn && addressable(s.p[0]) && (!gated || addressable(s.p[1])) &&
          s.M * ((s.K[0] + 7) / 8 * 8) * 2 <= (int64_t)TOKEN_SMEM && g_drop_limit_us.load() == 0;
 }
 int run_token(int type, bool gated, const Product& s, int sms, cudaStream_t stream) {
@@ -572,7 +595,9 @@ int device_state(DeviceState** out) {
     if (cudaGetSymbolAddress(reinterpret_cast<void**>(&st.status), g_hgemm_status_word) != cudaSuccess ||
         cudaGetSymbolAddress(reinterpret_cast<void**>(&st.counters), g_hgemm_counters) != cudaSuccess)
       return lm::cuda_failed();
-    if (!configure_plain_f16() || !configure_gated_f16() || !configure_plain_bf16() || !configure_gated_bf16()) return lm::cuda_failed();
+    if (!configure_plain_f16() || !configure_gated_f16() || !configure_plain_bf16() || !configure_gated_bf16() || !configure_plain8_f16() ||
+        !configure_gated8_f16() || !configure_plain8_bf16() || !configure_gated8_bf16())
+      return lm::cuda_failed();
     if (!g_encode) {
       void* fn = nullptr;
       cudaDriverEntryPointQueryResult qres;
@@ -935,6 +960,97 @@ int hgemm_gated_bwd(int type, int transw, int64_t M, int64_t F, int64_t K, const
   }
   return run_products(type, false, list, n, pl, st, ws, st->counters + hold.lease_index() * lm::kCounters, s,
                       gp.range.inverse);
+}
+
+int qgemm_epilogue(int type, int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* a_scale, const void* B, int64_t ldb,
+                   const float* b_scale, const void* bias, int act, const void* R, int64_t ldr, void* D, int64_t ldd, void* Z, int64_t ldz,
+                   void* stream) {
+  if (bad_type(type) || bad_act(act)) return DGEMM_ERR_VARIANT;
+  if (M < 0 || N < 0 || K < 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  if (M == 0 || N == 0) return DGEMM_OK;
+  HGEMM_TRY(check8(A, M, K, lda));
+  HGEMM_TRY(check8(B, N, K, ldb));
+  HGEMM_TRY(check(R, M, N, ldr, true));
+  HGEMM_TRY(check(D, M, N, ldd));
+  HGEMM_TRY(check(Z, M, N, ldz, true));
+  if (((uintptr_t)bias & 1) || (((uintptr_t)a_scale | (uintptr_t)b_scale) & 3)) return DGEMM_ERR_ALIGN;
+  const bool in_place = R == D && ldr == ldd;
+  const Range rg[8] = {{D, span(M, N, ldd)},   {Z, span(M, N, ldz)}, {A, span8(M, K, lda)}, {B, span8(N, K, ldb)},
+                       {a_scale, M * 4}, {b_scale, N * 4}, {bias, N * 2}, {in_place ? nullptr : R, span(M, N, ldr)}};
+  if (aliased(rg, 2, 8)) return DGEMM_ERR_ALIAS;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (K == 0) {
+    lm::DeviceState* st = nullptr;
+    HGEMM_TRY(lm::device_state(&st));
+    return run_empty(type, M, N, bias, act, R, ldr, D, ldd, Z, ldz, s);
+  }
+  Product pr;
+  pr.eight = true;
+  pr.row_scale = a_scale;
+  pr.col_scale[0] = b_scale;
+  pr.N = N;
+  pr.M = M;
+  pr.nseg = 1;
+  pr.K[0] = K;
+  pr.p[0] = Matrix{B, N, K, ldb, true};
+  pr.q[0] = Matrix{A, M, K, lda, true};
+  pr.p_mn = pr.q_mn = false;
+  pr.act = act;
+  pr.bias = bias;
+  pr.R = R;
+  pr.ldr = ldr;
+  pr.D = D;
+  pr.ldd = ldd;
+  pr.Z = Z;
+  pr.ldz = ldz;
+  return forward(type, false, &pr, s);
+}
+
+int qgemm_gated(int type, int64_t M, int64_t F, int64_t K, const void* X, int64_t ldx, const float* x_scale, const void* Wg, int64_t ldwg,
+                const float* g_scale, const void* Wu, int64_t ldwu, const float* u_scale, int act, void* H, int64_t ldh, void* G, int64_t ldg,
+                void* U, int64_t ldu, void* stream) {
+  if (bad_type(type) || bad_act(act)) return DGEMM_ERR_VARIANT;
+  if (M < 0 || F < 0 || K < 0 || M > kMaxDim || F > kMaxDim || K > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  if (M == 0 || F == 0) return DGEMM_OK;
+  HGEMM_TRY(check8(X, M, K, ldx));
+  HGEMM_TRY(check8(Wg, F, K, ldwg));
+  HGEMM_TRY(check8(Wu, F, K, ldwu));
+  HGEMM_TRY(check(H, M, F, ldh));
+  HGEMM_TRY(check(G, M, F, ldg, true));
+  HGEMM_TRY(check(U, M, F, ldu, true));
+  if ((G == nullptr) != (U == nullptr)) return DGEMM_ERR_NULL;
+  if (((uintptr_t)x_scale | (uintptr_t)g_scale | (uintptr_t)u_scale) & 3) return DGEMM_ERR_ALIGN;
+  const Range rg[9] = {{H, span(M, F, ldh)}, {G, span(M, F, ldg)}, {U, span(M, F, ldu)}, {X, span8(M, K, ldx)}, {Wg, span8(F, K, ldwg)},
+                       {Wu, span8(F, K, ldwu)}, {x_scale, M * 4}, {g_scale, F * 4}, {u_scale, F * 4}};
+  if (aliased(rg, 3, 9)) return DGEMM_ERR_ALIAS;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (K == 0) {  // G = U = 0, H = act(0) 0
+    lm::DeviceState* st = nullptr;
+    HGEMM_TRY(lm::device_state(&st));
+    HGEMM_TRY(run_empty(type, M, F, nullptr, HGEMM_ACT_NONE, nullptr, 0, H, ldh, G, ldg, s));
+    return U ? run_empty(type, M, F, nullptr, HGEMM_ACT_NONE, nullptr, 0, U, ldu, nullptr, 0, s) : (int)DGEMM_OK;
+  }
+  Product pr;
+  pr.eight = true;
+  pr.row_scale = x_scale;
+  pr.col_scale[0] = g_scale;
+  pr.col_scale[1] = u_scale;
+  pr.N = F;
+  pr.M = M;
+  pr.nseg = 1;
+  pr.K[0] = K;
+  pr.p[0] = Matrix{Wg, F, K, ldwg, true};
+  pr.p[1] = Matrix{Wu, F, K, ldwu, true};
+  pr.q[0] = Matrix{X, M, K, ldx, true};
+  pr.p_mn = pr.q_mn = false;
+  pr.act = act;
+  pr.D = H;
+  pr.ldd = ldh;
+  pr.Z = G;
+  pr.ldz = ldg;
+  pr.U = U;
+  pr.ldu = ldu;
+  return forward(type, true, &pr, s);
 }
 
 int hgemm_last_device_status(void* stream) {

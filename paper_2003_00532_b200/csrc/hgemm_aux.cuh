@@ -13,10 +13,10 @@ namespace hgemm {
 // ---- packing --------------------------------------------------------------------------------------
 
 struct PackOp {
-  const uint16_t* src;
+  const void* src;  // 16-bit or 8-bit values
   long long ld_src;
   int rows, cols;
-  uint16_t* dst;
+  void* dst;
   long long ld_dst;
 };
 struct PackOps {
@@ -75,9 +75,9 @@ __device__ __forceinline__ void pack_body(const PackOps& ops, unsigned block) {
   const long long total = (long long)per_row * o.rows, step = (long long)(ops.end[k] - first) * blockDim.x;
   for (long long i = (long long)(block - first) * blockDim.x + threadIdx.x; i < total; i += step) {
     const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 8;
-    const uint16_t* src = o.src + r * o.ld_src + c;
+    const uint16_t* src = static_cast<const uint16_t*>(o.src) + r * o.ld_src + c;
     const uint4 v = load8(src, c, o.cols, false);
-    *reinterpret_cast<uint4*>(o.dst + r * o.ld_dst + c) = v;
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(o.dst) + r * o.ld_dst + c) = v;
   }
 }
 // (Forward. The gradients' copies are blocks of the element-wise kernels below: a launch of their own cost 2 to 3 us,
@@ -86,6 +86,47 @@ __global__ void __launch_bounds__(256) hgemm_pack_kernel(const __grid_constant__
   ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
   pack_body(ops, blockIdx.x);
+}
+
+// 16 values of 8 bits at src[0 .. 16), the columns c .. of a row of `cols`; those beyond the row are zero. Five aligned words
+// shifted by the row's misalignment, or, where those would reach beyond the row, one value after the other.
+__device__ __forceinline__ uint4 load16(const uint8_t* src, int c, int cols) {
+  uint4 v;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  const int off = (int)(reinterpret_cast<uintptr_t>(src) & 3);  // bytes of the first word before the first value
+  if (c >= off && c + 20 - off <= cols) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(src - off);
+    uint32_t x[5];
+#pragma unroll
+    for (int j = 0; j < 5; ++j) x[j] = p[j];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(x[j], x[j + 1], 8 * off);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = 0;
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        if (c + 4 * j + b < cols) w[j] |= (uint32_t)src[4 * j + b] << 8 * b;
+    }
+  }
+  return v;
+}
+// The same copies for matrices of 8-bit values, 16 of them per thread.
+__global__ void __launch_bounds__(256) hgemm_pack8_kernel(const __grid_constant__ PackOps ops) {
+  ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  const unsigned block = blockIdx.x;
+  int k = 0;
+  while (block >= ops.end[k]) ++k;
+  const unsigned first = k ? ops.end[k - 1] : 0;
+  const PackOp& o = ops.op[k];
+  const int per_row = (o.cols + 15) / 16;
+  const long long total = (long long)per_row * o.rows, step = (long long)(ops.end[k] - first) * blockDim.x;
+  for (long long i = (long long)(block - first) * blockDim.x + threadIdx.x; i < total; i += step) {
+    const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * 16;
+    *reinterpret_cast<uint4*>(static_cast<uint8_t*>(o.dst) + r * o.ld_dst + c) = load16(static_cast<const uint8_t*>(o.src) + r * o.ld_src + c, c, o.cols);
+  }
 }
 
 // ---- empty sums -----------------------------------------------------------------------------------

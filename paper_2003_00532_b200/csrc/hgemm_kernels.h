@@ -21,6 +21,11 @@ bool launch_plain_f16(int act, int config, int clusters, cudaStream_t stream, co
 bool launch_plain_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
 bool launch_gated_f16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
 bool launch_gated_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+// ... for operands in e4m3 and outputs of that type.
+bool launch_plain8_f16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+bool launch_plain8_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+bool launch_gated8_f16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
+bool launch_gated8_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p);
 
 // Products of at most TOKEN_ROWS rows with 16-byte aligned weights stored N x K (hgemm_token.cuh). The tokens must fit in
 // TOKEN_SMEM bytes of shared memory.
@@ -32,5 +37,9 @@ bool configure_plain_f16();
 bool configure_plain_bf16();
 bool configure_gated_f16();
 bool configure_gated_bf16();
+bool configure_plain8_f16();
+bool configure_plain8_bf16();
+bool configure_gated8_f16();
+bool configure_gated8_bf16();
 
 }  // namespace hgemm

@@ -31,22 +31,22 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t addr, uint32_t cols) {
 __device__ __forceinline__ void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// ---- MMA: D (TMEM, binary32) (+)= A (smem) B (smem), K = 16; issued by one thread -------------------
+// ---- MMA: D (TMEM, binary32) (+)= A (smem) B (smem), 32 bytes of K (16 values of 16 bits, or 32 of 8: EIGHT); issued by one
+// thread ----
 
-template <int CG>
-__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-  if (CG == 1)
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
-        : "memory");
+template <int CG, bool EIGHT>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+#define HGEMM_MMA(form)                                                                                                            \
+  asm volatile(                                                                                                                    \
+      "{\n\t.reg .pred p;\n\t"                                                                                                    \
+      "setp.ne.b32 p, %4, 0;\n\t"                                                                                                  \
+      "tcgen05.mma." form " [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)             \
+      : "memory")
+  if (CG == 1 && !EIGHT) HGEMM_MMA("cta_group::1.kind::f16");
+  if (CG == 2 && !EIGHT) HGEMM_MMA("cta_group::2.kind::f16");
+  if (CG == 1 && EIGHT) HGEMM_MMA("cta_group::1.kind::f8f6f4");
+  if (CG == 2 && EIGHT) HGEMM_MMA("cta_group::2.kind::f8f6f4");
+#undef HGEMM_MMA
 }
 
 // Arrives on `bar` (for a pair: on the barrier at that offset in both CTAs) when all MMAs this

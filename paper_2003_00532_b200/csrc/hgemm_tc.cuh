@@ -25,6 +25,10 @@
 // counter per tile) adds all parts in order and runs the epilogue: one launch, no CTA waits for another, same bits
 // every time.
 //
+// Operands of 8 bits (e4m3, with a scale per row of each) run the same code: a 128-byte row of a box then holds 128 values, an MMA
+// instruction takes 32 of them in the time of 16 values of 16 bits, and the epilogue multiplies the sums by the two scales before
+// anything else. K-major only.
+//
 // The activation is a template argument of the whole kernel: with a switch over the five of them in it, the
 // registers of all shared one allocation and the epilogue without activation spilled (4096 x 9472 x 256: 50 us,
 // 40 alone).
@@ -49,12 +53,31 @@
 namespace hgemm {
 
 constexpr int TK = 64;           // k-block: 64 values of 16 bits = one 128-byte swizzled row
+constexpr int TK8 = 128;         // ... of 8 bits
 constexpr int BOX_BYTES = 8192;  // 64 x 64 values
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 128 + 32 * EPI_WARPS;
 constexpr int PITCH = 80;  // bytes per patch row in shared memory: 64 + 16, no two of 8 rows on the same banks
 constexpr int MAX_SMEM = 232448;  // 227 KB
 constexpr int MAX_PROBLEMS = 3;
+
+// A kernel's element type: T for operands and outputs of that type, Eight<T> for operands in e4m3 and outputs of type T.
+template <typename T>
+struct Eight {};
+template <typename T>
+struct Kind {
+  using Out = T;
+  static constexpr bool EIGHT = false;
+  static constexpr int TK = hgemm::TK;
+  static constexpr uint32_t FORMAT = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;  // in the instruction descriptor
+};
+template <typename T>
+struct Kind<Eight<T>> {
+  using Out = T;
+  static constexpr bool EIGHT = true;
+  static constexpr int TK = TK8;
+  static constexpr uint32_t FORMAT = 0u;
+};
 
 // CG: CTAs per tile (1, or a pair); BM: TMEM columns of the tile (rows of the output); NB: blocks of 128 lanes per CTA.
 // With NB = 1 the two accumulators are two tiles', filled and drained in turn; with NB = 2 they are the two lane
@@ -97,6 +120,8 @@ struct alignas(64) Problem {
   void* Z;                 // pre-activation; gated: gate pre-activation
   void* U;                 // gated: up pre-activation
   long long ldr, ldd, ldz, ldu;
+  const float* row_scale;     // operands of 8 bits: of op(A)'s rows and of op(B)'s columns (gated: gate, up), NULL: ones
+  const float* col_scale[2];
 };
 
 struct Params {
@@ -361,16 +386,42 @@ struct Epilogue {
   bool has_z, has_r;
   float unscale;  // see Params (read by the binary16 kernel without activation alone)
   float bias[4];  // bias[j]: of column 8 j + lane / 4 of the patch
+  const float* row_scale;  // operands of 8 bits: of the tile's rows, or NULL; and of the columns, as `bias`
+  float col[4], col_up[4];
+};
+
+// The scales of a patch's rows, in the order in which a thread holds them: row[b] of rows 8 b + 2 (lane % 4) and the next.
+template <int CH>
+struct RowScales {
+  float2 row[CH / 8];
+  __device__ __forceinline__ void fetch(const Epilogue<CH>& ep, int m) {
+#pragma unroll
+    for (int b = 0; b < CH / 8; ++b) {
+      const int r = m + 8 * b + 2 * (ep.pt.lane & 3);
+      row[b].x = ep.row_scale && r < ep.pt.rows ? __ldg(ep.row_scale + r) : 1.f;
+      row[b].y = ep.row_scale && r + 1 < ep.pt.rows ? __ldg(ep.row_scale + r + 1) : 1.f;
+    }
+  }
+  __device__ __forceinline__ void apply(const float* col, float* v) const {
+    constexpr int MB = CH / 8;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const float2 r = row[i / 4 % MB];
+      v[i] = v[i] * (i % 2 ? r.y : r.x) * col[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+    }
+  }
 };
 
 // The gradients' products, whose operand may have been scaled, run without activation; bfloat16 needs no scaling.
 template <typename T, int ACT>
 constexpr bool UNSCALED = std::is_same<T, __half>::value && ACT == HGEMM_ACT_NONE;
 
-template <typename T, int CH, int ACT>
-__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, float* v, const typename Patch<CH>::Raw& raw) {
+template <typename K, int CH, int ACT>
+__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, float* v, const typename Patch<CH>::Raw& raw, const RowScales<CH>& rs) {
+  using T = typename Kind<K>::Out;
   constexpr int MB = CH / 8;
-  if (UNSCALED<T, ACT> && ep.unscale != 1.f) {
+  if constexpr (Kind<K>::EIGHT) rs.apply(ep.col, v);
+  if (UNSCALED<K, ACT> && ep.unscale != 1.f) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) v[i] *= ep.unscale;
   }
@@ -398,8 +449,13 @@ __device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, float*
   ep.pt.store(ep.d, m, q);
 }
 
-template <typename T, int CH, int ACT>
-__device__ __forceinline__ void emit_gated(const Epilogue<CH>& ep, int m, const float* g, const float* u) {
+template <typename K, int CH, int ACT>
+__device__ __forceinline__ void emit_gated(const Epilogue<CH>& ep, int m, float* g, float* u, const RowScales<CH>& rs) {
+  using T = typename Kind<K>::Out;
+  if constexpr (Kind<K>::EIGHT) {
+    rs.apply(ep.col, g);
+    rs.apply(ep.col_up, u);
+  }
   uint32_t q[CH / 2];
   if (ep.has_z) {
 #pragma unroll
@@ -474,7 +530,7 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
                                               typename Patch<C::CH>::Raw& raw, const EpiWarp& ew, int rows, bool n_in) {
   using namespace dgemm::ptx;
   constexpr int CG = C::CG, BM = C::BM, CH = C::CH, BLOCKS = C::CG * C::NB, GROUPS = EPI_WARPS / 4;
-  constexpr bool GATED = C::GATED;
+  constexpr bool GATED = C::GATED, EIGHT = Kind<T>::EIGHT;
   // a part's sums in the workspace: [slot][block][quarter][chunk][CH / 4][lane] of float4
   constexpr long long WS_SLOT = (long long)BLOCKS * BM * 32;  // float4 per slot
   constexpr int WS_CHUNK = CH / 4 * 32;                   // float4 per quarter and chunk
@@ -494,6 +550,8 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
     if (!GATED) {
       for (int c = ew.group; c * CH < rows; c += GROUPS) {
         float v[CH];
+        RowScales<CH> rs;
+        if (EIGHT) rs.fetch(ep, c * CH);
         tmem_load<CH>(ew.acc + c * CH, v);
         ptx5::tmem_ld_wait<CH>(v);
         if ((c + GROUPS) * CH >= rows) release();
@@ -501,7 +559,7 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
           const typename Patch<CH>::Raw now = raw;
           // the next chunk's residual is on its way while this one is computed
           if (ep.has_r && (c + GROUPS) * CH < rows) ep.pt.fetch(raw, ep.r, (c + GROUPS) * CH);
-          emit_plain<T, CH, ACT>(ep, c * CH, v, now);
+          emit_plain<T, CH, ACT>(ep, c * CH, v, now, rs);
         }
       }
     } else {
@@ -511,6 +569,9 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
       const uint32_t mine = ew.bufs + ew.e * C::BUF_BYTES + ew.lane * 16, theirs = ew.bufs + (ew.e ^ 2) * C::BUF_BYTES + ew.lane * 16;
       for (int c = 2 * ew.group; c * CH < rows; c += 2 * GROUPS) {
         float v[CH], o[CH];
+        RowScales<CH> rs;
+        const int m = (is_g ? c : c + 1) * CH;
+        if (EIGHT) rs.fetch(ep, m);
         tmem_load<CH>(ew.acc + (is_g ? c + 1 : c) * CH, o);  // what the partner needs
         tmem_load<CH>(ew.acc + (is_g ? c : c + 1) * CH, v);  // what stays here
         ptx5::tmem_ld_wait<CH>(o);
@@ -522,10 +583,9 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
 #pragma unroll
         for (int j = 0; j < CH / 4; ++j) *reinterpret_cast<uint4*>(o + 4 * j) = ptx5::lds128(theirs + j * 512);
         named_barrier_sync(1 + ew.group * 2 + (ew.quad & 1), 64);
-        const int m = (is_g ? c : c + 1) * CH;
         if (n_in && m < rows) {
-          if (is_g) emit_gated<T, CH, ACT>(ep, m, v, o);
-          else emit_gated<T, CH, ACT>(ep, m, o, v);
+          if (is_g) emit_gated<T, CH, ACT>(ep, m, v, o, rs);
+          else emit_gated<T, CH, ACT>(ep, m, o, v, rs);
         }
       }
     }
@@ -558,8 +618,10 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
         for (int c = ew.group; c * CH < rows; c += GROUPS) {
           if (ep.has_r && n_in) ep.pt.fetch(raw, ep.r, c * CH);
           float v[CH];
+          RowScales<CH> rs;
+          if (EIGHT) rs.fetch(ep, c * CH);
           add_parts<CH>(first + c * WS_CHUNK, next + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, v);
-          if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw);
+          if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw, rs);
         }
       } else {
         const float4* first = ws_cta + w.first_slot * WS_SLOT + ((ew.quad & 1) * (BM / CH)) * WS_CHUNK;
@@ -567,9 +629,11 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
         constexpr int UP = 2 * (BM / CH) * WS_CHUNK;  // the up projection's quarters
         for (int c = 2 * ew.group + (ew.quad >> 1); c * CH < rows; c += 2 * GROUPS) {
           float g[CH], uu[CH];
+          RowScales<CH> rs;
+          if (EIGHT) rs.fetch(ep, c * CH);
           add_parts<CH>(first + c * WS_CHUNK, next + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, g);
           add_parts<CH>(first + UP + c * WS_CHUNK, next + UP + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, uu);
-          if (n_in) emit_gated<T, CH, ACT>(ep, c * CH, g, uu);
+          if (n_in) emit_gated<T, CH, ACT>(ep, c * CH, g, uu, rs);
         }
       }
     }
@@ -589,6 +653,8 @@ template <typename T, int CG, int BM, int NB, bool GATED, int ACT>
 __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_constant__ Params p) {
   using namespace dgemm::ptx;
   using C = Cfg<CG, BM, NB, GATED>;
+  using Out = typename Kind<T>::Out;
+  constexpr bool EIGHT = Kind<T>::EIGHT;
   constexpr int STAGES = C::STAGES, CH = C::CH;
 
   extern __shared__ uint8_t smem_raw[];
@@ -657,7 +723,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         const uint32_t fb = CG == 1 ? full_bar + 8 * s : map_to_cta(full_bar + 8 * s, 0);
         if (warp == 0 && rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, bytes);
         const int seg = kb >= pr.kb_seg0 ? 1 : 0;
-        const int k0 = (kb - (seg ? pr.kb_seg0 : 0)) * TK;
+        const int k0 = (kb - (seg ? pr.kb_seg0 : 0)) * Kind<T>::TK;
         const uint32_t dst = base + s * C::STAGE_BYTES;
         const auto load_p = [&](int i) {
           const CUtensorMap* map = &pr.p[GATED ? i & 1 : seg];
@@ -690,7 +756,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     }
   } else if (warp == 1 && lane == 0 && rank == 0) {
     // ---- MMAs ----
-    constexpr uint32_t fmt = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    constexpr uint32_t fmt = Kind<T>::FORMAT;
     constexpr uint32_t idesc0 = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(BM >> 3) << 17) | ((uint32_t)((128 * CG) >> 4) << 24);
     uint32_t it = 0, acc_it = 0;
     bool ok = true;
@@ -703,7 +769,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
         const uint32_t src = base + stage * C::STAGE_BYTES;
         const uint64_t pd = smem_desc(src + block * 2 * BOX_BYTES, pr.p_mn), qd = smem_desc(src + C::P_BYTES, pr.q_mn);
 #pragma unroll
-        for (int k = 0; k < TK / 16; ++k) ptx5::mma_f16<CG>(d, pd + k * p_step, qd + k * q_step, idesc, !first || k > 0);
+        for (int k = 0; k < 4; ++k) ptx5::mma<CG, EIGHT>(d, pd + k * p_step, qd + k * q_step, idesc, !first || k > 0);
       };
       const auto staged = [&](uint32_t i) {
         if (!wait_bounded(full_bar + 8 * (i % STAGES), (i / STAGES) & 1u, abort_flag, p)) return false;
@@ -791,8 +857,13 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int n = n0 + 8 * j + (lane >> 2);
-          ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const T*>(pr.bias)[n]) : 0.f;
+          ep.bias[j] = !GATED && pr.bias && n < pr.N ? to_f32(static_cast<const Out*>(pr.bias)[n]) : 0.f;
+          if (EIGHT) {
+            ep.col[j] = pr.col_scale[0] && n < pr.N ? __ldg(pr.col_scale[0] + n) : 1.f;
+            if (GATED) ep.col_up[j] = pr.col_scale[1] && n < pr.N ? __ldg(pr.col_scale[1] + n) : 1.f;
+          }
         }
+        if (EIGHT) ep.row_scale = pr.row_scale ? pr.row_scale + m_base : nullptr;
         typename Patch<CH>::Raw raw;
         if (ep.has_r && n_in && w.slot < 0) ep.pt.fetch(raw, ep.r, group * CH);
         const uint32_t a = NB == 1 ? acc_it & 1u : (uint32_t)h;

@@ -1,0 +1,11 @@
+// Gated projections of 8-bit operands with outputs in bfloat16 on the tensor cores.
+#include "hgemm_kernels.cuh"
+
+namespace hgemm {
+
+bool launch_gated8_bf16(int act, int config, int clusters, cudaStream_t stream, const Params& p) {
+  return launch_config<Eight<__nv_bfloat16>, true>(act, config, clusters, stream, p);
+}
+bool configure_gated8_bf16() { return configure_all<Eight<__nv_bfloat16>, true>(); }
+
+}  // namespace hgemm

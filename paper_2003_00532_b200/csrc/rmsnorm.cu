@@ -1,0 +1,278 @@
+// C ABI of root-mean-square norm (include/rmsnorm.h): validation, choice of kernel, launches.
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+
+#include <cuda_runtime.h>
+
+#include "../../include/rmsnorm.h"
+#include "lm_state.h"
+#include "rmsnorm.cuh"
+#include "row_launch.h"
+
+namespace {
+
+using namespace rmsn;
+using namespace rowop;
+
+// How a row is spread over threads: vectors per thread, and threads (32: one warp per row).
+struct Shape {
+  int items, threads;
+  bool longer;  // does not fit in registers
+};
+
+// Forward: a warp for rows of up to 16 values per lane; a block with 16 values per thread beyond (or up to 32, for rows
+// that need them). Few rows are spread over as many threads as there are vectors, because then the latency of
+// one row counts.
+Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms) {
+  const int64_t nv = (cols + vec - 1) / vec;
+  const int most = 32 / vec, warp_most = 16 / vec;
+  const bool spread = rows * ((nv + 32 * most - 1) / (32 * most)) < (int64_t)sms * 16;  // warps in all
+  if (nv <= 32 || (!spread && nv <= 32 * warp_most)) return Shape{pow2((nv + 31) / 32), 32, false};
+  int items = spread ? 1 : 16 / vec;
+  while (items < most && threads_for(nv, items) > fwd_threads(items * vec)) items *= 2;
+  const int threads = threads_for(nv, items);
+  if (threads > fwd_threads(items * vec)) return Shape{0, 1024, true};
+  return Shape{items, threads, false};
+}
+// Backward: a warp for rows of up to 16 values per lane; a block with 16 values per thread beyond; 32 (`WIDE`) for rows that need
+// them: 8193 to 16384 columns.
+Shape bwd_shape(int64_t cols, int vec) {
+  const int64_t nv = (cols + vec - 1) / vec;
+  const int most = 16 / vec;
+  if (nv <= 32 * most) return Shape{pow2((nv + 31) / 32), 32, false};
+  for (int items = most; items <= 2 * most; items *= 2)
+    if (threads_for(nv, items) <= BWD_THREADS) return Shape{items, threads_for(nv, items), false};
+  return Shape{0, 1024, true};
+}
+
+template <typename T, int VEC, int ITEMS, int OUT>
+bool launch_fwd(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
+  const auto go = [&](auto k, int threads, int64_t need) {
+    constexpr auto kernel = decltype(k)::value;
+    const unsigned blocks = resident_blocks<std::remove_const_t<decltype(kernel)>, kernel>(sms, threads, 0, need);
+    return blocks > 0 && lm::launch(kernel, dim3(blocks), dim3(threads), 0, 1, stream, p);
+  };
+  if (s.threads == 32) {
+    if constexpr (VEC * ITEMS <= 16)
+      return go(std::integral_constant<void (*)(const Params), &fwd_kernel<T, VEC, ITEMS, true, OUT>>(), 128, (p.rows + 3) / 4);
+    return false;
+  }
+  return go(std::integral_constant<void (*)(const Params), &fwd_kernel<T, VEC, ITEMS, false, OUT>>(), s.threads, p.rows);
+}
+template <typename T, int VEC, int OUT>
+bool run_fwd_vec(int sms, const Params& p, cudaStream_t stream) {
+  const Shape s = fwd_shape(p.rows, p.cols, VEC, sms);
+  if (s.longer) return lm::launch(fwd_long_kernel<T, VEC, OUT>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p);
+  switch (s.items) {
+    case 1: return launch_fwd<T, VEC, 1, OUT>(sms, s, p, stream);
+    case 2: return launch_fwd<T, VEC, 2, OUT>(sms, s, p, stream);
+    case 4: return launch_fwd<T, VEC, 4, OUT>(sms, s, p, stream);
+    case 8: return VEC <= 4 && launch_fwd<T, VEC <= 4 ? VEC : 1, 8, OUT>(sms, s, p, stream);
+    case 16: return VEC == 1 && launch_fwd<T, 1, 16, OUT>(sms, s, p, stream);
+    default: return VEC == 1 && launch_fwd<T, 1, 32, OUT>(sms, s, p, stream);
+  }
+}
+template <int OUT>
+bool run_fwd(int type, bool aligned, const Params& p, const lm::DeviceState* st, cudaStream_t stream) {
+  const int sms = st->sm_count;
+  if (type == HGEMM_TYPE_F32) return aligned ? run_fwd_vec<float, 4, OUT>(sms, p, stream) : run_fwd_vec<float, 1, OUT>(sms, p, stream);
+  if (type == HGEMM_TYPE_F16) return aligned ? run_fwd_vec<__half, 8, OUT>(sms, p, stream) : run_fwd_vec<__half, 1, OUT>(sms, p, stream);
+  return aligned ? run_fwd_vec<__nv_bfloat16, 8, OUT>(sms, p, stream) : run_fwd_vec<__nv_bfloat16, 1, OUT>(sms, p, stream);
+}
+
+// Blocks of the backward pass: as many as fit at once, but for few rows at least eight rows each (every block leaves
+// its own sums to be added), down to one per SM.
+template <typename K, K kernel>
+int bwd_blocks(int sms, int threads, size_t smem, int64_t rows, int rows_per_block) {
+  const int64_t need = (rows + rows_per_block - 1) / rows_per_block;
+  const int64_t some = (int)resident_blocks<K, kernel>(sms, threads, smem, need);
+  const int64_t eighth = (rows + 8 * rows_per_block - 1) / (8 * rows_per_block);
+  const int64_t want = eighth > sms ? eighth : sms;
+  return (int)(some < want ? some : want);
+}
+
+// Runs the row kernel; `partial` is asked for the matrix of the blocks' sums. Returns the number of blocks, 0 on failure.
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE, typename F>
+int launch_bwd(int sms, int threads, Params& p, cudaStream_t stream, F partial) {
+  constexpr auto kernel = &bwd_kernel<T, VEC, ITEMS, WARP_ROW, WIDE>;
+  const size_t smem = WIDE ? (size_t)threads * ITEMS * VEC * 8 : WARP_ROW && p.want_params ? (size_t)p.cols * 4 : 0;
+  if (WIDE && !allow_smem<decltype(kernel), kernel>(BWD_THREADS * ITEMS * VEC * 8)) return 0;
+  const size_t most = WIDE ? smem : WARP_ROW ? (size_t)32 * ITEMS * VEC * 4 : 0;
+  const int blocks = bwd_blocks<decltype(kernel), kernel>(sms, threads, most, p.rows, WARP_ROW ? 8 : 1);
+  if (blocks == 0 || !partial(blocks)) return 0;
+  return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p) ? blocks : 0;
+}
+template <typename T, int VEC, typename F>
+int run_bwd_vec(int sms, Params& p, cudaStream_t stream, F partial) {
+  const Shape s = bwd_shape(p.cols, VEC);
+  if (s.longer) {
+    const int chunks = (int)((p.rows + 15) / 16 < sms * 2 ? (p.rows + 15) / 16 : sms * 2);
+    if (!partial(chunks)) return 0;
+    if (p.out && !lm::launch(bwd_long_kernel<T, VEC>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p)) return 0;
+    if (p.want_params && !lm::launch(bwd_long_params_kernel<T>, dim3((unsigned)((p.cols + 255) / 256), chunks), dim3(256), 0, 1, stream, p))
+      return 0;
+    return chunks;
+  }
+  constexpr int MOST = 16 / VEC;
+  if (s.threads == 32) {
+    if (s.items == 1) return launch_bwd<T, VEC, 1, true, false>(sms, 256, p, stream, partial);
+    if (s.items == 2) return launch_bwd<T, VEC, 2, true, false>(sms, 256, p, stream, partial);
+    if constexpr (MOST >= 4)
+      if (s.items == 4) return launch_bwd<T, VEC, 4, true, false>(sms, 256, p, stream, partial);
+    if constexpr (MOST >= 16) {
+      if (s.items == 8) return launch_bwd<T, VEC, 8, true, false>(sms, 256, p, stream, partial);
+      if (s.items == 16) return launch_bwd<T, VEC, 16, true, false>(sms, 256, p, stream, partial);
+    }
+    return 0;
+  }
+  if (s.items == MOST) return launch_bwd<T, VEC, MOST, false, false>(sms, s.threads, p, stream, partial);
+  return launch_bwd<T, VEC, 2 * MOST, false, true>(sms, s.threads, p, stream, partial);
+}
+template <typename T, int VEC, typename F>
+int run_bwd(int sms, bool aligned, Params& p, cudaStream_t stream, F partial) {
+  return aligned ? run_bwd_vec<T, VEC>(sms, p, stream, partial) : run_bwd_vec<T, 1>(sms, p, stream, partial);
+}
+
+struct Range {
+  const void* ptr;
+  int64_t bytes;
+};
+// Outputs must not overlap inputs or one another; the first `nout` ranges are the outputs. `skip`: an input that is an output itself.
+bool aliased(const Range* r, int nout, int n) {
+  for (int i = 0; i < nout; ++i)
+    for (int j = i + 1; j < n; ++j)
+      if (r[i].ptr && r[j].ptr && r[i].bytes > 0 && r[j].bytes > 0 && lm::ranges_overlap(r[i].ptr, r[i].bytes, r[j].ptr, r[j].bytes))
+        return true;
+  return false;
+}
+
+// The forward pass in its three forms.
+template <int OUT>
+int forward(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* gamma, float eps,
+            void* S, int64_t lds, void* out, int64_t ldo, float* scale, float* rstd, cudaStream_t stream) {
+  constexpr bool EIGHT = OUT != OUT_Y;
+  if (bad_type(type) || !std::isfinite(eps) || eps < 0.f) return DGEMM_ERR_VARIANT;
+  if (rows < 0 || cols < 0 || rows > kMaxDim || cols > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  if (rows == 0 || cols == 0) return DGEMM_OK;
+  int rc = check(type, X, rows, cols, ldx);
+  if (rc == DGEMM_OK && R) rc = check(type, R, rows, cols, ldr);
+  if (rc == DGEMM_OK && S) rc = check(type, S, rows, cols, lds);
+  if (rc != DGEMM_OK) return rc;
+  if (EIGHT) {
+    if (ldo < cols || ldo > (int64_t)1 << 38) return DGEMM_ERR_BAD_LD;
+    if (!out || !scale) return DGEMM_ERR_NULL;
+  } else if ((rc = check(type, out, rows, cols, ldo)) != DGEMM_OK) {
+    return rc;
+  }
+  if (((uintptr_t)gamma & (elem_bytes(type) - 1)) || (((uintptr_t)scale | (uintptr_t)rstd) & 3)) return DGEMM_ERR_ALIGN;
+  // S in the place of an input: the same values in the same places
+  const bool on_x = S && S == X && lds == ldx, on_r = S && R && S == R && lds == ldr;
+  const int64_t nx = span(type, rows, cols, ldx), nr = R ? span(type, rows, cols, ldr) : 0, ns = S ? span(type, rows, cols, lds) : 0;
+  const int64_t no = EIGHT ? (rows - 1) * ldo + cols : span(type, rows, cols, ldo);
+  const Range r[] = {{S, ns}, {out, no}, {rstd, rows * 4}, {scale, rows * 4}, {gamma, cols * elem_bytes(type)}, {on_x ? nullptr : X, nx}, {on_r ? nullptr : R, nr}};
+  if (aliased(r, 4, 7)) return DGEMM_ERR_ALIAS;
+  lm::DeviceState* st = nullptr;
+  if ((rc = lm::device_state(&st)) != DGEMM_OK) return rc;
+  Params p;
+  memset(&p, 0, sizeof(p));
+  p.rows = rows;
+  p.cols = (int)cols;
+  p.X = X;
+  p.ldx = ldx;
+  p.R = R;
+  p.ldr = R ? ldr : 0;
+  p.gamma = gamma;
+  p.eps = eps;
+  p.S = S;
+  p.lds = S ? lds : 0;
+  p.out = out;
+  p.ldo = ldo;
+  p.scale = scale;
+  p.rstd = rstd;
+  const int vec = 16 / elem_bytes(type);
+  const bool aligned = rows_aligned(type, X, ldx) && (!R || rows_aligned(type, R, ldr)) && (!S || rows_aligned(type, S, lds)) &&
+                       ((uintptr_t)gamma & 15) == 0 &&
+                       (EIGHT ? (((uintptr_t)out | (uintptr_t)ldo) & (vec - 1)) == 0 : rows_aligned(type, out, ldo));
+  return run_fwd<OUT>(type, aligned, p, st, stream) ? DGEMM_OK : lm::cuda_failed();
+}
+
+}  // namespace
+
+extern "C" {
+
+int rmsnorm_fwd(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* gamma, float eps,
+                void* S, int64_t lds, void* Y, int64_t ldy, float* rstd, void* stream) {
+  return forward<OUT_Y>(type, rows, cols, X, ldx, R, ldr, gamma, eps, S, lds, Y, ldy, nullptr, rstd, static_cast<cudaStream_t>(stream));
+}
+
+int rmsnorm_fwd_e4m3(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* gamma,
+                     float eps, void* S, int64_t lds, void* Q, int64_t ldq, float* scale, float* rstd, void* stream) {
+  return forward<OUT_E4M3>(type, rows, cols, X, ldx, R, ldr, gamma, eps, S, lds, Q, ldq, scale, rstd, static_cast<cudaStream_t>(stream));
+}
+
+int quantize_rows_e4m3(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, void* Q, int64_t ldq, float* scale, void* stream) {
+  return forward<OUT_ROWS>(type, rows, cols, X, ldx, nullptr, 0, nullptr, 0.f, nullptr, 0, Q, ldq, scale, nullptr,
+                           static_cast<cudaStream_t>(stream));
+}
+
+int rmsnorm_bwd(int type, int64_t rows, int64_t cols, const void* S, int64_t lds, const void* gamma, const float* rstd, const void* dY,
+                int64_t lddy, const void* dS, int64_t ldds, void* dX, int64_t lddx, float* dgamma, void* stream) {
+  if (bad_type(type)) return DGEMM_ERR_VARIANT;
+  if (rows < 0 || cols < 0 || rows > kMaxDim || cols > kMaxDim) return DGEMM_ERR_BAD_DIM;
+  if (cols == 0) return DGEMM_OK;
+  int rc = check(type, S, rows, cols, lds);
+  if (rc == DGEMM_OK) rc = check(type, dY, rows, cols, lddy);
+  if (rc == DGEMM_OK && dS) rc = check(type, dS, rows, cols, ldds);
+  if (rc == DGEMM_OK && dX) rc = check(type, dX, rows, cols, lddx);
+  if (rc != DGEMM_OK) return rc;
+  if (rows > 0 && !rstd) return DGEMM_ERR_NULL;
+  if (((uintptr_t)gamma & (elem_bytes(type) - 1)) || (((uintptr_t)rstd | (uintptr_t)dgamma) & 3)) return DGEMM_ERR_ALIGN;
+  const bool in_place = dX && dX == dS && lddx == ldds;
+  const Range r[] = {{dX, span(type, rows, cols, lddx)}, {dgamma, cols * 4}, {S, span(type, rows, cols, lds)}, {gamma, cols * elem_bytes(type)},
+                     {rstd, rows * 4}, {dY, span(type, rows, cols, lddy)}, {in_place ? nullptr : dS, span(type, rows, cols, ldds)}};
+  if (aliased(r, 2, 7) || (in_place && dgamma && lm::ranges_overlap(dgamma, cols * 4, dS, span(type, rows, cols, ldds)))) return DGEMM_ERR_ALIAS;
+  lm::DeviceState* st = nullptr;
+  if ((rc = lm::device_state(&st)) != DGEMM_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    if (dgamma && cudaMemsetAsync(dgamma, 0, (size_t)cols * 4, s) != cudaSuccess) return lm::cuda_failed();
+    return DGEMM_OK;
+  }
+  if (!dX && !dgamma) return DGEMM_OK;
+  Params p;
+  memset(&p, 0, sizeof(p));
+  p.rows = rows;
+  p.cols = (int)cols;
+  p.X = S;
+  p.ldx = lds;
+  p.gamma = gamma;
+  p.dY = dY;
+  p.ldy = lddy;
+  p.R = dX ? dS : nullptr;
+  p.ldr = p.R ? ldds : 0;
+  p.out = dX;
+  p.ldo = dX ? lddx : 0;
+  p.rstd = const_cast<float*>(rstd);
+  p.want_params = dgamma != nullptr;
+  p.ldp = (cols + 3) / 4 * 4;
+  const bool aligned = rows_aligned(type, S, lds) && rows_aligned(type, dY, lddy) && (!p.R || rows_aligned(type, dS, ldds)) &&
+                       (!dX || rows_aligned(type, dX, lddx)) && ((uintptr_t)gamma & 15) == 0;
+  scratch::Hold hold(st->scratch, s);
+  const auto partial = [&](int blocks) {
+    if (p.want_params) p.partial = static_cast<float*>(hold.workspace((size_t)blocks * p.ldp * 4));
+    return !p.want_params || p.partial != nullptr;
+  };
+  const int blocks = type == HGEMM_TYPE_F32   ? run_bwd<float, 4>(st->sm_count, aligned, p, s, partial)
+                     : type == HGEMM_TYPE_F16 ? run_bwd<__half, 8>(st->sm_count, aligned, p, s, partial)
+                                              : run_bwd<__nv_bfloat16, 8>(st->sm_count, aligned, p, s, partial);
+  if (blocks == 0) return lm::cuda_failed();
+  const bool many = blocks > lnorm::MANY_BLOCKS;
+  if (p.want_params && !lm::launch(many ? lnorm::bwd_reduce_kernel<32> : lnorm::bwd_reduce_kernel<16>, dim3((unsigned)((cols + 31) / 32)),
+                                   dim3(many ? 1024 : 512), 0, 1, s, (const float*)p.partial, blocks, (int)cols, (int)p.ldp, dgamma,
+                                   (float*)nullptr))
+    return lm::cuda_failed();
+  return DGEMM_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,552 @@
+// Root-mean-square norm with the residual's addition, forward (to the operands' type or to 8 bits with a scale per row)
+// and backward. Bound by memory: each kernel reads its rows once, holds them in registers through all sums, and writes once.
+//
+// A row belongs to one warp (short rows: no block barrier at all) or to one block; a thread holds ITEMS vectors of VEC
+// values (VEC = 16 bytes where all rows are 16-byte aligned, else single values). Blocks are persistent: a thread keeps its
+// columns' gamma in registers from row to row, and the next row's loads are in flight while a row is computed.
+//
+// Forward: one reduction per row. For 8 bits the sum of squares and the largest |s gamma| go through it together:
+// y = s rstd gamma, so max |y| = rstd max |s gamma|, and q = s gamma (rstd / scale).
+//
+// Backward: while a block walks over its rows, each thread also keeps dgamma of its own columns in registers. The blocks'
+// sums go to a partial matrix [block][column] that a second kernel (layer norm's) adds in order of the blocks: no atomics,
+// same bits every time.
+//
+// Rows too long for the registers are streamed twice (the second time mostly from L2).
+#pragma once
+
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "hgemm_ptx.cuh"
+#include "layernorm.cuh"
+
+namespace rmsn {
+
+using lnorm::both;
+using lnorm::cvt;
+using lnorm::fma2;
+using lnorm::load;
+using lnorm::load_row;
+using lnorm::mul2;
+using lnorm::add2;
+using lnorm::Pairs;
+using lnorm::rnd;
+using lnorm::store;
+using lnorm::store_row;
+using lnorm::Vec;
+using lnorm::warp_sum;
+
+struct Params {
+  long long rows;
+  int cols;
+  const void* X;      // backward: S
+  const void* R;      // backward: dS
+  const void* gamma;
+  const void* dY;
+  void* S;
+  void* out;          // Y, Q or dX
+  long long ldx, ldr, lds, ldo, ldy;  // ldy: of dY
+  float* rstd;
+  float* scale;       // of Q's rows
+  float* partial;     // backward: [blocks][ldp], dgamma's
+  long long ldp;      // cols rounded up to 4: every row can be written as vectors
+  float eps;
+  int want_params;
+};
+
+// What the forward kernel makes of a row: y, y in 8 bits, or x itself in 8 bits.
+constexpr int OUT_Y = 0, OUT_E4M3 = 1, OUT_ROWS = 2;
+
+constexpr float E4M3_TOP = 448.f;          // largest finite e4m3 value
+constexpr float LEAST_MAX = 0x1p-100f;     // rows that are smaller are scaled as if this were their largest value
+// Sums of squares from here on (or below, with an eps that is not above) are taken again from scaled values.
+constexpr float SUM_TOP = 0x1p+120f, SUM_LOW = 0x1p-90f;
+
+// max(x, least) that keeps a NaN.
+__device__ __forceinline__ float at_least(float x, float least) { return x < least ? least : x; }
+
+// Two values in e4m3, `lo` in the lower byte; to nearest, ties to even, beyond 448 to 448, NaN to NaN.
+__device__ __forceinline__ uint16_t e4m3_pair(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Magnitudes as integers: their order is that of the values, with infinity above them all and NaN above infinity.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+template <int N>
+__device__ __forceinline__ uint32_t magnitude_max(const float2 (&v)[N]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = max(m, max(magnitude(v[k].x), magnitude(v[k].y)));
+  return m;
+}
+template <int N>
+__device__ __forceinline__ float squares(const float2 (&v)[N]) {
+  float2 s = both(0.f);
+#pragma unroll
+  for (int k = 0; k < N; ++k) s = fma2(v[k], v[k], s);
+  return s.x + s.y;
+}
+
+// A row's sum and largest magnitude, for one warp per row or for the whole block (one barrier). `red` is one of two
+// buffers that are used in turn: a warp can be one reduction ahead of another.
+template <bool WARP_ROW, bool SUM, bool MAX>
+__device__ __forceinline__ void reduce(float& sum, uint32_t& top, uint2* red) {
+  if (SUM) sum = warp_sum(sum);
+  if (MAX) top = __reduce_max_sync(0xffffffffu, top);
+  if (WARP_ROW) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) red[warp] = make_uint2(__float_as_uint(sum), top);
+  __syncthreads();
+  const uint2 part = lane < (int)(blockDim.x >> 5) ? red[lane] : make_uint2(0u, 0u);
+  if (SUM) sum = warp_sum(__uint_as_float(part.x));
+  if (MAX) top = __reduce_max_sync(0xffffffffu, part.y);
+}
+
+// 2^-k, k the exponent of the larger one of the row's largest magnitude and sqrt(eps); 1 where that is 0 or not finite.
+__device__ __forceinline__ float row_unit(uint32_t top, float eps) {
+  const uint32_t bits = max(top, magnitude(sqrtf(eps)));
+  if (top == 0 || top >= 0x7f800000u) return 1.f;
+  const int k = max(-126, min(126, (int)(bits >> 23) - 127));
+  return __uint_as_float((uint32_t)(127 - k) << 23);
+}
+
+// Item i times f in 8 bits, at `at` + its columns.
+template <typename T, int VEC, int ITEMS>
+__device__ __forceinline__ void store_e4m3(uint8_t* at, const Pairs<T, VEC, ITEMS>& v, float f, int c0, int cols, bool full) {
+  const auto value = [&](int j) { return (j % 2 ? v.v[j / 2].y : v.v[j / 2].x) * f; };
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    uint8_t* o = at + i * 32 * VEC;
+    const int c = c0 + i * 32 * VEC;
+    if constexpr (VEC == 1) {
+      if (c < cols) *o = (uint8_t)e4m3_pair(value(i), 0.f);
+    } else {
+      uint16_t q[VEC / 2];
+#pragma unroll
+      for (int j = 0; j < VEC / 2; ++j) q[j] = e4m3_pair(value(i * VEC + 2 * j), value(i * VEC + 2 * j + 1));
+      if (full || c + VEC <= cols) {
+        if constexpr (VEC == 8) *reinterpret_cast<uint2*>(o) = make_uint2((uint32_t)q[0] | (uint32_t)q[1] << 16, (uint32_t)q[2] | (uint32_t)q[3] << 16);
+        else *reinterpret_cast<uint32_t*>(o) = (uint32_t)q[0] | (uint32_t)q[1] << 16;
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (c + j < cols) o[j] = (uint8_t)(q[j / 2] >> 8 * (j % 2));
+      }
+    }
+  }
+}
+
+// ---- forward ----------------------------------------------------------------------------------------
+
+// Most threads per row, by the values a thread holds.
+constexpr int fwd_threads(int values) { return values <= 8 ? 1024 : 512; }
+
+// WARP_ROW: four rows per block of 128 threads, one warp each; otherwise one row per block.
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, int OUT>
+__global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_kernel(const __grid_constant__ Params p) {
+  __shared__ uint2 red[2][32];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  using P = Pairs<T, VEC, ITEMS>;
+  constexpr int N = P::N;
+  constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c0 = ((WARP_ROW ? 0 : warp * ITEMS * 32) + lane) * VEC;  // first column of this thread
+  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
+  const long long step = WARP_ROW ? (long long)gridDim.x * 4 : (long long)gridDim.x;
+  long long row = WARP_ROW ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
+  T* s_at = static_cast<T*>(p.S) + row * p.lds + c0;
+  Vec<T, VEC> xr[ITEMS], rr[ITEMS], gr[ITEMS];
+  if (NORM && p.gamma) load_row<T, VEC, ITEMS>(gr, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+  if (row < p.rows) {
+    load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
+    if (NORM && p.R) load_row<T, VEC, ITEMS>(rr, r_at, c0, p.cols, full);
+  }
+  if (NORM && !p.gamma) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) gr[i].set(j, rnd<T>(1.f));
+  }
+  const float inv_n = 1.f / (float)p.cols;
+  int parity = 0;
+  const auto next = [&]() {  // the buffer of the next reduction
+    parity ^= 1;
+    return red[parity];
+  };
+  for (; row < p.rows;) {
+    P x;
+    x.unpack(xr);
+    if (NORM && p.R) {
+      P r;
+      r.unpack(rr);
+#pragma unroll
+      for (int k = 0; k < N; ++k) x.v[k] = add2(x.v[k], r.v[k]);
+    }
+    const long long at = row;
+    row += step;
+    x_at += step * p.ldx;
+    r_at += step * p.ldr;
+    if (row < p.rows) {
+      load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
+      if (NORM && p.R) load_row<T, VEC, ITEMS>(rr, r_at, c0, p.cols, full);
+    }
+    float f = 1.f;  // what is left to multiply by
+    uint32_t top = 0;
+    if (NORM) {
+      if (p.S) {
+        store_row<T, VEC, ITEMS>(s_at, x, c0, p.cols, full);
+        s_at += step * p.lds;
+      }
+      float sum = squares(x.v), unit = 1.f;
+      P z;
+      const auto weigh = [&]() {
+        z.unpack(gr);
+#pragma unroll
+        for (int k = 0; k < N; ++k) z.v[k] = mul2(x.v[k], z.v[k]);
+        if (EIGHT) top = magnitude_max(z.v);
+      };
+      weigh();
+      reduce<WARP_ROW, true, EIGHT>(sum, top, next());
+      f = lnorm::inv_sqrt(sum * inv_n + p.eps);
+      // (the same for all threads of a row)
+      if (!(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u)) {
+        uint32_t most = magnitude_max(x.v);
+        float none = 0.f;
+        reduce<WARP_ROW, false, true>(none, most, next());
+        unit = row_unit(most, p.eps);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(unit));
+        sum = squares(x.v);
+        uint32_t no = 0;
+        reduce<WARP_ROW, true, false>(sum, no, next());
+        f = lnorm::inv_sqrt(sum * inv_n + p.eps * unit * unit);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
+        unit *= f;  // rstd
+        f = 1.f;
+        weigh();
+        if (EIGHT) reduce<WARP_ROW, false, true>(none, top, next());
+      } else {
+        unit = f;
+      }
+      if (lane == 0 && (WARP_ROW || warp == 0) && p.rstd) p.rstd[at] = unit;
+      x = z;
+    } else {
+      top = magnitude_max(x.v);
+      float none = 0.f;
+      reduce<WARP_ROW, false, true>(none, top, next());
+    }
+    if constexpr (EIGHT) {
+      const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
+      if (lane == 0 && (WARP_ROW || warp == 0)) p.scale[at] = most / E4M3_TOP;
+      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * (E4M3_TOP / most), c0, p.cols, full);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
+      store_row<T, VEC, ITEMS>(static_cast<T*>(p.out) + at * p.ldo + c0, x, c0, p.cols, full);
+    }
+  }
+}
+
+// Rows of any length: one block per row, two passes. Sums in binary64, whose range the squares cannot leave.
+template <typename T, int VEC, int OUT>
+__global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ Params p) {
+  __shared__ double red_sum[32];
+  __shared__ uint32_t red_top[32];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
+  const long long row = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const T* X = static_cast<const T*>(p.X) + row * p.ldx;
+  const T* R = NORM && p.R ? static_cast<const T*>(p.R) + row * p.ldr : nullptr;
+  const T* G = NORM ? static_cast<const T*>(p.gamma) : nullptr;
+  const auto sum_at = [&](int c, float* v) {  // s in the VEC columns from c
+    const Vec<T, VEC> x = load<T, VEC>(X, c, p.cols, 0.f);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[j] = cvt(x.get(j));
+    if (R) {
+      const Vec<T, VEC> r = load<T, VEC>(R, c, p.cols, 0.f);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[j] += cvt(r.get(j));
+    }
+  };
+  double sum = 0.0, rstd = 1.0;
+  for (int c = threadIdx.x * VEC; NORM && c < p.cols; c += blockDim.x * VEC) {
+    float v[VEC];
+    sum_at(c, v);
+    double part = 0.0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) part += (double)v[j] * v[j];
+    sum += part;
+  }
+  if (NORM) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) red_sum[warp] = sum;
+    __syncthreads();
+    sum = red_sum[lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    rstd = 1.0 / sqrt(sum / p.cols + (double)p.eps);
+    if (threadIdx.x == 0 && p.rstd) p.rstd[row] = (float)rstd;
+  }
+  // s rstd as (s a) b, both factors in range whatever rstd is
+  const float b = NORM ? (float)fmin(fmax(rstd, 0x1p-100), 0x1p+100) : 1.f, a = NORM ? (float)(rstd / b) : 1.f;
+  const auto value = [&](const float* v, const Vec<T, VEC>& g, int j) {
+    const float y = NORM ? v[j] * b * a : v[j];
+    return G ? y * cvt(g.get(j)) : y;
+  };
+  float f = 1.f;
+  if (EIGHT) {
+    uint32_t top = 0;
+    for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
+      float v[VEC];
+      sum_at(c, v);
+      Vec<T, VEC> g;
+      if (G) g = load<T, VEC>(G, c, p.cols, 0.f);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (c + j < p.cols) top = max(top, magnitude(value(v, g, j)));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) red_top[warp] = top;
+    __syncthreads();
+    const float most = at_least(__uint_as_float(__reduce_max_sync(0xffffffffu, red_top[lane])), LEAST_MAX);
+    if (threadIdx.x == 0) p.scale[row] = most / E4M3_TOP;
+    f = E4M3_TOP / most;
+  }
+  for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
+    float v[VEC];
+    sum_at(c, v);
+    Vec<T, VEC> g, o;
+    if (G) g = load<T, VEC>(G, c, p.cols, 0.f);
+    if (NORM && p.S) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) o.set(j, rnd<T>(v[j]));
+      store<T, VEC>(static_cast<T*>(p.S) + row * p.lds, c, p.cols, o);
+    }
+    if constexpr (EIGHT) {
+      Pairs<T, VEC, 1> q;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) (j % 2 ? q.v[j / 2].y : q.v[j / 2].x) = value(v, g, j);
+      store_e4m3<T, VEC, 1>(static_cast<uint8_t*>(p.out) + row * p.ldo + c, q, f, c, p.cols, false);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) o.set(j, rnd<T>(value(v, g, j)));
+      store<T, VEC>(static_cast<T*>(p.out) + row * p.ldo, c, p.cols, o);
+    }
+  }
+}
+
+// ---- backward ---------------------------------------------------------------------------------------
+
+// Most threads per row: 512 with 16 values each in 128 registers.
+constexpr int BWD_THREADS = 512;
+
+// WARP_ROW: eight rows per block, one warp each; otherwise one row per block. WIDE: 32 values per thread, gamma and the
+// sums for dgamma in shared memory (each thread's own entries) instead of registers.
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE>
+__global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const __grid_constant__ Params p) {
+  extern __shared__ float sums[];  // WARP_ROW with dgamma: [cols]; WIDE: gamma, dgamma as [pair][thread] of float2
+  __shared__ uint2 red[2][32];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  using P = Pairs<T, VEC, ITEMS>;
+  constexpr int N = P::N;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c0 = ((WARP_ROW ? 0 : warp * ITEMS * 32) + lane) * VEC;  // first column of this thread
+  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
+  const long long step = WARP_ROW ? (long long)gridDim.x * 8 : (long long)gridDim.x;
+  long long row = WARP_ROW ? (long long)blockIdx.x * 8 + warp : (long long)blockIdx.x;
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  const T* d_at = static_cast<const T*>(p.dY) + row * p.ldy + c0;
+  const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
+  T* o_at = static_cast<T*>(p.out) + row * p.ldo + c0;
+  const T* gamma = static_cast<const T*>(p.gamma);
+  const bool add = p.R && p.out;  // dS joins
+  float2* w_g = reinterpret_cast<float2*>(sums) + threadIdx.x;
+  float2* w_dg = w_g + N * blockDim.x;
+  const float inv_n = 1.f / (float)p.cols;
+  // gamma's loads and the first row's are in flight together
+  Vec<T, VEC> xr[ITEMS], dr[ITEMS], gr[ITEMS];
+  if (gamma) load_row<T, VEC, ITEMS>(gr, gamma + c0, c0, p.cols, full);
+  float rstd = 0.f;
+  if (row < p.rows) {
+    load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
+    load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
+    rstd = p.rstd[row];
+  }
+  P g, dg;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    g.v[k] = both(1.f);
+    dg.v[k] = both(0.f);
+  }
+  if (gamma) g.unpack(gr);
+  if (WIDE) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      w_g[k * blockDim.x] = g.v[k];
+      w_dg[k * blockDim.x] = both(0.f);
+    }
+  }
+  int parity = 0;
+  for (; row < p.rows; parity ^= 1) {
+    // xh and w = dy gamma of this row; beyond `cols` all are 0 (rstd may be infinite: 0 rstd is not taken there)
+    P xh, w;
+    xh.unpack(xr);
+    w.unpack(dr);
+    const float rs = rstd;
+    Vec<T, VEC> rr[ITEMS];
+    if (add) load_row<T, VEC, ITEMS>(rr, r_at, c0, p.cols, full);
+    row += step;
+    x_at += step * p.ldx;
+    d_at += step * p.ldy;
+    r_at += step * p.ldr;
+    if (row < p.rows) {
+      load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
+      load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
+      rstd = p.rstd[row];
+    }
+    if (full && VEC * ITEMS % 2 == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) xh.v[k] = mul2(xh.v[k], both(rs));
+    } else {
+#pragma unroll
+      for (int f = 0; f < VEC * ITEMS; ++f) {
+        float& h = f % 2 ? xh.v[f / 2].y : xh.v[f / 2].x;
+        h = c0 + f / VEC * 32 * VEC + f % VEC < p.cols ? h * rs : 0.f;
+      }
+    }
+    float2 t = both(0.f);
+    if (!WIDE) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        dg.v[k] = fma2(w.v[k], xh.v[k], dg.v[k]);
+        w.v[k] = mul2(w.v[k], g.v[k]);
+        t = fma2(w.v[k], xh.v[k], t);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        w_dg[k * blockDim.x] = fma2(w.v[k], xh.v[k], w_dg[k * blockDim.x]);
+        w.v[k] = mul2(w.v[k], w_g[k * blockDim.x]);
+        t = fma2(w.v[k], xh.v[k], t);
+      }
+    }
+    if (p.out) {
+      float sum = t.x + t.y;
+      uint32_t none = 0;
+      reduce<WARP_ROW, true, false>(sum, none, red[parity]);
+      const float minus = -sum * inv_n;
+#pragma unroll
+      for (int k = 0; k < N; ++k) w.v[k] = mul2(fma2(xh.v[k], both(minus), w.v[k]), both(rs));
+      if (add) {
+        P r;
+        r.unpack(rr);
+#pragma unroll
+        for (int k = 0; k < N; ++k) w.v[k] = add2(w.v[k], r.v[k]);
+      }
+      store_row<T, VEC, ITEMS>(o_at, w, c0, p.cols, full);
+      o_at += step * p.ldo;
+    }
+  }
+  if (!p.want_params) return;
+  float* out = p.partial + blockIdx.x * p.ldp;
+  if (WIDE) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) dg.v[k] = w_dg[k * blockDim.x];
+  }
+  const auto value = [&](int f) { return f % 2 ? dg.v[f / 2].y : dg.v[f / 2].x; };
+  const auto column = [&](int f) { return c0 + f / VEC * 32 * VEC + f % VEC; };
+  if (!WARP_ROW) {
+    if constexpr (VEC >= 4) {
+#pragma unroll
+      for (int f = 0; f < VEC * ITEMS; f += 4)
+        if (column(f) < p.cols) *reinterpret_cast<float4*>(out + column(f)) = make_float4(value(f), value(f + 1), value(f + 2), value(f + 3));
+    } else {
+#pragma unroll
+      for (int f = 0; f < VEC * ITEMS; ++f)
+        if (column(f) < p.cols) out[column(f)] = value(f);
+    }
+  } else {
+    // the eight warps add their sums one after the other, in order
+    for (int k = 0; k < 8; ++k) {
+      if (warp == k) {
+#pragma unroll
+        for (int f = 0; f < VEC * ITEMS; ++f)
+          if (column(f) < p.cols) sums[column(f)] = k ? sums[column(f)] + value(f) : value(f);
+      }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < p.cols; c += blockDim.x) out[c] = sums[c];
+  }
+}
+
+// Rows of any length, dx: one block per row, two passes.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(1024) bwd_long_kernel(const __grid_constant__ Params p) {
+  __shared__ float red[32];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  const long long row = blockIdx.x;
+  const T* X = static_cast<const T*>(p.X) + row * p.ldx;
+  const T* D = static_cast<const T*>(p.dY) + row * p.ldy;
+  const T* R = p.R ? static_cast<const T*>(p.R) + row * p.ldr : nullptr;
+  const T* G = static_cast<const T*>(p.gamma);
+  const float rstd = p.rstd[row];
+  const auto pass = [&](auto body) {
+    for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
+      const Vec<T, VEC> x = load<T, VEC>(X, c, p.cols, 0.f), d = load<T, VEC>(D, c, p.cols, 0.f);
+      Vec<T, VEC> g;
+      if (G) g = load<T, VEC>(G, c, p.cols, 0.f);
+      float xh[VEC], w[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        xh[j] = c + j < p.cols ? cvt(x.get(j)) * rstd : 0.f;
+        w[j] = G ? cvt(d.get(j)) * cvt(g.get(j)) : cvt(d.get(j));
+      }
+      body(c, xh, w);
+    }
+  };
+  float sum = 0.f;
+  pass([&](int, const float* xh, const float* w) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum += w[j] * xh[j];
+  });
+  sum = lnorm::block_sum(sum, red) / (float)p.cols;
+  pass([&](int c, const float* xh, const float* w) {
+    Vec<T, VEC> r, o;
+    if (R) r = load<T, VEC>(R, c, p.cols, 0.f);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const float dx = rstd * (w[j] - xh[j] * sum);
+      o.set(j, rnd<T>(R ? dx + cvt(r.get(j)) : dx));
+    }
+    store<T, VEC>(static_cast<T*>(p.out) + row * p.ldo, c, p.cols, o);
+  });
+}
+// Rows of any length, dgamma: a thread per column, gridDim.y chunks of rows.
+template <typename T>
+__global__ void __launch_bounds__(256) bwd_long_params_kernel(const __grid_constant__ Params p) {
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  const int c = blockIdx.x * blockDim.x + threadIdx.x;
+  if (c >= p.cols) return;
+  const long long per = (p.rows + gridDim.y - 1) / gridDim.y;
+  const long long r0 = blockIdx.y * per, r1 = r0 + per < p.rows ? r0 + per : p.rows;
+  float dg = 0.f;
+  for (long long r = r0; r < r1; ++r)
+    dg += cvt(static_cast<const T*>(p.dY)[r * p.ldy + c]) * (cvt(static_cast<const T*>(p.X)[r * p.ldx + c]) * p.rstd[r]);
+  p.partial[blockIdx.y * p.ldp + c] = dg;
+}
+
+}  // namespace rmsn
