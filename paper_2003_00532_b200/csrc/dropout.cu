@@ -14,13 +14,54 @@ namespace {
 using namespace drop;
 using namespace rowop;
 
-template <typename T, int VEC, bool ALIGNED>
-bool run(int sms, Params& p, cudaStream_t stream) {
-  constexpr int UNROLL = 2;
-  p.nv = (p.cols + VEC - 1) / VEC;
-  const auto kernel = &dropout_kernel<T, VEC, ALIGNED, UNROLL>;
-  const int64_t need = (p.rows * p.nv + (int64_t)THREADS * UNROLL - 1) / ((int64_t)THREADS * UNROLL), most = (int64_t)sms * 8;
-  return lm::launch(kernel, dim3((unsigned)(need < most ? need : most)), dim3(THREADS), 0, 1, stream, p);
+// Vectors and rows of a block: whole rows, or strips of equal width where they have over 256 vectors; as many rows as
+// leave the fewest threads of the last warp idle.
+Shape shape_of(int nv) {
+  const int strips = (nv + MAX_THREADS - 1) / MAX_THREADS, tx = (nv + strips - 1) / strips;
+  Shape best{tx, 1};
+  double most = 0.0;
+  for (int ty = 1; ty * tx <= MAX_THREADS; ++ty) {
+    const double used = (double)(ty * tx) / ((ty * tx + 31) / 32 * 32);
+    if (used >= most - 0.02) {
+      best.ty = ty;
+      if (used > most) most = used;
+    }
+  }
+  return best;
+}
+
+template <typename T, int VEC, bool RES>
+bool launch(int sms, const Params& p, cudaStream_t stream) {
+  constexpr auto kernel = &dropout_kernel<T, VEC, RES>;
+  const Shape s = shape_of(p.nv);
+  const int threads = (s.tx * s.ty + 31) / 32 * 32;
+  const int64_t strips = (p.nv + s.tx - 1) / s.tx, steps = (p.rows + s.ty - 1) / s.ty;
+  const int64_t resident = resident_blocks<std::remove_const_t<decltype(kernel)>, kernel>(sms, threads, 0, INT32_MAX);
+  if (resident == 0) return false;
+  // blocks down the rows: as many as fit at once, each with the same number of steps
+  int64_t most = resident / strips;
+  if (most < 1) most = 1;
+  if (most > 65535) most = 65535;
+  const int64_t each = (steps + most - 1) / most;
+  return lm::launch(kernel, dim3((unsigned)strips, (unsigned)((steps + each - 1) / each)), dim3(threads), 0, 1, stream, p, s);
+}
+template <typename T, bool RES>
+bool launch_any(int sms, const Params& p, cudaStream_t stream) {
+  constexpr auto kernel = &dropout_any_kernel<T, RES>;
+  const int64_t resident = resident_blocks<std::remove_const_t<decltype(kernel)>, kernel>(sms, 256, 0, INT32_MAX);
+  if (resident == 0) return false;
+  int64_t sweep = resident * 8 / p.nv;  // rows at a time
+  if (sweep < 1) sweep = 1;
+  const int64_t each = (p.rows + sweep - 1) / sweep;
+  sweep = (p.rows + each - 1) / each;
+  return lm::launch(kernel, dim3((unsigned)((sweep * p.nv + 7) / 8)), dim3(256), 0, 1, stream, p, (int)sweep);
+}
+template <typename T, int VEC>
+bool run(int sms, bool aligned, Params& p, cudaStream_t stream) {
+  const int per = aligned ? VEC : 128;
+  p.nv = (p.cols + per - 1) / per;
+  if (!aligned) return p.R ? launch_any<T, true>(sms, p, stream) : launch_any<T, false>(sms, p, stream);
+  return p.R ? launch<T, VEC, true>(sms, p, stream) : launch<T, VEC, false>(sms, p, stream);
 }
 
 int dropout(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const void* R, int64_t ldr, double prob, uint64_t seed,
@@ -46,9 +87,11 @@ int dropout(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, co
   const uint64_t threshold = (uint64_t)(prob * 4294967296.0 + 0.5);
   p.none = threshold >> 32 != 0;
   p.threshold = (uint32_t)threshold;
-  p.scale = (float)(1.0 / (1.0 - prob));
-  p.key0 = (uint32_t)seed;
-  p.key1 = (uint32_t)(seed >> 32);
+  p.scale = prob < 1.0 ? (float)(1.0 / (1.0 - prob)) : 0.f;
+  for (int i = 0; i < 10; ++i) {
+    p.key[0][i] = (uint32_t)seed + i * W0;
+    p.key[1][i] = (uint32_t)(seed >> 32) + i * W1;
+  }
   p.offset = offset;
   p.step = reinterpret_cast<const long long*>(step);
   p.X = X;
@@ -59,9 +102,9 @@ int dropout(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, co
   p.ldy = ldy;
   const bool aligned = rows_aligned(type, X, ldx) && (!R || rows_aligned(type, R, ldr)) && rows_aligned(type, Y, ldy);
   const int sms = st->sm_count;
-  const bool ok = type == HGEMM_TYPE_F32   ? (aligned ? run<float, 4, true>(sms, p, stream) : run<float, 4, false>(sms, p, stream))
-                  : type == HGEMM_TYPE_F16 ? (aligned ? run<__half, 8, true>(sms, p, stream) : run<__half, 4, false>(sms, p, stream))
-                                           : (aligned ? run<__nv_bfloat16, 8, true>(sms, p, stream) : run<__nv_bfloat16, 4, false>(sms, p, stream));
+  const bool ok = type == HGEMM_TYPE_F32   ? run<float, 4>(sms, aligned, p, stream)
+                  : type == HGEMM_TYPE_F16 ? run<__half, 8>(sms, aligned, p, stream)
+                                           : run<__nv_bfloat16, 8>(sms, aligned, p, stream);
   return ok ? DGEMM_OK : lm::cuda_failed();
 }
 

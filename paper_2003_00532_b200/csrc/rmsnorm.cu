@@ -35,15 +35,47 @@ Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms) {
   if (threads > fwd_threads(items * vec)) return Shape{0, 1024, true};
   return Shape{items, threads, false};
 }
-// Backward: a warp for rows of up to 16 values per lane; a block with 16 values per thread beyond; 32 (`WIDE`) for rows that need
-// them: 8193 to 16384 columns.
+// Backward, rows that are not 16-byte aligned or too long for the ring: a warp for rows of up to 16 values per lane; a block with 8 values
+// per thread beyond (4097 x 1537, binary32: 21 us, with 16 values 24), 16 up to 8192 columns, 32 (`WIDE`) up to 16384.
 Shape bwd_shape(int64_t cols, int vec) {
   const int64_t nv = (cols + vec - 1) / vec;
-  const int most = 16 / vec;
-  if (nv <= 32 * most) return Shape{pow2((nv + 31) / 32), 32, false};
-  for (int items = most; items <= 2 * most; items *= 2)
-    if (threads_for(nv, items) <= BWD_THREADS) return Shape{items, threads_for(nv, items), false};
+  if (vec == 1 && cols <= 512) return Shape{pow2((nv + 31) / 32), 32, false};
+  for (int values = vec == 1 ? 8 : 32; values <= 32; values *= 2)
+    if (threads_for(nv, values / vec) <= BWD_THREADS) return Shape{values / vec, threads_for(nv, values / vec), false};
   return Shape{0, 1024, true};
+}
+
+// The kernels with rows on their way through shared memory: 16 values per thread (8 for rows of up to 256), so many warps to a row, as
+// many groups of them as make 16 warps.
+constexpr int64_t RING_COLS = (int64_t)RING_THREADS * 16;
+Groups ring_groups(int64_t cols, int values) {
+  const int warps = (int)((cols + 32 * values - 1) / (32 * values));
+  return Groups{warps, RING_THREADS / 32 / warps};
+}
+
+// Blocks of one of them, `bytes` of shared memory per thread at the most; 0 on failure.
+template <typename K, K kernel>
+int ring_blocks(int sms, const Groups& gr, int bytes, int64_t rows) {
+  const int threads = gr.warps * gr.groups * 32;
+  if (!allow_smem<K, kernel>(RING_THREADS * bytes)) return 0;
+  return (int)resident_blocks<K, kernel>(sms, threads, (size_t)threads * bytes, (rows + gr.groups - 1) / gr.groups);
+}
+template <typename T, int VEC, int OUT>
+bool launch_fwd_ring(int sms, const Params& p, cudaStream_t stream) {
+  constexpr int DEPTH = OUT == OUT_Y ? 2 : 3, BYTES = 16 * (int)sizeof(T) * DEPTH * 2;  // of shared memory per thread
+  constexpr auto kernel = &fwd_ring_kernel<T, VEC, 16 / VEC, DEPTH, OUT>;
+  const Groups gr = ring_groups(p.cols, 16);
+  const int threads = gr.warps * gr.groups * 32, blocks = ring_blocks<std::remove_const_t<decltype(kernel)>, kernel>(sms, gr, BYTES, p.rows);
+  return blocks > 0 && lm::launch(kernel, dim3(blocks), dim3(threads), (size_t)threads * BYTES, 1, stream, p, gr);
+}
+template <typename T, int VEC, int VALUES, typename F>
+int launch_bwd_ring(int sms, Params& p, cudaStream_t stream, F partial) {
+  constexpr int DEPTH = 2, BYTES = VALUES * (int)sizeof(T) * DEPTH;  // per stream
+  constexpr auto kernel = &bwd_ring_kernel<T, VEC, VALUES / VEC, DEPTH>;
+  const Groups gr = ring_groups(p.cols, VALUES);
+  const int threads = gr.warps * gr.groups * 32, blocks = ring_blocks<std::remove_const_t<decltype(kernel)>, kernel>(sms, gr, 3 * BYTES, p.rows);
+  if (blocks == 0 || !partial(blocks)) return 0;
+  return lm::launch(kernel, dim3(blocks), dim3(threads), (size_t)threads * BYTES * (p.R && p.out ? 3 : 2), 1, stream, p, gr) ? blocks : 0;
 }
 
 template <typename T, int VEC, int ITEMS, int OUT>
@@ -63,6 +95,11 @@ bool launch_fwd(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
 template <typename T, int VEC, int OUT>
 bool run_fwd_vec(int sms, const Params& p, cudaStream_t stream) {
   const Shape s = fwd_shape(p.rows, p.cols, VEC, sms);
+  // Long rows with a residual, where there are many: the ring's copies in flight bring the kernel from 85 to 97 % of the copy rate (8192 x
+  // 4096, Y: 44.4 -> 42.4 us, 8 bits: 41.2 -> 36.8; 1500 x 5000: 12.2 -> 12.0, 11.7 -> 11.4); but 16384 x 2048 38.0 either way, 700 x 4096
+  // 4.7 -> 5.2, and without a residual or in binary32 level or slower.
+  if constexpr (VEC == 8 && OUT != OUT_ROWS)
+    if (p.R && p.cols > 2048 && p.cols <= RING_COLS && p.rows >= 8 * (int64_t)sms) return launch_fwd_ring<T, VEC, OUT>(sms, p, stream);
   if (s.longer) return lm::launch(fwd_long_kernel<T, VEC, OUT>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p);
   switch (s.items) {
     case 1: return launch_fwd<T, VEC, 1, OUT>(sms, s, p, stream);
@@ -105,6 +142,9 @@ int launch_bwd(int sms, int threads, Params& p, cudaStream_t stream, F partial) 
 }
 template <typename T, int VEC, typename F>
 int run_bwd_vec(int sms, Params& p, cudaStream_t stream, F partial) {
+  if constexpr (VEC > 1)
+    if (p.cols <= RING_COLS)
+      return p.cols <= 256 ? launch_bwd_ring<T, VEC, 8>(sms, p, stream, partial) : launch_bwd_ring<T, VEC, 16>(sms, p, stream, partial);
   const Shape s = bwd_shape(p.cols, VEC);
   if (s.longer) {
     const int chunks = (int)((p.rows + 15) / 16 < sms * 2 ? (p.rows + 15) / 16 : sms * 2);
@@ -114,20 +154,18 @@ int run_bwd_vec(int sms, Params& p, cudaStream_t stream, F partial) {
       return 0;
     return chunks;
   }
-  constexpr int MOST = 16 / VEC;
-  if (s.threads == 32) {
-    if (s.items == 1) return launch_bwd<T, VEC, 1, true, false>(sms, 256, p, stream, partial);
-    if (s.items == 2) return launch_bwd<T, VEC, 2, true, false>(sms, 256, p, stream, partial);
-    if constexpr (MOST >= 4)
-      if (s.items == 4) return launch_bwd<T, VEC, 4, true, false>(sms, 256, p, stream, partial);
-    if constexpr (MOST >= 16) {
-      if (s.items == 8) return launch_bwd<T, VEC, 8, true, false>(sms, 256, p, stream, partial);
-      if (s.items == 16) return launch_bwd<T, VEC, 16, true, false>(sms, 256, p, stream, partial);
+  if constexpr (VEC == 1) {
+    if (s.threads == 32) {
+      if (s.items == 1) return launch_bwd<T, 1, 1, true, false>(sms, 256, p, stream, partial);
+      if (s.items == 2) return launch_bwd<T, 1, 2, true, false>(sms, 256, p, stream, partial);
+      if (s.items == 4) return launch_bwd<T, 1, 4, true, false>(sms, 256, p, stream, partial);
+      if (s.items == 8) return launch_bwd<T, 1, 8, true, false>(sms, 256, p, stream, partial);
+      return launch_bwd<T, 1, 16, true, false>(sms, 256, p, stream, partial);
     }
-    return 0;
+    if (s.items == 8) return launch_bwd<T, 1, 8, false, false>(sms, s.threads, p, stream, partial);
+    if (s.items == 16) return launch_bwd<T, 1, 16, false, false>(sms, s.threads, p, stream, partial);
   }
-  if (s.items == MOST) return launch_bwd<T, VEC, MOST, false, false>(sms, s.threads, p, stream, partial);
-  return launch_bwd<T, VEC, 2 * MOST, false, true>(sms, s.threads, p, stream, partial);
+  return launch_bwd<T, VEC, 32 / VEC, false, true>(sms, s.threads, p, stream, partial);
 }
 template <typename T, int VEC, typename F>
 int run_bwd(int sms, bool aligned, Params& p, cudaStream_t stream, F partial) {

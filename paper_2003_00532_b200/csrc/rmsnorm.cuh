@@ -76,12 +76,26 @@ __device__ __forceinline__ uint16_t e4m3_pair(float lo, float hi) {
 
 // Magnitudes as integers: their order is that of the values, with infinity above them all and NaN above infinity.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// The largest of three magnitudes, NaN if one is: one instruction.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 template <int N>
 __device__ __forceinline__ uint32_t magnitude_max(const float2 (&v)[N]) {
-  uint32_t m = 0;
+  float m = 0.f;
 #pragma unroll
-  for (int k = 0; k < N; ++k) m = max(m, max(magnitude(v[k].x), magnitude(v[k].y)));
-  return m;
+  for (int k = 0; k < N; ++k) m = max_abs(m, v[k].x, v[k].y);
+  return __float_as_uint(m);
+}
+// 448 / x: the approximate reciprocal and one correction of the quotient. 0, infinities and NaN give what the division gives.
+__device__ __forceinline__ float top_over(float x) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  const float q = E4M3_TOP * r;
+  const float c = fmaf(r, fmaf(-q, x, E4M3_TOP), q);
+  return x < __uint_as_float(0x7f800000u) ? c : q;
 }
 template <int N>
 __device__ __forceinline__ float squares(const float2 (&v)[N]) {
@@ -117,7 +131,10 @@ __device__ __forceinline__ float row_unit(uint32_t top, float eps) {
 // Item i times f in 8 bits, at `at` + its columns.
 template <typename T, int VEC, int ITEMS>
 __device__ __forceinline__ void store_e4m3(uint8_t* at, const Pairs<T, VEC, ITEMS>& v, float f, int c0, int cols, bool full) {
-  const auto value = [&](int j) { return (j % 2 ? v.v[j / 2].y : v.v[j / 2].x) * f; };
+  Pairs<T, VEC, ITEMS> w;
+#pragma unroll
+  for (int k = 0; k < Pairs<T, VEC, ITEMS>::N; ++k) w.v[k] = mul2(v.v[k], both(f));
+  const auto value = [&](int j) { return j % 2 ? w.v[j / 2].y : w.v[j / 2].x; };
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
     uint8_t* o = at + i * 32 * VEC;
@@ -174,6 +191,8 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
 #pragma unroll
       for (int j = 0; j < VEC; ++j) gr[i].set(j, rnd<T>(1.f));
   }
+  P g;
+  if (NORM) g.unpack(gr);
   const float inv_n = 1.f / (float)p.cols;
   int parity = 0;
   const auto next = [&]() {  // the buffer of the next reduction
@@ -207,9 +226,8 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
       float sum = squares(x.v), unit = 1.f;
       P z;
       const auto weigh = [&]() {
-        z.unpack(gr);
 #pragma unroll
-        for (int k = 0; k < N; ++k) z.v[k] = mul2(x.v[k], z.v[k]);
+        for (int k = 0; k < N; ++k) z.v[k] = mul2(x.v[k], g.v[k]);
         if (EIGHT) top = magnitude_max(z.v);
       };
       weigh();
@@ -246,7 +264,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
     if constexpr (EIGHT) {
       const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && (WARP_ROW || warp == 0)) p.scale[at] = most / E4M3_TOP;
-      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * (E4M3_TOP / most), c0, p.cols, full);
+      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * top_over(most), c0, p.cols, full);
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
@@ -321,7 +339,7 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
     __syncthreads();
     const float most = at_least(__uint_as_float(__reduce_max_sync(0xffffffffu, red_top[lane])), LEAST_MAX);
     if (threadIdx.x == 0) p.scale[row] = most / E4M3_TOP;
-    f = E4M3_TOP / most;
+    f = top_over(most);
   }
   for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
     float v[VEC];
@@ -488,6 +506,315 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
       __syncthreads();
     }
     for (int c = threadIdx.x; c < p.cols; c += blockDim.x) out[c] = sums[c];
+  }
+}
+
+// ---- rows through shared memory ---------------------------------------------------------------------
+
+// The kernels for many rows. A block is `groups` groups of `warps` warps, each on a row of its own; a thread holds ITEMS vectors
+// of VEC values, 32 vectors apart. The next DEPTH - 1 rows are on their way into shared memory by asynchronous copies of every thread's own
+// vectors (no barrier: a thread reads only what it has copied), so that what is in flight takes no registers.
+struct Groups {
+  int warps, groups;
+};
+
+// One vector of 16 bytes: `bytes` of it from `src`, zeros behind them.
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+}
+
+// One thread's vectors of the rows on their way: [row % DEPTH][stream][item][thread].
+template <typename T, int VEC, int ITEMS, int DEPTH>
+struct Ring {
+  static constexpr int SIZE = 16;
+  static_assert(VEC * sizeof(T) == SIZE, "vectors of 16 bytes");
+  uint32_t base;     // of this thread
+  int pitch;         // bytes between items
+  int streams;
+  int bytes[ITEMS];  // of each vector that lie inside the row
+  __device__ __forceinline__ Ring(void* smem, int streams_, int c0, int cols) : streams(streams_) {
+    base = dgemm::ptx::smem_u32(smem) + threadIdx.x * SIZE;
+    pitch = blockDim.x * SIZE;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) bytes[i] = max(0, min(SIZE, (cols - c0 - i * 32 * VEC) * (int)sizeof(T)));
+  }
+  __device__ __forceinline__ uint32_t at(int slot, int stream) const { return base + (slot * streams + stream) * ITEMS * pitch; }
+  __device__ __forceinline__ void copy(int slot, int stream, const T* src) const {
+    const uint32_t dst = at(slot, stream);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) copy_async(dst + i * pitch, bytes[i] > 0 ? src + i * 32 * VEC : src, bytes[i]);
+  }
+  __device__ __forceinline__ void take(int slot, int stream, Vec<T, VEC> (&raw)[ITEMS]) const {
+    const uint32_t src = at(slot, stream);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) raw[i].bits = hgemm::ptx5::lds128(src + i * pitch);
+  }
+};
+
+// Sum and largest magnitude of a row over the warps of its group; `red` as in reduce(), a part per group.
+template <bool SUM, bool MAX>
+__device__ __forceinline__ void reduce_group(float& sum, uint32_t& top, uint2* red, const Groups& gr, int group, int warp) {
+  if (SUM) sum = warp_sum(sum);
+  if (MAX) top = __reduce_max_sync(0xffffffffu, top);
+  if (gr.warps == 1) return;
+  const int lane = threadIdx.x & 31;
+  red += group * gr.warps;
+  if (lane == 0) red[warp] = make_uint2(__float_as_uint(sum), top);
+  dgemm::ptx::named_barrier_sync(1 + group, gr.warps * 32);
+  const uint2 part = lane < gr.warps ? red[lane] : make_uint2(0u, 0u);
+  if (SUM) sum = warp_sum(__uint_as_float(part.x));
+  if (MAX) top = __reduce_max_sync(0xffffffffu, part.y);
+}
+
+constexpr int RING_THREADS = 512;
+
+template <typename T, int VEC, int ITEMS, int DEPTH, int OUT>
+__global__ void __launch_bounds__(RING_THREADS) fwd_ring_kernel(const __grid_constant__ Params p, const Groups gr) {
+  extern __shared__ uint4 ring_smem[];
+  __shared__ uint2 red[2][16];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  using P = Pairs<T, VEC, ITEMS>;
+  constexpr int N = P::N;
+  constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
+  const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / gr.warps, warp = (threadIdx.x >> 5) - group * gr.warps;
+  const int c0 = (warp * ITEMS * 32 + lane) * VEC;
+  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
+  const long long step = (long long)gridDim.x * gr.groups;
+  long long row = (long long)blockIdx.x * gr.groups + group;
+  const bool add = NORM && p.R;
+  const Ring<T, VEC, ITEMS, DEPTH> ring(ring_smem, add ? 2 : 1, c0, p.cols);
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
+  long long ahead = row;
+  const auto send = [&](int slot) {
+    if (ahead < p.rows) {
+      ring.copy(slot, 0, x_at);
+      if (add) ring.copy(slot, 1, r_at);
+    }
+    copies_commit();
+    ahead += step;
+    x_at += step * p.ldx;
+    r_at += step * p.ldr;
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d) send(d);
+  Vec<T, VEC> g_raw[ITEMS];
+  if (NORM) {
+    if (p.gamma) {
+      load_row<T, VEC, ITEMS>(g_raw, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+    } else {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) g_raw[i].set(j, rnd<T>(1.f));
+    }
+  }
+  const float inv_n = 1.f / (float)p.cols;
+  int parity = 0, slot = 0;
+  const auto next = [&]() {  // the buffer of the next reduction
+    parity ^= 1;
+    return red[parity];
+  };
+  for (; row < p.rows; row += step) {
+    send(slot == 0 ? DEPTH - 1 : slot - 1);
+    copies_wait<DEPTH - 1>();
+    P x;
+    const auto take = [&]() {  // s
+      Vec<T, VEC> raw[ITEMS];
+      ring.take(slot, 0, raw);
+      x.unpack(raw);
+      if (add) {
+        P r;
+        ring.take(slot, 1, raw);
+        r.unpack(raw);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x.v[k] = add2(x.v[k], r.v[k]);
+      }
+    };
+    take();
+    float f = 1.f;  // what is left to multiply by
+    uint32_t top = 0;
+    float none = 0.f;
+    if (NORM) {
+      if (p.S) store_row<T, VEC, ITEMS>(static_cast<T*>(p.S) + row * p.lds + c0, x, c0, p.cols, full);
+      float sum = squares(x.v), rstd;
+      const auto weigh = [&]() {
+        P g;
+        g.unpack(g_raw);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], g.v[k]);
+        if (EIGHT) top = magnitude_max(x.v);
+      };
+      weigh();
+      reduce_group<true, EIGHT>(sum, top, next(), gr, group, warp);
+      f = rstd = lnorm::inv_sqrt(sum * inv_n + p.eps);
+      // (the same for all threads of a row)
+      if (!(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u)) {
+        take();
+        uint32_t most = magnitude_max(x.v);
+        reduce_group<false, true>(none, most, next(), gr, group, warp);
+        const float unit = row_unit(most, p.eps);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(unit));
+        sum = squares(x.v);
+        reduce_group<true, false>(sum, top, next(), gr, group, warp);
+        f = lnorm::inv_sqrt(sum * inv_n + p.eps * unit * unit);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
+        rstd = unit * f;
+        f = 1.f;
+        weigh();
+        if (EIGHT) reduce_group<false, true>(none, top, next(), gr, group, warp);
+      }
+      if (lane == 0 && warp == 0 && p.rstd) p.rstd[row] = rstd;
+    } else {
+      top = magnitude_max(x.v);
+      reduce_group<false, true>(none, top, next(), gr, group, warp);
+    }
+    if constexpr (EIGHT) {
+      const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
+      if (lane == 0 && warp == 0) p.scale[row] = most / E4M3_TOP;
+      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + row * p.ldo + c0, x, f * top_over(most), c0, p.cols, full);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
+      store_row<T, VEC, ITEMS>(static_cast<T*>(p.out) + row * p.ldo + c0, x, c0, p.cols, full);
+    }
+    slot = slot == DEPTH - 1 ? 0 : slot + 1;
+  }
+  copies_wait<0>();
+}
+
+// dgamma: each thread keeps the sums of its own columns in registers; the block's groups add theirs up at the end, in order.
+template <typename T, int VEC, int ITEMS, int DEPTH>
+__global__ void __launch_bounds__(RING_THREADS) bwd_ring_kernel(const __grid_constant__ Params p, const Groups gr) {
+  extern __shared__ float4 ring_smem4[];
+  __shared__ uint2 red[2][16];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  using P = Pairs<T, VEC, ITEMS>;
+  constexpr int N = P::N;
+  const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / gr.warps, warp = (threadIdx.x >> 5) - group * gr.warps;
+  const int c0 = (warp * ITEMS * 32 + lane) * VEC;
+  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
+  const long long step = (long long)gridDim.x * gr.groups;
+  long long row = (long long)blockIdx.x * gr.groups + group;
+  const bool add = p.R && p.out;  // dS joins
+  const Ring<T, VEC, ITEMS, DEPTH> ring(ring_smem4, add ? 3 : 2, c0, p.cols);
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  const T* d_at = static_cast<const T*>(p.dY) + row * p.ldy + c0;
+  const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
+  long long ahead = row;
+  const auto send = [&](int slot) {
+    if (ahead < p.rows) {
+      ring.copy(slot, 0, x_at);
+      ring.copy(slot, 1, d_at);
+      if (add) ring.copy(slot, 2, r_at);
+    }
+    copies_commit();
+    ahead += step;
+    x_at += step * p.ldx;
+    d_at += step * p.ldy;
+    r_at += step * p.ldr;
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d) send(d);
+  Vec<T, VEC> g_raw[ITEMS];
+  if (p.gamma) {
+    load_row<T, VEC, ITEMS>(g_raw, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+  } else {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) g_raw[i].set(j, rnd<T>(1.f));
+  }
+  const float inv_n = 1.f / (float)p.cols;
+  P dg;
+#pragma unroll
+  for (int k = 0; k < N; ++k) dg.v[k] = both(0.f);
+  float rstd = row < p.rows ? p.rstd[row] : 0.f;
+  int parity = 0, slot = 0;
+  for (; row < p.rows; row += step, parity ^= 1) {
+    send(slot == 0 ? DEPTH - 1 : slot - 1);
+    const float rs = rstd;
+    if (row + step < p.rows) rstd = p.rstd[row + step];
+    copies_wait<DEPTH - 1>();
+    // xh and w = dy gamma; beyond `cols` all are 0 (rstd may be infinite: 0 rstd is not taken there)
+    P xh, w;
+    {
+      Vec<T, VEC> raw[ITEMS];
+      ring.take(slot, 0, raw);
+      xh.unpack(raw);
+      ring.take(slot, 1, raw);
+      w.unpack(raw);
+    }
+    if (full) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) xh.v[k] = mul2(xh.v[k], both(rs));
+    } else {
+#pragma unroll
+      for (int f = 0; f < VEC * ITEMS; ++f) {
+        float& h = f % 2 ? xh.v[f / 2].y : xh.v[f / 2].x;
+        h = c0 + f / VEC * 32 * VEC + f % VEC < p.cols ? h * rs : 0.f;
+      }
+    }
+    float2 t = both(0.f);
+    {
+      P g;
+      g.unpack(g_raw);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        dg.v[k] = fma2(w.v[k], xh.v[k], dg.v[k]);
+        w.v[k] = mul2(w.v[k], g.v[k]);
+        t = fma2(w.v[k], xh.v[k], t);
+      }
+    }
+    if (p.out) {
+      float sum = t.x + t.y;
+      uint32_t none = 0;
+      reduce_group<true, false>(sum, none, red[parity], gr, group, warp);
+      const float minus = -sum * inv_n;
+#pragma unroll
+      for (int k = 0; k < N; ++k) w.v[k] = mul2(fma2(xh.v[k], both(minus), w.v[k]), both(rs));
+      if (add) {
+        Vec<T, VEC> raw[ITEMS];
+        ring.take(slot, 2, raw);
+        P r;
+        r.unpack(raw);
+#pragma unroll
+        for (int k = 0; k < N; ++k) w.v[k] = add2(w.v[k], r.v[k]);
+      }
+      store_row<T, VEC, ITEMS>(static_cast<T*>(p.out) + row * p.ldo + c0, w, c0, p.cols, full);
+    }
+    slot = slot == DEPTH - 1 ? 0 : slot + 1;
+  }
+  copies_wait<0>();
+  if (!p.want_params) return;
+  // All groups' sums side by side in shared memory, four columns at a time, then added over the groups in order.
+  static_assert(VEC % 4 == 0, "four columns at a time");
+  float4* sums = ring_smem4;
+  const int per = gr.warps * 32;  // threads of a group
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < N / 2; ++q) sums[q * blockDim.x + threadIdx.x] = make_float4(dg.v[2 * q].x, dg.v[2 * q].y, dg.v[2 * q + 1].x, dg.v[2 * q + 1].y);
+  __syncthreads();
+  float* out = p.partial + blockIdx.x * p.ldp;
+  for (int e = threadIdx.x; e < per * (N / 2); e += blockDim.x) {
+    const int q = e / per, t = e - q * per;
+    const int c = ((t >> 5) * ITEMS * 32 + 4 * q / VEC * 32 + (t & 31)) * VEC + 4 * q % VEC;
+    if (c >= p.cols) continue;
+    float4 a = sums[q * blockDim.x + t];
+    for (int g = 1; g < gr.groups; ++g) {
+      const float4 b = sums[q * blockDim.x + g * per + t];
+      a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    }
+    *reinterpret_cast<float4*>(out + c) = a;
   }
 }
 
