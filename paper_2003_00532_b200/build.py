@@ -17,7 +17,7 @@ EXT = os.path.join(HERE, "_marshal.so")  # compiled argument marshalling (csrc/b
 EXT_SOURCE = os.path.join(CSRC, "binding_ext.cpp")
 EXT_STAMP = EXT + ".torch"  # the torch and the Python that it was built against
 SOURCES = [os.path.join(CSRC, name) for name in ("dgemm_api.cu", "sgemm_api.cu", "hgemm_api.cu", "hgemm_plain_f16.cu", "hgemm_plain_bf16.cu",
-                                                "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "hgemm_token.cu", "qgemm_plain_f16.cu", "qgemm_plain_bf16.cu",
+                                                "hgemm_gated_f16.cu", "hgemm_gated_bf16.cu", "hgemm_token.cu", "qgemm_token.cu", "qgemm_plain_f16.cu", "qgemm_plain_bf16.cu",
                                                 "qgemm_gated_f16.cu", "qgemm_gated_bf16.cu", "layernorm.cu", "rmsnorm.cu", "dropout.cu")]
 HEADERS = sorted(glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) +
                  glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h")))

@@ -88,30 +88,6 @@ __global__ void __launch_bounds__(256) hgemm_pack_kernel(const __grid_constant__
   pack_body(ops, blockIdx.x);
 }
 
-// 16 values of 8 bits at src[0 .. 16), the columns c .. of a row of `cols`; those beyond the row are zero. Five aligned words
-// shifted by the row's misalignment, or, where those would reach beyond the row, one value after the other.
-__device__ __forceinline__ uint4 load16(const uint8_t* src, int c, int cols) {
-  uint4 v;
-  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-  const int off = (int)(reinterpret_cast<uintptr_t>(src) & 3);  // bytes of the first word before the first value
-  if (c >= off && c + 20 - off <= cols) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(src - off);
-    uint32_t x[5];
-#pragma unroll
-    for (int j = 0; j < 5; ++j) x[j] = p[j];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(x[j], x[j + 1], 8 * off);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] = 0;
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-        if (c + 4 * j + b < cols) w[j] |= (uint32_t)src[4 * j + b] << 8 * b;
-    }
-  }
-  return v;
-}
 // The same copies for matrices of 8-bit values, 16 of them per thread.
 __global__ void __launch_bounds__(256) hgemm_pack8_kernel(const __grid_constant__ PackOps ops) {
   ptx5::launch_dependents();

@@ -32,6 +32,21 @@ bool launch_gated8_bf16(int act, int config, int clusters, cudaStream_t stream, 
 constexpr size_t TOKEN_SMEM = 160 * 1024;
 bool launch_token(int type, bool gated, int sms, cudaStream_t stream, const TokenParams& p);
 
+// Products of at most TOKEN8_ROWS rows of 8-bit operands with 16-byte aligned weight rows (qgemm_token.cuh).
+constexpr int TOKEN8_ROWS = 8;
+struct Token8Params {
+  int M, N, K;
+  const uint8_t* X;     // M x K
+  const uint8_t* W[2];  // weights, N x K; gated: gate, up
+  long long ldx, ldw[2];
+  int x_vec;            // rows of X may be read as 16-byte vectors
+  int wk;               // warps that share a row
+  const float* row_scale;
+  const float* col_scale[2];
+  TokenParams out;      // bias, activation and outputs
+};
+bool launch_token8(int type, bool gated, int sms, cudaStream_t stream, const Token8Params& p);
+
 // Once per device: shared-memory limits.
 bool configure_plain_f16();
 bool configure_plain_bf16();
