@@ -48,9 +48,9 @@ Shape bwd_shape(int64_t cols, int vec) {
 // The kernels with rows on their way through shared memory: 16 values per thread (8 for rows of up to 256), so many warps to a row, as
 // many groups of them as make 16 warps.
 constexpr int64_t RING_COLS = (int64_t)RING_THREADS * 16;
-Groups ring_groups(int64_t cols, int values) {
+Groups ring_groups(int64_t cols, int values, int threads = RING_THREADS) {
   const int warps = (int)((cols + 32 * values - 1) / (32 * values));
-  return Groups{warps, RING_THREADS / 32 / warps};
+  return Groups{warps, threads / 32 / warps};
 }
 
 // Blocks of one of them, `bytes` of shared memory per thread at the most; 0 on failure.
@@ -60,13 +60,14 @@ int ring_blocks(int sms, const Groups& gr, int bytes, int64_t rows) {
   if (!allow_smem<K, kernel>(RING_THREADS * bytes)) return 0;
   return (int)resident_blocks<K, kernel>(sms, threads, (size_t)threads * bytes, (rows + gr.groups - 1) / gr.groups);
 }
-template <typename T, int VEC, int OUT>
+template <typename T, int OUT, int THREADS>
 bool launch_fwd_ring(int sms, const Params& p, cudaStream_t stream) {
-  constexpr int DEPTH = OUT == OUT_Y ? 2 : 3, BYTES = 16 * (int)sizeof(T) * DEPTH * 2;  // of shared memory per thread
-  constexpr auto kernel = &fwd_ring_kernel<T, VEC, 16 / VEC, DEPTH, OUT>;
-  const Groups gr = ring_groups(p.cols, 16);
+  constexpr int VEC = 16 / (int)sizeof(T), DEPTH = OUT == OUT_E4M3 && THREADS == RING_THREADS ? 3 : 2;
+  constexpr int BYTES = 16 * (int)sizeof(T) * DEPTH * 2;  // of shared memory per thread
+  constexpr auto kernel = &fwd_ring_kernel<T, VEC, 16 / VEC, DEPTH, OUT, THREADS>;
+  const Groups gr = ring_groups(p.cols, 16, THREADS);
   const int threads = gr.warps * gr.groups * 32, blocks = ring_blocks<std::remove_const_t<decltype(kernel)>, kernel>(sms, gr, BYTES, p.rows);
-  return blocks > 0 && lm::launch(kernel, dim3(blocks), dim3(threads), (size_t)threads * BYTES, 1, stream, p, gr);
+  return blocks > 0 && lm::launch(kernel, dim3(blocks), dim3(threads), (size_t)threads * BYTES / (p.R ? 1 : 2), 1, stream, p, gr);
 }
 template <typename T, int VEC, int VALUES, typename F>
 int launch_bwd_ring(int sms, Params& p, cudaStream_t stream, F partial) {
@@ -95,11 +96,16 @@ bool launch_fwd(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
 template <typename T, int VEC, int OUT>
 bool run_fwd_vec(int sms, const Params& p, cudaStream_t stream) {
   const Shape s = fwd_shape(p.rows, p.cols, VEC, sms);
-  // Long rows with a residual, where there are many: the ring's copies in flight bring the kernel from 85 to 97 % of the copy rate (8192 x
-  // 4096, Y: 44.4 -> 42.4 us, 8 bits: 41.2 -> 36.8; 1500 x 5000: 12.2 -> 12.0, 11.7 -> 11.4); but 16384 x 2048 38.0 either way, 700 x 4096
-  // 4.7 -> 5.2, and without a residual or in binary32 level or slower.
+  // 16-bit rows through shared memory, where there are many. Blocks of 256 threads (8192 x 4096 without a residual: Y 29.1 -> 24.2 us, to
+  // 8 bits 27.3 -> 24.1; 1500 x 4000 with one 10.9 -> 9.7 and 10.5 -> 9.2); but with a residual beyond L2 so many streams of reads and
+  // writes slow each other down (8192 x 4096: 47.1, 16384 x 2048 46.5), and one block of 512 (42.3), or for shorter rows the registers
+  // (42.9), are better. Rows of up to 512 columns, few rows, single precision and rows to 8 bits without norm: level or slower.
   if constexpr (VEC == 8 && OUT != OUT_ROWS)
-    if (p.R && p.cols > 2048 && p.cols <= RING_COLS && p.rows >= 8 * (int64_t)sms) return launch_fwd_ring<T, VEC, OUT>(sms, p, stream);
+    if (p.cols > 512 && p.cols <= RING_COLS && p.rows > 2 * (int64_t)sms) {
+      const bool large = p.R && p.rows * p.cols > 16ll << 20;
+      if (!large && p.cols <= RING_COLS / 2) return launch_fwd_ring<T, OUT, SMALL_RING_THREADS>(sms, p, stream);
+      if (p.R && p.cols > 2048 && p.rows >= 8 * (int64_t)sms) return launch_fwd_ring<T, OUT, RING_THREADS>(sms, p, stream);
+    }
   if (s.longer) return lm::launch(fwd_long_kernel<T, VEC, OUT>, dim3((unsigned)p.rows), dim3(1024), 0, 1, stream, p);
   switch (s.items) {
     case 1: return launch_fwd<T, VEC, 1, OUT>(sms, s, p, stream);

@@ -571,10 +571,11 @@ __device__ __forceinline__ void reduce_group(float& sum, uint32_t& top, uint2* r
   if (MAX) top = __reduce_max_sync(0xffffffffu, part.y);
 }
 
-constexpr int RING_THREADS = 512;
+constexpr int RING_THREADS = 512, SMALL_RING_THREADS = 256;
 
-template <typename T, int VEC, int ITEMS, int DEPTH, int OUT>
-__global__ void __launch_bounds__(RING_THREADS) fwd_ring_kernel(const __grid_constant__ Params p, const Groups gr) {
+// THREADS: most of a block; three blocks of 256 fit on an SM, one of 512.
+template <typename T, int VEC, int ITEMS, int DEPTH, int OUT, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1) fwd_ring_kernel(const __grid_constant__ Params p, const Groups gr) {
   extern __shared__ uint4 ring_smem[];
   __shared__ uint2 red[2][16];
   hgemm::ptx5::launch_dependents();
