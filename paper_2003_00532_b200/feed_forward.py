@@ -1,13 +1,18 @@
-"""A transformer's feed-forward sublayer on the library's 16-bit operators, forward and backward.
+"""A transformer's feed-forward sublayer on the library's 16-bit operators, forward and backward, and on its 8-bit operators for
+answering.
 
-    y = x + (act(n Wg^T) * (n Wu^T)) Wd^T + bd,   n = layer norm of x
+    s = x + delta,   y = s + dropout((act(n Wg^T) * (n Wu^T)) Wd^T + bd),   n = norm of s
 
-The normalisation, the gated projections and the product with bias and residual each run as one kernel
-(:func:`layernorm_fwd`, :func:`hgemm_gated`, :func:`hgemm_epilogue`); the backward pass uses their gradients.
-What lies between them is kept in the object's buffers, one per name, grown to the largest number of tokens so far; results are
-new tensors. Run as a command it trains the sublayer on a synthetic target and then answers single tokens:
+The norm is layer norm or root-mean-square norm; ``delta`` is what the sublayer before leaves to be added to the residual stream
+(root-mean-square norm adds it in its own pass). The normalisation, the gated projections and the product with bias and residual each
+run as one kernel (:func:`layernorm_fwd` or :func:`rmsnorm_fwd`, :func:`hgemm_gated`, :func:`hgemm_epilogue`, and :func:`dropout_fwd`
+behind it); the backward pass uses their gradients. What lies between them is kept in the object's buffers, one per name, grown to the
+largest number of tokens so far; results are new tensors. :meth:`FeedForward.eight_bit` gives the sublayer with its weights in 8 bits,
+whose activations are brought there by :func:`rmsnorm_fwd_e4m3` and :func:`quantize_rows_e4m3` and multiplied by
+:func:`qgemm_gated` and :func:`qgemm_epilogue`. Run as a command it trains the sublayer on a synthetic target and then answers
+single tokens:
 
-    python -m paper_2003_00532_b200.feed_forward [--model 1024] [--hidden 4096] [--tokens 2048] [--steps 20]
+    python -m paper_2003_00532_b200.feed_forward [--model 1024] [--hidden 4096] [--tokens 2048] [--steps 20] [--norm rms] [--dropout 0.1]
 """
 from __future__ import annotations
 
@@ -19,21 +24,11 @@ import torch
 import paper_2003_00532_b200 as dg
 
 
-class FeedForward:
-    """Weights of one sublayer (``float16`` or ``bfloat16``, stored output x input) and its two passes."""
+class _Buffers:
+    """Scratch tensors by name, each grown to the most tokens asked for."""
 
-    def __init__(self, model: int, hidden: int, dtype=torch.bfloat16, act: int = dg.HGEMM_ACT_SILU, seed: int = 0):
-        g = torch.Generator(device="cuda").manual_seed(seed)
-
-        def weight(rows, cols):
-            return (torch.randn(rows, cols, device="cuda", generator=g) * cols ** -0.5).to(dtype)
-
-        self.model, self.hidden, self.dtype, self.act = model, hidden, dtype, act
-        self.gamma, self.beta = torch.ones(model, dtype=dtype, device="cuda"), torch.zeros(model, dtype=dtype, device="cuda")
-        self.wg, self.wu, self.wd = weight(hidden, model), weight(hidden, model), weight(model, hidden)
-        self.bd = torch.zeros(model, dtype=dtype, device="cuda")
+    def __init__(self):
         self._buffers = {}
-        self._kept = None
 
     def _buffer(self, name, tokens, *width, dtype=None):
         """``tokens`` rows of the buffer ``name``, which grows to the most tokens asked for and never shrinks."""
@@ -41,10 +36,41 @@ class FeedForward:
             self._buffers[name] = torch.empty(tokens, *width, dtype=dtype or self.dtype, device="cuda")
         return self._buffers[name][:tokens]
 
-    def forward(self, x, keep: bool = True):
+
+class FeedForward(_Buffers):
+    """Weights of one sublayer (``float16`` or ``bfloat16``, stored output x input) and its two passes. ``norm``: ``"layer"`` or
+    ``"rms"``; ``dropout``: the probability with which a kept (training) pass drops a value of the sublayer's output."""
+
+    def __init__(self, model: int, hidden: int, dtype=torch.bfloat16, act: int = dg.HGEMM_ACT_SILU, seed: int = 0, norm: str = "layer",
+                 dropout: float = 0.0):
+        super().__init__()
+        if norm not in ("layer", "rms"):
+            raise ValueError("norm: 'layer' or 'rms'")
+        if not 0.0 <= dropout < 1.0:
+            raise ValueError("dropout: a probability below 1")
+        g = torch.Generator(device="cuda").manual_seed(seed)
+
+        def weight(rows, cols):
+            return (torch.randn(rows, cols, device="cuda", generator=g) * cols ** -0.5).to(dtype)
+
+        self.model, self.hidden, self.dtype, self.act = model, hidden, dtype, act
+        self.norm, self.dropout, self.seed, self.uses = norm, dropout, seed, 0
+        self.gamma = torch.ones(model, dtype=dtype, device="cuda")
+        self.beta = torch.zeros(model, dtype=dtype, device="cuda") if norm == "layer" else None
+        self.wg, self.wu, self.wd = weight(hidden, model), weight(hidden, model), weight(model, hidden)
+        self.bd = torch.zeros(model, dtype=dtype, device="cuda")
+        self._kept = None
+
+    def parameters(self):
+        """The parameters' names."""
+        return ("gamma", "beta", "wg", "wu", "wd", "bd") if self.norm == "layer" else ("gamma", "wg", "wu", "wd", "bd")
+
+    def forward(self, x, keep: bool = True, delta=None):
         """The sublayer's output for ``x`` (tokens x model), a new tensor. ``keep``: also keep what :meth:`backward` needs
-        (``x`` itself by reference: it has to stay as it is until then); a call that does not keep leaves alone what an earlier
-        one kept."""
+        (``x`` itself by reference: it has to stay as it is until then) and drop values, with another mask every time; a call that does
+        not keep drops nothing and leaves alone what an earlier one kept. ``delta`` (root-mean-square norm only): added to ``x`` first."""
+        if delta is not None and self.norm != "rms":
+            raise ValueError("delta: needs norm='rms'")
         t, which = x.shape[0], "kept " if keep else ""
         n, h, y = self._buffer(which + "n", t, self.model), self._buffer(which + "h", t, self.hidden), torch.empty_like(x)
         mean, rstd, gate, up = None, None, None, None
@@ -52,28 +78,53 @@ class FeedForward:
             self._kept = None   # (its buffers are about to be written)
             mean, rstd = (self._buffer(name, t, dtype=torch.float32) for name in ("mean", "rstd"))
             gate, up = self._buffer("gate", t, self.hidden), self._buffer("up", t, self.hidden)
-        dg.layernorm_fwd(x, self.gamma, self.beta, n, mean=mean, rstd=rstd)
+        s = x
+        if self.norm == "layer":
+            dg.layernorm_fwd(x, self.gamma, self.beta, n, mean=mean, rstd=rstd)
+        else:
+            if delta is not None:
+                s = self._buffer(which + "s", t, self.model)
+            dg.rmsnorm_fwd(x, self.gamma, n, residual=delta, sum=s if delta is not None else None, rstd=rstd)
         dg.hgemm_gated(n, self.wg, self.wu, h, act=self.act, gate=gate, up=up, transw=True)
-        dg.hgemm_epilogue(h, self.wd, y, bias=self.bd, residual=x, transb=True)
+        p, use = self.dropout if keep else 0.0, self.uses
+        if p > 0.0:
+            self.uses += 1
+            d = self._buffer("d", t, self.model)
+            dg.hgemm_epilogue(h, self.wd, d, bias=self.bd, transb=True)
+            dg.dropout_fwd(d, y, p, self.seed, use, residual=s)
+        else:
+            dg.hgemm_epilogue(h, self.wd, y, bias=self.bd, residual=s, transb=True)
         if keep:
-            self._kept = (x, n, mean, rstd, gate, up, h)
+            self._kept = (s, n, mean, rstd, gate, up, h, p, use)
         return y
 
     def backward(self, dy):
-        """Gradients of the last kept :meth:`forward` for the incoming ``dy``: a dict of new tensors with ``x`` and every
-        parameter's name."""
+        """Gradients of the last kept :meth:`forward` for the incoming ``dy``: a dict of new tensors with ``x`` (which is ``delta``'s,
+        too) and every parameter's name."""
         if self._kept is None:
             raise RuntimeError("backward: no forward pass has been kept (forward(x, keep=True) comes first)")
-        x, n, mean, rstd, gate, up, h = self._kept
+        s, n, mean, rstd, gate, up, h, p, use = self._kept
         out = {name: torch.empty_like(getattr(self, name)) for name in ("wg", "wu", "wd")}
-        out.update({name: torch.empty(self.model, dtype=torch.float32, device="cuda") for name in ("gamma", "beta", "bd")})
-        t = x.shape[0]
-        dh, dn, dx = self._buffer("dh", t, self.hidden), self._buffer("dn", t, self.model), torch.empty_like(x)
-        dg.hgemm_epilogue_bwd(h, self.wd, dy, dA=dh, dB=out["wd"], dbias=out["bd"], transb=True)
+        out.update({name: torch.empty(self.model, dtype=torch.float32, device="cuda") for name in self.parameters() if name not in out})
+        t = s.shape[0]
+        dh, dn, dx = self._buffer("dh", t, self.hidden), self._buffer("dn", t, self.model), torch.empty_like(s)
+        dd = dy
+        if p > 0.0:
+            dd = self._buffer("d", t, self.model)
+            dg.dropout_bwd(dy, dd, p, self.seed, use)
+        dg.hgemm_epilogue_bwd(h, self.wd, dd, dA=dh, dB=out["wd"], dbias=out["bd"], transb=True)
         dg.hgemm_gated_bwd(n, self.wg, self.wu, gate, up, dh, act=self.act, dX=dn, dWg=out["wg"], dWu=out["wu"], transw=True)
-        dg.layernorm_bwd(x, self.gamma, mean, rstd, dn, dX=dx, dgamma=out["gamma"], dbeta=out["beta"])
-        out["x"] = dx.add_(dy)   # the residual
+        if self.norm == "layer":
+            dg.layernorm_bwd(s, self.gamma, mean, rstd, dn, dX=dx, dgamma=out["gamma"], dbeta=out["beta"])
+            out["x"] = dx.add_(dy)   # the residual
+        else:
+            dg.rmsnorm_bwd(s, self.gamma, rstd, dn, dsum=dy, dX=dx, dgamma=out["gamma"])   # the residual's gradient joins
+            out["x"] = dx
         return out
+
+    def eight_bit(self):
+        """The sublayer for answering, its weights in 8 bits with a scale per row (root-mean-square norm only)."""
+        return EightBitFeedForward(self)
 
     def step(self, x, target, rate: float) -> float:
         """One step of gradient descent on the squared error per token (its sum over the model's width, averaged over the
@@ -81,10 +132,52 @@ class FeedForward:
         y = self.forward(x)
         diff = y.float() - target.float()
         grads = self.backward((diff * (2.0 / diff.shape[0])).to(self.dtype))
-        for name in ("gamma", "beta", "wg", "wu", "wd", "bd"):
+        for name in self.parameters():
             p = getattr(self, name)
             p.copy_(p.float() - rate * grads[name].float())
         return float((diff * diff).mean())
+
+
+class EightBitFeedForward(_Buffers):
+    """A sublayer's forward pass with weights and activations in 8 bits (e4m3), a scale for each weight row and token."""
+
+    def __init__(self, layer: FeedForward):
+        super().__init__()
+        if layer.norm != "rms":
+            raise ValueError("eight_bit: needs norm='rms'")
+        self.model, self.hidden, self.dtype, self.act = layer.model, layer.hidden, layer.dtype, layer.act
+        self.gamma, self.bd = layer.gamma.clone(), layer.bd.clone()
+        for name in ("wg", "wu", "wd"):
+            w = getattr(layer, name)
+            q = torch.empty(w.shape, dtype=torch.float8_e4m3fn, device="cuda")
+            scale = torch.empty(w.shape[0], dtype=torch.float32, device="cuda")
+            dg.quantize_rows_e4m3(w, q, scale)
+            setattr(self, name, q)
+            setattr(self, "s" + name[1:], scale)
+
+    def forward(self, x, delta=None):
+        """As :meth:`FeedForward.forward` with ``keep=False``."""
+        t, e4m3, f32 = x.shape[0], torch.float8_e4m3fn, torch.float32
+        n, sn = self._buffer("n", t, self.model, dtype=e4m3), self._buffer("sn", t, dtype=f32)
+        h, y = self._buffer("h", t, self.hidden), torch.empty_like(x)
+        q, sq = self._buffer("q", t, self.hidden, dtype=e4m3), self._buffer("sq", t, dtype=f32)
+        s = x if delta is None else self._buffer("s", t, self.model)
+        dg.rmsnorm_fwd_e4m3(x, self.gamma, n, sn, residual=delta, sum=None if delta is None else s)
+        dg.qgemm_gated(n, self.wg, self.wu, h, x_scale=sn, g_scale=self.sg, u_scale=self.su, act=self.act)
+        dg.quantize_rows_e4m3(h, q, sq)
+        dg.qgemm_epilogue(q, self.wd, y, a_scale=sq, b_scale=self.sd, bias=self.bd, residual=s)
+        return y
+
+
+def _time_per_token(layer, x, **more) -> float:
+    """Microseconds of one token's pass."""
+    layer.forward(x[:1], **more)
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    for _ in range(200):
+        layer.forward(x[:1], **more)
+    torch.cuda.synchronize()
+    return (time.perf_counter() - t) / 200 * 1e6
 
 
 def main() -> None:
@@ -93,8 +186,10 @@ def main() -> None:
     ap.add_argument("--hidden", type=int, default=4096)
     ap.add_argument("--tokens", type=int, default=2048)
     ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--norm", choices=("layer", "rms"), default="layer")
+    ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args()
-    layer, teacher = FeedForward(a.model, a.hidden, seed=1), FeedForward(a.model, a.hidden, seed=2)
+    layer, teacher = FeedForward(a.model, a.hidden, seed=1, norm=a.norm, dropout=a.dropout), FeedForward(a.model, a.hidden, seed=2, norm=a.norm)
     g = torch.Generator(device="cuda").manual_seed(3)
     x = torch.randn(a.tokens, a.model, device="cuda", generator=g).to(layer.dtype)
     target = teacher.forward(x, keep=False)
@@ -107,12 +202,11 @@ def main() -> None:
     batch = layer.forward(x[:8], keep=False)
     rows = [layer.forward(x[i:i + 1], keep=False) for i in range(8)]
     off = float((torch.cat(rows).float() - batch.float()).abs().max())
-    torch.cuda.synchronize()
-    t = time.perf_counter()
-    for _ in range(200):
-        layer.forward(x[:1], keep=False)
-    torch.cuda.synchronize()
-    print("answering: %.1f us per token, largest difference from the batch %.3g" % ((time.perf_counter() - t) / 200 * 1e6, off))
+    print("answering: %.1f us per token, largest difference from the batch %.3g" % (_time_per_token(layer, x, keep=False), off))
+    if a.norm == "rms":
+        eight = layer.eight_bit()
+        far = float((eight.forward(x[:8]).float() - batch.float()).norm() / (batch.float() - x[:8].float()).norm())
+        print("answering in 8 bits: %.1f us per token, off by %.3g of the sublayer's part" % (_time_per_token(eight, x), far))
 
 
 if __name__ == "__main__":
