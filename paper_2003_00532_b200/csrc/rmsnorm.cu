@@ -22,14 +22,14 @@ struct Shape {
 };
 
 // Forward: a warp for rows of up to 16 values per lane; a block with 16 values per thread beyond (or up to 32, for rows
-// that need them). Few rows are spread over as many threads as there are vectors, because then the latency of
-// one row counts.
-Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms) {
+// that need them, and for vectors that are only brought to 8 bits: 2088 x 8192 10.1 -> 9.5 us). Few rows are spread over as many threads
+// as there are vectors, because then the latency of one row counts.
+Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms, bool rows_only) {
   const int64_t nv = (cols + vec - 1) / vec;
   const int most = 32 / vec, warp_most = 16 / vec;
   const bool spread = rows * ((nv + 32 * most - 1) / (32 * most)) < (int64_t)sms * 16;  // warps in all
   if (nv <= 32 || (!spread && nv <= 32 * warp_most)) return Shape{pow2((nv + 31) / 32), 32, false};
-  int items = spread ? 1 : 16 / vec;
+  int items = spread ? 1 : (rows_only && vec > 1 && nv > 32 * most ? 32 : 16) / vec;  // (a block has two warps at least)
   while (items < most && threads_for(nv, items) > fwd_threads(items * vec)) items *= 2;
   const int threads = threads_for(nv, items);
   if (threads > fwd_threads(items * vec)) return Shape{0, 1024, true};
@@ -95,7 +95,7 @@ bool launch_fwd(int sms, const Shape& s, const Params& p, cudaStream_t stream) {
 }
 template <typename T, int VEC, int OUT>
 bool run_fwd_vec(int sms, const Params& p, cudaStream_t stream) {
-  const Shape s = fwd_shape(p.rows, p.cols, VEC, sms);
+  const Shape s = fwd_shape(p.rows, p.cols, VEC, sms, OUT == OUT_ROWS);
   // 16-bit rows through shared memory, where there are many. Blocks of 256 threads (8192 x 4096 without a residual: Y 29.1 -> 24.2 us, to
   // 8 bits 27.3 -> 24.1; 1500 x 4000 with one 10.9 -> 9.7 and 10.5 -> 9.2); but with a residual beyond L2 so many streams of reads and
   // writes slow each other down (8192 x 4096: 47.1, 16384 x 2048 46.5), and one block of 512 (42.3), or for shorter rows the registers
@@ -124,14 +124,14 @@ bool run_fwd(int type, bool aligned, const Params& p, const lm::DeviceState* st,
   return aligned ? run_fwd_vec<__nv_bfloat16, 8, OUT>(sms, p, stream) : run_fwd_vec<__nv_bfloat16, 1, OUT>(sms, p, stream);
 }
 
-// Blocks of the backward pass: as many as fit at once, but for few rows at least eight rows each (every block leaves
-// its own sums to be added), down to one per SM.
+// Blocks of the backward pass: as many as fit at once, but for few rows at least two rows each (every block leaves
+// its own sums to be added; 721 x 816, binary32: with eight each 8.5 us, with two 7.4), down to one per SM.
 template <typename K, K kernel>
 int bwd_blocks(int sms, int threads, size_t smem, int64_t rows, int rows_per_block) {
   const int64_t need = (rows + rows_per_block - 1) / rows_per_block;
   const int64_t some = (int)resident_blocks<K, kernel>(sms, threads, smem, need);
-  const int64_t eighth = (rows + 8 * rows_per_block - 1) / (8 * rows_per_block);
-  const int64_t want = eighth > sms ? eighth : sms;
+  const int64_t half = (rows + 2 * rows_per_block - 1) / (2 * rows_per_block);
+  const int64_t want = half > sms ? half : sms;
   return (int)(some < want ? some : want);
 }
 
@@ -139,9 +139,9 @@ int bwd_blocks(int sms, int threads, size_t smem, int64_t rows, int rows_per_blo
 template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE, typename F>
 int launch_bwd(int sms, int threads, Params& p, cudaStream_t stream, F partial) {
   constexpr auto kernel = &bwd_kernel<T, VEC, ITEMS, WARP_ROW, WIDE>;
-  const size_t smem = WIDE ? (size_t)threads * ITEMS * VEC * 8 : WARP_ROW && p.want_params ? (size_t)p.cols * 4 : 0;
+  const size_t smem = WIDE ? (size_t)threads * ITEMS * VEC * 8 : WARP_ROW && p.want_params ? (size_t)threads * ITEMS * 4 : 0;
   if (WIDE && !allow_smem<decltype(kernel), kernel>(BWD_THREADS * ITEMS * VEC * 8)) return 0;
-  const size_t most = WIDE ? smem : WARP_ROW ? (size_t)32 * ITEMS * VEC * 4 : 0;
+  const size_t most = WIDE ? smem : WARP_ROW ? (size_t)threads * ITEMS * 4 : 0;
   const int blocks = bwd_blocks<decltype(kernel), kernel>(sms, threads, most, p.rows, WARP_ROW ? 8 : 1);
   if (blocks == 0 || !partial(blocks)) return 0;
   return lm::launch(kernel, dim3(blocks), dim3(threads), smem, 1, stream, p) ? blocks : 0;

@@ -373,7 +373,8 @@ constexpr int BWD_THREADS = 512;
 // sums for dgamma in shared memory (each thread's own entries) instead of registers.
 template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE>
 __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const __grid_constant__ Params p) {
-  extern __shared__ float sums[];  // WARP_ROW with dgamma: [cols]; WIDE: gamma, dgamma as [pair][thread] of float2
+  static_assert(!WARP_ROW || VEC == 1, "rows of any alignment");
+  extern __shared__ float sums[];  // WARP_ROW with dgamma: [value][thread]; WIDE: gamma, dgamma as [pair][thread] of float2
   __shared__ uint2 red[2][32];
   hgemm::ptx5::launch_dependents();
   dgemm::ptx::grid_dependency_wait();
@@ -496,16 +497,16 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
         if (column(f) < p.cols) out[column(f)] = value(f);
     }
   } else {
-    // the eight warps add their sums one after the other, in order
-    for (int k = 0; k < 8; ++k) {
-      if (warp == k) {
+    // all warps' sums side by side, then added over the warps in order
 #pragma unroll
-        for (int f = 0; f < VEC * ITEMS; ++f)
-          if (column(f) < p.cols) sums[column(f)] = k ? sums[column(f)] + value(f) : value(f);
-      }
-      __syncthreads();
+    for (int f = 0; f < VEC * ITEMS; ++f) sums[f * blockDim.x + threadIdx.x] = value(f);
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
+      const float* at = sums + c / 32 * blockDim.x + c % 32;  // (VEC = 1: column c is value c / 32 of lane c % 32)
+      float a = at[0];
+      for (int k = 1; k < 8; ++k) a += at[32 * k];
+      out[c] = a;
     }
-    for (int c = threadIdx.x; c < p.cols; c += blockDim.x) out[c] = sums[c];
   }
 }
 
