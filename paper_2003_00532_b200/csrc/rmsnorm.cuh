@@ -12,6 +12,13 @@
 // sums go to a partial matrix [block][column] that a second kernel (layer norm's) adds in order of the blocks: no atomics,
 // same bits every time.
 //
+// Rows that are not 16-byte aligned (ANY), as long as all matrices are misaligned alike (which they are where a program's matrices have
+// the same odd number of columns): a thread's vectors begin at the aligned address before the row, `shift` columns to the left of it, and only
+// the two vectors at the row's ends are taken value by value. Every VEC-th row has the same shift, so rows are dealt out by multiples
+// of VEC and a thread has the same columns for good, as with aligned rows. Matrices of different alignment are read and
+// written value by value (VEC = 1). 8192 x 4089 bfloat16, with residual and by single values: Y 70 -> 47.4 us, to 8 bits 73 -> 41.9,
+// gradients 108 -> 54.5; 4097 x 1537 binary32, gradients without residual 22.7 -> 19.4.
+//
 // Rows too long for the registers are streamed twice (the second time mostly from L2).
 #pragma once
 
@@ -54,7 +61,72 @@ struct Params {
   long long ldp;      // cols rounded up to 4: every row can be written as vectors
   float eps;
   int want_params;
+  int shift, shift_ld;  // ANY: columns from the aligned address to the first row; what a row adds to them (modulo VEC)
 };
+
+// Columns between the row and the aligned address before it.
+template <int VEC, bool ANY>
+__device__ __forceinline__ int shift_of(const Params& p, long long row) {
+  return ANY ? (p.shift + (int)(row % VEC) * p.shift_ld) % VEC : 0;
+}
+// Items of a row whose first vector may begin before its first column (c0 < 0); values outside the row are 0, and not read or written.
+template <typename T, int VEC, int ITEMS, bool ANY>
+__device__ __forceinline__ void take_row(Vec<T, VEC> (&raw)[ITEMS], const T* at, int c0, int cols, bool full) {
+  if constexpr (ANY) {
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int c = c0 + i * 32 * VEC;
+        const T* src = at + i * 32 * VEC;
+        if (c >= 0 && c + VEC <= cols) {
+          raw[i].bits = *reinterpret_cast<const decltype(raw[i].bits)*>(src);
+        } else {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) raw[i].set(j, (unsigned)(c + j) < (unsigned)cols ? src[j] : rnd<T>(0.f));
+        }
+      }
+      return;
+    }
+  }
+  load_row<T, VEC, ITEMS>(raw, at, c0, cols, full);
+}
+template <typename T, int VEC, int ITEMS, bool ANY>
+__device__ __forceinline__ void put_row(T* at, const Pairs<T, VEC, ITEMS>& v, int c0, int cols, bool full) {
+  if constexpr (ANY) {
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int c = c0 + i * 32 * VEC;
+        T* dst = at + i * 32 * VEC;
+        const Vec<T, VEC> o = v.pack(i);
+        if (c >= 0 && c + VEC <= cols) {
+          *reinterpret_cast<decltype(v.pack(0).bits)*>(dst) = o.bits;
+        } else {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if ((unsigned)(c + j) < (unsigned)cols) dst[j] = o.get(j);
+        }
+      }
+      return;
+    }
+  }
+  store_row<T, VEC, ITEMS>(at, v, c0, cols, full);
+}
+// gamma in the columns of a thread, at any address.
+template <typename T, int VEC, int ITEMS, bool ANY>
+__device__ __forceinline__ void take_gamma(Vec<T, VEC> (&raw)[ITEMS], const T* gamma, int c0, int cols, bool full) {
+  if constexpr (ANY) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const int c = c0 + i * 32 * VEC + j;
+        raw[i].set(j, (unsigned)c < (unsigned)cols ? gamma[c] : rnd<T>(0.f));
+      }
+  } else {
+    load_row<T, VEC, ITEMS>(raw, gamma + c0, c0, cols, full);
+  }
+}
 
 // What the forward kernel makes of a row: y, y in 8 bits, or x itself in 8 bits.
 constexpr int OUT_Y = 0, OUT_E4M3 = 1, OUT_ROWS = 2;
@@ -145,13 +217,13 @@ __device__ __forceinline__ void store_e4m3(uint8_t* at, const Pairs<T, VEC, ITEM
       uint16_t q[VEC / 2];
 #pragma unroll
       for (int j = 0; j < VEC / 2; ++j) q[j] = e4m3_pair(value(i * VEC + 2 * j), value(i * VEC + 2 * j + 1));
-      if (full || c + VEC <= cols) {
+      if (full || (c >= 0 && c + VEC <= cols)) {
         if constexpr (VEC == 8) *reinterpret_cast<uint2*>(o) = make_uint2((uint32_t)q[0] | (uint32_t)q[1] << 16, (uint32_t)q[2] | (uint32_t)q[3] << 16);
         else *reinterpret_cast<uint32_t*>(o) = (uint32_t)q[0] | (uint32_t)q[1] << 16;
       } else {
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-          if (c + j < cols) o[j] = (uint8_t)(q[j / 2] >> 8 * (j % 2));
+          if ((unsigned)(c + j) < (unsigned)cols) o[j] = (uint8_t)(q[j / 2] >> 8 * (j % 2));
       }
     }
   }
@@ -163,7 +235,7 @@ __device__ __forceinline__ void store_e4m3(uint8_t* at, const Pairs<T, VEC, ITEM
 constexpr int fwd_threads(int values) { return values <= 8 ? 1024 : 512; }
 
 // WARP_ROW: four rows per block of 128 threads, one warp each; otherwise one row per block.
-template <typename T, int VEC, int ITEMS, bool WARP_ROW, int OUT>
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, int OUT, bool ANY>
 __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_kernel(const __grid_constant__ Params p) {
   __shared__ uint2 red[2][32];
   hgemm::ptx5::launch_dependents();
@@ -172,18 +244,18 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
   constexpr int N = P::N;
   constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int c0 = ((WARP_ROW ? 0 : warp * ITEMS * 32) + lane) * VEC;  // first column of this thread
-  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const long long step = WARP_ROW ? (long long)gridDim.x * 4 : (long long)gridDim.x;
   long long row = WARP_ROW ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
+  const int c0 = ((WARP_ROW ? 0 : warp * ITEMS * 32) + lane) * VEC - shift_of<VEC, ANY>(p, row);  // first column of this thread
+  const bool full = c0 >= 0 && c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
   const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
   T* s_at = static_cast<T*>(p.S) + row * p.lds + c0;
   Vec<T, VEC> xr[ITEMS], rr[ITEMS], gr[ITEMS];
-  if (NORM && p.gamma) load_row<T, VEC, ITEMS>(gr, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+  if (NORM && p.gamma) take_gamma<T, VEC, ITEMS, ANY>(gr, static_cast<const T*>(p.gamma), c0, p.cols, full);
   if (row < p.rows) {
-    load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
-    if (NORM && p.R) load_row<T, VEC, ITEMS>(rr, r_at, c0, p.cols, full);
+    take_row<T, VEC, ITEMS, ANY>(xr, x_at, c0, p.cols, full);
+    if (NORM && p.R) take_row<T, VEC, ITEMS, ANY>(rr, r_at, c0, p.cols, full);
   }
   if (NORM && !p.gamma) {
 #pragma unroll
@@ -213,14 +285,14 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
     x_at += step * p.ldx;
     r_at += step * p.ldr;
     if (row < p.rows) {
-      load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
-      if (NORM && p.R) load_row<T, VEC, ITEMS>(rr, r_at, c0, p.cols, full);
+      take_row<T, VEC, ITEMS, ANY>(xr, x_at, c0, p.cols, full);
+      if (NORM && p.R) take_row<T, VEC, ITEMS, ANY>(rr, r_at, c0, p.cols, full);
     }
     float f = 1.f;  // what is left to multiply by
     uint32_t top = 0;
     if (NORM) {
       if (p.S) {
-        store_row<T, VEC, ITEMS>(s_at, x, c0, p.cols, full);
+        put_row<T, VEC, ITEMS, ANY>(s_at, x, c0, p.cols, full);
         s_at += step * p.lds;
       }
       float sum = squares(x.v), unit = 1.f;
@@ -268,7 +340,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
-      store_row<T, VEC, ITEMS>(static_cast<T*>(p.out) + at * p.ldo + c0, x, c0, p.cols, full);
+      put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.out) + at * p.ldo + c0, x, c0, p.cols, full);
     }
   }
 }
@@ -364,6 +436,8 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
   }
 }
 
+__device__ __forceinline__ bool finite(float x) { return magnitude(x) < 0x7f800000u; }
+
 // ---- backward ---------------------------------------------------------------------------------------
 
 // Most threads per row: 512 with 16 values each in 128 registers.
@@ -371,7 +445,7 @@ constexpr int BWD_THREADS = 512;
 
 // WARP_ROW: eight rows per block, one warp each; otherwise one row per block. WIDE: 32 values per thread, gamma and the
 // sums for dgamma in shared memory (each thread's own entries) instead of registers.
-template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE>
+template <typename T, int VEC, int ITEMS, bool WARP_ROW, bool WIDE, bool ANY>
 __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const __grid_constant__ Params p) {
   static_assert(!WARP_ROW || VEC == 1, "rows of any alignment");
   extern __shared__ float sums[];  // WARP_ROW with dgamma: [value][thread]; WIDE: gamma, dgamma as [pair][thread] of float2
@@ -381,10 +455,10 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
   using P = Pairs<T, VEC, ITEMS>;
   constexpr int N = P::N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int c0 = ((WARP_ROW ? 0 : warp * ITEMS * 32) + lane) * VEC;  // first column of this thread
-  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const long long step = WARP_ROW ? (long long)gridDim.x * 8 : (long long)gridDim.x;
   long long row = WARP_ROW ? (long long)blockIdx.x * 8 + warp : (long long)blockIdx.x;
+  const int c0 = ((WARP_ROW ? 0 : warp * ITEMS * 32) + lane) * VEC - shift_of<VEC, ANY>(p, row);  // first column of this thread
+  const bool full = c0 >= 0 && c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
   const T* d_at = static_cast<const T*>(p.dY) + row * p.ldy + c0;
   const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
@@ -396,11 +470,11 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
   const float inv_n = 1.f / (float)p.cols;
   // gamma's loads and the first row's are in flight together
   Vec<T, VEC> xr[ITEMS], dr[ITEMS], gr[ITEMS];
-  if (gamma) load_row<T, VEC, ITEMS>(gr, gamma + c0, c0, p.cols, full);
+  if (gamma) take_gamma<T, VEC, ITEMS, ANY>(gr, gamma, c0, p.cols, full);
   float rstd = 0.f;
   if (row < p.rows) {
-    load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
-    load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
+    take_row<T, VEC, ITEMS, ANY>(xr, x_at, c0, p.cols, full);
+    take_row<T, VEC, ITEMS, ANY>(dr, d_at, c0, p.cols, full);
     rstd = p.rstd[row];
   }
   P g, dg;
@@ -425,24 +499,24 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
     w.unpack(dr);
     const float rs = rstd;
     Vec<T, VEC> rr[ITEMS];
-    if (add) load_row<T, VEC, ITEMS>(rr, r_at, c0, p.cols, full);
+    if (add) take_row<T, VEC, ITEMS, ANY>(rr, r_at, c0, p.cols, full);
     row += step;
     x_at += step * p.ldx;
     d_at += step * p.ldy;
     r_at += step * p.ldr;
     if (row < p.rows) {
-      load_row<T, VEC, ITEMS>(xr, x_at, c0, p.cols, full);
-      load_row<T, VEC, ITEMS>(dr, d_at, c0, p.cols, full);
+      take_row<T, VEC, ITEMS, ANY>(xr, x_at, c0, p.cols, full);
+      take_row<T, VEC, ITEMS, ANY>(dr, d_at, c0, p.cols, full);
       rstd = p.rstd[row];
     }
-    if (full && VEC * ITEMS % 2 == 0) {
+    if ((full || finite(rs)) && VEC * ITEMS % 2 == 0) {
 #pragma unroll
       for (int k = 0; k < N; ++k) xh.v[k] = mul2(xh.v[k], both(rs));
     } else {
 #pragma unroll
       for (int f = 0; f < VEC * ITEMS; ++f) {
         float& h = f % 2 ? xh.v[f / 2].y : xh.v[f / 2].x;
-        h = c0 + f / VEC * 32 * VEC + f % VEC < p.cols ? h * rs : 0.f;
+        h = (unsigned)(c0 + f / VEC * 32 * VEC + f % VEC) < (unsigned)p.cols ? h * rs : 0.f;
       }
     }
     float2 t = both(0.f);
@@ -474,7 +548,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
 #pragma unroll
         for (int k = 0; k < N; ++k) w.v[k] = add2(w.v[k], r.v[k]);
       }
-      store_row<T, VEC, ITEMS>(o_at, w, c0, p.cols, full);
+      put_row<T, VEC, ITEMS, ANY>(o_at, w, c0, p.cols, full);
       o_at += step * p.ldo;
     }
   }
@@ -487,14 +561,14 @@ __global__ void __launch_bounds__(WARP_ROW ? 256 : BWD_THREADS) bwd_kernel(const
   const auto value = [&](int f) { return f % 2 ? dg.v[f / 2].y : dg.v[f / 2].x; };
   const auto column = [&](int f) { return c0 + f / VEC * 32 * VEC + f % VEC; };
   if (!WARP_ROW) {
-    if constexpr (VEC >= 4) {
+    if constexpr (VEC >= 4 && !ANY) {
 #pragma unroll
       for (int f = 0; f < VEC * ITEMS; f += 4)
         if (column(f) < p.cols) *reinterpret_cast<float4*>(out + column(f)) = make_float4(value(f), value(f + 1), value(f + 2), value(f + 3));
     } else {
 #pragma unroll
       for (int f = 0; f < VEC * ITEMS; ++f)
-        if (column(f) < p.cols) out[column(f)] = value(f);
+        if ((unsigned)column(f) < (unsigned)p.cols) out[column(f)] = value(f);
     }
   } else {
     // all warps' sums side by side, then added over the warps in order
@@ -529,27 +603,64 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
 }
 
+__device__ __forceinline__ void copy_word_async(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void sts32(uint32_t dst, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst), "r"(v) : "memory"); }
+__device__ __forceinline__ uint32_t upper(__half x) { return (uint32_t)__half_as_ushort(x) << 16; }
+__device__ __forceinline__ uint32_t upper(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x) << 16; }
+__device__ __forceinline__ uint32_t upper(float) { return 0; }
+
 // One thread's vectors of the rows on their way: [row % DEPTH][stream][item][thread].
-template <typename T, int VEC, int ITEMS, int DEPTH>
+//
+// ANY: of the vector that begins before the row (`skip` bytes of it) the words inside the row are copied one by one. Where the row begins
+// in the middle of a word (16-bit values), its first value goes through a register: load_odd() with the copies, put_odd() any time before
+// the row is taken.
+template <typename T, int VEC, int ITEMS, int DEPTH, bool ANY>
 struct Ring {
   static constexpr int SIZE = 16;
   static_assert(VEC * sizeof(T) == SIZE, "vectors of 16 bytes");
   uint32_t base;     // of this thread
   int pitch;         // bytes between items
   int streams;
-  int bytes[ITEMS];  // of each vector that lie inside the row
+  int bytes[ITEMS];  // of each vector up to the row's end
+  int skip;
+  bool odd;          // the row begins in the middle of a word of this thread's
   __device__ __forceinline__ Ring(void* smem, int streams_, int c0, int cols) : streams(streams_) {
     base = dgemm::ptx::smem_u32(smem) + threadIdx.x * SIZE;
     pitch = blockDim.x * SIZE;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) bytes[i] = max(0, min(SIZE, (cols - c0 - i * 32 * VEC) * (int)sizeof(T)));
+    skip = ANY && c0 < 0 ? -c0 * (int)sizeof(T) : 0;
+    odd = ANY && skip % 4 != 0;
+    if (skip > 0)  // the words outside the row stay 0
+      for (int k = 0; k < DEPTH * streams; ++k)
+        for (int w = 0; w < 4; ++w)
+          if (4 * w < skip || 4 * w >= bytes[0]) sts32(base + k * ITEMS * pitch + 4 * w, 0);
   }
   __device__ __forceinline__ uint32_t at(int slot, int stream) const { return base + (slot * streams + stream) * ITEMS * pitch; }
   __device__ __forceinline__ void copy(int slot, int stream, const T* src) const {
     const uint32_t dst = at(slot, stream);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) copy_async(dst + i * pitch, bytes[i] > 0 ? src + i * 32 * VEC : src, bytes[i]);
+    for (int i = 0; i < ITEMS; ++i) {
+      if (ANY && i == 0 && skip > 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+          if (4 * w >= skip && 4 * w < bytes[0]) copy_word_async(dst + 4 * w, src + 4 * w / (int)sizeof(T), min(4, bytes[0] - 4 * w));
+      } else {
+        copy_async(dst + i * pitch, bytes[i] > 0 ? src + i * 32 * VEC : src, bytes[i]);
+      }
+    }
   }
+  __device__ __forceinline__ Pairs<T, VEC, 1> item(int slot, int stream, int i) const {
+    Vec<T, VEC> raw[1];
+    raw[0].bits = hgemm::ptx5::lds128(at(slot, stream) + i * pitch);
+    Pairs<T, VEC, 1> v;
+    v.unpack(raw);
+    return v;
+  }
+  __device__ __forceinline__ T load_odd(const T* src) const { return src[skip / (int)sizeof(T)]; }
+  __device__ __forceinline__ void put_odd(int slot, int stream, T v) const { sts32(at(slot, stream) + skip / 4 * 4, upper(v)); }
   __device__ __forceinline__ void take(int slot, int stream, Vec<T, VEC> (&raw)[ITEMS]) const {
     const uint32_t src = at(slot, stream);
 #pragma unroll
@@ -575,7 +686,7 @@ __device__ __forceinline__ void reduce_group(float& sum, uint32_t& top, uint2* r
 constexpr int RING_THREADS = 512, SMALL_RING_THREADS = 256;
 
 // THREADS: most of a block; three blocks of 256 fit on an SM, one of 512.
-template <typename T, int VEC, int ITEMS, int DEPTH, int OUT, int THREADS>
+template <typename T, int VEC, int ITEMS, int DEPTH, int OUT, int THREADS, bool ANY>
 __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1) fwd_ring_kernel(const __grid_constant__ Params p, const Groups gr) {
   extern __shared__ uint4 ring_smem[];
   __shared__ uint2 red[2][16];
@@ -585,31 +696,48 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
   constexpr int N = P::N;
   constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
   const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / gr.warps, warp = (threadIdx.x >> 5) - group * gr.warps;
-  const int c0 = (warp * ITEMS * 32 + lane) * VEC;
-  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const long long step = (long long)gridDim.x * gr.groups;
   long long row = (long long)blockIdx.x * gr.groups + group;
+  const int c0 = (warp * ITEMS * 32 + lane) * VEC - shift_of<VEC, ANY>(p, row);
+  const bool full = c0 >= 0 && c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const bool add = NORM && p.R;
-  const Ring<T, VEC, ITEMS, DEPTH> ring(ring_smem, add ? 2 : 1, c0, p.cols);
+  const Ring<T, VEC, ITEMS, DEPTH, ANY> ring(ring_smem, add ? 2 : 1, c0, p.cols);
   const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
   const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
   long long ahead = row;
+  T odd_x, odd_r;
+  int late = -1;  // the slot that waits for them
   const auto send = [&](int slot) {
     if (ahead < p.rows) {
       ring.copy(slot, 0, x_at);
       if (add) ring.copy(slot, 1, r_at);
+      if (ANY && ring.odd) {
+        odd_x = ring.load_odd(x_at);
+        if (add) odd_r = ring.load_odd(r_at);
+        late = slot;
+      }
     }
     copies_commit();
     ahead += step;
     x_at += step * p.ldx;
     r_at += step * p.ldr;
   };
+  const auto settle = [&]() {
+    if (ANY && late >= 0) {
+      ring.put_odd(late, 0, odd_x);
+      if (add) ring.put_odd(late, 1, odd_r);
+      late = -1;
+    }
+  };
 #pragma unroll
-  for (int d = 0; d < DEPTH - 1; ++d) send(d);
+  for (int d = 0; d < DEPTH - 1; ++d) {
+    if (d > 0) settle();
+    send(d);
+  }
   Vec<T, VEC> g_raw[ITEMS];
   if (NORM) {
     if (p.gamma) {
-      load_row<T, VEC, ITEMS>(g_raw, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+      take_gamma<T, VEC, ITEMS, ANY>(g_raw, static_cast<const T*>(p.gamma), c0, p.cols, full);
     } else {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i)
@@ -617,6 +745,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
         for (int j = 0; j < VEC; ++j) g_raw[i].set(j, rnd<T>(1.f));
     }
   }
+  settle();  // (behind gamma's loads)
   const float inv_n = 1.f / (float)p.cols;
   int parity = 0, slot = 0;
   const auto next = [&]() {  // the buffer of the next reduction
@@ -644,7 +773,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     uint32_t top = 0;
     float none = 0.f;
     if (NORM) {
-      if (p.S) store_row<T, VEC, ITEMS>(static_cast<T*>(p.S) + row * p.lds + c0, x, c0, p.cols, full);
+      if (p.S) put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.S) + row * p.lds + c0, x, c0, p.cols, full);
       float sum = squares(x.v), rstd;
       const auto weigh = [&]() {
         P g;
@@ -686,15 +815,183 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
-      store_row<T, VEC, ITEMS>(static_cast<T*>(p.out) + row * p.ldo + c0, x, c0, p.cols, full);
+      put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.out) + row * p.ldo + c0, x, c0, p.cols, full);
     }
+    settle();
     slot = slot == DEPTH - 1 ? 0 : slot + 1;
   }
   copies_wait<0>();
 }
 
+// The same for longer rows, 32 values per thread: too many to be kept in registers through the reduction beside gamma, so they are read from
+// shared memory once for the sums and once for the outputs.
+template <typename T, int VEC, int ITEMS, int OUT, int THREADS, bool ANY>
+__global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1) fwd_again_kernel(const __grid_constant__ Params p, const Groups gr) {
+  extern __shared__ uint4 ring_smem[];
+  __shared__ uint2 red[2][16];
+  hgemm::ptx5::launch_dependents();
+  dgemm::ptx::grid_dependency_wait();
+  using Item = Pairs<T, VEC, 1>;
+  constexpr int DEPTH = 2;
+  constexpr bool EIGHT = OUT == OUT_E4M3;
+  const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / gr.warps, warp = (threadIdx.x >> 5) - group * gr.warps;
+  const long long step = (long long)gridDim.x * gr.groups;
+  long long row = (long long)blockIdx.x * gr.groups + group;
+  const int c0 = (warp * ITEMS * 32 + lane) * VEC - shift_of<VEC, ANY>(p, row);
+  const bool full = c0 >= 0 && c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols, add = p.R != nullptr;
+  const Ring<T, VEC, ITEMS, DEPTH, ANY> ring(ring_smem, add ? 2 : 1, c0, p.cols);
+  const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
+  const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
+  long long ahead = row;
+  T odd_x, odd_r;
+  int late = -1;  // the slot that waits for them
+  const auto send = [&](int slot) {
+    if (ahead < p.rows) {
+      ring.copy(slot, 0, x_at);
+      if (add) ring.copy(slot, 1, r_at);
+      if (ANY && ring.odd) {
+        odd_x = ring.load_odd(x_at);
+        if (add) odd_r = ring.load_odd(r_at);
+        late = slot;
+      }
+    }
+    copies_commit();
+    ahead += step;
+    x_at += step * p.ldx;
+    r_at += step * p.ldr;
+  };
+  const auto settle = [&]() {
+    if (ANY && late >= 0) {
+      ring.put_odd(late, 0, odd_x);
+      if (add) ring.put_odd(late, 1, odd_r);
+      late = -1;
+    }
+  };
+  send(0);
+  Vec<T, VEC> g_raw[ITEMS];
+  if (p.gamma) {
+    take_gamma<T, VEC, ITEMS, ANY>(g_raw, static_cast<const T*>(p.gamma), c0, p.cols, full);
+  } else {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) g_raw[i].set(j, rnd<T>(1.f));
+  }
+  settle();  // (behind gamma's loads)
+  const float inv_n = 1.f / (float)p.cols;
+  int parity = 0, slot = 0;
+  const auto next = [&]() {  // the buffer of the next reduction
+    parity ^= 1;
+    return red[parity];
+  };
+  for (; row < p.rows; row += step) {
+    send(slot ^ 1);
+    copies_wait<1>();
+    const auto item = [&](int i) {  // s
+      Item x = ring.item(slot, 0, i);
+      if (add) {
+        const Item r = ring.item(slot, 1, i);
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) x.v[k] = add2(x.v[k], r.v[k]);
+      }
+      return x;
+    };
+    const auto times = [&](Item& x, float f) {
+#pragma unroll
+      for (int k = 0; k < VEC / 2; ++k) x.v[k] = mul2(x.v[k], both(f));
+    };
+    const auto weigh = [&](Item& x, int i) {
+      Vec<T, VEC> raw[1] = {g_raw[i]};
+      Item g;
+      g.unpack(raw);
+#pragma unroll
+      for (int k = 0; k < VEC / 2; ++k) x.v[k] = mul2(x.v[k], g.v[k]);
+    };
+    float2 part = both(0.f);
+    float most = 0.f, none = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      Item x = item(i);
+      if (p.S) put_row<T, VEC, 1, ANY>(static_cast<T*>(p.S) + row * p.lds + c0 + i * 32 * VEC, x, c0 + i * 32 * VEC, p.cols, full);
+#pragma unroll
+      for (int k = 0; k < VEC / 2; ++k) part = fma2(x.v[k], x.v[k], part);
+      if (EIGHT) {
+        weigh(x, i);
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) most = max_abs(most, x.v[k].x, x.v[k].y);
+      }
+    }
+    float sum = part.x + part.y, rstd;
+    uint32_t top = __float_as_uint(most);
+    reduce_group<true, EIGHT>(sum, top, next(), gr, group, warp);
+    float f = rstd = lnorm::inv_sqrt(sum * inv_n + p.eps), unit = 1.f, g = 1.f;  // s unit g gamma f: y
+    // (the same for all threads of a row)
+    const bool rescale = !(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u);
+    if (rescale) {
+      most = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < ITEMS; ++i) {
+        const Item x = item(i);
+        most = max_abs(most, __uint_as_float(magnitude_max(x.v)), 0.f);
+      }
+      uint32_t all = __float_as_uint(most);
+      reduce_group<false, true>(none, all, next(), gr, group, warp);
+      unit = row_unit(all, p.eps);
+      sum = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < ITEMS; ++i) {
+        Item x = item(i);
+        times(x, unit);
+        sum += squares(x.v);
+      }
+      reduce_group<true, false>(sum, all, next(), gr, group, warp);
+      g = lnorm::inv_sqrt(sum * inv_n + p.eps * unit * unit);
+      rstd = unit * g;
+      f = 1.f;
+      if (EIGHT) {
+        most = 0.f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          Item x = item(i);
+          times(x, unit);
+          times(x, g);
+          weigh(x, i);
+          most = max_abs(most, __uint_as_float(magnitude_max(x.v)), 0.f);
+        }
+        top = __float_as_uint(most);
+        reduce_group<false, true>(none, top, next(), gr, group, warp);
+      }
+    }
+    if (lane == 0 && warp == 0 && p.rstd) p.rstd[row] = rstd;
+    if (EIGHT) {
+      const float largest = at_least(f * __uint_as_float(top), LEAST_MAX);
+      if (lane == 0 && warp == 0) p.scale[row] = largest / E4M3_TOP;
+      f *= top_over(largest);
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      Item x = item(i);
+      if (rescale) {
+        times(x, unit);
+        times(x, g);
+      }
+      weigh(x, i);
+      const int c = c0 + i * 32 * VEC;
+      if constexpr (EIGHT) {
+        store_e4m3<T, VEC, 1>(static_cast<uint8_t*>(p.out) + row * p.ldo + c, x, f, c, p.cols, full);
+      } else {
+        times(x, f);
+        put_row<T, VEC, 1, ANY>(static_cast<T*>(p.out) + row * p.ldo + c, x, c, p.cols, full);
+      }
+    }
+    settle();
+    slot ^= 1;
+  }
+  copies_wait<0>();
+}
+
 // dgamma: each thread keeps the sums of its own columns in registers; the block's groups add theirs up at the end, in order.
-template <typename T, int VEC, int ITEMS, int DEPTH>
+template <typename T, int VEC, int ITEMS, int DEPTH, bool ANY>
 __global__ void __launch_bounds__(RING_THREADS) bwd_ring_kernel(const __grid_constant__ Params p, const Groups gr) {
   extern __shared__ float4 ring_smem4[];
   __shared__ uint2 red[2][16];
@@ -702,22 +999,31 @@ __global__ void __launch_bounds__(RING_THREADS) bwd_ring_kernel(const __grid_con
   dgemm::ptx::grid_dependency_wait();
   using P = Pairs<T, VEC, ITEMS>;
   constexpr int N = P::N;
+  constexpr bool AGAIN = VEC * ITEMS > 16;  // rows are read twice, because two of their matrices do not fit in registers beside dgamma
   const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / gr.warps, warp = (threadIdx.x >> 5) - group * gr.warps;
-  const int c0 = (warp * ITEMS * 32 + lane) * VEC;
-  const bool full = c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const long long step = (long long)gridDim.x * gr.groups;
   long long row = (long long)blockIdx.x * gr.groups + group;
+  const int c0 = (warp * ITEMS * 32 + lane) * VEC - shift_of<VEC, ANY>(p, row);
+  const bool full = c0 >= 0 && c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
   const bool add = p.R && p.out;  // dS joins
-  const Ring<T, VEC, ITEMS, DEPTH> ring(ring_smem4, add ? 3 : 2, c0, p.cols);
+  const Ring<T, VEC, ITEMS, DEPTH, ANY> ring(ring_smem4, add ? 3 : 2, c0, p.cols);
   const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
   const T* d_at = static_cast<const T*>(p.dY) + row * p.ldy + c0;
   const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
   long long ahead = row;
+  T odd_x, odd_d, odd_r;
+  int late = -1;  // the slot that waits for them
   const auto send = [&](int slot) {
     if (ahead < p.rows) {
       ring.copy(slot, 0, x_at);
       ring.copy(slot, 1, d_at);
       if (add) ring.copy(slot, 2, r_at);
+      if (ANY && ring.odd) {
+        odd_x = ring.load_odd(x_at);
+        odd_d = ring.load_odd(d_at);
+        if (add) odd_r = ring.load_odd(r_at);
+        late = slot;
+      }
     }
     copies_commit();
     ahead += step;
@@ -725,11 +1031,22 @@ __global__ void __launch_bounds__(RING_THREADS) bwd_ring_kernel(const __grid_con
     d_at += step * p.ldy;
     r_at += step * p.ldr;
   };
+  const auto settle = [&]() {
+    if (ANY && late >= 0) {
+      ring.put_odd(late, 0, odd_x);
+      ring.put_odd(late, 1, odd_d);
+      if (add) ring.put_odd(late, 2, odd_r);
+      late = -1;
+    }
+  };
 #pragma unroll
-  for (int d = 0; d < DEPTH - 1; ++d) send(d);
+  for (int d = 0; d < DEPTH - 1; ++d) {
+    if (d > 0) settle();
+    send(d);
+  }
   Vec<T, VEC> g_raw[ITEMS];
   if (p.gamma) {
-    load_row<T, VEC, ITEMS>(g_raw, static_cast<const T*>(p.gamma) + c0, c0, p.cols, full);
+    take_gamma<T, VEC, ITEMS, ANY>(g_raw, static_cast<const T*>(p.gamma), c0, p.cols, full);
   } else {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
@@ -741,82 +1058,157 @@ __global__ void __launch_bounds__(RING_THREADS) bwd_ring_kernel(const __grid_con
 #pragma unroll
   for (int k = 0; k < N; ++k) dg.v[k] = both(0.f);
   float rstd = row < p.rows ? p.rstd[row] : 0.f;
+  settle();  // (behind gamma's loads)
   int parity = 0, slot = 0;
   for (; row < p.rows; row += step, parity ^= 1) {
     send(slot == 0 ? DEPTH - 1 : slot - 1);
     const float rs = rstd;
     if (row + step < p.rows) rstd = p.rstd[row + step];
     copies_wait<DEPTH - 1>();
-    // xh and w = dy gamma; beyond `cols` all are 0 (rstd may be infinite: 0 rstd is not taken there)
-    P xh, w;
-    {
-      Vec<T, VEC> raw[ITEMS];
-      ring.take(slot, 0, raw);
-      xh.unpack(raw);
-      ring.take(slot, 1, raw);
-      w.unpack(raw);
-    }
-    if (full) {
+    if constexpr (AGAIN) {
+      // item by item, both times out of shared memory
+      const auto scaled = [&](int i) {  // xh
+        Pairs<T, VEC, 1> v = ring.item(slot, 0, i);
+        if (full || finite(rs)) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) xh.v[k] = mul2(xh.v[k], both(rs));
+          for (int k = 0; k < VEC / 2; ++k) v.v[k] = mul2(v.v[k], both(rs));
+        } else {
+#pragma unroll
+          for (int f = 0; f < VEC; ++f) {
+            float& h = f % 2 ? v.v[f / 2].y : v.v[f / 2].x;
+            h = (unsigned)(c0 + i * 32 * VEC + f) < (unsigned)p.cols ? h * rs : 0.f;
+          }
+        }
+        return v;
+      };
+      const auto weight = [&](int i) {
+        Vec<T, VEC> raw[1] = {g_raw[i]};
+        Pairs<T, VEC, 1> g;
+        g.unpack(raw);
+        return g;
+      };
+      float2 t = both(0.f);
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const Pairs<T, VEC, 1> xh = scaled(i), d = ring.item(slot, 1, i), g = weight(i);
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) {
+          dg.v[i * VEC / 2 + k] = fma2(d.v[k], xh.v[k], dg.v[i * VEC / 2 + k]);
+          t = fma2(mul2(d.v[k], g.v[k]), xh.v[k], t);
+        }
+      }
+      if (p.out) {
+        float sum = t.x + t.y;
+        uint32_t none = 0;
+        reduce_group<true, false>(sum, none, red[parity], gr, group, warp);
+        const float minus = -sum * inv_n;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          const Pairs<T, VEC, 1> xh = scaled(i), g = weight(i);
+          Pairs<T, VEC, 1> w = ring.item(slot, 1, i);
+#pragma unroll
+          for (int k = 0; k < VEC / 2; ++k) w.v[k] = mul2(fma2(xh.v[k], both(minus), mul2(w.v[k], g.v[k])), both(rs));
+          if (add) {
+            const Pairs<T, VEC, 1> r = ring.item(slot, 2, i);
+#pragma unroll
+            for (int k = 0; k < VEC / 2; ++k) w.v[k] = add2(w.v[k], r.v[k]);
+          }
+          put_row<T, VEC, 1, ANY>(static_cast<T*>(p.out) + row * p.ldo + c0 + i * 32 * VEC, w, c0 + i * 32 * VEC, p.cols, full);
+        }
+      }
     } else {
-#pragma unroll
-      for (int f = 0; f < VEC * ITEMS; ++f) {
-        float& h = f % 2 ? xh.v[f / 2].y : xh.v[f / 2].x;
-        h = c0 + f / VEC * 32 * VEC + f % VEC < p.cols ? h * rs : 0.f;
-      }
-    }
-    float2 t = both(0.f);
-    {
-      P g;
-      g.unpack(g_raw);
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        dg.v[k] = fma2(w.v[k], xh.v[k], dg.v[k]);
-        w.v[k] = mul2(w.v[k], g.v[k]);
-        t = fma2(w.v[k], xh.v[k], t);
-      }
-    }
-    if (p.out) {
-      float sum = t.x + t.y;
-      uint32_t none = 0;
-      reduce_group<true, false>(sum, none, red[parity], gr, group, warp);
-      const float minus = -sum * inv_n;
-#pragma unroll
-      for (int k = 0; k < N; ++k) w.v[k] = mul2(fma2(xh.v[k], both(minus), w.v[k]), both(rs));
-      if (add) {
+      // xh and w = dy gamma; beyond `cols` all are 0 (rstd may be infinite: 0 rstd is not taken there)
+      P xh, w;
+      {
         Vec<T, VEC> raw[ITEMS];
-        ring.take(slot, 2, raw);
-        P r;
-        r.unpack(raw);
-#pragma unroll
-        for (int k = 0; k < N; ++k) w.v[k] = add2(w.v[k], r.v[k]);
+        ring.take(slot, 0, raw);
+        xh.unpack(raw);
+        ring.take(slot, 1, raw);
+        w.unpack(raw);
       }
-      store_row<T, VEC, ITEMS>(static_cast<T*>(p.out) + row * p.ldo + c0, w, c0, p.cols, full);
+      if (full || finite(rs)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) xh.v[k] = mul2(xh.v[k], both(rs));
+      } else {
+#pragma unroll
+        for (int f = 0; f < VEC * ITEMS; ++f) {
+          float& h = f % 2 ? xh.v[f / 2].y : xh.v[f / 2].x;
+          h = (unsigned)(c0 + f / VEC * 32 * VEC + f % VEC) < (unsigned)p.cols ? h * rs : 0.f;
+        }
+      }
+      float2 t = both(0.f);
+      {
+        P g;
+        g.unpack(g_raw);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          dg.v[k] = fma2(w.v[k], xh.v[k], dg.v[k]);
+          w.v[k] = mul2(w.v[k], g.v[k]);
+          t = fma2(w.v[k], xh.v[k], t);
+        }
+      }
+      if (p.out) {
+        float sum = t.x + t.y;
+        uint32_t none = 0;
+        reduce_group<true, false>(sum, none, red[parity], gr, group, warp);
+        const float minus = -sum * inv_n;
+#pragma unroll
+        for (int k = 0; k < N; ++k) w.v[k] = mul2(fma2(xh.v[k], both(minus), w.v[k]), both(rs));
+        if (add) {
+          Vec<T, VEC> raw[ITEMS];
+          ring.take(slot, 2, raw);
+          P r;
+          r.unpack(raw);
+#pragma unroll
+          for (int k = 0; k < N; ++k) w.v[k] = add2(w.v[k], r.v[k]);
+        }
+        put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.out) + row * p.ldo + c0, w, c0, p.cols, full);
+      }
     }
+    settle();
     slot = slot == DEPTH - 1 ? 0 : slot + 1;
   }
   copies_wait<0>();
   if (!p.want_params) return;
-  // All groups' sums side by side in shared memory, four columns at a time, then added over the groups in order.
-  static_assert(VEC % 4 == 0, "four columns at a time");
-  float4* sums = ring_smem4;
-  const int per = gr.warps * 32;  // threads of a group
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < N / 2; ++q) sums[q * blockDim.x + threadIdx.x] = make_float4(dg.v[2 * q].x, dg.v[2 * q].y, dg.v[2 * q + 1].x, dg.v[2 * q + 1].y);
+  // All groups' sums side by side in shared memory, then added over the groups in order.
   __syncthreads();
   float* out = p.partial + blockIdx.x * p.ldp;
-  for (int e = threadIdx.x; e < per * (N / 2); e += blockDim.x) {
-    const int q = e / per, t = e - q * per;
-    const int c = ((t >> 5) * ITEMS * 32 + 4 * q / VEC * 32 + (t & 31)) * VEC + 4 * q % VEC;
-    if (c >= p.cols) continue;
-    float4 a = sums[q * blockDim.x + t];
-    for (int g = 1; g < gr.groups; ++g) {
-      const float4 b = sums[q * blockDim.x + g * per + t];
-      a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+  if constexpr (ANY) {
+    // by columns, which lie elsewhere in every group's threads; a word is left out behind every 32, so that eight columns per
+    // lane do not meet in the same banks
+    float* sums = reinterpret_cast<float*>(ring_smem4);
+    const int pitch = p.cols + p.cols / 32 + 1;
+#pragma unroll
+    for (int f = 0; f < VEC * ITEMS; ++f) {
+      const int c = c0 + f / VEC * 32 * VEC + f % VEC;
+      if ((unsigned)c < (unsigned)p.cols) sums[group * pitch + c + c / 32] = f % 2 ? dg.v[f / 2].y : dg.v[f / 2].x;
     }
-    *reinterpret_cast<float4*>(out + c) = a;
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
+      const float* at = sums + c + c / 32;
+      float a = at[0];
+      for (int g = 1; g < gr.groups; ++g) a += at[g * pitch];
+      out[c] = a;
+    }
+  } else {
+    // four columns at a time
+    static_assert(VEC % 4 == 0, "four columns at a time");
+    float4* sums = ring_smem4;
+    const int per = gr.warps * 32;  // threads of a group
+#pragma unroll
+    for (int q = 0; q < N / 2; ++q) sums[q * blockDim.x + threadIdx.x] = make_float4(dg.v[2 * q].x, dg.v[2 * q].y, dg.v[2 * q + 1].x, dg.v[2 * q + 1].y);
+    __syncthreads();
+    for (int e = threadIdx.x; e < per * (N / 2); e += blockDim.x) {
+      const int q = e / per, t = e - q * per;
+      const int c = ((t >> 5) * ITEMS * 32 + 4 * q / VEC * 32 + (t & 31)) * VEC + 4 * q % VEC;
+      if (c >= p.cols) continue;
+      float4 a = sums[q * blockDim.x + t];
+      for (int g = 1; g < gr.groups; ++g) {
+        const float4 b = sums[q * blockDim.x + g * per + t];
+        a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+      }
+      *reinterpret_cast<float4*>(out + c) = a;
+    }
   }
 }
 
