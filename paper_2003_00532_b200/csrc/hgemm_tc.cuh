@@ -49,14 +49,13 @@
 #include "../../include/hgemm.h"
 #include "hgemm_act.cuh"
 #include "hgemm_ptx.cuh"
+#include "layernorm.cuh"
 
 namespace hgemm {
 
 constexpr int TK = 64;           // k-block: 64 values of 16 bits = one 128-byte swizzled row
 constexpr int TK8 = 128;         // ... of 8 bits
 constexpr int BOX_BYTES = 8192;  // 64 x 64 values
-constexpr int EPI_WARPS = 8;
-constexpr int THREADS = 128 + 32 * EPI_WARPS;
 constexpr int PITCH = 80;  // bytes per patch row in shared memory: 64 + 16, no two of 8 rows on the same banks
 constexpr int MAX_SMEM = 232448;  // 227 KB
 constexpr int MAX_PROBLEMS = 3;
@@ -82,9 +81,14 @@ struct Kind<Eight<T>> {
 // CG: CTAs per tile (1, or a pair); BM: TMEM columns of the tile (rows of the output); NB: blocks of 128 lanes per CTA.
 // With NB = 1 the two accumulators are two tiles', filled and drained in turn; with NB = 2 they are the two lane
 // blocks of one tile, which share each staged Q.
-template <int CG_, int BM_, int NB_, bool GATED_>
+template <int CG_, int BM_, int NB_, bool GATED_, bool EIGHT_>
 struct Cfg {
   static constexpr int CG = CG_, BM = BM_, NB = NB_;
+  // The epilogue is a chain of latencies: for 8-bit operands, whose products are done in half the time, more warps (4096 x 8192 x 512 with
+  // tanh-GELU 59.9 -> 52.5 us, with residual 71.7 -> 60.8; with 16 of them, and 96 registers each, 56.8 and 70.8). Not the gated one, whose
+  // partners would wait for one another more often (4097 x 8192 x 2048 116.3 us, with 12 warps 119.0).
+  static constexpr int EPI_WARPS = EIGHT_ && !GATED_ && BM >= 128 ? 12 : 8;
+  static constexpr int THREADS = 128 + 32 * EPI_WARPS;
   static constexpr bool GATED = GATED_;
   static constexpr int QROWS = BM / CG;  // rows of Q that one CTA stages
   static constexpr int QBOXES = (QROWS + 63) / 64;
@@ -390,25 +394,38 @@ struct Epilogue {
   float col[4], col_up[4];
 };
 
-// The scales of a patch's rows, in the order in which a thread holds them: row[b] of rows 8 b + 2 (lane % 4) and the next.
+// The scales of a patch's rows. Lane l holds that of row l % CH: one load, which is on its way since the patch before; a thread's rows,
+// 8 b + 2 (lane % 4) and the next, come from the lanes that hold them. (With loads of its own in every thread, products value by value and
+// eight epilogue warps, 4096 x 8192 x 512 took 44.5 us without activation, 58.1 with tanh-GELU and 78.6 with residual; now 36.5, 48.4 and 63.)
 template <int CH>
 struct RowScales {
-  float2 row[CH / 8];
+  float mine;
   __device__ __forceinline__ void fetch(const Epilogue<CH>& ep, int m) {
-#pragma unroll
-    for (int b = 0; b < CH / 8; ++b) {
-      const int r = m + 8 * b + 2 * (ep.pt.lane & 3);
-      row[b].x = ep.row_scale && r < ep.pt.rows ? __ldg(ep.row_scale + r) : 1.f;
-      row[b].y = ep.row_scale && r + 1 < ep.pt.rows ? __ldg(ep.row_scale + r + 1) : 1.f;
-    }
+    mine = ep.row_scale ? __ldg(ep.row_scale + min(m + (ep.pt.lane & (CH - 1)), ep.pt.rows - 1)) : 1.f;
   }
-  __device__ __forceinline__ void apply(const float* col, float* v) const {
+  // Those of this thread.
+  struct Own {
+    float2 row[CH / 8];
+  };
+  __device__ __forceinline__ Own own() const {
+    Own o;
+    const int from = 2 * (threadIdx.x & 3);
+#pragma unroll
+    for (int b = 0; b < CH / 8; ++b) o.row[b] = make_float2(__shfl_sync(0xffffffffu, mine, 8 * b + from), __shfl_sync(0xffffffffu, mine, 8 * b + from + 1));
+    return o;
+  }
+  // v row col + bias
+  static __device__ __forceinline__ void apply(const Own& o, const float* col, const float* bias, float* v) {
     constexpr int MB = CH / 8;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const float2 r = row[i / 4 % MB];
-      v[i] = v[i] * (i % 2 ? r.y : r.x) * col[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
-    }
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {  // columns
+        float* x = v + 4 * ((j >> 1) * MB + b) + 2 * (j & 1);
+        const float2 y = lnorm::fma2(lnorm::mul2(make_float2(x[0], x[1]), o.row[b]), lnorm::both(col[j]), lnorm::both(bias ? bias[j] : 0.f));
+        x[0] = y.x;
+        x[1] = y.y;
+      }
   }
 };
 
@@ -416,28 +433,33 @@ struct RowScales {
 template <typename T, int ACT>
 constexpr bool UNSCALED = std::is_same<T, __half>::value && ACT == HGEMM_ACT_NONE;
 
+// next: the row whose residual is fetched in the place of this one's, or -1.
 template <typename K, int CH, int ACT>
-__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, float* v, const typename Patch<CH>::Raw& raw, const RowScales<CH>& rs) {
+__device__ __forceinline__ void emit_plain(const Epilogue<CH>& ep, int m, float* v, typename Patch<CH>::Raw& raw, const RowScales<CH>& rs, int next) {
   using T = typename Kind<K>::Out;
   constexpr int MB = CH / 8;
-  if constexpr (Kind<K>::EIGHT) rs.apply(ep.col, v);
+  if constexpr (Kind<K>::EIGHT) rs.apply(rs.own(), ep.col, ep.bias, v);
+  const auto bias = [&](int i) { return Kind<K>::EIGHT ? 0.f : ep.bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)]; };  // still to be added to v[i]
   if (UNSCALED<K, ACT> && ep.unscale != 1.f) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) v[i] *= ep.unscale;
   }
   uint32_t q[CH / 2], r[CH / 2];
-  if (ep.has_r) ep.pt.take(raw, ep.r.vec, r);
+  if (ep.has_r) {
+    ep.pt.take(raw, ep.r.vec, r);
+    if (next >= 0) ep.pt.fetch(raw, ep.r, next);
+  }
   if (ep.has_z) {
 #pragma unroll
     for (int i = 0; i < CH; i += 2) {
-      const float b = ep.bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+      const float b = bias(i);
       q[i / 2] = pack2<T>(v[i] + b, v[i + 1] + b);
     }
     ep.pt.store(ep.z, m, q);
   }
 #pragma unroll
   for (int i = 0; i < CH; i += 2) {
-    const float b = ep.bias[2 * (i / (4 * MB)) + ((i >> 1) & 1)];
+    const float b = bias(i);
     float x = act_fwd<ACT>(v[i] + b), y = act_fwd<ACT>(v[i + 1] + b);
     if (ep.has_r) {
       const float2 a = unpack2<T>(r[i / 2]);
@@ -453,8 +475,9 @@ template <typename K, int CH, int ACT>
 __device__ __forceinline__ void emit_gated(const Epilogue<CH>& ep, int m, float* g, float* u, const RowScales<CH>& rs) {
   using T = typename Kind<K>::Out;
   if constexpr (Kind<K>::EIGHT) {
-    rs.apply(ep.col, g);
-    rs.apply(ep.col_up, u);
+    const typename RowScales<CH>::Own own = rs.own();
+    rs.apply(own, ep.col, nullptr, g);
+    rs.apply(own, ep.col_up, nullptr, u);
   }
   uint32_t q[CH / 2];
   if (ep.has_z) {
@@ -529,7 +552,7 @@ template <typename T, typename C, int ACT>
 __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr, const Work& w, const Epilogue<C::CH>& ep,
                                               typename Patch<C::CH>::Raw& raw, const EpiWarp& ew, int rows, bool n_in) {
   using namespace dgemm::ptx;
-  constexpr int CG = C::CG, BM = C::BM, CH = C::CH, BLOCKS = C::CG * C::NB, GROUPS = EPI_WARPS / 4;
+  constexpr int CG = C::CG, BM = C::BM, CH = C::CH, BLOCKS = C::CG * C::NB, EPI_WARPS = C::EPI_WARPS, GROUPS = EPI_WARPS / 4;
   constexpr bool GATED = C::GATED, EIGHT = Kind<T>::EIGHT;
   // a part's sums in the workspace: [slot][block][quarter][chunk][CH / 4][lane] of float4
   constexpr long long WS_SLOT = (long long)BLOCKS * BM * 32;  // float4 per slot
@@ -547,19 +570,31 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
     released = true;
   };
   if (w.slot < 0) {
-    if (!GATED) {
+    if constexpr (EIGHT && !GATED) {
+      // the next chunk's scales and residual are on their way while this one is computed
+      RowScales<CH> rs;
+      if (ew.group * CH < rows) rs.fetch(ep, ew.group * CH);
       for (int c = ew.group; c * CH < rows; c += GROUPS) {
         float v[CH];
-        RowScales<CH> rs;
-        if (EIGHT) rs.fetch(ep, c * CH);
+        tmem_load<CH>(ew.acc + c * CH, v);
+        ptx5::tmem_ld_wait<CH>(v);
+        const RowScales<CH> rows_now = rs;
+        const int next = (c + GROUPS) * CH;
+        if (next < rows) rs.fetch(ep, next);
+        else release();
+        if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw, rows_now, next < rows ? next : -1);
+      }
+    } else if constexpr (!GATED) {
+      for (int c = ew.group; c * CH < rows; c += GROUPS) {
+        float v[CH];
         tmem_load<CH>(ew.acc + c * CH, v);
         ptx5::tmem_ld_wait<CH>(v);
         if ((c + GROUPS) * CH >= rows) release();
         if (n_in) {
-          const typename Patch<CH>::Raw now = raw;
+          typename Patch<CH>::Raw now = raw;
           // the next chunk's residual is on its way while this one is computed
           if (ep.has_r && (c + GROUPS) * CH < rows) ep.pt.fetch(raw, ep.r, (c + GROUPS) * CH);
-          emit_plain<T, CH, ACT>(ep, c * CH, v, now, rs);
+          emit_plain<T, CH, ACT>(ep, c * CH, v, now, RowScales<CH>{1.f}, -1);
         }
       }
     } else {
@@ -621,7 +656,7 @@ __device__ __forceinline__ void epilogue_unit(const Params& p, const Problem& pr
           RowScales<CH> rs;
           if (EIGHT) rs.fetch(ep, c * CH);
           add_parts<CH>(first + c * WS_CHUNK, next + c * WS_CHUNK, w.parts - 1, 2 * WS_SLOT, v);
-          if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw, rs);
+          if (n_in) emit_plain<T, CH, ACT>(ep, c * CH, v, raw, rs, -1);
         }
       } else {
         const float4* first = ws_cta + w.first_slot * WS_SLOT + ((ew.quad & 1) * (BM / CH)) * WS_CHUNK;
@@ -650,9 +685,9 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major) {
 }
 
 template <typename T, int CG, int BM, int NB, bool GATED, int ACT>
-__global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(Cfg<CG, BM, NB, GATED, Kind<T>::EIGHT>::THREADS, 1) hgemm_tc_kernel(const __grid_constant__ Params p) {
   using namespace dgemm::ptx;
-  using C = Cfg<CG, BM, NB, GATED>;
+  using C = Cfg<CG, BM, NB, GATED, Kind<T>::EIGHT>;
   using Out = typename Kind<T>::Out;
   constexpr bool EIGHT = Kind<T>::EIGHT;
   constexpr int STAGES = C::STAGES, CH = C::CH;
@@ -682,7 +717,7 @@ __global__ void __launch_bounds__(THREADS, 1) hgemm_tc_kernel(const __grid_const
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full + 8 * a, 1);
-      mbar_init(acc_empty + 8 * a, EPI_WARPS * CG);
+      mbar_init(acc_empty + 8 * a, C::EPI_WARPS * CG);
     }
     mbar_init(drain_bar, 1);
     *abort_flag = 0;

@@ -127,9 +127,10 @@ bool run_fwd_vec(int sms, const Params& p, cudaStream_t stream) {
     const bool many = p.rows > 2 * (int64_t)sms && p.rows * cols >= (ANY ? 3ll << 20 : 1ll << 20);
     // Beyond 8192 columns, and from 4096 on, 32 values per thread (2000 x 16384 Y with residual 50.0 -> 46.6 us, to 8 bits 44.8 -> 38.0; 6000 x
     // 5120 to 8 bits 36.2, by 16 values about 50; 8192 x 4097 Y 37.9 -> 30.3); aligned and with residual Y is better off with 16
-    // (8192 x 4600 49.4, about 53), and 8 bits without residual in registers (8192 x 5000 31.2, 39.6).
+    // (8192 x 4600 49.4, about 53), 8 bits too where 16 leave no warp of a block idle (4097 x 8192 40.0, 41.7), and 8 bits without
+    // residual in registers (8192 x 5000 31.2, 39.6).
     if (many && cols > RING_COLS && cols <= 2 * RING_COLS) return launch_fwd_again<T, OUT, RING_THREADS, ANY>(sms, p, stream);
-    if (many && cols > RING_COLS / 2 && cols <= RING_COLS && (ANY || (p.R != nullptr) == (OUT == OUT_E4M3)))
+    if (many && cols > RING_COLS / 2 && cols <= RING_COLS && (ANY || (p.R ? OUT == OUT_E4M3 && cols <= RING_COLS - 512 : OUT == OUT_Y)))
       return p.R ? launch_fwd_again<T, OUT, RING_THREADS, ANY>(sms, p, stream) : launch_fwd_again<T, OUT, SMALL_RING_THREADS, ANY>(sms, p, stream);
     // Blocks of 256 threads (8192 x 4096 without a residual: Y 29.1 -> 24.2 us, to 8 bits 27.3 -> 24.1; 1500 x 4000 with one 10.9 -> 9.7 and
     // 10.5 -> 9.2); but with a residual beyond L2 so many streams of reads and writes slow each other down (8192 x 4096: 47.1, 16384 x 2048
