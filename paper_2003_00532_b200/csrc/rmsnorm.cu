@@ -35,7 +35,7 @@ Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms, bool rows_only) {
   if (threads > fwd_threads(items * vec)) return Shape{0, 1024, true};
   return Shape{items, threads, false};
 }
-// Backward, rows that are not 16-byte aligned or too long for the ring: a warp for rows of up to 16 values per lane; a block with 8 values
+// Backward, by single values or rows too long for the ring: a warp for rows of up to 16 values per lane; a block with 8 values
 // per thread beyond (4097 x 1537, binary32: 21 us, with 16 values 24), 16 up to 8192 columns, 32 (`WIDE`) up to 16384.
 Shape bwd_shape(int64_t cols, int vec) {
   const int64_t nv = (cols + vec - 1) / vec;

@@ -694,13 +694,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
   dgemm::ptx::grid_dependency_wait();
   using P = Pairs<T, VEC, ITEMS>;
   constexpr int N = P::N;
-  constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
+  constexpr bool EIGHT = OUT == OUT_E4M3;
   const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / gr.warps, warp = (threadIdx.x >> 5) - group * gr.warps;
   const long long step = (long long)gridDim.x * gr.groups;
   long long row = (long long)blockIdx.x * gr.groups + group;
   const int c0 = (warp * ITEMS * 32 + lane) * VEC - shift_of<VEC, ANY>(p, row);
   const bool full = c0 >= 0 && c0 + (ITEMS - 1) * 32 * VEC + VEC <= p.cols;
-  const bool add = NORM && p.R;
+  const bool add = p.R != nullptr;
   const Ring<T, VEC, ITEMS, DEPTH, ANY> ring(ring_smem, add ? 2 : 1, c0, p.cols);
   const T* x_at = static_cast<const T*>(p.X) + row * p.ldx + c0;
   const T* r_at = static_cast<const T*>(p.R) + row * p.ldr + c0;
@@ -735,15 +735,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     send(d);
   }
   Vec<T, VEC> g_raw[ITEMS];
-  if (NORM) {
-    if (p.gamma) {
-      take_gamma<T, VEC, ITEMS, ANY>(g_raw, static_cast<const T*>(p.gamma), c0, p.cols, full);
-    } else {
+  if (p.gamma) {
+    take_gamma<T, VEC, ITEMS, ANY>(g_raw, static_cast<const T*>(p.gamma), c0, p.cols, full);
+  } else {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i)
+    for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) g_raw[i].set(j, rnd<T>(1.f));
-    }
+      for (int j = 0; j < VEC; ++j) g_raw[i].set(j, rnd<T>(1.f));
   }
   settle();  // (behind gamma's loads)
   const float inv_n = 1.f / (float)p.cols;
@@ -772,42 +770,37 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     float f = 1.f;  // what is left to multiply by
     uint32_t top = 0;
     float none = 0.f;
-    if (NORM) {
-      if (p.S) put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.S) + row * p.lds + c0, x, c0, p.cols, full);
-      float sum = squares(x.v), rstd;
-      const auto weigh = [&]() {
-        P g;
-        g.unpack(g_raw);
+    if (p.S) put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.S) + row * p.lds + c0, x, c0, p.cols, full);
+    float sum = squares(x.v), rstd;
+    const auto weigh = [&]() {
+      P g;
+      g.unpack(g_raw);
 #pragma unroll
-        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], g.v[k]);
-        if (EIGHT) top = magnitude_max(x.v);
-      };
+      for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], g.v[k]);
+      if (EIGHT) top = magnitude_max(x.v);
+    };
+    weigh();
+    reduce_group<true, EIGHT>(sum, top, next(), gr, group, warp);
+    f = rstd = lnorm::inv_sqrt(sum * inv_n + p.eps);
+    // (the same for all threads of a row)
+    if (!(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u)) {
+      take();
+      uint32_t most = magnitude_max(x.v);
+      reduce_group<false, true>(none, most, next(), gr, group, warp);
+      const float unit = row_unit(most, p.eps);
+#pragma unroll
+      for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(unit));
+      sum = squares(x.v);
+      reduce_group<true, false>(sum, top, next(), gr, group, warp);
+      f = lnorm::inv_sqrt(sum * inv_n + p.eps * unit * unit);
+#pragma unroll
+      for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
+      rstd = unit * f;
+      f = 1.f;
       weigh();
-      reduce_group<true, EIGHT>(sum, top, next(), gr, group, warp);
-      f = rstd = lnorm::inv_sqrt(sum * inv_n + p.eps);
-      // (the same for all threads of a row)
-      if (!(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u)) {
-        take();
-        uint32_t most = magnitude_max(x.v);
-        reduce_group<false, true>(none, most, next(), gr, group, warp);
-        const float unit = row_unit(most, p.eps);
-#pragma unroll
-        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(unit));
-        sum = squares(x.v);
-        reduce_group<true, false>(sum, top, next(), gr, group, warp);
-        f = lnorm::inv_sqrt(sum * inv_n + p.eps * unit * unit);
-#pragma unroll
-        for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
-        rstd = unit * f;
-        f = 1.f;
-        weigh();
-        if (EIGHT) reduce_group<false, true>(none, top, next(), gr, group, warp);
-      }
-      if (lane == 0 && warp == 0 && p.rstd) p.rstd[row] = rstd;
-    } else {
-      top = magnitude_max(x.v);
-      reduce_group<false, true>(none, top, next(), gr, group, warp);
+      if (EIGHT) reduce_group<false, true>(none, top, next(), gr, group, warp);
     }
+    if (lane == 0 && warp == 0 && p.rstd) p.rstd[row] = rstd;
     if constexpr (EIGHT) {
       const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && warp == 0) p.scale[row] = most / E4M3_TOP;
