@@ -136,6 +136,19 @@ constexpr float LEAST_MAX = 0x1p-100f;     // rows that are smaller are scaled a
 // Sums of squares from here on (or below, with an eps that is not above) are taken again from scaled values.
 constexpr float SUM_TOP = 0x1p+120f, SUM_LOW = 0x1p-90f;
 
+// For 8 bits y / scale is taken as (s gamma) (rstd 448 / max|y|). With an eps that lets rstd become large beside a row of zeros or of very small
+// values that factor leaves binary32's range (max|y| is not taken below 2^-100: from rstd = 2^19 on), and s gamma loses the bits below
+// 2^-149. Up to rstd = RSTD_TOP, or from max|s gamma| = WEIGHED_LOW on, the factor is at most 2^119 and what s gamma has lost stays below 2^-30
+// in q; beyond them, as where s gamma overflows, the row is taken again with rstd before gamma.
+constexpr float RSTD_TOP = 0x1p+10f, WEIGHED_LOW = 0x1p-110f;
+
+// Whether a row's values have to be scaled before they are squared or multiplied by gamma; `top`: for 8 bits, the magnitude of max|s gamma|.
+template <bool EIGHT>
+__device__ __forceinline__ bool out_of_range(float sum, float eps, float rstd, uint32_t top) {
+  return !(sum < SUM_TOP) || (sum < SUM_LOW && eps < SUM_LOW) ||
+         (EIGHT && (top >= 0x7f800000u || (rstd > RSTD_TOP && top < __float_as_uint(WEIGHED_LOW))));
+}
+
 // max(x, least) that keeps a NaN.
 __device__ __forceinline__ float at_least(float x, float least) { return x < least ? least : x; }
 
@@ -306,7 +319,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
       reduce<WARP_ROW, true, EIGHT>(sum, top, next());
       f = lnorm::inv_sqrt(sum * inv_n + p.eps);
       // (the same for all threads of a row)
-      if (!(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u)) {
+      if (out_of_range<EIGHT>(sum, p.eps, f, top)) {
         uint32_t most = magnitude_max(x.v);
         float none = 0.f;
         reduce<WARP_ROW, false, true>(none, most, next());
@@ -783,7 +796,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     reduce_group<true, EIGHT>(sum, top, next(), gr, group, warp);
     f = rstd = lnorm::inv_sqrt(sum * inv_n + p.eps);
     // (the same for all threads of a row)
-    if (!(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u)) {
+    if (out_of_range<EIGHT>(sum, p.eps, f, top)) {
       take();
       uint32_t most = magnitude_max(x.v);
       reduce_group<false, true>(none, most, next(), gr, group, warp);
@@ -919,7 +932,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     reduce_group<true, EIGHT>(sum, top, next(), gr, group, warp);
     float f = rstd = lnorm::inv_sqrt(sum * inv_n + p.eps), unit = 1.f, g = 1.f;  // s unit g gamma f: y
     // (the same for all threads of a row)
-    const bool rescale = !(sum < SUM_TOP) || (sum < SUM_LOW && p.eps < SUM_LOW) || (EIGHT && top >= 0x7f800000u);
+    const bool rescale = out_of_range<EIGHT>(sum, p.eps, rstd, top);
     if (rescale) {
       most = 0.f;
 #pragma unroll 1
