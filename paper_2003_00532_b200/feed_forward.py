@@ -25,16 +25,27 @@ import paper_2003_00532_b200 as dg
 
 
 class _Buffers:
-    """Scratch tensors by name, each grown to the most tokens asked for."""
+    """Scratch tensors by name, each grown to the most tokens asked for. One that a captured pass was given stays for the object's life,
+    also when a larger one takes its place: the graph writes to it in every replay.
+
+    The next pass writes over them: an object's passes, replays among them, follow one another on one stream or are made to wait for each
+    other, and belong to one thread at a time."""
 
     def __init__(self):
-        self._buffers = {}
+        self._buffers, self._captured, self._capturing = {}, [], False
+
+    def _begin(self):
+        """Called once at the beginning of a pass (asked of CUDA for every buffer, a token's pass took 1 to 2 us longer)."""
+        self._capturing = torch.cuda.is_current_stream_capturing()
 
     def _buffer(self, name, tokens, *width, dtype=None):
         """``tokens`` rows of the buffer ``name``, which grows to the most tokens asked for and never shrinks."""
-        if name not in self._buffers or self._buffers[name].shape[0] < tokens:
-            self._buffers[name] = torch.empty(tokens, *width, dtype=dtype or self.dtype, device="cuda")
-        return self._buffers[name][:tokens]
+        buffer = self._buffers.get(name)
+        if buffer is None or buffer.shape[0] < tokens:
+            buffer = self._buffers[name] = torch.empty(tokens, *width, dtype=dtype or self.dtype, device="cuda")
+        if self._capturing and not any(held is buffer for held in self._captured):
+            self._captured.append(buffer)
+        return buffer[:tokens]
 
 
 class FeedForward(_Buffers):
@@ -71,6 +82,7 @@ class FeedForward(_Buffers):
         not keep drops nothing and leaves alone what an earlier one kept. ``delta`` (root-mean-square norm only): added to ``x`` first."""
         if delta is not None and self.norm != "rms":
             raise ValueError("delta: needs norm='rms'")
+        self._begin()
         t, which = x.shape[0], "kept " if keep else ""
         n, h, y = self._buffer(which + "n", t, self.model), self._buffer(which + "h", t, self.hidden), torch.empty_like(x)
         mean, rstd, gate, up = None, None, None, None
@@ -103,6 +115,7 @@ class FeedForward(_Buffers):
         too) and every parameter's name."""
         if self._kept is None:
             raise RuntimeError("backward: no forward pass has been kept (forward(x, keep=True) comes first)")
+        self._begin()
         s, n, mean, rstd, gate, up, h, p, use = self._kept
         out = {name: torch.empty_like(getattr(self, name)) for name in ("wg", "wu", "wd")}
         out.update({name: torch.empty(self.model, dtype=torch.float32, device="cuda") for name in self.parameters() if name not in out})
@@ -157,6 +170,7 @@ class EightBitFeedForward(_Buffers):
 
     def forward(self, x, delta=None):
         """As :meth:`FeedForward.forward` with ``keep=False``."""
+        self._begin()
         t, e4m3, f32 = x.shape[0], torch.float8_e4m3fn, torch.float32
         n, sn = self._buffer("n", t, self.model, dtype=e4m3), self._buffer("sn", t, dtype=f32)
         h, y = self._buffer("h", t, self.hidden), torch.empty_like(x)
