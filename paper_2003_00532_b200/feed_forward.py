@@ -48,6 +48,10 @@ class _Buffers:
         return buffer[:tokens]
 
 
+#: Where the masks of captured passes begin among the uses of a seed; those of other passes begin at 0.
+CAPTURED_USES = 1 << 62
+
+
 class FeedForward(_Buffers):
     """Weights of one sublayer (``float16`` or ``bfloat16``, stored output x input) and its two passes. ``norm``: ``"layer"`` or
     ``"rms"``; ``dropout``: the probability with which a kept (training) pass drops a value of the sublayer's output."""
@@ -66,6 +70,7 @@ class FeedForward(_Buffers):
 
         self.model, self.hidden, self.dtype, self.act = model, hidden, dtype, act
         self.norm, self.dropout, self.seed, self.uses = norm, dropout, seed, 0
+        self._replays = torch.zeros(1, dtype=torch.int64, device="cuda")   # passes of captured graphs, counted when they run
         self.gamma = torch.ones(model, dtype=dtype, device="cuda")
         self.beta = torch.zeros(model, dtype=dtype, device="cuda") if norm == "layer" else None
         self.wg, self.wu, self.wd = weight(hidden, model), weight(hidden, model), weight(model, hidden)
@@ -78,8 +83,9 @@ class FeedForward(_Buffers):
 
     def forward(self, x, keep: bool = True, delta=None):
         """The sublayer's output for ``x`` (tokens x model), a new tensor. ``keep``: also keep what :meth:`backward` needs
-        (``x`` itself by reference: it has to stay as it is until then) and drop values, with another mask every time; a call that does
-        not keep drops nothing and leaves alone what an earlier one kept. ``delta`` (root-mean-square norm only): added to ``x`` first."""
+        (``x`` itself by reference: it has to stay as it is until then) and drop values, with another mask every time, also in every
+        replay of a captured call (whose gradients are taken before the next replay); a call that does not keep drops nothing and leaves
+        alone what an earlier one kept. ``delta`` (root-mean-square norm only): added to ``x`` first."""
         if delta is not None and self.norm != "rms":
             raise ValueError("delta: needs norm='rms'")
         self._begin()
@@ -98,16 +104,19 @@ class FeedForward(_Buffers):
                 s = self._buffer(which + "s", t, self.model)
             dg.rmsnorm_fwd(x, self.gamma, n, residual=delta, sum=s if delta is not None else None, rstd=rstd)
         dg.hgemm_gated(n, self.wg, self.wu, h, act=self.act, gate=gate, up=up, transw=True)
-        p, use = self.dropout if keep else 0.0, self.uses
+        p, use, step = self.dropout if keep else 0.0, self.uses, None
         if p > 0.0:
-            self.uses += 1
+            if self._capturing:
+                use, step = CAPTURED_USES, self._replays.add_(1)
+            else:
+                self.uses += 1
             d = self._buffer("d", t, self.model)
             dg.hgemm_epilogue(h, self.wd, d, bias=self.bd, transb=True)
-            dg.dropout_fwd(d, y, p, self.seed, use, residual=s)
+            dg.dropout_fwd(d, y, p, self.seed, use, residual=s, step=step)
         else:
             dg.hgemm_epilogue(h, self.wd, y, bias=self.bd, residual=s, transb=True)
         if keep:
-            self._kept = (s, n, mean, rstd, gate, up, h, p, use)
+            self._kept = (s, n, mean, rstd, gate, up, h, p, use, step)
         return y
 
     def backward(self, dy):
@@ -116,7 +125,7 @@ class FeedForward(_Buffers):
         if self._kept is None:
             raise RuntimeError("backward: no forward pass has been kept (forward(x, keep=True) comes first)")
         self._begin()
-        s, n, mean, rstd, gate, up, h, p, use = self._kept
+        s, n, mean, rstd, gate, up, h, p, use, step = self._kept
         out = {name: torch.empty_like(getattr(self, name)) for name in ("wg", "wu", "wd")}
         out.update({name: torch.empty(self.model, dtype=torch.float32, device="cuda") for name in self.parameters() if name not in out})
         t = s.shape[0]
@@ -124,7 +133,7 @@ class FeedForward(_Buffers):
         dd = dy
         if p > 0.0:
             dd = self._buffer("d", t, self.model)
-            dg.dropout_bwd(dy, dd, p, self.seed, use)
+            dg.dropout_bwd(dy, dd, p, self.seed, use, step=step)
         dg.hgemm_epilogue_bwd(h, self.wd, dd, dA=dh, dB=out["wd"], dbias=out["bd"], transb=True)
         dg.hgemm_gated_bwd(n, self.wg, self.wu, gate, up, dh, act=self.act, dX=dn, dWg=out["wg"], dWu=out["wu"], transw=True)
         if self.norm == "layer":

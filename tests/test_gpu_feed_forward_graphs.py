@@ -1,8 +1,10 @@
 """Passes of the feed-forward sublayer that are captured into CUDA graphs, with larger passes between capture and replay. Needs a B200. Every
-comparison is between equal bits."""
+comparison is between equal bits, but for the sums in ``test_every_replay_drops_others``: 60 binary32 additions of exact values, each off by
+2^-24 of a partial sum."""
 import pytest
 import torch
 
+import rows_reference as rr
 from paper_2003_00532_b200.feed_forward import FeedForward
 
 pytestmark = pytest.mark.gpu
@@ -107,3 +109,41 @@ def test_a_forward_pass_and_its_gradients_in_two_graphs():
     for k in want:
         assert torch.equal(got[k], want[k]), k
     assert _intact(others)
+
+
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+def test_every_replay_drops_others(norm):
+    """Two captured training passes with dropout, and others between their replays: a mask of its own each time, the same in its gradients."""
+    layer = FeedForward(MODEL, HIDDEN, seed=1, norm=norm, dropout=0.5)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.randn(60, MODEL, device="cuda", generator=g).bfloat16() for _ in range(2))
+
+    def both():
+        y = layer.forward(x)
+        return y, layer.backward(dy)["bd"]
+
+    seen = []
+
+    def check(y, bd):
+        torch.cuda.synchronize()
+        dropped = y == x     # (what is kept is nowhere so small that it is lost in the addition, or few times)
+        for mask in seen:
+            assert 0.4 < float((dropped == mask).float().mean()) < 0.6
+        seen.append(dropped)
+        assert 0.45 < float(dropped.float().mean()) < 0.55
+        return dropped
+
+    def exactly(y, bd, use):
+        keep = rr.words(60, MODEL, layer.seed, use, "cuda") >= 2 ** 31
+        dropped = check(y, bd)
+        assert bool(dropped[~keep].all()) and float(dropped[keep].float().mean()) < 0.05
+        parts = dy.double() * 2 * keep
+        assert bool(((bd.double() - parts.sum(0)).abs() <= 60 * 2.0 ** -24 * parts.abs().sum(0)).all())
+
+    exactly(*both(), 0)
+    graphs = [_capture(both) for _ in range(2)]
+    for k, which in enumerate((0, 1, 1, 0)):
+        graph, result = graphs[which]
+        graph.replay()
+        exactly(*result, (1 << 62) + k + 1)
+        exactly(*both(), k + 1)
