@@ -32,9 +32,10 @@ extern "C" {
  *   rstd   one binary32 value per row (what the backward pass needs), or NULL
  *   eps    finite, >= 0
  *
- * y and rstd are computed from the sum before it is rounded. Rows whose squares leave binary32's range
- * (values from about 2^54 up, or all below 2^-50 with an eps as small) are scaled by a power of two
- * first. rows == 0 or cols == 0: DGEMM_OK, nothing is written. Y must not overlap an input or another output.
+ * y and rstd are computed from the sum before it is rounded. Rows whose squares or whose products with gamma could leave
+ * binary32's range (a root of the sum of squares from 2^27 up, or an rstd above 2^20) are scaled by a power of two and multiplied
+ * by rstd before gamma. |gamma| up to 2^100 (beyond that s gamma may overflow in other rows); a y that is not 0 may be off by
+ * 2^-130 beside its rounding. rows == 0 or cols == 0: DGEMM_OK, nothing is written. Y must not overlap an input or another output.
  */
 DGEMM_API int rmsnorm_fwd(int type, int64_t rows, int64_t cols, const void *X, int64_t ldx, const void *R, int64_t ldr,
                           const void *gamma, float eps, void *S, int64_t lds, void *Y, int64_t ldy, float *rstd,

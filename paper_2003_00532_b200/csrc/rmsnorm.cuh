@@ -136,6 +136,12 @@ constexpr float LEAST_MAX = 0x1p-100f;     // rows that are smaller are scaled a
 // Sums of squares from here on (or below, with an eps that is not above) are taken again from scaled values.
 constexpr float SUM_TOP = 0x1p+120f, SUM_LOW = 0x1p-90f;
 
+// y is taken as (s gamma) rstd: the product with gamma then lies in front of the row's reduction (behind it: 8192 x 4089 bfloat16 60.3 us instead
+// of 47.4, 6000 x 5120 46.4 instead of 41.7). So that it stays in binary32's range, rows whose sum of squares is Y_SUM_TOP or more (below it
+// |s| < 2^27: enough for weights up to 2^100) or whose rstd is above Y_RSTD_TOP (below it what s gamma loses under 2^-149 is below 2^-130 in y) are
+// taken again with rstd first. A choice by each thread's own weights cost registers in every row: 8192 x 4089 58.7 us, 16384 x 500 16.3 instead of 14.4.
+constexpr float Y_SUM_TOP = 0x1p+54f, Y_RSTD_TOP = 0x1p+20f;
+
 // For 8 bits y / scale is taken as (s gamma) (rstd 448 / max|y|). With an eps that lets rstd become large beside a row of zeros or of very small
 // values that factor leaves binary32's range (max|y| is not taken below 2^-100: from rstd = 2^19 on), and s gamma loses the bits below
 // 2^-149. Up to rstd = RSTD_TOP, or from max|s gamma| = WEIGHED_LOW on, the factor is at most 2^119 and what s gamma has lost stays below 2^-30
@@ -145,6 +151,7 @@ constexpr float RSTD_TOP = 0x1p+10f, WEIGHED_LOW = 0x1p-110f;
 // Whether a row's values have to be scaled before they are squared or multiplied by gamma; `top`: for 8 bits, the magnitude of max|s gamma|.
 template <bool EIGHT>
 __device__ __forceinline__ bool out_of_range(float sum, float eps, float rstd, uint32_t top) {
+  if (!EIGHT) return !(sum < Y_SUM_TOP) || rstd > Y_RSTD_TOP;
   return !(sum < SUM_TOP) || (sum < SUM_LOW && eps < SUM_LOW) ||
          (EIGHT && (top >= 0x7f800000u || (rstd > RSTD_TOP && top < __float_as_uint(WEIGHED_LOW))));
 }
@@ -256,6 +263,9 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
   using P = Pairs<T, VEC, ITEMS>;
   constexpr int N = P::N;
   constexpr bool NORM = OUT != OUT_ROWS, EIGHT = OUT != OUT_Y;
+  // y with 32 values per thread: gamma behind rstd, because s gamma beside s does not fit in the registers (2000 x 16384 binary32 99.5 us, the
+  // other way round 120)
+  constexpr bool BEHIND = !EIGHT && VEC * ITEMS > 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long step = WARP_ROW ? (long long)gridDim.x * 4 : (long long)gridDim.x;
   long long row = WARP_ROW ? (long long)blockIdx.x * 4 + warp : (long long)blockIdx.x;
@@ -312,7 +322,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
       P z;
       const auto weigh = [&]() {
 #pragma unroll
-        for (int k = 0; k < N; ++k) z.v[k] = mul2(x.v[k], g.v[k]);
+        for (int k = 0; k < N; ++k) z.v[k] = BEHIND ? x.v[k] : mul2(x.v[k], g.v[k]);
         if (EIGHT) top = magnitude_max(z.v);
       };
       weigh();
@@ -352,7 +362,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
       store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * top_over(most), c0, p.cols, full);
     } else {
 #pragma unroll
-      for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
+      for (int k = 0; k < N; ++k) x.v[k] = BEHIND ? mul2(mul2(x.v[k], both(f)), g.v[k]) : mul2(x.v[k], both(f));
       put_row<T, VEC, ITEMS, ANY>(static_cast<T*>(p.out) + at * p.ldo + c0, x, c0, p.cols, full);
     }
   }
