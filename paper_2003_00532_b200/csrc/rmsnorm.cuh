@@ -181,14 +181,6 @@ __device__ __forceinline__ uint32_t magnitude_max(const float2 (&v)[N]) {
   for (int k = 0; k < N; ++k) m = max_abs(m, v[k].x, v[k].y);
   return __float_as_uint(m);
 }
-// 448 / x: the approximate reciprocal and one correction of the quotient. 0, infinities and NaN give what the division gives.
-__device__ __forceinline__ float top_over(float x) {
-  float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-  const float q = E4M3_TOP * r;
-  const float c = fmaf(r, fmaf(-q, x, E4M3_TOP), q);
-  return x < __uint_as_float(0x7f800000u) ? c : q;
-}
 template <int N>
 __device__ __forceinline__ float squares(const float2 (&v)[N]) {
   float2 s = both(0.f);
@@ -359,7 +351,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
     if constexpr (EIGHT) {
       const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && (WARP_ROW || warp == 0)) p.scale[at] = most / E4M3_TOP;
-      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * top_over(most), c0, p.cols, full);
+      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * (E4M3_TOP / most), c0, p.cols, full);
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = BEHIND ? mul2(mul2(x.v[k], both(f)), g.v[k]) : mul2(x.v[k], both(f));
@@ -434,7 +426,7 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
     __syncthreads();
     const float most = at_least(__uint_as_float(__reduce_max_sync(0xffffffffu, red_top[lane])), LEAST_MAX);
     if (threadIdx.x == 0) p.scale[row] = most / E4M3_TOP;
-    f = top_over(most);
+    f = E4M3_TOP / most;
   }
   for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
     float v[VEC];
@@ -827,7 +819,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     if constexpr (EIGHT) {
       const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && warp == 0) p.scale[row] = most / E4M3_TOP;
-      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + row * p.ldo + c0, x, f * top_over(most), c0, p.cols, full);
+      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + row * p.ldo + c0, x, f * (E4M3_TOP / most), c0, p.cols, full);
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
@@ -982,7 +974,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     if (EIGHT) {
       const float largest = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && warp == 0) p.scale[row] = largest / E4M3_TOP;
-      f *= top_over(largest);
+      f *= E4M3_TOP / largest;
     }
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
