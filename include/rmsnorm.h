@@ -54,7 +54,9 @@ DGEMM_API int rmsnorm_fwd_e4m3(int type, int64_t rows, int64_t cols, const void 
                                const void *gamma, float eps, void *S, int64_t lds, void *Q, int64_t ldq, float *scale,
                                float *rstd, void *stream);
 
-/* Rows brought to 8 bits as they are: y = x in the formulas of rmsnorm_fwd_e4m3. */
+/* Rows brought to 8 bits as they are: y = x in the formulas of rmsnorm_fwd_e4m3. q is the value nearest to 448 x / max |x|, exactly
+ * for 16-bit types; in binary32 (and under the norm, whose y is known to binary32's precision) values next to the middle between two
+ * e4m3 values may fall to either. */
 DGEMM_API int quantize_rows_e4m3(int type, int64_t rows, int64_t cols, const void *X, int64_t ldx, void *Q, int64_t ldq,
                                  float *scale, void *stream);
 

@@ -212,12 +212,25 @@ __device__ __forceinline__ float row_unit(uint32_t top, float eps) {
   return __uint_as_float((uint32_t)(127 - k) << 23);
 }
 
-// Item i times f in 8 bits, at `at` + its columns.
-template <typename T, int VEC, int ITEMS>
-__device__ __forceinline__ void store_e4m3(uint8_t* at, const Pairs<T, VEC, ITEMS>& v, float f, int c0, int cols, bool full) {
+// By what rows are multiplied that are brought to 8 bits as they are: 448 / most in two parts. f is a quotient that is too small by 2^-22 to 2^-20 of
+// itself (an approximate division is within 2^-22; scaled by 16, because it gives 0 for divisors above 2^126), rest is what its remainder
+// stands for, known to 2^-40 of f and not negative, so that a zero keeps its sign. x f + x rest is rounded once: a quotient
+// of 16-bit values that lies half-way between two e4m3 values is met exactly (with one rounded factor 2861 of 2088 x 8192 bfloat16 values went
+// to the odd neighbour).
+struct Factor {
+  float f, rest;
+};
+__device__ __forceinline__ Factor top_over(float most) {
+  const float f = __fdividef(E4M3_TOP / 16, most / 16) * (1.f - 0x1p-21f);
+  return Factor{f, f > 0.f ? fmaf(-f, most, E4M3_TOP) * (1.f / E4M3_TOP) * f : 0.f};
+}
+
+// Item i times f (ROWS: times f + rest) in 8 bits, at `at` + its columns.
+template <bool ROWS, typename T, int VEC, int ITEMS>
+__device__ __forceinline__ void store_e4m3(uint8_t* at, const Pairs<T, VEC, ITEMS>& v, float f, float rest, int c0, int cols, bool full) {
   Pairs<T, VEC, ITEMS> w;
 #pragma unroll
-  for (int k = 0; k < Pairs<T, VEC, ITEMS>::N; ++k) w.v[k] = mul2(v.v[k], both(f));
+  for (int k = 0; k < Pairs<T, VEC, ITEMS>::N; ++k) w.v[k] = ROWS ? fma2(v.v[k], both(f), mul2(v.v[k], both(rest))) : mul2(v.v[k], both(f));
   const auto value = [&](int j) { return j % 2 ? w.v[j / 2].y : w.v[j / 2].x; };
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
@@ -351,7 +364,8 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : fwd_threads(VEC* ITEMS)) fwd_
     if constexpr (EIGHT) {
       const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && (WARP_ROW || warp == 0)) p.scale[at] = most / E4M3_TOP;
-      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, f * (E4M3_TOP / most), c0, p.cols, full);
+      const Factor q = NORM ? Factor{f * (E4M3_TOP / most), 0.f} : top_over(most);
+      store_e4m3<!NORM>(static_cast<uint8_t*>(p.out) + at * p.ldo + c0, x, q.f, q.rest, c0, p.cols, full);
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = BEHIND ? mul2(mul2(x.v[k], both(f)), g.v[k]) : mul2(x.v[k], both(f));
@@ -409,7 +423,7 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
     const float y = NORM ? v[j] * b * a : v[j];
     return G ? y * cvt(g.get(j)) : y;
   };
-  float f = 1.f;
+  Factor f{1.f, 0.f};
   if (EIGHT) {
     uint32_t top = 0;
     for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
@@ -426,7 +440,7 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
     __syncthreads();
     const float most = at_least(__uint_as_float(__reduce_max_sync(0xffffffffu, red_top[lane])), LEAST_MAX);
     if (threadIdx.x == 0) p.scale[row] = most / E4M3_TOP;
-    f = E4M3_TOP / most;
+    f = NORM ? Factor{E4M3_TOP / most, 0.f} : top_over(most);
   }
   for (int c = threadIdx.x * VEC; c < p.cols; c += blockDim.x * VEC) {
     float v[VEC];
@@ -442,7 +456,7 @@ __global__ void __launch_bounds__(1024) fwd_long_kernel(const __grid_constant__ 
       Pairs<T, VEC, 1> q;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) (j % 2 ? q.v[j / 2].y : q.v[j / 2].x) = value(v, g, j);
-      store_e4m3<T, VEC, 1>(static_cast<uint8_t*>(p.out) + row * p.ldo + c, q, f, c, p.cols, false);
+      store_e4m3<!NORM>(static_cast<uint8_t*>(p.out) + row * p.ldo + c, q, f.f, f.rest, c, p.cols, false);
     } else {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) o.set(j, rnd<T>(value(v, g, j)));
@@ -819,7 +833,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
     if constexpr (EIGHT) {
       const float most = at_least(f * __uint_as_float(top), LEAST_MAX);
       if (lane == 0 && warp == 0) p.scale[row] = most / E4M3_TOP;
-      store_e4m3<T, VEC, ITEMS>(static_cast<uint8_t*>(p.out) + row * p.ldo + c0, x, f * (E4M3_TOP / most), c0, p.cols, full);
+      store_e4m3<false>(static_cast<uint8_t*>(p.out) + row * p.ldo + c0, x, f * (E4M3_TOP / most), 0.f, c0, p.cols, full);
     } else {
 #pragma unroll
       for (int k = 0; k < N; ++k) x.v[k] = mul2(x.v[k], both(f));
@@ -986,7 +1000,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == SMALL_RING_THREADS ? 3 : 1
       weigh(x, i);
       const int c = c0 + i * 32 * VEC;
       if constexpr (EIGHT) {
-        store_e4m3<T, VEC, 1>(static_cast<uint8_t*>(p.out) + row * p.ldo + c, x, f, c, p.cols, full);
+        store_e4m3<false>(static_cast<uint8_t*>(p.out) + row * p.ldo + c, x, f, 0.f, c, p.cols, full);
       } else {
         times(x, f);
         put_row<T, VEC, 1, ANY>(static_cast<T*>(p.out) + row * p.ldo + c, x, c, p.cols, full);
