@@ -499,14 +499,18 @@ int run_empty(int type, int64_t M, int64_t N, const void* bias, int act, const v
   return ok ? DGEMM_OK : lm::cuda_failed();
 }
 
-// Whether a product runs on the kernels for one or two rows (16-bit operands) or up to eight (8-bit). Those of 8 bits against the
-// tensor-core kernel, one and eight rows: 4096 x 4096 6.9 and 8.0 us against 10.0, gated 9.2 and 10.1 against 13.2, 28672 x 8192 gated 76 and 80
-// against 86; but from 8192 columns on not with several rows, unless gated: 8192 x 4096 11.1 and 13.5 against 12.7, 28672 x 8192 46.7 and 50.8
-// against 45.7.
-bool by_token(const Product& s, bool gated) {
-  if (s.eight)
-    return s.M <= TOKEN8_ROWS && (gated || s.M == 1 || s.N < 8192) && addressable(s.p[0]) && (!gated || addressable(s.p[1])) &&
-           g_drop_limit_us.load() == 0;
+// Whether a product runs on the kernels for one or two rows (16-bit operands) or up to eight (8-bit).
+//
+// 8 bits, time of the token kernel over that of the tensor-core kernel, for K from 512 to 8192 (the tensor-core kernel's time rises where its tiles
+// begin another round, at 32 and at 64 columns per SM):
+//   several rows     N = 4096: 0.58 to 0.91, gated 0.70 to 0.91   6144: 0.95 to 1.3, 1.03 to 1.19   16384: 1.25 to 2.0, 1.05 to 1.7
+//   one row          N = 4096: 0.57 to 0.79, gated 0.63 to 0.85   8192: 0.82 to 0.96, 0.95 to 1.01  16384: 1.15 to 1.5, 0.98 to 1.3
+// and gated over the wider N: several rows 0.92 to 1.08 where K >= 4096, one row 0.81 to 1.07 where K >= 2048.
+bool by_token(const Product& s, bool gated, int sms) {
+  if (s.eight) {
+    const bool one = s.M == 1, narrow = s.N <= (int64_t)(one ? 64 : 32) * sms, deep = gated && s.K[0] >= (one ? 2048 : 4096);
+    return s.M <= TOKEN8_ROWS && (narrow || deep) && addressable(s.p[0]) && (!gated || addressable(s.p[1])) && g_drop_limit_us.load() == 0;
+  }
   return s.M <= TOKEN_ROWS && !s.p_mn && addressable(s.p[0]) && (!gated || addressable(s.p[1])) &&
          s.M * ((s.K[0] + 7) / 8 * 8) * 2 <= (int64_t)TOKEN_SMEM && g_drop_limit_us.load() == 0;
 }
@@ -568,7 +572,7 @@ unsigned rescale_blocks(const lm::DeviceState* st, int64_t rows, int64_t cols) {
 int forward(int type, bool gated, Product* prod, cudaStream_t stream) {
   lm::DeviceState* st = nullptr;
   HGEMM_TRY(lm::device_state(&st));
-  if (by_token(*prod, gated)) return run_token(type, gated, *prod, st->sm_count, stream);
+  if (by_token(*prod, gated, st->sm_count)) return run_token(type, gated, *prod, st->sm_count, stream);
   Plan pl;
   if (!plan_products(&prod, 1, gated, st->sm_count, &pl)) return DGEMM_ERR_BAD_DIM;
   scratch::Hold hold(st->scratch, stream);
