@@ -221,9 +221,11 @@ int run_bwd_vec(int sms, Params& p, cudaStream_t stream, F partial) {
   const int64_t cols = wide(p.cols, VEC, ANY);
   if constexpr (VEC == 8)
     if (cols > (!ANY && p.rows > 2 * (int64_t)sms ? RING_COLS / 2 : RING_COLS) && cols <= RING_COLS * 2) return launch_bwd_ring<T, VEC, 32, ANY>(sms, p, stream, partial);
-  if constexpr (VEC > 1)
-    if (cols <= RING_COLS)
-      return cols <= 256 ? launch_bwd_ring<T, VEC, 8, ANY>(sms, p, stream, partial) : launch_bwd_ring<T, VEC, 16, ANY>(sms, p, stream, partial);
+  if constexpr (VEC > 1) {
+    if constexpr (!ANY)  // (misaligned rows of up to 256 columns go by single values)
+      if (cols <= 256) return launch_bwd_ring<T, VEC, 8, false>(sms, p, stream, partial);
+    if (cols <= RING_COLS) return launch_bwd_ring<T, VEC, 16, ANY>(sms, p, stream, partial);
+  }
   const Shape s = bwd_shape(cols, VEC);
   if (s.longer) {
     const int chunks = (int)((p.rows + 15) / 16 < sms * 2 ? (p.rows + 15) / 16 : sms * 2);
@@ -261,7 +263,7 @@ struct Range {
   const void* ptr;
   int64_t bytes;
 };
-// Outputs must not overlap inputs or one another; the first `nout` ranges are the outputs. `skip`: an input that is an output itself.
+// Outputs must not overlap inputs or one another; the first `nout` ranges are the outputs.
 bool aliased(const Range* r, int nout, int n) {
   for (int i = 0; i < nout; ++i)
     for (int j = i + 1; j < n; ++j)
