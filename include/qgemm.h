@@ -33,6 +33,9 @@ extern "C" {
  *   R        M x N residual, or NULL. It may be D itself (same address and leading dimension)
  *   Z        M x N output for the pre-activation, or NULL
  *
+ * The sum is multiplied by a_scale[m] first and then by b_scale[n]: with an a_scale from 2^-109 (the least of a row in 8 bits) to 2^80 the
+ * product in between stays in binary32's range whatever b_scale is; beyond, it may leave it where Z does not. The same for qgemm_gated.
+ *
  * K == 0 is an empty sum: D = act(bias) + R. M == 0 or N == 0: DGEMM_OK, nothing is inspected.
  */
 DGEMM_API int qgemm_epilogue(int type, int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const float *a_scale,
