@@ -85,7 +85,7 @@ template <int CG_, int BM_, int NB_, bool GATED_, bool EIGHT_>
 struct Cfg {
   static constexpr int CG = CG_, BM = BM_, NB = NB_;
   // The epilogue is a chain of latencies: for 8-bit operands, whose products are done in half the time, more warps (4096 x 8192 x 512 with
-  // tanh-GELU 59.9 -> 52.5 us, with residual 71.7 -> 60.8; with 16 of them, and 96 registers each, 56.8 and 70.8). Not the gated one, whose
+  // tanh-GELU 59.9 -> 52.5 us, with residual 71.7 -> 60.8; with 16 of them, and 96 registers each, 56.8 and 70.8; before RowScales). Not the gated one, whose
   // partners would wait for one another more often (4097 x 8192 x 2048 116.3 us, with 12 warps 119.0).
   static constexpr int EPI_WARPS = EIGHT_ && !GATED_ && BM >= 128 ? 12 : 8;
   static constexpr int THREADS = 128 + 32 * EPI_WARPS;
@@ -396,7 +396,8 @@ struct Epilogue {
 
 // The scales of a patch's rows. Lane l holds that of row l % CH: one load, which is on its way since the patch before; a thread's rows,
 // 8 b + 2 (lane % 4) and the next, come from the lanes that hold them. (With loads of its own in every thread, products value by value and
-// eight epilogue warps, 4096 x 8192 x 512 took 44.5 us without activation, 58.1 with tanh-GELU and 78.6 with residual; now 36.5, 48.4 and 63.)
+// eight epilogue warps, 4096 x 8192 x 512 took 44.5 us without activation, 58.1 with tanh-GELU and 78.6 with residual; now 37, 48.5 and 62.
+// Twelve warps with loads of their own: 52.5 with tanh-GELU, 60.8 with residual, so that the residual's form gains nothing from this.)
 template <int CH>
 struct RowScales {
   float mine;

@@ -22,7 +22,7 @@ struct Shape {
 };
 
 // Forward: a warp for rows of up to 16 values per lane; a block with 16 values per thread beyond (or up to 32, for rows
-// that need them, and for vectors that are only brought to 8 bits: 2088 x 8192 10.1 -> 9.5 us). Few rows are spread over as many threads
+// that need them, and for vectors that are only brought to 8 bits: 2088 x 8192 10.1 -> 9.5 us when chosen, now 9.6). Few rows are spread over as many threads
 // as there are vectors, because then the latency of one row counts.
 Shape fwd_shape(int64_t rows, int64_t cols, int vec, int sms, bool rows_only) {
   const int64_t nv = (cols + vec - 1) / vec;

@@ -1,12 +1,14 @@
 // Root-mean-square norm with the residual's addition, forward (to the operands' type or to 8 bits with a scale per row)
-// and backward. Bound by memory: each kernel reads its rows once, holds them in registers through all sums, and writes once.
+// and backward. Bound by memory: each kernel reads its rows once and holds them through all sums, in registers or, with 32 values of 16 bits
+// per thread, in shared memory (from where they are taken twice), and writes once.
 //
 // A row belongs to one warp (short rows: no block barrier at all) or to one block; a thread holds ITEMS vectors of VEC
 // values (VEC = 16 bytes where all rows are 16-byte aligned, else single values). Blocks are persistent: a thread keeps its
 // columns' gamma in registers from row to row, and the next row's loads are in flight while a row is computed.
 //
 // Forward: one reduction per row. For 8 bits the sum of squares and the largest |s gamma| go through it together:
-// y = s rstd gamma, so max |y| = rstd max |s gamma|, and q = s gamma (rstd / scale).
+// y = s rstd gamma, so max |y| = rstd max |s gamma|, and q = s gamma (rstd / scale). Rows in which these products could leave binary32's range
+// take two or three more, with rstd before gamma (out_of_range()).
 //
 // Backward: while a block walks over its rows, each thread also keeps dgamma of its own columns in registers. The blocks'
 // sums go to a partial matrix [block][column] that a second kernel (layer norm's) adds in order of the blocks: no atomics,
