@@ -8,7 +8,7 @@
 // Rows that are 16-byte aligned: a thread takes vectors of 16 bytes. Any other: a warp takes 128 columns, lane l makes the words of columns
 // 4 l to 4 l + 3 and votes on each, and loads and stores the columns l, l + 32, ..., whose bits it picks from the votes.
 //
-// With a residual bound by memory once the arithmetic is short enough: 8192 x 4096 bfloat16 35 to 37 us (84 to 89 % of the copy rate), where words
+// With a residual bound by memory once the arithmetic is short enough: 8192 x 4096 bfloat16 35 to 38 us (82 to 89 % of the copy rate), where words
 // made anew for every four values, converted and rounded one by one, took 47 us. Without one (the gradient) 32 to 33 us, 65 %: the same words
 // are made beside two thirds of the bytes. Rows that are not aligned, by two-byte accesses in 16 bits: 8192 x 4097 53 and 52 us (binary32, whose
 // single values are words: 64 and 55, aligned 66 and 45.5).
